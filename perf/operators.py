@@ -285,6 +285,7 @@ def prepare(case, seed):
             from paper_2609_30342_gb300 import gradients
             s.clipper = gradients.GradientClipper([_numel(v) for v in s.shapes], case["grad"],
                                                   case["out"] if case["clip"] else None)
+            s.ptrs = s.clipper.pack(s.grads, s.outs if case["clip"] else None)
     elif case["op"] == "norm":
         s.t = _norm_inputs(case, seed)
         if own:
@@ -310,9 +311,9 @@ def _run_clip(s):
     case = s.case
     if own:
         if case["clip"]:
-            total, norms = s.clipper.clip(s.grads, case["max_norm"], out=s.outs)
+            total, norms = s.clipper.clip(case["max_norm"], ptrs=s.ptrs)
         else:
-            total, norms = s.clipper.norm(s.grads)
+            total, norms = s.clipper.norm(ptrs=s.ptrs)
     else:
         norms = torch.stack([(g.float() * g.float()).sum().sqrt() for g in s.grads])
         total = (norms * norms).sum().sqrt()
