@@ -417,6 +417,169 @@ RIKFAD_API int rikfad_quadratic_run(int64_t batch, int64_t m, int64_t n, const f
                                     void *stream);
 
 /*
+ * Operators of a training step beside the optimiser's own.  None of them has a
+ * counterpart in the paper.  Element types: float32, bfloat16, float16.
+ * All arithmetic is in float32 (sums over a list of gradients are joined in
+ * float64); a result is rounded once, when it is stored.
+ */
+enum rikfad_dtype { RIKFAD_F32 = 0, RIKFAD_BF16 = 1, RIKFAD_F16 = 2 };
+
+/*
+ * Norm of a gradient list and clipping.
+ *   norm_t = ||g_t||_2,  total = sqrt(sum_t norm_t^2)
+ *   out_t = c g_t,  c = max_norm / total if max_norm < total < inf, else 1
+ * A total that is not finite scales nothing: the gradients stay as they are and
+ * the step's non-finite guard names the tensor.  Squares that leave float32's
+ * range do not spoil a norm within it.  The sums' order is fixed by the list
+ * and the GPU, so equal gradients give equal results.
+ *
+ *   numel      host array, elements (>= 0) of each of the ntensors >= 0 tensors
+ *   grad_dtype host array, rikfad_dtype of each gradient
+ *   out_dtype  host array, rikfad_dtype of each clipped gradient (NULL: as
+ *              grad_dtype)
+ * The plan (work shares, partial sums) is allocated here; a handle serves one
+ * list at a time, as a rikfad_handle does.
+ */
+typedef struct rikfad_clip_s *rikfad_clip;
+
+RIKFAD_API int rikfad_clip_create(const int64_t *numel, const int *grad_dtype, const int *out_dtype,
+                                  int ntensors, rikfad_clip *out);
+RIKFAD_API void rikfad_clip_destroy(rikfad_clip c);
+RIKFAD_API size_t rikfad_clip_workspace_bytes(rikfad_clip c);
+
+/*
+ * Enqueue the norms and, unless out is NULL, the clipped gradients.
+ *   grad      host array of ntensors pointers (device, or page-locked host
+ *             memory), dense, aligned to their element type; 16-byte aligned
+ *             tensors take the wide loads.  NULL for empty tensors
+ *   out       host array of ntensors pointers, as grad.  out[t] may be grad[t]
+ *             when the types are equal (in place: nothing is written when c = 1);
+ *             otherwise outputs overlap no gradient.  NULL: norms only
+ *   max_norm  >= 0, not NaN (read only with out)
+ *   norms     device, ntensors + 1 floats: norm_t, then total
+ * Nothing is synchronised or allocated; the call can be captured in a graph.
+ */
+RIKFAD_API int rikfad_clip_run(rikfad_clip c, const void *const *grad, void *const *out, double max_norm,
+                               float *norms, void *stream);
+
+/*
+ * Residual sum of a transformer block with the norms around it, for `rows`
+ * rows of `cols` elements:
+ *   n = post(z),  u = residual_scale x + branch_scale gate (.) n,  h = pre(u)
+ * post norms the branch's output and pre the sum, for the branch that follows.
+ *   RIKFAD_NORM_NONE   v
+ *   RIKFAD_NORM_RMS    v / sqrt(mean(v^2) + eps) (.) weight + bias
+ *   RIKFAD_NORM_LAYER  (v - mean(v)) / sqrt(var(v) + eps) (.) weight + bias
+ * with weight 1 and bias 0 where the pointer is NULL.  The gradients, given du
+ * and dh (either may be absent; u counts as used by both):
+ *   dx, dz, dgate and those of the weights and biases.
+ *
+ * Every member of the form rikfad_rows points to rows of `cols` contiguous
+ * elements, `stride` elements apart (>= cols where rows > 1).  Sizes: rows >= 0,
+ * 1 <= cols <= 32768.
+ *   x, u, du, dx     residual_dtype (RIKFAD_F32 or dtype)
+ *   z, h, dh, dz     dtype
+ *   gate, dgate      gate_dtype (RIKFAD_F32 or dtype); gate row i serves rows
+ *                    [i gate_rows, (i + 1) gate_rows), gate_rows divides rows;
+ *                    dgate sums over them
+ *   weights, biases  param_dtype (RIKFAD_F32 or dtype), cols elements, and so
+ *                    their gradients, which are summed over the rows
+ * Absent (data NULL): z (u = residual_scale x; no post norm, gate or dz),
+ * gate, u or h as an output (not stored), du, dh, dx, dz, dgate, the gradients
+ * of weights and biases.  Pointers are aligned to their element type; rows that
+ * start on 16 bytes load fastest.  u may be x, h may be z, dx may be du and dz
+ * may be dh or z (same type and stride); otherwise outputs overlap nothing.
+ *   stats      device, 4 floats a row: mean and 1/deviation of post and of pre.
+ *              Written by the forward call (NULL: not kept), read by the
+ *              backward call, which takes the forward call's x, z, gate and
+ *              weights as well
+ *   workspace  device memory of rikfad_residual_norm_workspace bytes, 16-byte
+ *              aligned: partial sums of the backward call, nothing kept
+ * Squares of elements beyond float32's range (above about 1e19) are infinite.
+ * With rows = 0 the backward call writes zeros to the gradients of weights and
+ * biases.  Nothing is synchronised or allocated.
+ */
+enum rikfad_norm { RIKFAD_NORM_NONE = 0, RIKFAD_NORM_RMS = 1, RIKFAD_NORM_LAYER = 2 };
+
+typedef struct {
+    void *data;
+    int64_t stride;
+} rikfad_rows;
+
+typedef struct {
+    int64_t rows, cols, gate_rows;
+    int32_t dtype, residual_dtype, param_dtype, gate_dtype;
+    int32_t post, pre;
+    double post_eps, pre_eps, residual_scale, branch_scale;
+    rikfad_rows x, z, gate;
+    const void *post_weight, *post_bias, *pre_weight, *pre_bias;
+    rikfad_rows u, h;
+    float *stats;
+    rikfad_rows du, dh;
+    rikfad_rows dx, dz, dgate;
+    void *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;
+    void *workspace;
+    size_t workspace_bytes;
+} rikfad_residual_norm;
+
+RIKFAD_API int rikfad_residual_norm_forward(const rikfad_residual_norm *p, void *stream);
+RIKFAD_API int rikfad_residual_norm_backward(const rikfad_residual_norm *p, void *stream);
+
+/* Workspace bytes of the backward call for p's sizes, types and outputs (0 if
+ * it needs none); 0 with a message in rikfad_last_error for sizes out of range. */
+RIKFAD_API size_t rikfad_residual_norm_workspace(const rikfad_residual_norm *p);
+
+/*
+ * Rotary positions: pair i of every head of token t turns by the angle
+ * position(t) f_i,
+ *   (a, b) -> magnitude (a cos - b sin, b cos + a sin),
+ * the angle negated with inverse != 0 (the gradient of the rotation, with the
+ * same magnitude).  Elements of a head beyond rotary_dim are copied.
+ *   layout  RIKFAD_ROTARY_HALF         pair i = elements i, i + rotary_dim / 2
+ *           RIKFAD_ROTARY_INTERLEAVED  pair i = elements 2 i, 2 i + 1
+ *   turns   device, rotary_dim / 2 values: f_i / (2 pi) in 64-bit fixed point
+ *           (units of 2^-64 turns, rikfad_rotary_turns).  The product with the
+ *           position wraps at a whole turn, so angles keep their precision at
+ *           any position
+ *   positions  device, position_bytes (4 or 8) bytes each, token t of sequence b
+ *           at b position_batch + t; NULL: start + t
+ *   lists   up to two sets of heads (queries and keys); element d of head j of
+ *           token t of sequence b at b batch + t token + j head + d in src and
+ *           in dst, strides in elements.  src = dst with equal strides rotates
+ *           in place; otherwise dst overlaps no src.  Pointers aligned to the
+ *           element type
+ * batch, tokens, heads >= 0; 1 <= head_dim <= 4096; rotary_dim even,
+ * 0 <= rotary_dim <= head_dim.
+ */
+enum rikfad_rotary_layout { RIKFAD_ROTARY_HALF = 0, RIKFAD_ROTARY_INTERLEAVED = 1 };
+
+typedef struct {
+    const void *src;
+    void *dst;
+    int64_t heads;
+    int64_t src_batch, src_token, src_head;
+    int64_t dst_batch, dst_token, dst_head;
+} rikfad_rotary_heads;
+
+typedef struct {
+    int64_t batch, tokens;
+    int32_t head_dim, rotary_dim, layout, dtype;
+    const uint64_t *turns;
+    const void *positions;
+    int64_t position_batch, start;
+    int32_t position_bytes, inverse;
+    int32_t nlists, reserved;
+    double magnitude;
+    rikfad_rotary_heads lists[2];
+} rikfad_rotary;
+
+RIKFAD_API int rikfad_rotary_apply(const rikfad_rotary *p, void *stream);
+
+/* turns[i] = radians[i] / (2 pi) in units of 2^-64, modulo a turn (host arrays;
+ * RIKFAD_ERR_ARG for a value that is not finite). */
+RIKFAD_API int rikfad_rotary_turns(const double *radians, int64_t n, uint64_t *turns);
+
+/*
  * Testing hooks.  These have no counterpart in the paper.
  *
  * rikfad_debug_check_failures: a library compiled with -DRIKFAD_CHECKED

@@ -15,6 +15,7 @@
 #include "rikfad_aux_kernels.cuh"
 #include "rikfad_sweep.cuh"
 #include "rikfad_diag_kernels.cuh"
+#include "rikfad_host.hpp"
 #include "rikfad_planner.hpp"
 
 using namespace rikfad;
@@ -137,6 +138,28 @@ int report_error(int code, const std::string &msg)
 {
     g_last_error = msg;
     return code;
+}
+
+cudaError_t counted_malloc(void **p, size_t bytes) { return rk_malloc(p, bytes); }
+void counted_free(void *p) { rk_free(p); }
+
+int check_address(const void *p, int device, const char *what, int64_t index)
+{
+    const std::string where = index < 0 ? std::string(what) : std::string(what) + " " + std::to_string(index);
+    cudaPointerAttributes a{};
+    if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
+        cudaGetLastError();
+        return fail(RIKFAD_ERR_ARG, where + " is not an address CUDA recognises");
+    }
+    if (a.type == cudaMemoryTypeDevice && a.device != device)
+        return fail(RIKFAD_ERR_ARG, where + " is memory of device " + std::to_string(a.device) +
+                                        ", not of device " + std::to_string(device));
+    if (a.type == cudaMemoryTypeUnregistered) {
+        int pageable = 0;
+        if (cudaDeviceGetAttribute(&pageable, cudaDevAttrPageableMemoryAccess, device) != cudaSuccess || !pageable)
+            return fail(RIKFAD_ERR_ARG, where + " is pageable host memory, which this device cannot address");
+    }
+    return RIKFAD_OK;
 }
 }  // namespace rikfad
 

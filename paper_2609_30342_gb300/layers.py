@@ -1,0 +1,346 @@
+"""Row operators of a transformer block: the residual sum with the norms around it, and rotary positions.
+
+``ResidualNorm``   u = residual_scale x + branch_scale gate * post(z),  h = pre(u), and all gradients
+``Rotary``         heads turned by their token's position, and back
+
+Each has explicit calls on CUDA tensors (``forward``/``backward``, ``rotate``) and is callable inside autograd.
+Argument checks and marshalling only: the work runs in the kernels behind ``rikfad_residual_norm_forward``,
+``rikfad_residual_norm_backward`` and ``rikfad_rotary_apply``, enqueued on the current stream of the tensors' device (or
+``stream``).
+"""
+import ctypes
+import math
+import struct
+from collections import namedtuple
+
+import torch
+
+from . import rikfad
+
+_TORCH = {torch.float32: rikfad.F32, torch.bfloat16: rikfad.BF16, torch.float16: rikfad.F16}
+_KINDS = {None: 0, "rms": 1, "layer": 2}
+_F32 = torch.float32
+
+# struct rikfad_residual_norm: sizes, types, scales, then (pointer, stride) pairs and pointers
+_NORM = struct.Struct("=3q 4i 2i 4d 6q 4q 4q q 4q 6q 4q qQ")
+# struct rikfad_rotary: sizes, types, pointers, magnitude, two sets of heads
+_ROTARY = struct.Struct("=2q 4i qq2q 2i 2i d 18q")
+
+ResidualNormGrads = namedtuple("ResidualNormGrads", "x z gate post_weight post_bias pre_weight pre_bias")
+
+
+def _rows(name, t, cols, dtype, device, rows=None):
+    """A tensor as rows of ``cols`` contiguous elements: (pointer, row stride, number of rows)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
+        raise ValueError("%s must be a CUDA tensor on the device of x" % name)
+    if t.dtype is not dtype:
+        raise ValueError("%s must be %s, not %s" % (name, dtype, t.dtype))
+    shape = t.shape
+    if len(shape) == 0 or shape[-1] != cols:
+        raise ValueError("%s must have %d columns" % (name, cols))
+    if t.dim() != 2:
+        try:
+            t = t.view(-1, cols)
+        except RuntimeError:
+            raise ValueError("the rows of %s must be evenly spaced" % name) from None
+    n = t.shape[0]
+    if rows is not None and n != rows:
+        raise ValueError("%s has %d rows, expected %d" % (name, n, rows))
+    stride = t.stride()
+    if cols > 1 and stride[1] != 1:
+        raise ValueError("the rows of %s must be contiguous" % name)
+    if n > 1 and stride[0] < cols:
+        raise ValueError("the rows of %s must not overlap" % name)
+    return t.data_ptr(), (stride[0] if n > 1 else cols), n
+
+
+def _stream(stream, device):
+    return torch.cuda.current_stream(device).cuda_stream if stream is None else rikfad._stream_ptr(stream)
+
+
+class ResidualNorm:
+    """u = residual_scale x + branch_scale gate * post(z) and h = pre(u), over rows of ``cols`` elements.
+
+    ``post``, ``pre``: None, "rms" or "layer"; weights and biases are arguments of the calls (absent: 1 and 0).
+    x, u and their gradients are float32 or of z's type; weights and biases float32 or of z's type; a gate float32 or of
+    z's type, with one row per row of z or one for every run of rows (its row count divides theirs)."""
+
+    def __init__(self, cols, post=None, pre="rms", post_eps=1e-6, pre_eps=1e-6, residual_scale=1.0, branch_scale=1.0):
+        if not 1 <= int(cols) <= 32768:
+            raise ValueError("cols must be in [1, 32768]")
+        if post not in _KINDS or pre not in _KINDS:
+            raise ValueError("post and pre must be None, 'rms' or 'layer'")
+        for v in (post_eps, pre_eps):
+            if not (math.isfinite(v) and v >= 0):
+                raise ValueError("eps must be finite and >= 0")
+        for v in (residual_scale, branch_scale):
+            if not math.isfinite(v):
+                raise ValueError("scales must be finite")
+        self.cols, self.post, self.pre = int(cols), post, pre
+        self.post_eps, self.pre_eps = float(post_eps), float(pre_eps)
+        self.residual_scale, self.branch_scale = float(residual_scale), float(branch_scale)
+
+    def _vector(self, name, v, dtype, device):
+        if v is None:
+            return 0
+        if not isinstance(v, torch.Tensor) or v.device != device:
+            raise ValueError("%s must be a CUDA tensor on the device of x" % name)
+        if v.dtype is not dtype or v.dim() != 1 or v.shape[0] != self.cols or not v.is_contiguous():
+            raise ValueError("%s must be %d contiguous elements of %s" % (name, self.cols, dtype))
+        return v.data_ptr()
+
+    def _inputs(self, x, z, gate, weights, dtype):
+        """The head of the parameter block up to the weights, and (rows, types)."""
+        cols = self.cols
+        if not isinstance(x, torch.Tensor) or not x.is_cuda:
+            raise ValueError("x must be a CUDA tensor")
+        device = x.device
+        dt = z.dtype if z is not None else (x.dtype if dtype is None else dtype)
+        if dt not in _TORCH:
+            raise ValueError("z must be float32, bfloat16 or float16")
+        rt = x.dtype
+        pt = next((w.dtype for w in weights if w is not None), _F32)
+        gt = _F32 if gate is None else gate.dtype
+        for name, t in (("x", rt), ("weights and biases", pt), ("gate", gt)):
+            if t is not _F32 and t is not dt:
+                raise ValueError("%s must be float32 or %s" % (name, dt))
+        px, sx, rows = _rows("x", x, cols, rt, device)
+        pz, sz, _ = (0, 0, 0) if z is None else _rows("z", z, cols, dt, device, rows)
+        pg, sg, per = 0, 0, 1
+        if gate is not None:
+            if z is None:
+                raise ValueError("a gate needs z")
+            pg, sg, n = _rows("gate", gate, cols, gt, device)
+            if n == 0 and rows or n and rows % n:
+                raise ValueError("the gate's rows must divide those of x")
+            per = rows // n if n and rows else 1
+        if z is None and (self.post is not None or weights[0] is not None or weights[1] is not None):
+            raise ValueError("a post norm needs z")
+        if self.post is None and (weights[0] is not None or weights[1] is not None):
+            raise ValueError("post_weight and post_bias need a post norm")
+        if self.pre is None and (weights[2] is not None or weights[3] is not None):
+            raise ValueError("pre_weight and pre_bias need a pre norm")
+        names = ("post_weight", "post_bias", "pre_weight", "pre_bias")
+        head = (rows, cols, per, _TORCH[dt], _TORCH[rt], _TORCH[pt], _TORCH[gt], _KINDS[self.post], _KINDS[self.pre],
+                self.post_eps, self.pre_eps, self.residual_scale, self.branch_scale, px, sx, pz, sz, pg, sg,
+                *(self._vector(n, w, pt, device) for n, w in zip(names, weights)))
+        return head, rows, dt, pt
+
+    def forward(self, x, z=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None,
+                need_stats=True, dtype=None, out=None, stream=None):
+        """(u, h, stats).  ``stats`` (None without ``need_stats``) is what ``backward`` needs besides the inputs.
+        Without z, u = residual_scale x and ``dtype`` gives h's type (default x's).  ``out``: (u, h) to write to; u may
+        be x and h may be z; None for one that is not wanted."""
+        head, rows, dt, _ = self._inputs(x, z, gate, (post_weight, post_bias, pre_weight, pre_bias), dtype)
+        device, cols = x.device, self.cols
+        if out is None:
+            u = torch.empty(x.shape, dtype=x.dtype, device=device)
+            h = torch.empty(x.shape, dtype=dt, device=device)
+        else:
+            u, h = out
+        pu, su, _ = (0, 0, 0) if u is None else _rows("u", u, cols, x.dtype, device, rows)
+        ph, sh, _ = (0, 0, 0) if h is None else _rows("h", h, cols, dt, device, rows)
+        stats = torch.empty(rows, 4, dtype=_F32, device=device) if need_stats else None
+        block = _NORM.pack(*head, pu, su, ph, sh, 0 if stats is None else stats.data_ptr(), *([0] * 16))
+        with torch.cuda.device(device):
+            rikfad._check(rikfad.lib().rikfad_residual_norm_forward(block, _stream(stream, device)))
+        return u, h, stats
+
+    def backward(self, du, dh, x, z=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None,
+                 stats=None, stream=None):
+        """``ResidualNormGrads`` of the forward call's inputs (None where the input is None), from the gradients of u
+        and h (either may be None)."""
+        weights = (post_weight, post_bias, pre_weight, pre_bias)
+        dt = dh.dtype if dh is not None else None
+        head, rows, dt, pt = self._inputs(x, z, gate, weights, dt)
+        device, cols = x.device, self.cols
+        pdu, sdu, _ = (0, 0, 0) if du is None else _rows("du", du, cols, x.dtype, device, rows)
+        pdh, sdh, _ = (0, 0, 0) if dh is None else _rows("dh", dh, cols, dt, device, rows)
+        if stats is None or stats.dtype is not _F32 or tuple(stats.shape) != (rows, 4) or not stats.is_contiguous() \
+                or stats.device != device:
+            raise ValueError("stats must be what forward returned for these inputs")
+        dx = torch.empty(x.shape, dtype=x.dtype, device=device)
+        dz = None if z is None else torch.empty(z.shape, dtype=dt, device=device)
+        dgate = None if gate is None else torch.empty(gate.shape, dtype=gate.dtype, device=device)
+        dw = [None if w is None else torch.empty(cols, dtype=pt, device=device) for w in weights]
+        tail = [dx.data_ptr(), cols, 0 if z is None else dz.data_ptr(), cols, 0 if gate is None else dgate.data_ptr(), cols]
+        tail += [0 if w is None else w.data_ptr() for w in dw]
+        body = (*head, 0, 0, 0, 0, stats.data_ptr(), pdu, sdu, pdh, sdh, *tail)
+        L = rikfad.lib()
+        with torch.cuda.device(device):
+            nbytes = L.rikfad_residual_norm_workspace(_NORM.pack(*body, 0, 0))
+            work = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+            if stream is not None and not isinstance(stream, int) and work is not None:
+                work.record_stream(stream)
+            rikfad._check(L.rikfad_residual_norm_backward(_NORM.pack(*body, work.data_ptr() if nbytes else 0, nbytes),
+                                                          _stream(stream, device)))
+        return ResidualNormGrads(dx, dz, dgate, *dw)
+
+    def __call__(self, x, z=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None,
+                 dtype=None):
+        """(u, h) inside autograd."""
+        return _ResidualNormFunction.apply(self, dtype, x, z, gate, post_weight, post_bias, pre_weight, pre_bias)
+
+
+class _ResidualNormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, op, dtype, x, *rest):
+        u, h, stats = op.forward(x, *rest, dtype=dtype)
+        ctx.op = op
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(x, *rest, stats)
+        return u, h
+
+    @staticmethod
+    def backward(ctx, du, dh):
+        x, *rest, stats = ctx.saved_tensors
+        du, dh = (None if g is None else g.contiguous() for g in (du, dh))
+        return (None, None, *ctx.op.backward(du, dh, x, *rest, stats=stats))
+
+
+def rotary_frequencies(rotary_dim, base=10000.0, scaling=None):
+    """(radians per position of every pair, magnitude of the rotated values), in double precision.
+
+    Pair i turns by base^(-2 i / rotary_dim).  ``scaling``: None, or a dict with "kind" and "factor":
+      linear  every frequency divided by the factor
+      base    the base times factor^(rotary_dim / (rotary_dim - 2)): the fastest pair keeps its frequency, the slowest
+              one's is divided by the factor
+      ramp    pairs that turn more than "fast" (32) times within "original_context" keep their frequency, those that turn
+              less than "slow" (1) times are divided by the factor, with a straight ramp between; the magnitude is
+              0.1 ln(factor) + 1"""
+    factor = 1.0
+    kind = None
+    if scaling is not None:
+        kind, factor = scaling.get("kind"), float(scaling.get("factor", 1.0))
+        if kind not in ("linear", "base", "ramp"):
+            raise ValueError("scaling kind must be 'linear', 'base' or 'ramp'")
+        if not (math.isfinite(factor) and factor >= 1.0):
+            raise ValueError("the scaling factor must be >= 1")
+    if not (math.isfinite(base) and base > 0):
+        raise ValueError("base must be > 0")
+    if rotary_dim % 2 or rotary_dim < 0:
+        raise ValueError("rotary_dim must be even and >= 0")
+    if kind == "base" and rotary_dim > 2:
+        base = base * factor ** (rotary_dim / (rotary_dim - 2))
+    f = [base ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)]
+    if kind == "linear":
+        return [v / factor for v in f], 1.0
+    if kind != "ramp":
+        return f, 1.0
+    original, fast, slow = scaling.get("original_context"), scaling.get("fast", 32.0), scaling.get("slow", 1.0)
+    if not original or original <= 0 or not fast > slow:
+        raise ValueError("ramp scaling needs original_context > 0 and fast > slow")
+    keep = [min(1.0, max(0.0, (original * v / (2.0 * math.pi) - slow) / (fast - slow))) for v in f]
+    return [v * (k + (1.0 - k) / factor) for v, k in zip(f, keep)], 0.1 * math.log(factor) + 1.0
+
+
+class Rotary:
+    """Rotary positions of heads of ``head_dim`` elements, the first ``rotary_dim`` (all by default) of which turn, as
+    pairs (i, i + rotary_dim / 2) ("half") or (2 i, 2 i + 1) ("interleaved").  ``scaling`` as for
+    ``rotary_frequencies``, or ``frequencies`` (radians per position) with ``magnitude``."""
+
+    def __init__(self, head_dim, rotary_dim=None, base=10000.0, layout="half", scaling=None, frequencies=None,
+                 magnitude=None, device="cuda"):
+        self.head_dim = int(head_dim)
+        self.rotary_dim = self.head_dim if rotary_dim is None else int(rotary_dim)
+        if not 1 <= self.head_dim <= 4096:
+            raise ValueError("head_dim must be in [1, 4096]")
+        if self.rotary_dim % 2 or not 0 <= self.rotary_dim <= self.head_dim:
+            raise ValueError("rotary_dim must be even and in [0, head_dim]")
+        if layout not in ("half", "interleaved"):
+            raise ValueError("layout must be 'half' or 'interleaved'")
+        self.layout = layout
+        if frequencies is None:
+            frequencies, m = rotary_frequencies(self.rotary_dim, float(base), scaling)
+        else:
+            frequencies, m = [float(v) for v in frequencies], 1.0
+        self.magnitude = m if magnitude is None else float(magnitude)
+        n = self.rotary_dim // 2
+        if len(frequencies) != n:
+            raise ValueError("need rotary_dim / 2 frequencies")
+        turns = (ctypes.c_uint64 * max(n, 1))()
+        rikfad._check(rikfad.lib().rikfad_rotary_turns((ctypes.c_double * max(n, 1))(*frequencies), n, turns))
+        self.frequencies = frequencies
+        signed = [v - (1 << 64) if v >= 1 << 63 else v for v in turns[:n]]
+        self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
+
+    def _heads(self, name, t, shape, dtype, device):
+        """(batch, token, head) strides of a [tokens, heads, head_dim] or [batch, tokens, heads, head_dim] tensor."""
+        if not isinstance(t, torch.Tensor) or t.device != device:
+            raise ValueError("%s must be a CUDA tensor on the device of q" % name)
+        if t.dtype is not dtype:
+            raise ValueError("%s must be %s, not %s" % (name, dtype, t.dtype))
+        if t.shape[:-2] != shape or t.shape[-1] != self.head_dim:
+            raise ValueError("%s must be [tokens, heads, %d] or [batch, tokens, heads, %d], with the tokens of q"
+                             % (name, self.head_dim, self.head_dim))
+        s = t.stride()
+        if s[-1] != 1 and self.head_dim > 1:
+            raise ValueError("the heads of %s must be contiguous" % name)
+        return (0, *s[:2]) if len(s) == 3 else s[:3]
+
+    def rotate(self, q, k=None, positions=None, start=0, inverse=False, out=None, stream=None):
+        """(q', k') of queries and keys [tokens, heads, head_dim] or [batch, tokens, heads, head_dim] (k' None without
+        k).  ``positions``: int32 or int64 CUDA tensor [tokens] or [batch, tokens]; default ``start`` + 0, 1, ...
+        ``inverse`` turns back: the gradient of the rotation.  ``out``: (q', k') to write to; q and k themselves
+        rotate in place."""
+        if not isinstance(q, torch.Tensor) or not q.is_cuda:
+            raise ValueError("q must be a CUDA tensor")
+        if q.dtype not in _TORCH:
+            raise ValueError("q must be float32, bfloat16 or float16")
+        if q.dim() not in (3, 4):
+            raise ValueError("q must be [tokens, heads, head_dim] or [batch, tokens, heads, head_dim]")
+        device, lead = q.device, q.shape[:-2]
+        if self.turns.device != device:
+            raise ValueError("q must be on %s, the device of the frequencies" % self.turns.device)
+        batch, tokens = (1, lead[0]) if len(lead) == 1 else lead
+        pp, pb, width = 0, 0, 8
+        if positions is not None:
+            if not isinstance(positions, torch.Tensor) or positions.device != device or \
+                    positions.dtype not in (torch.int32, torch.int64):
+                raise ValueError("positions must be an int32 or int64 CUDA tensor on the device of q")
+            if positions.shape == lead and len(lead) == 2:
+                pb = positions.stride(0)
+            elif tuple(positions.shape) != (tokens,):
+                raise ValueError("positions must be [tokens] or [batch, tokens]")
+            if tokens > 1 and positions.stride(-1) != 1:
+                raise ValueError("positions must be contiguous along the tokens")
+            pp, width = positions.data_ptr(), positions.element_size()
+        if out is None:
+            out = (torch.empty(q.shape, dtype=q.dtype, device=device),
+                   None if k is None else torch.empty(k.shape, dtype=q.dtype, device=device))
+        lists, sets = [], [("q", q, out[0])] + ([] if k is None else [("k", k, out[1])])
+        for name, src, dst in sets:
+            strides = self._heads(name, src, lead, q.dtype, device)
+            if dst.shape != src.shape:
+                raise ValueError("the output of %s must have its shape" % name)
+            lists += [src.data_ptr(), dst.data_ptr(), src.shape[-2], *strides,
+                      *self._heads("the output of " + name, dst, lead, q.dtype, device)]
+        block = _ROTARY.pack(batch, tokens, self.head_dim, self.rotary_dim, 0 if self.layout == "half" else 1,
+                             _TORCH[q.dtype], self.turns.data_ptr(), pp, pb, int(start), width, 1 if inverse else 0,
+                             len(sets), 0, self.magnitude, *lists, *([0] * (18 - len(lists))))
+        with torch.cuda.device(device):
+            rikfad._check(rikfad.lib().rikfad_rotary_apply(block, _stream(stream, device)))
+        return out[0], (None if k is None else out[1])
+
+    def __call__(self, q, k, positions=None, start=0):
+        """(q', k') inside autograd."""
+        return _RotaryFunction.apply(self, q, k, positions, start)
+
+
+class _RotaryFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, op, q, k, positions, start):
+        ctx.op, ctx.start = op, start
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(*([] if positions is None else [positions]))
+        return op.rotate(q, k, positions=positions, start=start)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        positions = ctx.saved_tensors[0] if ctx.saved_tensors else None
+        if dq is None:
+            dk, _ = ctx.op.rotate(dk.contiguous(), positions=positions, start=ctx.start, inverse=True)
+        else:
+            dq, dk = ctx.op.rotate(dq.contiguous(), None if dk is None else dk.contiguous(), positions=positions,
+                                   start=ctx.start, inverse=True)
+        return None, dq, dk, None, None

@@ -12,12 +12,14 @@ Parameters and their gradients must be contiguous float32 CUDA tensors of one
 device (autograd gives a float32 parameter a float32 gradient; bfloat16
 gradients are for the pointer API, ``rikfad.RIKFAD``).  A parameter without a
 gradient at a step takes a zero gradient, since the handle steps a fixed list.
+``clip_grad_norm(max_norm)`` scales all gradients to a largest global norm
+before a step.
 """
 from operator import attrgetter, is_, itemgetter
 
 import torch
 
-from . import rikfad
+from . import gradients, rikfad
 
 # The marshalling below runs over every parameter at every step: C-level maps
 # of these keep it within a small model's kernel time.
@@ -31,6 +33,7 @@ class RIKFADOptimizer(torch.optim.Optimizer):
         defaults = dict(lr=lr, alpha=alpha, mu=mu, gamma=gamma, eps_stab=eps_stab)
         super().__init__(params, defaults)
         self._groups = {}     # group index -> (handle, parameter list, zero gradients)
+        self._clipper = None  # plan of the last clip_grad_norm's list of sizes
 
     @staticmethod
     def _shape(p):
@@ -82,6 +85,22 @@ class RIKFADOptimizer(torch.optim.Optimizer):
         return loss
 
     @torch.no_grad()
+    def clip_grad_norm(self, max_norm):
+        """Scale the gradients of every group in place so that their global 2-norm is at most ``max_norm``, and return
+        the norm before (a scalar CUDA tensor; nothing waits).  A norm that is not finite scales nothing."""
+        grads = [p.grad for group in self.param_groups for p in group["params"] if p.grad is not None]
+        if not (all(map(torch.Tensor.is_contiguous, grads)) and set(map(_dtype, grads)) <= {torch.float32}):
+            raise ValueError("gradients must be contiguous float32 tensors")
+        if len({g.device for g in grads}) > 1:
+            raise ValueError("gradients must share one device")
+        sizes = list(map(torch.Tensor.numel, grads))
+        if self._clipper is None or self._clipper.numels != sizes:
+            if self._clipper is not None:
+                self._clipper.close()
+            self._clipper = gradients.GradientClipper(sizes, "f32")
+        return self._clipper.clip(max_norm, grads)[0]
+
+    @torch.no_grad()
     def materialize(self):
         """Turn every momentum buffer into the paper's P_{n+1} (in place)."""
         for handle, params, _ in self._groups.values():
@@ -124,3 +143,6 @@ class RIKFADOptimizer(torch.optim.Optimizer):
         for handle, _, _ in self._groups.values():
             handle.close()
         self._groups.clear()
+        if self._clipper is not None:
+            self._clipper.close()
+            self._clipper = None

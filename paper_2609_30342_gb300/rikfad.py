@@ -26,6 +26,8 @@ ERR_NONFINITE = -5
 ERR_STATE = -6
 GRAD_F32 = 0
 GRAD_BF16 = 1
+F32, BF16, F16 = 0, 1, 2        # enum rikfad_dtype
+DTYPE_CODES = {"f32": F32, "bf16": BF16, "f16": F16}
 
 
 class RikfadError(RuntimeError):
@@ -94,6 +96,18 @@ SIGNATURES = [
     ("rikfad_quadratic_run", ctypes.c_int, [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, _VP, _VP,
                                             _VP, _VP, _VP, ctypes.c_double, ctypes.POINTER(HParams),
                                             ctypes.c_int64, _VP, ctypes.c_int64, _VP, _VP]),
+    ("rikfad_clip_create", ctypes.c_int, [ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int),
+                                          ctypes.POINTER(ctypes.c_int), ctypes.c_int,
+                                          ctypes.POINTER(_VP)]),
+    ("rikfad_clip_destroy", None, [_VP]),
+    ("rikfad_clip_workspace_bytes", ctypes.c_size_t, [_VP]),
+    ("rikfad_clip_run", ctypes.c_int, [_VP, _PP, _PP, ctypes.c_double, _VP, _VP]),
+    ("rikfad_residual_norm_forward", ctypes.c_int, [_VP, _VP]),
+    ("rikfad_residual_norm_backward", ctypes.c_int, [_VP, _VP]),
+    ("rikfad_residual_norm_workspace", ctypes.c_size_t, [_VP]),
+    ("rikfad_rotary_apply", ctypes.c_int, [_VP, _VP]),
+    ("rikfad_rotary_turns", ctypes.c_int, [ctypes.POINTER(ctypes.c_double), ctypes.c_int64,
+                                           ctypes.POINTER(ctypes.c_uint64)]),
     ("rikfad_last_error", ctypes.c_char_p, []),
     ("rikfad_abi_version", ctypes.c_int, []),
 ]
