@@ -8,12 +8,14 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <new>
 #include <string>
 
 #include "rikfad.h"
 #include "rikfad_host.hpp"
+#include "rikfad_kernels.cuh"
 #include "rikfad_types.cuh"
 
 using namespace rikfad;
@@ -21,49 +23,143 @@ using namespace rikfad;
 namespace {
 
 constexpr int kRotaryThreads = 256;
+constexpr int kSms = 152;
+constexpr int kTableFloats = 8192;      // cosines and sines of a tile of tokens: 32 KB at most
 
 struct RotaryParams {
     rikfad_rotary d;
-    float magnitude;
+    float magnitude, sine_sign;
+    int32_t tile;                       // tokens of one block
+    int32_t turn_units, units;          // of a head: units that turn, all units
+    int32_t heads;                      // of both lists
+    bool copy;                          // elements beyond rotary_dim are copied
 };
 
-__device__ __forceinline__ void angle(const RotaryParams &p, int64_t batch, int64_t token, int pair, float &cosine, float &sine)
-{
-    int64_t position = p.d.start + token;
-    if (p.d.positions) {
-        const int64_t i = batch * p.d.position_batch + token;
-        position = p.d.position_bytes == 4 ? (int64_t)static_cast<const int32_t *>(p.d.positions)[i]
-                                           : static_cast<const int64_t *>(p.d.positions)[i];
-    }
-    // the turn's fraction in [-1/2, 1/2), in half turns for sincospi
-    const uint64_t turn = (uint64_t)position * p.d.turns[pair];
-    sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &sine, &cosine);
-    cosine *= p.magnitude;
-    sine *= p.d.inverse ? -p.magnitude : p.magnitude;
-}
+// V elements as one load.
+template <int BYTES> struct Word;
+template <> struct Word<2> { using type = uint16_t; };
+template <> struct Word<4> { using type = uint32_t; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<16> { using type = uint4; };
 
-template <typename T> __global__ void __launch_bounds__(kRotaryThreads) rikfad_rotary_kernel(const __grid_constant__ RotaryParams p)
-{
-    const rikfad_rotary_heads &l = p.d.lists[blockIdx.y];
-    const int pairs = p.d.rotary_dim / 2, slots = p.d.head_dim - pairs;     // pairs, then single elements
-    const int64_t work = p.d.batch * p.d.tokens * l.heads * slots;
-    for (int64_t w = (int64_t)blockIdx.x * kRotaryThreads + threadIdx.x; w < work; w += (int64_t)gridDim.x * kRotaryThreads) {
-        const int slot = (int)(w % slots);
-        const int64_t head = w / slots % l.heads, at = w / slots / l.heads;
-        const int64_t token = at % p.d.tokens, batch = at / p.d.tokens;
-        const T *src = static_cast<const T *>(l.src) + batch * l.src_batch + token * l.src_token + head * l.src_head;
-        T *dst = static_cast<T *>(l.dst) + batch * l.dst_batch + token * l.dst_token + head * l.dst_head;
-        if (slot >= pairs) {
-            dst[pairs + slot] = src[pairs + slot];
-            continue;
+template <typename T, int V> union Vec {
+    typename Word<V * sizeof(T)>::type word;
+    T v[V];
+    __device__ __forceinline__ Vec() {}
+};
+
+// A unit is V pairs of one head, as two vectors of V elements: in the half layout
+// one vector from each half, in the interleaved layout two neighbours.  Beyond
+// the turning units, a unit is up to two vectors of elements that are copied.
+template <typename T, int V> struct Unit {
+    const T *src;
+    T *dst;
+    int first, second;      // elements of the head; second < 0: none
+    int pair;               // first pair, in the tile's table; < 0: copy
+    Vec<T, V> a, b;
+
+    __device__ __forceinline__ void locate(const RotaryParams &p, int64_t token0, int w)
+    {
+        const int u = w % p.units, rest = w / p.units;
+        int head = rest % p.heads;
+        const int slot = rest / p.heads;                        // token within the tile
+        const int64_t at = token0 + slot;
+        const int64_t batch = p.d.batch == 1 ? 0 : at / p.d.tokens, token = at - batch * p.d.tokens;
+        const int list = head >= (int)p.d.lists[0].heads;
+        head -= list ? (int)p.d.lists[0].heads : 0;
+        const rikfad_rotary_heads &l = p.d.lists[list];
+        src = static_cast<const T *>(l.src) + batch * l.src_batch + token * l.src_token + head * l.src_head;
+        dst = static_cast<T *>(l.dst) + batch * l.dst_batch + token * l.dst_token + head * l.dst_head;
+        if (u < p.turn_units) {
+            const bool half = p.d.layout == RIKFAD_ROTARY_HALF;
+            first = half ? u * V : 2 * u * V;
+            second = first + (half ? p.d.rotary_dim / 2 : V);
+            pair = slot * (p.d.rotary_dim / 2) + u * V;
+        } else {
+            first = p.d.rotary_dim + 2 * (u - p.turn_units) * V;
+            second = first + V < p.d.head_dim ? first + V : -1;
+            pair = -1;
         }
+    }
+
+    __device__ __forceinline__ void load()
+    {
+        a.word = __ldcs(reinterpret_cast<const decltype(a.word) *>(src + first));
+        if (second >= 0)
+            b.word = __ldcs(reinterpret_cast<const decltype(b.word) *>(src + second));
+    }
+
+    __device__ __forceinline__ void turn(const RotaryParams &p, const float2 *table)
+    {
+        if (pair < 0)
+            return;
+        const bool half = p.d.layout == RIKFAD_ROTARY_HALF;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float2 cs = table[pair + e];
+            // interleaved: pair e is elements 2 e and 2 e + 1 of the two vectors together
+            T &x = half ? a.v[e] : (2 * e < V ? a.v[2 * e % V] : b.v[2 * e % V]);
+            T &y = half ? b.v[e] : (2 * e + 1 < V ? a.v[(2 * e + 1) % V] : b.v[(2 * e + 1) % V]);
+            const float fx = to_f32(x), fy = to_f32(y);
+            x = from_f32<T>(fmaf(fx, cs.x, -fy * cs.y));
+            y = from_f32<T>(fmaf(fy, cs.x, fx * cs.y));
+        }
+    }
+
+    __device__ __forceinline__ void store() const
+    {
+        *reinterpret_cast<decltype(a.word) *>(dst + first) = a.word;
+        if (second >= 0)
+            *reinterpret_cast<decltype(b.word) *>(dst + second) = b.word;
+    }
+};
+
+// A block takes `tile` tokens: it forms their cosines and sines once, for all
+// heads, and its threads walk the tile's units, the next one's loads ahead of the
+// present one's arithmetic and the first one's ahead of the table.  blockIdx.y
+// splits the units of a tile where tokens are few.
+template <typename T, int V>
+__global__ void __launch_bounds__(kRotaryThreads) rikfad_rotary_kernel(const __grid_constant__ RotaryParams p)
+{
+    extern __shared__ float2 table[];
+    const int64_t tokens = p.d.batch * p.d.tokens, token0 = (int64_t)blockIdx.x * p.tile;
+    const int here = (int)min((int64_t)p.tile, tokens - token0);
+    const int work = here * p.heads * p.units, step = kRotaryThreads * gridDim.y;
+    int w = blockIdx.y * kRotaryThreads + threadIdx.x;
+    wait_for_predecessor();
+    Unit<T, V> unit;
+    if (w < work) {
+        unit.locate(p, token0, w);
+        unit.load();
+    }
+    const int pairs = p.d.rotary_dim / 2;
+    for (int i = threadIdx.x; i < here * pairs; i += kRotaryThreads) {
+        const int64_t at = token0 + i / pairs;
+        const int64_t batch = p.d.batch == 1 ? 0 : at / p.d.tokens, token = at - batch * p.d.tokens;
+        int64_t position = p.d.start + token;
+        if (p.d.positions) {
+            const int64_t k = batch * p.d.position_batch + token;
+            position = p.d.position_bytes == 4 ? (int64_t)static_cast<const int32_t *>(p.d.positions)[k]
+                                               : static_cast<const int64_t *>(p.d.positions)[k];
+        }
+        // the turn's fraction in [-1/2, 1/2), in half turns for sincospi
+        const uint64_t turn = (uint64_t)position * p.d.turns[i % pairs];
         float c, s;
-        angle(p, batch, token, slot, c, s);
-        const int i = p.d.layout == RIKFAD_ROTARY_HALF ? slot : 2 * slot;
-        const int j = p.d.layout == RIKFAD_ROTARY_HALF ? slot + pairs : 2 * slot + 1;
-        const float a = to_f32(src[i]), b = to_f32(src[j]);
-        dst[i] = from_f32<T>(fmaf(a, c, -b * s));
-        dst[j] = from_f32<T>(fmaf(b, c, a * s));
+        sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &s, &c);
+        table[i] = make_float2(c * p.magnitude, s * p.sine_sign);
+    }
+    __syncthreads();
+    allow_successor_launch();
+    while (w < work) {
+        Unit<T, V> next;
+        w += step;
+        if (w < work) {
+            next.locate(p, token0, w);
+            next.load();
+        }
+        unit.turn(p, table);
+        unit.store();
+        unit = next;
     }
 }
 
@@ -93,7 +189,7 @@ int check(const rikfad_rotary *p)
         return bad("position_bytes must be 4 or 8");
     for (int i = 0; i < p->nlists; ++i) {
         const rikfad_rotary_heads &l = p->lists[i];
-        if (l.heads < 0 || l.heads > (int64_t)1 << 24)
+        if (l.heads < 0 || l.heads > (int64_t)1 << 16)
             return bad("heads is out of range");
     }
     int device = -1;
@@ -131,17 +227,57 @@ int check(const rikfad_rotary *p)
     return rc;
 }
 
-template <typename T> cudaError_t launch(const RotaryParams &p, cudaStream_t s)
+template <typename T, int V> cudaError_t launch(RotaryParams p, cudaStream_t s)
 {
-    int64_t most = 0;
-    for (int i = 0; i < p.d.nlists; ++i)
-        most = std::max(most, p.d.lists[i].heads);
-    const int64_t work = p.d.batch * p.d.tokens * most * (p.d.head_dim - p.d.rotary_dim / 2);
-    if (work == 0)
+    const int rest = p.copy ? p.d.head_dim - p.d.rotary_dim : 0, pairs = p.d.rotary_dim / 2;
+    p.turn_units = pairs / V;
+    p.units = p.turn_units + (rest + 2 * V - 1) / (2 * V);
+    const int64_t per_token = (int64_t)p.heads * p.units, tokens = p.d.batch * p.d.tokens;
+    if (per_token == 0 || tokens == 0)
         return cudaSuccess;
-    const dim3 grid((unsigned)std::min<int64_t>((work + kRotaryThreads - 1) / kRotaryThreads, 152 * 16), (unsigned)p.d.nlists);
-    rikfad_rotary_kernel<T><<<grid, kRotaryThreads, 0, s>>>(p);
-    return cudaGetLastError();
+    // About four units for each thread, within the table's size.
+    const int64_t most = pairs ? std::max(1, kTableFloats / 2 / pairs) : 1 << 10;
+    p.tile = (int32_t)std::max<int64_t>(1, std::min(most, 4 * kRotaryThreads / per_token));
+    // Few tokens: smaller tiles, then several blocks for a tile, until the SMs have work.
+    while (p.tile > 1 && (tokens + p.tile - 1) / p.tile < 2 * kSms)
+        p.tile /= 2;
+    const int64_t tiles = (tokens + p.tile - 1) / p.tile;
+    const int64_t want = (p.tile * per_token + kRotaryThreads - 1) / kRotaryThreads;    // blocks of one unit a thread
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(want, 2 * kSms / tiles));
+    if (tiles > INT32_MAX || p.tile * per_token > INT32_MAX / 2)
+        return cudaErrorInvalidConfiguration;
+    return launch_chained(rikfad_rotary_kernel<T, V>, dim3((unsigned)tiles, (unsigned)splits), kRotaryThreads,
+                          sizeof(float2) * (size_t)p.tile * pairs, s, p);
+}
+
+// The widest vectors that the heads' layout and addresses allow: every part of a
+// head (half of the pairs, the elements beyond them) and every stride is a whole
+// number of vectors, and so are the addresses.
+template <typename T> cudaError_t launch(RotaryParams p, cudaStream_t s)
+{
+    uint64_t parts = (uint64_t)(p.d.rotary_dim / 2) | (uint64_t)(p.d.head_dim - p.d.rotary_dim);
+    uint64_t bytes = 0;
+    p.heads = 0;
+    p.copy = false;
+    for (int i = 0; i < p.d.nlists; ++i) {
+        const rikfad_rotary_heads &l = p.d.lists[i];
+        if (l.heads == 0)
+            continue;
+        p.heads += (int32_t)l.heads;
+        p.copy = p.copy || l.src != l.dst;
+        if (l.heads > 1)
+            parts |= (uint64_t)l.src_head | (uint64_t)l.dst_head;
+        if (p.d.tokens > 1)
+            parts |= (uint64_t)l.src_token | (uint64_t)l.dst_token;
+        if (p.d.batch > 1)
+            parts |= (uint64_t)l.src_batch | (uint64_t)l.dst_batch;
+        bytes |= (uint64_t)(uintptr_t)l.src | (uint64_t)(uintptr_t)l.dst;
+    }
+    parts |= bytes / sizeof(T);
+    if constexpr (sizeof(T) == 2)
+        if (parts % 8 == 0)
+            return launch<T, 8>(p, s);
+    return parts % 4 == 0 ? launch<T, 4>(p, s) : parts % 2 == 0 ? launch<T, 2>(p, s) : launch<T, 1>(p, s);
 }
 
 }  // namespace
@@ -174,6 +310,7 @@ RIKFAD_API int rikfad_rotary_apply(const rikfad_rotary *p, void *stream)
     RotaryParams r{};
     r.d = *p;
     r.magnitude = (float)p->magnitude;
+    r.sine_sign = p->inverse ? -r.magnitude : r.magnitude;
     const cudaStream_t s = (cudaStream_t)stream;
     e = p->dtype == RIKFAD_F32    ? launch<float>(r, s)
         : p->dtype == RIKFAD_BF16 ? launch<__nv_bfloat16>(r, s)
