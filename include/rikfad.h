@@ -456,11 +456,12 @@ RIKFAD_API size_t rikfad_clip_workspace_bytes(rikfad_clip c);
  *             when the types are equal (in place: nothing is written when c = 1);
  *             otherwise outputs overlap no gradient.  NULL: norms only
  *   max_norm  >= 0, not NaN (read only with out)
- *   norms     device, ntensors + 1 floats: norm_t, then total
+ *   norms     device, ntensors floats: norm_t
+ *   total     device, one float
  * Nothing is synchronised or allocated; the call can be captured in a graph.
  */
 RIKFAD_API int rikfad_clip_run(rikfad_clip c, const void *const *grad, void *const *out, double max_norm,
-                               float *norms, void *stream);
+                               float *norms, float *total, void *stream);
 
 /*
  * Residual sum of a transformer block with the norms around it, for `rows`
@@ -475,8 +476,8 @@ RIKFAD_API int rikfad_clip_run(rikfad_clip c, const void *const *grad, void *con
  *   dx, dz, dgate and those of the weights and biases.
  *
  * Every member of the form rikfad_rows points to rows of `cols` contiguous
- * elements, `stride` elements apart (>= cols where rows > 1).  Sizes: rows >= 0,
- * 1 <= cols <= 32768.
+ * elements, `stride` elements apart (>= cols where rows > 1).  Sizes:
+ * 0 <= rows <= 2^34, 1 <= cols <= 32768.
  *   x, u, du, dx     residual_dtype (RIKFAD_F32 or dtype)
  *   z, h, dh, dz     dtype
  *   gate, dgate      gate_dtype (RIKFAD_F32 or dtype); gate row i serves rows
@@ -548,8 +549,8 @@ RIKFAD_API size_t rikfad_residual_norm_workspace(const rikfad_residual_norm *p);
  *           in dst, strides in elements.  src = dst with equal strides rotates
  *           in place; otherwise dst overlaps no src.  Pointers aligned to the
  *           element type
- * batch, tokens, heads >= 0; 1 <= head_dim <= 4096; rotary_dim even,
- * 0 <= rotary_dim <= head_dim.
+ * batch, tokens, heads >= 0, heads <= 65536, batch x tokens <= 2^40; 1 <= head_dim <= 4096;
+ * rotary_dim even, 0 <= rotary_dim <= head_dim.
  */
 enum rikfad_rotary_layout { RIKFAD_ROTARY_HALF = 0, RIKFAD_ROTARY_INTERLEAVED = 1 };
 

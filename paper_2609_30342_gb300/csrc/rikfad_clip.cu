@@ -2,11 +2,15 @@
 //   norm_t = ||g_t||_2,  total = sqrt(sum_t norm_t^2),
 //   out_t = c g_t,  c = max_norm / total if max_norm < total < inf, else 1.
 //
-// The list is laid end to end and cut into equal shares, one per block, so that
-// a list of a few large and many small tensors keeps every SM busy to the end; a
-// share's part of one tensor is a segment.  The first kernel leaves one sum of
-// squares per segment, the second joins them in segment order (in float64) into
-// the norms and the factor c, the third scales.
+// The list is laid end to end and cut into equal shares, one per resident block,
+// so that a list of a few large and many small tensors keeps every SM busy to the
+// end; a share's part of one tensor is a segment.  The first kernel leaves one
+// sum of squares per segment.  The block that finishes a tensor's last segment adds
+// them up in order (float64), the block that finishes last adds the tensors and
+// forms c: one block joining everything would read its sums for tens of
+// microseconds after the others.  The second kernel scales.  It walks
+// every share from its end, so that what the first one read last is read from the
+// L2 cache.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -27,9 +31,13 @@ namespace {
 
 constexpr int kClipThreads = 256;
 constexpr int kClipWarps = kClipThreads / 32;
-constexpr int kClipBlocksPerSm = 2048 / kClipThreads;
+constexpr int kClipBlocksPerSm = 6;
+// 8-element loads in flight per thread: 64 bytes.
+template <typename T> constexpr int kClipUnroll = sizeof(T) == 4 ? 2 : 4;
 constexpr int64_t kMinShare = 8192;     // elements of the smallest share
 constexpr int64_t kShareStep = 64;      // shares begin at multiples of this within a tensor
+constexpr int64_t kMaxShare = 1 << 30;  // elements of the largest share (lists far beyond any memory are refused)
+constexpr int kShortSegment = 2048;     // elements of a segment that one warp reads
 constexpr int kMaxTensors = 1024;       // of one launch
 
 // Elements [begin, end) of tensor `tensor` (an index into the launch's pointers).
@@ -37,11 +45,15 @@ struct Segment {
     int64_t begin, end;
     int32_t tensor;
     int16_t grad_dtype, out_dtype;
+    int32_t list_tensor;            // index in the list
+    int32_t first, count;           // the tensor's segments
+    int32_t unused;                 // to 48 bytes
 };
 
 // What the kernels of a call leave for one another.
 struct ClipResult {
     float scale;
+    unsigned int blocks_done;       // of this call; the last block leaves 0
 };
 
 struct ClipParams {
@@ -49,7 +61,12 @@ struct ClipParams {
     const int32_t *block_segment;   // first segment of every block of the list, and the end
     int32_t block0;                 // the launch's first block
     double *partial;                // one per segment
+    double *tensor_sum;             // one per tensor of the list (empty ones stay 0)
+    unsigned int *tensor_done;      // its finished segments of this call; left at 0
     ClipResult *result;
+    int32_t ntensors, total_blocks; // of the list
+    double max_norm;
+    float *norms, *total;
 };
 
 // The pointers of a launch's tensors travel in the kernel's parameters: no copy
@@ -59,135 +76,242 @@ template <int CAP> struct ClipPointers {
     void *out[CAP];
 };
 
+template <typename T> __device__ __forceinline__ void add_squares(const Raw8<T> &r, float mul, float (&acc)[4])
+{
+    float v[8];
+    unpack8(r, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v[e] *= mul;
+        acc[e & 3] = fmaf(v[e], v[e], acc[e & 3]);
+    }
+}
+
 // Sum of squares of the elements of a segment that this thread reads, times
-// mul^2 (mul a power of two).
-template <typename T> __device__ float segment_squares(const T *g, int64_t n, float mul)
+// mul^2 (mul a power of two).  The first sums take at most 64 squares before they
+// move to the second: an error of a few units of 2^-24 whatever the share's
+// length.  Float64 sums would do without, but float64 additions are issued at a
+// 64th of the float32 rate: with them in every thread and in the block's tree the
+// kernel took 37 us instead of 14 for 60 MB of bfloat16 gradients.
+template <typename T> __device__ float segment_squares(const T *g, int n, float mul, int thread, int threads)
 {
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    int64_t done = 0;
+    float total = 0.f;
+    int done = 0, k = 0;
     if (aligned16(g)) {
-        const int64_t chunks = n / 8;
-        for (int64_t i = threadIdx.x; i < chunks; i += kClipThreads) {
-            float v[8];
-            unpack8(load_raw8(g + i * 8), v);
+        const int chunks = n / 8;
+        for (int i = thread; i < chunks; i += kClipUnroll<T> * threads) {
+            Raw8<T> r[kClipUnroll<T>] = {};        // a last, partial round is one round trip as well
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[e] *= mul;
-                acc[e & 3] = fmaf(v[e], v[e], acc[e & 3]);
+            for (int j = 0; j < kClipUnroll<T>; ++j)
+                if (i + j * threads < chunks)
+                    r[j] = load_raw8(g + (int64_t)(i + j * threads) * 8);
+#pragma unroll
+            for (int j = 0; j < kClipUnroll<T>; ++j)
+                add_squares(r[j], mul, acc);
+            if (++k * kClipUnroll<T> == 32) {
+                k = 0;
+                total += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+                acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
             }
         }
         done = chunks * 8;
+        k = 0;
     }
-    for (int64_t i = done + threadIdx.x; i < n; i += kClipThreads) {
+    for (int i = done + thread; i < n; i += threads) {
         const float v = to_f32(g[i]) * mul;
-        acc[0] = fmaf(v, v, acc[0]);
-    }
-    return (acc[0] + acc[1]) + (acc[2] + acc[3]);
-}
-
-__device__ float segment_squares(const void *grad, const Segment &s, float mul)
-{
-    const int64_t n = s.end - s.begin;
-    if (s.grad_dtype == RIKFAD_F32)
-        return segment_squares(static_cast<const float *>(grad) + s.begin, n, mul);
-    if (s.grad_dtype == RIKFAD_BF16)
-        return segment_squares(static_cast<const __nv_bfloat16 *>(grad) + s.begin, n, mul);
-    return segment_squares(static_cast<const __half *>(grad) + s.begin, n, mul);
-}
-
-// The block's total of `v`, in every thread: fixed trees in float64.
-__device__ double block_total(float v, double *red)
-{
-    double d = v;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        d += __shfl_xor_sync(0xffffffffu, d, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0)
-        red[threadIdx.x >> 5] = d;
-    __syncthreads();
-    d = 0.0;
-#pragma unroll
-    for (int w = 0; w < kClipWarps; ++w)
-        d += red[w];
-    return d;
-}
-
-template <int CAP>
-__global__ void __launch_bounds__(kClipThreads) rikfad_clip_squares_kernel(ClipParams a, const __grid_constant__ ClipPointers<CAP> ptrs)
-{
-    __shared__ double red[kClipWarps];
-    const int block = a.block0 + blockIdx.x;
-    for (int q = a.block_segment[block]; q < a.block_segment[block + 1]; ++q) {
-        const Segment s = a.segments[q];
-        const void *g = ptrs.grad[s.tensor];
-        double sum = block_total(segment_squares(g, s, 1.f), red);
-        // Squares that left float32's range (an infinite sum), or may have lost
-        // much below it (1e-30 against a smallest square of 1e-45): once more,
-        // with elements scaled by a power of two.  A true infinity stays one.
-        if (sum > 1e38 || sum < 1e-30) {
-            const bool big = sum > 1.0;
-            const float mul = big ? 0x1p-80f : 0x1p100f;
-            sum = block_total(segment_squares(g, s, mul), red) * (big ? 0x1p160 : 0x1p-200);
+        acc[k & 3] = fmaf(v, v, acc[k & 3]);
+        if (++k == 256) {
+            k = 0;
+            total += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+            acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
         }
-        if (threadIdx.x == 0)
-            a.partial[q] = sum;
     }
+    return total + ((acc[0] + acc[1]) + (acc[2] + acc[3]));
 }
 
-// Segment sums to tensor norms, their total and the factor, by one block.
-__global__ void __launch_bounds__(kClipThreads) rikfad_clip_join_kernel(ClipParams a, const int32_t *tensor_segment, int ntensors,
-                                                                        double max_norm, float *norms)
+__device__ float segment_squares(const void *grad, const Segment &s, float mul, int thread, int threads)
 {
-    __shared__ double red[kClipWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    double total = 0.0;             // of the warp's tensors, the same in its lanes
-    for (int t = warp; t < ntensors; t += kClipWarps) {
+    const int n = (int)(s.end - s.begin);
+    if (s.grad_dtype == RIKFAD_F32)
+        return segment_squares(static_cast<const float *>(grad) + s.begin, n, mul, thread, threads);
+    if (s.grad_dtype == RIKFAD_BF16)
+        return segment_squares(static_cast<const __nv_bfloat16 *>(grad) + s.begin, n, mul, thread, threads);
+    return segment_squares(static_cast<const __half *>(grad) + s.begin, n, mul, thread, threads);
+}
+
+// The sums of a block's segments [q0, q0 + n), n <= 32: lane i of warp 0 stores
+// segment q0 + i and, if it is its tensor's last, adds up the tensor.  The order
+// of the additions is the segments', whichever block makes them.
+__device__ void finish_segments(const ClipParams &a, const Segment *segments, int q0, int n, double sum)
+{
+    const int lane = threadIdx.x;
+    const bool mine = lane < n;
+    const int count = mine ? segments[lane].count : 0, tensor = mine ? segments[lane].list_tensor : 0;
+    bool last = count == 1;
+    if (count > 1) {
+        a.partial[q0 + lane] = sum;
+        __threadfence();
+        last = atomicInc(a.tensor_done + tensor, (unsigned)count - 1) == (unsigned)count - 1;
+        __threadfence();
+    }
+    for (unsigned todo = __ballot_sync(0xffffffffu, last && count > 1); todo; todo &= todo - 1) {
+        const int i = __ffs(todo) - 1;
+        const int first = segments[i].first, parts = segments[i].count;
         double d = 0.0;
-        for (int q = tensor_segment[t] + lane; q < tensor_segment[t + 1]; q += 32)
-            d += a.partial[q];
+#pragma unroll 4
+        for (int k = lane; k < parts; k += 32)
+            d += __ldcg(a.partial + first + k);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1)
             d += __shfl_xor_sync(0xffffffffu, d, o);
-        if (lane == 0)
-            norms[t] = (float)sqrt(d);
-        total += d;
+        if (lane == i)
+            sum = d;
     }
-    if (lane == 0)
-        red[warp] = total;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        total = 0.0;
-        for (int w = 0; w < kClipWarps; ++w)
-            total += red[w];
-        total = sqrt(total);
-        norms[ntensors] = (float)total;
-        a.result->scale = total > max_norm && total < (double)INFINITY ? (float)(max_norm / total) : 1.f;
+    if (last) {
+        a.tensor_sum[tensor] = sum;
+        a.norms[tensor] = (float)sqrt(sum);
     }
 }
 
-template <typename T, typename U> __device__ void scale_segment(const T *g, U *out, int64_t n, float c)
+// The total and the factor, by the first warp of the block that finishes last.
+__device__ void finish_list(const ClipParams &a)
 {
-    int64_t done = 0;
-    if (aligned16(g) && aligned16(out)) {
-        const int64_t chunks = n / 8;
-        for (int64_t i = threadIdx.x; i < chunks; i += kClipThreads) {
-            float v[8];
-            unpack8(load_raw8(g + i * 8), v);
+    const int lane = threadIdx.x;
+    double total = 0.0;
+#pragma unroll 8
+    for (int t = lane; t < a.ntensors; t += 32)
+        total += __ldcg(a.tensor_sum + t);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[e] *= c;
-            store_raw8_cs(out + i * 8, pack8(v, U()));
-        }
-        done = chunks * 8;
+    for (int o = 16; o > 0; o >>= 1)
+        total += __shfl_xor_sync(0xffffffffu, total, o);
+    if (lane == 0) {
+        total = sqrt(total);
+        *a.total = (float)total;
+        a.result->scale = total > a.max_norm && total < (double)INFINITY ? (float)(a.max_norm / total) : 1.f;
     }
-    for (int64_t i = done + threadIdx.x; i < n; i += kClipThreads)
+}
+
+// A block walks its segments without a barrier, so that the loads of the next one
+// follow at once; every warp leaves its sum of every segment in shared memory, and
+// warp 0 joins up to 32 segments at a time.  Short segments (vectors between a
+// list's matrices) are one warp's each, all of them under way together: as the
+// block's work, one after the other, each costs a round trip to memory.
+template <int CAP>
+__global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm)
+    rikfad_clip_squares_kernel(const __grid_constant__ ClipParams a, const __grid_constant__ ClipPointers<CAP> ptrs)
+{
+    __shared__ Segment segments[32];
+    __shared__ float red[kClipWarps][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int block = a.block0 + blockIdx.x;
+    wait_for_predecessor();
+    const int end = a.block_segment[block + 1];
+    for (int q0 = a.block_segment[block]; q0 < end; q0 += 32) {
+        const int n = min(32, end - q0);
+        __syncthreads();
+        if (threadIdx.x < n)
+            segments[threadIdx.x] = a.segments[q0 + threadIdx.x];
+        __syncthreads();
+        for (int pass = 0; pass < 2; ++pass)
+            for (int i = 0; i < n; ++i) {
+                const bool brief = segments[i].end - segments[i].begin <= kShortSegment;
+                if (brief != (pass == 0))
+                    continue;
+                float sum = 0.f;
+                if (!brief)
+                    sum = warp_sum(segment_squares(ptrs.grad[segments[i].tensor], segments[i], 1.f, threadIdx.x, kClipThreads));
+                else if (i % kClipWarps == warp)
+                    sum = warp_sum(segment_squares(ptrs.grad[segments[i].tensor], segments[i], 1.f, lane, 32));
+                if (lane == 0)
+                    red[warp][i] = sum;
+            }
+        __syncthreads();
+        // Squares that left float32's range (an infinite sum), or may have lost
+        // much below it (1e-30 against a smallest square of 1e-45): once more, with
+        // elements scaled by a power of two.  A true infinity stays one.  Every
+        // warp comes to the same verdicts.
+        float total = 0.f;
+#pragma unroll
+        for (int w = 0; w < kClipWarps; ++w)
+            total += lane < n ? red[w][lane] : 1.f;
+        double sum = total;
+        const bool big = total > 1e38f;
+        for (unsigned redo = __ballot_sync(0xffffffffu, big || total < 1e-30f); redo; redo &= redo - 1) {
+            const int i = __ffs(redo) - 1;
+            const bool down = __shfl_sync(0xffffffffu, big, i);
+            const float part = warp_sum(segment_squares(ptrs.grad[segments[i].tensor], segments[i], down ? 0x1p-80f : 0x1p100f,
+                                                        threadIdx.x, kClipThreads));
+            __syncthreads();
+            if (lane == 0)
+                red[warp][32] = part;
+            __syncthreads();
+            if (lane == i) {
+                total = 0.f;
+#pragma unroll
+                for (int w = 0; w < kClipWarps; ++w)
+                    total += red[w][32];
+                sum = total * (down ? 0x1p160 : 0x1p-200);
+            }
+        }
+        if (warp == 0)
+            finish_segments(a, segments, q0, n, sum);
+    }
+    allow_successor_launch();
+    if (warp == 0) {
+        bool last = false;
+        __syncwarp();               // the lanes' stores before lane 0's fence
+        if (lane == 0) {
+            __threadfence();
+            last = atomicInc(&a.result->blocks_done, (unsigned)a.total_blocks - 1) == (unsigned)a.total_blocks - 1;
+            __threadfence();
+        }
+        if (__shfl_sync(0xffffffffu, last, 0))
+            finish_list(a);
+    }
+}
+
+template <typename T, typename U> __device__ __forceinline__ void scale8(const Raw8<T> &r, U *out, float c)
+{
+    float v[8];
+    unpack8(r, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] *= c;
+    store_raw8_cs(out, pack8(v, U()));
+}
+
+// out = c g over a segment, from its end.
+template <typename T, typename U> __device__ void scale_segment(const T *g, U *out, int n, float c)
+{
+    const bool wide = aligned16(g) && aligned16(out);
+    const int chunks = wide ? n / 8 : 0;
+    for (int i = n - 1 - (int)threadIdx.x; i >= chunks * 8; i -= kClipThreads)
         out[i] = from_f32<U>(to_f32(g[i]) * c);
+    g += (int64_t)(chunks - 1 - (int)threadIdx.x) * 8;
+    out += (int64_t)(chunks - 1 - (int)threadIdx.x) * 8;
+    int left = chunks - (int)threadIdx.x;
+    for (; left > (kClipUnroll<T> - 1) * kClipThreads; left -= kClipUnroll<T> * kClipThreads) {
+        Raw8<T> r[kClipUnroll<T>];
+#pragma unroll
+        for (int j = 0; j < kClipUnroll<T>; ++j)
+            r[j] = load_raw8_cs(g - j * kClipThreads * 8);
+#pragma unroll
+        for (int j = 0; j < kClipUnroll<T>; ++j)
+            scale8(r[j], out - j * kClipThreads * 8, c);
+        g -= kClipUnroll<T> * kClipThreads * 8;
+        out -= kClipUnroll<T> * kClipThreads * 8;
+    }
+    for (; left > 0; left -= kClipThreads) {
+        scale8(load_raw8_cs(g), out, c);
+        g -= kClipThreads * 8;
+        out -= kClipThreads * 8;
+    }
 }
 
 template <typename T> __device__ void scale_segment(const T *g, void *out, const Segment &s, float c)
 {
-    const int64_t n = s.end - s.begin;
+    const int n = (int)(s.end - s.begin);
     if (s.out_dtype == RIKFAD_F32)
         scale_segment(g + s.begin, static_cast<float *>(out) + s.begin, n, c);
     else if (s.out_dtype == RIKFAD_BF16)
@@ -197,11 +321,13 @@ template <typename T> __device__ void scale_segment(const T *g, void *out, const
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(kClipThreads) rikfad_clip_scale_kernel(ClipParams a, const __grid_constant__ ClipPointers<CAP> ptrs)
+__global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm)
+    rikfad_clip_scale_kernel(const __grid_constant__ ClipParams a, const __grid_constant__ ClipPointers<CAP> ptrs)
 {
+    wait_for_predecessor();
     const float c = a.result->scale;
     const int block = a.block0 + blockIdx.x;
-    for (int q = a.block_segment[block]; q < a.block_segment[block + 1]; ++q) {
+    for (int q = a.block_segment[block + 1] - 1; q >= a.block_segment[block]; --q) {
         const Segment s = a.segments[q];
         const void *g = ptrs.grad[s.tensor];
         void *out = ptrs.out[s.tensor];
@@ -226,6 +352,7 @@ struct Part {
 struct rikfad_clip_s {
     int device = 0;
     int ntensors = 0;
+    int blocks = 0;
     std::vector<int64_t> numel;
     std::vector<int> grad_dtype, out_dtype;
     std::vector<Part> parts;
@@ -233,8 +360,9 @@ struct rikfad_clip_s {
     std::vector<void *> seen_out;
     Segment *d_segments = nullptr;
     int32_t *d_block_segment = nullptr;
-    int32_t *d_tensor_segment = nullptr;
     double *d_partial = nullptr;
+    double *d_tensor_sum = nullptr;
+    unsigned int *d_tensor_done = nullptr;
     ClipResult *d_result = nullptr;
     size_t workspace = 0;
 };
@@ -243,8 +371,8 @@ namespace {
 
 void release(rikfad_clip c)
 {
-    for (void *p : {(void *)c->d_segments, (void *)c->d_block_segment, (void *)c->d_tensor_segment,
-                    (void *)c->d_partial, (void *)c->d_result})
+    for (void *p : {(void *)c->d_segments, (void *)c->d_block_segment, (void *)c->d_partial,
+                    (void *)c->d_tensor_sum, (void *)c->d_tensor_done, (void *)c->d_result})
         counted_free(p);
     delete c;
 }
@@ -264,8 +392,8 @@ template <typename T> int allocate(rikfad_clip c, T **dst, size_t count, const T
 }
 
 // Cuts tensors [t0, t1) into at most `most` shares of equal size.
-void plan_part(const rikfad_clip c, int t0, int t1, int64_t most, std::vector<Segment> &segments,
-               std::vector<int32_t> &block_segment, std::vector<int32_t> &tensor_segment)
+bool plan_part(const rikfad_clip c, int t0, int t1, int64_t most, std::vector<Segment> &segments,
+               std::vector<int32_t> &block_segment)
 {
     double n = 0.0;
     for (int t = t0; t < t1; ++t)
@@ -273,21 +401,27 @@ void plan_part(const rikfad_clip c, int t0, int t1, int64_t most, std::vector<Se
     const double want = std::min((double)most, std::ceil(n / (double)kMinShare));
     const int64_t share = std::max<int64_t>(
         kShareStep, (int64_t)std::ceil(n / std::max(want, 1.0) / (double)kShareStep) * kShareStep);
+    if (share > kMaxShare)
+        return false;
     int64_t room = 0;       // left in the open share
     for (int t = t0; t < t1; ++t) {
-        tensor_segment.push_back((int32_t)segments.size());
-        for (int64_t at = 0; at < c->numel[t];) {
+        const int32_t first = (int32_t)segments.size();
+        int64_t at = 0;
+        do {                        // an empty tensor has one empty segment
             if (room <= 0) {
                 block_segment.push_back((int32_t)segments.size());
                 room = share;
             }
             // a cut at a multiple of kShareStep, or the tensor's end
             const int64_t take = std::min(c->numel[t] - at, (room + kShareStep - 1) / kShareStep * kShareStep);
-            segments.push_back({at, at + take, t - t0, (int16_t)c->grad_dtype[t], (int16_t)c->out_dtype[t]});
+            segments.push_back({at, at + take, t - t0, (int16_t)c->grad_dtype[t], (int16_t)c->out_dtype[t], t, first, 0, 0});
             at += take;
             room -= take;
-        }
+        } while (at < c->numel[t]);
+        for (size_t q = first; q < segments.size(); ++q)
+            segments[q].count = (int32_t)segments.size() - first;
     }
+    return true;
 }
 
 int create(rikfad_clip c, const int64_t *numel, const int *grad_dtype, const int *out_dtype, int ntensors)
@@ -305,21 +439,30 @@ int create(rikfad_clip c, const int64_t *numel, const int *grad_dtype, const int
     c->seen_grad.assign(ntensors, nullptr);
     c->seen_out.assign(ntensors, nullptr);
     std::vector<Segment> segments;
-    std::vector<int32_t> block_segment, tensor_segment;
+    std::vector<int32_t> block_segment;
     for (int t0 = 0; t0 < ntensors; t0 += kMaxTensors) {
         const int t1 = std::min(ntensors, t0 + kMaxTensors);
         const int b0 = (int)block_segment.size();
-        plan_part(c, t0, t1, (int64_t)sms * kClipBlocksPerSm, segments, block_segment, tensor_segment);
+        if (!plan_part(c, t0, t1, (int64_t)sms * kClipBlocksPerSm, segments, block_segment))
+            return report_error(RIKFAD_ERR_ARG, "the tensors are too large");
         if ((int)block_segment.size() > b0)
             c->parts.push_back({t0, t1, b0, (int)block_segment.size()});
     }
+    if (c->parts.empty()) {         // no tensors: one block without segments
+        c->parts.push_back({0, 0, 0, 1});
+        block_segment.push_back(0);
+    }
+    c->blocks = (int)block_segment.size();
     block_segment.push_back((int32_t)segments.size());
-    tensor_segment.push_back((int32_t)segments.size());
     int rc = allocate(c, &c->d_segments, segments.size(), segments.data());
     if (!rc) rc = allocate(c, &c->d_block_segment, block_segment.size(), block_segment.data());
-    if (!rc) rc = allocate(c, &c->d_tensor_segment, tensor_segment.size(), tensor_segment.data());
     if (!rc) rc = allocate<double>(c, &c->d_partial, segments.size(), nullptr);
-    if (!rc) rc = allocate<ClipResult>(c, &c->d_result, 1, nullptr);
+    const std::vector<double> zeros(ntensors, 0.0);
+    if (!rc) rc = allocate(c, &c->d_tensor_sum, zeros.size(), zeros.data());
+    const std::vector<unsigned int> none_done(ntensors, 0u);
+    if (!rc) rc = allocate(c, &c->d_tensor_done, none_done.size(), none_done.data());
+    const ClipResult none = {1.f, 0u};
+    if (!rc) rc = allocate(c, &c->d_result, 1, &none);
     return rc;
 }
 
@@ -332,11 +475,8 @@ template <int CAP> int launch(rikfad_clip c, const Part &part, const ClipParams 
         ptrs.out[t - part.tensor0] = out ? out[t] : nullptr;
     }
     const dim3 blocks((unsigned)(part.block1 - part.block0));
-    if (scale)
-        rikfad_clip_scale_kernel<CAP><<<blocks, kClipThreads, 0, s>>>(a, ptrs);
-    else
-        rikfad_clip_squares_kernel<CAP><<<blocks, kClipThreads, 0, s>>>(a, ptrs);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_chained(scale ? rikfad_clip_scale_kernel<CAP> : rikfad_clip_squares_kernel<CAP>, blocks,
+                                         kClipThreads, 0, s, a, ptrs);
     return e == cudaSuccess ? RIKFAD_OK : report_cuda(e, scale ? "launch rikfad_clip_scale_kernel" : "launch rikfad_clip_squares_kernel");
 }
 
@@ -418,7 +558,7 @@ RIKFAD_API void rikfad_clip_destroy(rikfad_clip c)
 RIKFAD_API size_t rikfad_clip_workspace_bytes(rikfad_clip c) { return c ? c->workspace : 0; }
 
 RIKFAD_API int rikfad_clip_run(rikfad_clip c, const void *const *grad, void *const *out, double max_norm, float *norms,
-                               void *stream)
+                               float *total, void *stream)
 {
     RK_ENTRY_BEGIN
     if (c == nullptr)
@@ -431,13 +571,15 @@ RIKFAD_API int rikfad_clip_run(rikfad_clip c, const void *const *grad, void *con
         return report_error(RIKFAD_ERR_STATE, "current CUDA device differs from the handle's device");
     if (c->ntensors > 0 && grad == nullptr)
         return report_error(RIKFAD_ERR_ARG, "grad is NULL");
-    if (norms == nullptr)
-        return report_error(RIKFAD_ERR_ARG, "norms is NULL");
-    if ((uintptr_t)norms % sizeof(float))
-        return report_error(RIKFAD_ERR_ALIGN, "norms is not aligned");
+    if (total == nullptr || (c->ntensors > 0 && norms == nullptr))
+        return report_error(RIKFAD_ERR_ARG, "norms or total is NULL");
+    if ((uintptr_t)norms % sizeof(float) || (uintptr_t)total % sizeof(float))
+        return report_error(RIKFAD_ERR_ALIGN, "norms or total is not aligned");
     if (out && !(max_norm >= 0))
         return report_error(RIKFAD_ERR_ARG, "max_norm must be >= 0");
-    int rc = check_address(norms, dev, "norms");
+    int rc = check_address(total, dev, "total");
+    if (!rc && c->ntensors > 0)
+        rc = check_address(norms, dev, "norms");
     for (int t = 0; !rc && t < c->ntensors; ++t) {
         if (c->numel[t] == 0)
             continue;
@@ -462,11 +604,15 @@ RIKFAD_API int rikfad_clip_run(rikfad_clip c, const void *const *grad, void *con
     a.block_segment = c->d_block_segment;
     a.partial = c->d_partial;
     a.result = c->d_result;
+    a.tensor_sum = c->d_tensor_sum;
+    a.tensor_done = c->d_tensor_done;
+    a.ntensors = c->ntensors;
+    a.total_blocks = c->blocks;
+    a.max_norm = max_norm;
+    a.norms = norms;
+    a.total = total;
     if ((rc = launch_parts(c, a, grad, out, false, s)))
         return rc;
-    rikfad_clip_join_kernel<<<1, kClipThreads, 0, s>>>(a, c->d_tensor_segment, c->ntensors, max_norm, norms);
-    if ((e = cudaGetLastError()) != cudaSuccess)
-        return report_cuda(e, "launch rikfad_clip_join_kernel");
     return out ? launch_parts(c, a, grad, out, true, s) : RIKFAD_OK;
     RK_ENTRY_END
 }

@@ -31,6 +31,9 @@ class ClipPointers:
     def __init__(self, grads, out, grad_array, out_array):
         self.keep = (grads, out)
         self.grads, self.out = grad_array, out_array
+        self.device = next((t.device for t in grads if t.is_cuda), None)
+        if self.device is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
 
 
 class GradientClipper:
@@ -93,15 +96,17 @@ class GradientClipper:
         return ClipPointers(grads, out, g, o)
 
     def _run(self, ptrs, out, max_norm, stream):
-        n = len(self.numels)
-        device = next((t.device for t in ptrs.keep[0] if t.is_cuda), torch.device("cuda", torch.cuda.current_device()))
-        res = torch.empty(n + 1, dtype=torch.float32, device=device)
-        s = torch.cuda.current_stream(device) if stream is None else stream
-        if stream is not None and not isinstance(stream, int):
-            res.record_stream(stream)
-        rikfad._check(rikfad.lib().rikfad_clip_run(self.handle, ptrs.grads, out, max_norm, res.data_ptr(),
-                                                   rikfad._stream_ptr(s)))
-        return res[n], res[:n]
+        device = ptrs.device
+        total = torch.empty((), dtype=torch.float32, device=device)
+        norms = torch.empty(len(self.numels), dtype=torch.float32, device=device)
+        if stream is None:
+            stream = torch.cuda.current_stream(device)
+        elif not isinstance(stream, int):
+            total.record_stream(stream)
+            norms.record_stream(stream)
+        rikfad._check(rikfad.lib().rikfad_clip_run(self.handle, ptrs.grads, out, max_norm, norms.data_ptr(),
+                                                   total.data_ptr(), rikfad._stream_ptr(stream)))
+        return total, norms
 
     def norm(self, grads=None, stream=None, ptrs=None):
         """(total, norms): the 2-norm of all gradients (a scalar CUDA tensor) and of each, enqueued on ``stream``."""

@@ -101,7 +101,7 @@ SIGNATURES = [
                                           ctypes.POINTER(_VP)]),
     ("rikfad_clip_destroy", None, [_VP]),
     ("rikfad_clip_workspace_bytes", ctypes.c_size_t, [_VP]),
-    ("rikfad_clip_run", ctypes.c_int, [_VP, _PP, _PP, ctypes.c_double, _VP, _VP]),
+    ("rikfad_clip_run", ctypes.c_int, [_VP, _PP, _PP, ctypes.c_double, _VP, _VP, _VP]),
     ("rikfad_residual_norm_forward", ctypes.c_int, [_VP, _VP]),
     ("rikfad_residual_norm_backward", ctypes.c_int, [_VP, _VP]),
     ("rikfad_residual_norm_workspace", ctypes.c_size_t, [_VP]),

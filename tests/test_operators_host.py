@@ -33,7 +33,7 @@ def test_clip_null_arguments():
     assert L.rikfad_clip_create(None, None, None, 2, ctypes.byref(ctypes.c_void_p())) == rikfad.ERR_ARG
     assert L.rikfad_clip_create(None, None, None, -1, ctypes.byref(ctypes.c_void_p())) == rikfad.ERR_ARG
     assert L.rikfad_clip_create(None, None, None, 0, None) == rikfad.ERR_ARG
-    assert L.rikfad_clip_run(None, None, None, 1.0, None, None) == rikfad.ERR_ARG
+    assert L.rikfad_clip_run(None, None, None, 1.0, None, None, None) == rikfad.ERR_ARG
     L.rikfad_clip_destroy(None)
     assert L.rikfad_clip_workspace_bytes(None) == 0
 
