@@ -1,13 +1,7 @@
-// rikfad_norm.cu -- residual sum of a transformer block with the norms around it,
-//   n = post(z),  u = a x + b gate (.) n,  h = pre(u),
-// and its gradients.  With y2 = (z - m2) r2 and y1 = (u - m1) r1 (m = 0 for an
-// RMS norm) and given du, dh:
-//   g1 = dh w1,  e = du + r1 (g1 - [mean g1] - y1 mean(g1 y1))   ([.]: layer norm)
-//   dx = a e,  dgate = sum over the gate's rows of b e n,  q = b gate e
-//   g2 = q w2,  dz = r2 (g2 - [mean g2] - y2 mean(g2 y2))
-//   dw1 = sum dh y1,  db1 = sum dh,  dw2 = sum q y2,  db2 = sum q.
-// The backward kernels form u again from x, z and the gate: the same bytes as
-// reading u, without the rounding that a stored u has.
+// rikfad_norm.cu -- residual sum of a transformer block with the norms around it:
+// argument checks, workspace and launch shapes.  The mathematics and the kernels
+// are in rikfad_norm_kernels.cuh, instantiated per element type in
+// rikfad_norm_f32.cu, rikfad_norm_bf16.cu and rikfad_norm_f16.cu.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -17,237 +11,11 @@
 
 #include "rikfad.h"
 #include "rikfad_host.hpp"
-#include "rikfad_kernels.cuh"
-#include "rikfad_types.cuh"
+#include "rikfad_norm.hpp"
 
 using namespace rikfad;
 
 namespace {
-
-constexpr int kNormThreads = 256;
-
-// Element i of an array of a type known at run time.
-__device__ __forceinline__ float get(const void *p, int dtype, int64_t i)
-{
-    return dtype == RIKFAD_F32    ? static_cast<const float *>(p)[i]
-           : dtype == RIKFAD_BF16 ? to_f32(static_cast<const __nv_bfloat16 *>(p)[i])
-                                  : to_f32(static_cast<const __half *>(p)[i]);
-}
-
-__device__ __forceinline__ void put(void *p, int dtype, int64_t i, float v)
-{
-    if (dtype == RIKFAD_F32)
-        static_cast<float *>(p)[i] = v;
-    else if (dtype == RIKFAD_BF16)
-        static_cast<__nv_bfloat16 *>(p)[i] = from_f32<__nv_bfloat16>(v);
-    else
-        static_cast<__half *>(p)[i] = from_f32<__half>(v);
-}
-
-struct NormParams {
-    rikfad_residual_norm d;
-    float a, b, post_eps, pre_eps;
-    float *means;       // backward: 4 floats a row (mean g1, mean g1 y1, mean g2, mean g2 y2)
-};
-
-__device__ float block_sum(float v, float *red)
-{
-    v = warp_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0)
-        red[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = 0.f;
-    for (int w = 0; w < kNormThreads / 32; ++w)
-        v += red[w];
-    return v;
-}
-
-struct Row {
-    float m2, r2, m1, r1;
-};
-
-// Column c of a row: the branch before the gate, the sum, and the gate.
-__device__ __forceinline__ float branch(const NormParams &p, const Row &s, int64_t row, int64_t c, float &y2)
-{
-    if (p.d.z.data == nullptr)
-        return y2 = 0.f;
-    const float z = get(p.d.z.data, p.d.dtype, row * p.d.z.stride + c);
-    y2 = (z - s.m2) * s.r2;
-    float n = p.d.post_weight ? y2 * get(p.d.post_weight, p.d.param_dtype, c) : y2;
-    return p.d.post_bias ? n + get(p.d.post_bias, p.d.param_dtype, c) : n;
-}
-
-__device__ __forceinline__ float gate_at(const NormParams &p, int64_t row, int64_t c)
-{
-    return p.d.gate.data ? get(p.d.gate.data, p.d.gate_dtype, row / p.d.gate_rows * p.d.gate.stride + c) : 1.f;
-}
-
-__device__ __forceinline__ float sum_at(const NormParams &p, const Row &s, int64_t row, int64_t c)
-{
-    float y2;
-    const float n = branch(p, s, row, c, y2);
-    return fmaf(p.b, gate_at(p, row, c) * n, p.a * get(p.d.x.data, p.d.residual_dtype, row * p.d.x.stride + c));
-}
-
-template <typename F> __device__ void norm_stats(int kind, float eps, int64_t cols, float *red, F at, float &m, float &r)
-{
-    m = 0.f;
-    r = 1.f;
-    if (kind == RIKFAD_NORM_NONE)
-        return;
-    if (kind == RIKFAD_NORM_LAYER) {
-        float s = 0.f;
-        for (int64_t c = threadIdx.x; c < cols; c += kNormThreads)
-            s += at(c);
-        m = block_sum(s, red) / (float)cols;
-    }
-    float s = 0.f;
-    for (int64_t c = threadIdx.x; c < cols; c += kNormThreads) {
-        const float v = at(c) - m;
-        s = fmaf(v, v, s);
-    }
-    r = rsqrtf(block_sum(s, red) / (float)cols + eps);
-}
-
-__global__ void __launch_bounds__(kNormThreads) rikfad_norm_forward_kernel(const __grid_constant__ NormParams p)
-{
-    __shared__ float red[kNormThreads / 32];
-    for (int64_t row = blockIdx.x; row < p.d.rows; row += gridDim.x) {
-        Row s{0.f, 1.f, 0.f, 1.f};
-        if (p.d.z.data)
-            norm_stats(p.d.post, p.post_eps, p.d.cols, red,
-                       [&](int64_t c) { return get(p.d.z.data, p.d.dtype, row * p.d.z.stride + c); }, s.m2, s.r2);
-        norm_stats(p.d.pre, p.pre_eps, p.d.cols, red, [&](int64_t c) { return sum_at(p, s, row, c); }, s.m1, s.r1);
-        __syncthreads();        // every read of the row's inputs before the writes, which may go to them
-        for (int64_t c = threadIdx.x; c < p.d.cols; c += kNormThreads) {
-            const float u = sum_at(p, s, row, c);
-            if (p.d.u.data)
-                put(p.d.u.data, p.d.residual_dtype, row * p.d.u.stride + c, u);
-            if (p.d.h.data) {
-                float h = (u - s.m1) * s.r1;
-                if (p.d.pre_weight)
-                    h *= get(p.d.pre_weight, p.d.param_dtype, c);
-                if (p.d.pre_bias)
-                    h += get(p.d.pre_bias, p.d.param_dtype, c);
-                put(p.d.h.data, p.d.dtype, row * p.d.h.stride + c, h);
-            }
-        }
-        if (p.d.stats && threadIdx.x == 0)
-            reinterpret_cast<float4 *>(p.d.stats)[row] = make_float4(s.m2, s.r2, s.m1, s.r1);
-    }
-}
-
-// One element of the backward pass.
-struct Element {
-    float y1, y2, n, gate, g1, dh, e, q, g2;
-};
-
-__device__ __forceinline__ Element element(const NormParams &p, const Row &s, int64_t row, int64_t c, float mg1, float mg1y)
-{
-    Element v;
-    v.n = branch(p, s, row, c, v.y2);
-    v.gate = gate_at(p, row, c);
-    const float u = fmaf(p.b, v.gate * v.n, p.a * get(p.d.x.data, p.d.residual_dtype, row * p.d.x.stride + c));
-    v.y1 = (u - s.m1) * s.r1;
-    v.dh = p.d.dh.data ? get(p.d.dh.data, p.d.dtype, row * p.d.dh.stride + c) : 0.f;
-    v.g1 = p.d.pre_weight ? v.dh * get(p.d.pre_weight, p.d.param_dtype, c) : v.dh;
-    v.e = s.r1 * (v.g1 - mg1 - v.y1 * mg1y);
-    if (p.d.du.data)
-        v.e += get(p.d.du.data, p.d.residual_dtype, row * p.d.du.stride + c);
-    v.q = p.b * v.gate * v.e;
-    v.g2 = p.d.post_weight ? v.q * get(p.d.post_weight, p.d.param_dtype, c) : v.q;
-    return v;
-}
-
-__global__ void __launch_bounds__(kNormThreads) rikfad_norm_rows_kernel(const __grid_constant__ NormParams p)
-{
-    __shared__ float red[kNormThreads / 32];
-    const float inv = 1.f / (float)p.d.cols;
-    for (int64_t row = blockIdx.x; row < p.d.rows; row += gridDim.x) {
-        const float4 st = reinterpret_cast<const float4 *>(p.d.stats)[row];
-        const Row s{st.x, st.y, st.z, st.w};
-        float s1 = 0.f, s2 = 0.f, mg1 = 0.f, mg1y = 0.f, mg2 = 0.f, mg2y = 0.f;
-        if (p.d.pre != RIKFAD_NORM_NONE) {
-            for (int64_t c = threadIdx.x; c < p.d.cols; c += kNormThreads) {
-                const Element v = element(p, s, row, c, 0.f, 0.f);
-                s1 += v.g1;
-                s2 = fmaf(v.g1, v.y1, s2);
-            }
-            mg1 = p.d.pre == RIKFAD_NORM_LAYER ? block_sum(s1, red) * inv : 0.f;
-            mg1y = block_sum(s2, red) * inv;
-        }
-        if (p.d.z.data && p.d.post != RIKFAD_NORM_NONE) {
-            s1 = s2 = 0.f;
-            for (int64_t c = threadIdx.x; c < p.d.cols; c += kNormThreads) {
-                const Element v = element(p, s, row, c, mg1, mg1y);
-                s1 += v.g2;
-                s2 = fmaf(v.g2, v.y2, s2);
-            }
-            mg2 = p.d.post == RIKFAD_NORM_LAYER ? block_sum(s1, red) * inv : 0.f;
-            mg2y = block_sum(s2, red) * inv;
-        }
-        if (threadIdx.x == 0)
-            reinterpret_cast<float4 *>(p.means)[row] = make_float4(mg1, mg1y, mg2, mg2y);
-    }
-}
-
-// dx, dz and the gate's gradient where every row has its own gate.
-__global__ void __launch_bounds__(kNormThreads) rikfad_norm_elements_kernel(const __grid_constant__ NormParams p)
-{
-    for (int64_t row = blockIdx.x; row < p.d.rows; row += gridDim.x) {
-        const float4 st = reinterpret_cast<const float4 *>(p.d.stats)[row];
-        const float4 mean = reinterpret_cast<const float4 *>(p.means)[row];
-        const Row s{st.x, st.y, st.z, st.w};
-        for (int64_t c = threadIdx.x; c < p.d.cols; c += kNormThreads) {
-            const Element v = element(p, s, row, c, mean.x, mean.y);
-            if (p.d.dgate.data && p.d.gate_rows == 1)
-                put(p.d.dgate.data, p.d.gate_dtype, row * p.d.dgate.stride + c, p.b * v.e * v.n);
-            if (p.d.dx.data)
-                put(p.d.dx.data, p.d.residual_dtype, row * p.d.dx.stride + c, p.a * v.e);
-            if (p.d.dz.data)
-                put(p.d.dz.data, p.d.dtype, row * p.d.dz.stride + c, s.r2 * (v.g2 - mean.z - v.y2 * mean.w));
-        }
-    }
-}
-
-// Sums over rows: blockIdx.y = 0 over all of them for the weights and biases,
-// 1 + i over gate row i's.  A thread owns a column.  Runs before the kernel
-// that may overwrite the inputs.
-__global__ void __launch_bounds__(kNormThreads) rikfad_norm_columns_kernel(const __grid_constant__ NormParams p)
-{
-    const int64_t c = (int64_t)blockIdx.x * kNormThreads + threadIdx.x;
-    if (c >= p.d.cols)
-        return;
-    const int64_t groups = p.d.dgate.data && p.d.gate_rows != 1 ? p.d.rows / p.d.gate_rows : 0;
-    for (int64_t g = blockIdx.y; g <= groups; g += gridDim.y) {
-        const int64_t begin = g == 0 ? 0 : (g - 1) * p.d.gate_rows;
-        const int64_t end = g == 0 ? p.d.rows : g * p.d.gate_rows;
-        float dw1 = 0.f, db1 = 0.f, dw2 = 0.f, db2 = 0.f, dg = 0.f;
-        for (int64_t row = begin; row < end; ++row) {
-            const float4 st = reinterpret_cast<const float4 *>(p.d.stats)[row];
-            const float4 mean = reinterpret_cast<const float4 *>(p.means)[row];
-            const Element v = element(p, Row{st.x, st.y, st.z, st.w}, row, c, mean.x, mean.y);
-            dw1 = fmaf(v.dh, v.y1, dw1);
-            db1 += v.dh;
-            dw2 = fmaf(v.q, v.y2, dw2);
-            db2 += v.q;
-            dg = fmaf(p.b * v.e, v.n, dg);
-        }
-        if (g > 0) {
-            put(p.d.dgate.data, p.d.gate_dtype, (g - 1) * p.d.dgate.stride + c, dg);
-            continue;
-        }
-        if (p.d.dpre_weight)
-            put(p.d.dpre_weight, p.d.param_dtype, c, dw1);
-        if (p.d.dpre_bias)
-            put(p.d.dpre_bias, p.d.param_dtype, c, db1);
-        if (p.d.dpost_weight)
-            put(p.d.dpost_weight, p.d.param_dtype, c, dw2);
-        if (p.d.dpost_bias)
-            put(p.d.dpost_bias, p.d.param_dtype, c, db2);
-    }
-}
 
 int bad(const std::string &msg) { return report_error(RIKFAD_ERR_ARG, msg); }
 
@@ -255,7 +23,7 @@ int check_sizes(const rikfad_residual_norm *p)
 {
     if (p == nullptr)
         return bad("p is NULL");
-    if (p->rows < 0 || p->rows > (int64_t)1 << 40)
+    if (p->rows < 0 || p->rows > (int64_t)1 << 34)
         return bad("rows is out of range");
     if (p->cols < 1 || p->cols > 32768)
         return bad("cols must be in [1, 32768]");
@@ -326,19 +94,123 @@ int check_inputs(const rikfad_residual_norm *p, int &device)
     return rc;
 }
 
-NormParams params(const rikfad_residual_norm *p)
+bool wide(const rikfad_rows &r, int dtype, int64_t rows)
+{
+    return (uintptr_t)r.data % 16 == 0 && (rows <= 1 || r.stride * dtype_bytes(dtype) % 16 == 0);
+}
+
+NormParams params(const rikfad_residual_norm *p, bool backward)
 {
     NormParams n{};
-    n.d = *p;
+    n.rows = p->rows;
+    n.cols = (int32_t)p->cols;
+    n.inv_cols = 1.f / (float)p->cols;
+    n.post = p->post;
+    n.pre = p->pre;
     n.a = (float)p->residual_scale;
     n.b = (float)p->branch_scale;
     n.post_eps = (float)p->post_eps;
     n.pre_eps = (float)p->pre_eps;
-    n.means = static_cast<float *>(p->workspace);
+    n.gate_rows = p->gate.data ? p->gate_rows : 1;
+    n.gate_f32 = p->gate_dtype == RIKFAD_F32;
+    n.param_f32 = p->param_dtype == RIKFAD_F32;
+    n.x = p->x;
+    n.z = p->z;
+    n.gate = p->gate;
+    n.post_weight = p->post_weight;
+    n.post_bias = p->post_bias;
+    n.pre_weight = p->pre_weight;
+    n.pre_bias = p->pre_bias;
+    n.stats = reinterpret_cast<float4 *>(p->stats);
+    const int64_t gates = p->rows / std::max<int64_t>(n.gate_rows, 1);
+    n.wide_x = wide(p->x, p->residual_dtype, p->rows);
+    n.wide_z = wide(p->z, p->dtype, p->rows);
+    n.wide_gate = wide(p->gate, p->gate_dtype, gates);
+    n.wide_params = true;
+    for (const void *v : {p->post_weight, p->post_bias, p->pre_weight, p->pre_bias})
+        n.wide_params = n.wide_params && (uintptr_t)v % 16 == 0;
+    if (!backward) {
+        n.u = p->u;
+        n.h = p->h;
+        n.wide_u = wide(p->u, p->residual_dtype, p->rows);
+        n.wide_h = wide(p->h, p->dtype, p->rows);
+        return n;
+    }
+    n.du = p->du;
+    n.dh = p->dh;
+    n.dx = p->dx;
+    n.dz = p->dz;
+    n.dgate = p->dgate;
+    n.dpost_weight = p->dpost_weight;
+    n.dpost_bias = p->dpost_bias;
+    n.dpre_weight = p->dpre_weight;
+    n.dpre_bias = p->dpre_bias;
+    n.wide_du = wide(p->du, p->residual_dtype, p->rows);
+    n.wide_dh = wide(p->dh, p->dtype, p->rows);
+    n.wide_dx = wide(p->dx, p->residual_dtype, p->rows);
+    n.wide_dz = wide(p->dz, p->dtype, p->rows);
+    n.wide_dgate = wide(p->dgate, p->gate_dtype, gates);
     return n;
 }
 
-unsigned row_blocks(int64_t rows) { return (unsigned)std::min<int64_t>(rows, 152 * 8); }
+// Threads of a row, columns of a block and blocks of a cluster, from the width
+// alone (rikfad_norm.hpp).
+void shape(NormParams &n)
+{
+    const int vectors = (n.cols + 7) / 8;
+    n.cluster = 1;
+    while ((vectors + n.cluster - 1) / n.cluster > kNormMaxThreads)
+        n.cluster *= 2;
+    const int here = (vectors + n.cluster - 1) / n.cluster;
+    n.cta_cols = here * 8;
+    n.lanes = here <= 8 ? 8 : here <= 16 ? 16 : (here + 31) / 32 * 32;
+    n.threads = n.lanes < 64 ? 128 : n.lanes;
+    n.row_groups = n.threads / n.lanes;
+}
+
+// Clusters of a launch: as many as are resident at once (`threads_per_sm` by the
+// kernel's register bound, and by the shared memory of their stages), no more than
+// there are rows.
+void grid(NormParams &n, int threads_per_sm, int units, int most_stages)
+{
+    const size_t unit_bytes = (size_t)n.threads * 16 * units;
+    n.stages = std::max(2, std::min<int>(most_stages, (int)(kNormSmemPerSm / (threads_per_sm / n.threads * unit_bytes))));
+    n.smem = unit_bytes * n.stages;
+    int resident = std::max(1, std::min<int>(threads_per_sm / n.threads, (int)(kNormSmemPerSm / n.smem)));
+    const int64_t groups = (n.rows + n.row_groups - 1) / n.row_groups;
+    n.ctas = (int)std::max<int64_t>(1, std::min<int64_t>(groups, (int64_t)kNormSms * resident / n.cluster));
+}
+
+struct Workspace {
+    int64_t weights = 0, gates = 0;     // floats
+};
+
+// Partial sums: one row of each kind for every cluster, and two of the gate's for
+// every worker whose rows share gates with others.
+Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n)
+{
+    shape(n);
+    n.shared_gate = p->dgate.data && p->gate_rows != 1;
+    const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
+    const int g = p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0;
+    n.units = 2 * a + 2 * r + g;
+    grid(n, kNormBackwardThreads, n.units, 3);
+    n.sums = 0;
+    for (const void *v : {p->dpre_weight, p->dpost_weight, p->dpre_bias, p->dpost_bias})
+        n.sums += v != nullptr;
+    Workspace w;
+    w.weights = (int64_t)n.sums * n.ctas * n.cols;
+    w.gates = n.shared_gate ? (int64_t)2 * n.ctas * n.row_groups * n.cols : 0;
+    return w;
+}
+
+cudaError_t launch_norm(const NormParams &n, int dtype, int residual_dtype, bool backward, cudaStream_t s)
+{
+    const bool f32 = residual_dtype == RIKFAD_F32;
+    return dtype == RIKFAD_F32 ? launch_norm_f32(n, backward, s)
+           : dtype == RIKFAD_BF16 ? launch_norm_bf16(n, f32, backward, s)
+                                  : launch_norm_f16(n, f32, backward, s);
+}
 
 }  // namespace
 
@@ -349,7 +221,11 @@ RIKFAD_API size_t rikfad_residual_norm_workspace(const rikfad_residual_norm *p)
     if (check_sizes(p))
         return 0;
     report_error(RIKFAD_OK, "");
-    return (size_t)p->rows * 4 * sizeof(float);
+    if (p->rows == 0)
+        return 0;
+    NormParams n = params(p, true);
+    const Workspace w = backward_shape(p, n);
+    return (size_t)(w.weights + w.gates) * sizeof(float);
 }
 
 RIKFAD_API int rikfad_residual_norm_forward(const rikfad_residual_norm *p, void *stream)
@@ -366,9 +242,13 @@ RIKFAD_API int rikfad_residual_norm_forward(const rikfad_residual_norm *p, void 
         return report_cuda(e, "earlier CUDA error");
     if (p->rows == 0)
         return RIKFAD_OK;
-    rikfad_norm_forward_kernel<<<row_blocks(p->rows), kNormThreads, 0, (cudaStream_t)stream>>>(params(p));
-    e = cudaGetLastError();
-    return e == cudaSuccess ? RIKFAD_OK : report_cuda(e, "launch rikfad_norm_forward_kernel");
+    NormParams n = params(p, false);
+    shape(n);
+    const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
+    n.units = r + (p->z.data ? a : 0) + (p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
+    grid(n, kNormForwardThreads, n.units, 3);
+    e = launch_norm(n, p->dtype, p->residual_dtype, false, (cudaStream_t)stream);
+    return e == cudaSuccess ? RIKFAD_OK : report_cuda(e, "launch of a residual norm's forward kernel");
     RK_ENTRY_END
 }
 
@@ -400,21 +280,24 @@ RIKFAD_API int rikfad_residual_norm_backward(const rikfad_residual_norm *p, void
         return bad("gradients of weights and biases need their norm");
     if (p->rows > 0 && p->stats == nullptr)
         return bad("stats is NULL");
-    if (p->workspace_bytes < rikfad_residual_norm_workspace(p) || (p->rows > 0 && p->workspace == nullptr))
+    NormParams n = params(p, true);
+    const Workspace w = p->rows > 0 ? backward_shape(p, n) : Workspace();
+    const int64_t floats = w.weights + w.gates;
+    if (p->workspace_bytes / sizeof(float) < (size_t)floats || (floats > 0 && p->workspace == nullptr))
         return bad("the workspace is smaller than rikfad_residual_norm_workspace");
     cudaError_t e = cudaPeekAtLastError();
     if (e != cudaSuccess)
         return report_cuda(e, "earlier CUDA error");
     const cudaStream_t s = (cudaStream_t)stream;
-    const NormParams n = params(p);
-    if (p->rows > 0)
-        rikfad_norm_rows_kernel<<<row_blocks(p->rows), kNormThreads, 0, s>>>(n);
-    const int64_t sums = 1 + (p->dgate.data && p->gate_rows != 1 ? groups : 0);
-    const dim3 grid((unsigned)((p->cols + kNormThreads - 1) / kNormThreads), (unsigned)std::min<int64_t>(sums, 1024));
-    rikfad_norm_columns_kernel<<<grid, kNormThreads, 0, s>>>(n);
-    if (p->rows > 0)
-        rikfad_norm_elements_kernel<<<row_blocks(p->rows), kNormThreads, 0, s>>>(n);
-    e = cudaGetLastError();
+    if (p->rows == 0) {
+        for (void *v : {p->dpre_weight, p->dpost_weight, p->dpre_bias, p->dpost_bias})
+            if (v && (e = cudaMemsetAsync(v, 0, pb * (size_t)p->cols, s)) != cudaSuccess)
+                return report_cuda(e, "cudaMemsetAsync");
+        return RIKFAD_OK;
+    }
+    n.sum_part = static_cast<float *>(p->workspace);
+    n.gate_part = n.sum_part + w.weights;
+    e = launch_norm(n, p->dtype, p->residual_dtype, true, s);
     return e == cudaSuccess ? RIKFAD_OK : report_cuda(e, "launch of a residual norm's backward kernels");
     RK_ENTRY_END
 }
