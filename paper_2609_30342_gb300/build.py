@@ -70,7 +70,7 @@ def build(force=False, verbose=False, extra_flags=(), checked=False):
             print(r.stdout + r.stderr, flush=True)
         return obj
 
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
         objs = list(ex.map(compile_one, sources()))
     tmp = lib + ".tmp%d" % os.getpid()
     cmd = [cc] + ARCH + ["-shared", "-Xcompiler", "-fPIC", "-o", tmp] + objs

@@ -18,8 +18,11 @@ int report_error(int code, const std::string &msg);
 cudaError_t counted_malloc(void **p, size_t bytes);
 void counted_free(void *p);
 
+// The runtime's record of `e` is cleared: a refused launch is reported once.  (An
+// error of work already enqueued stays and is reported by every later call.)
 inline int report_cuda(cudaError_t e, const char *what)
 {
+    cudaGetLastError();
     return report_error(RIKFAD_ERR_CUDA, std::string(what) + ": " + cudaGetErrorName(e) + " (" +
                                              cudaGetErrorString(e) + ")");
 }

@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <new>
 #include <string>
@@ -112,11 +113,12 @@ NormParams params(const rikfad_residual_norm *p, bool backward)
     n.post_eps = (float)p->post_eps;
     n.pre_eps = (float)p->pre_eps;
     n.gate_rows = p->gate.data ? p->gate_rows : 1;
+    n.gate_period = (int32_t)std::min<int64_t>(n.gate_rows, INT32_MAX);
     n.gate_f32 = p->gate_dtype == RIKFAD_F32;
     n.param_f32 = p->param_dtype == RIKFAD_F32;
-    n.x = p->x;
-    n.z = p->z;
-    n.gate = p->gate;
+    n.x = {p->x.data, p->x.stride, 0};
+    n.z = {p->z.data, p->z.stride, 0};
+    n.gate = {p->gate.data, p->gate.stride, 0};
     n.post_weight = p->post_weight;
     n.post_bias = p->post_bias;
     n.pre_weight = p->pre_weight;
@@ -130,17 +132,17 @@ NormParams params(const rikfad_residual_norm *p, bool backward)
     for (const void *v : {p->post_weight, p->post_bias, p->pre_weight, p->pre_bias})
         n.wide_params = n.wide_params && (uintptr_t)v % 16 == 0;
     if (!backward) {
-        n.u = p->u;
-        n.h = p->h;
+        n.u = {p->u.data, p->u.stride, 0};
+        n.h = {p->h.data, p->h.stride, 0};
         n.wide_u = wide(p->u, p->residual_dtype, p->rows);
         n.wide_h = wide(p->h, p->dtype, p->rows);
         return n;
     }
-    n.du = p->du;
-    n.dh = p->dh;
-    n.dx = p->dx;
-    n.dz = p->dz;
-    n.dgate = p->dgate;
+    n.du = {p->du.data, p->du.stride, 0};
+    n.dh = {p->dh.data, p->dh.stride, 0};
+    n.dx = {p->dx.data, p->dx.stride, 0};
+    n.dz = {p->dz.data, p->dz.stride, 0};
+    n.dgate = {p->dgate.data, p->dgate.stride, 0};
     n.dpost_weight = p->dpost_weight;
     n.dpost_bias = p->dpost_bias;
     n.dpre_weight = p->dpre_weight;
@@ -154,31 +156,57 @@ NormParams params(const rikfad_residual_norm *p, bool backward)
 }
 
 // Threads of a row, columns of a block and blocks of a cluster, from the width
-// alone (rikfad_norm.hpp).
-void shape(NormParams &n)
+// and the most threads that a block's registers allow (rikfad_norm.hpp).
+void shape(NormParams &n, int most_threads)
 {
     const int vectors = (n.cols + 7) / 8;
     n.cluster = 1;
-    while ((vectors + n.cluster - 1) / n.cluster > kNormMaxThreads)
+    while ((vectors + n.cluster - 1) / n.cluster > most_threads)
         n.cluster *= 2;
     const int here = (vectors + n.cluster - 1) / n.cluster;
     n.cta_cols = here * 8;
     n.lanes = here <= 8 ? 8 : here <= 16 ? 16 : (here + 31) / 32 * 32;
-    n.threads = n.lanes < 64 ? 128 : n.lanes;
+    n.threads = n.lanes <= 32 ? 128 : n.lanes;
     n.row_groups = n.threads / n.lanes;
+}
+
+// A thread's rows are `row_groups` apart, or neighbours where rows share gates.
+void steps(NormParams &n, int dtype, int residual_dtype, int gate_dtype)
+{
+    const int64_t rows = n.gate_rows > 1 ? 1 : n.row_groups;
+    const int64_t a = rows * dtype_bytes(dtype), r = rows * dtype_bytes(residual_dtype), g = rows * dtype_bytes(gate_dtype);
+    for (NormRows *t : {&n.z, &n.h, &n.dh, &n.dz})
+        t->step = t->stride * a;
+    for (NormRows *t : {&n.x, &n.u, &n.du, &n.dx})
+        t->step = t->stride * r;
+    for (NormRows *t : {&n.gate, &n.dgate})
+        t->step = t->stride * g;
 }
 
 // Clusters of a launch: as many as are resident at once (`threads_per_sm` by the
 // kernel's register bound, and by the shared memory of their stages), no more than
-// there are rows.
-void grid(NormParams &n, int threads_per_sm, int units, int most_stages)
+// there are rows.  Two rows at a time once every group has them.
+void grid(NormParams &n, int threads_per_sm, bool one_row)
 {
-    const size_t unit_bytes = (size_t)n.threads * 16 * units;
-    n.stages = std::max(2, std::min<int>(most_stages, (int)(kNormSmemPerSm / (threads_per_sm / n.threads * unit_bytes))));
-    n.smem = unit_bytes * n.stages;
-    int resident = std::max(1, std::min<int>(threads_per_sm / n.threads, (int)(kNormSmemPerSm / n.smem)));
+    const int by_registers = std::max(1, threads_per_sm / n.threads);
     const int64_t groups = (n.rows + n.row_groups - 1) / n.row_groups;
+    n.at_once = !one_row && groups >= (int64_t)kNormRows * kNormSms * by_registers / n.cluster ? kNormRows : 1;
+    const size_t stage = (size_t)n.threads * 16 * n.units * n.at_once;
+    n.stages = stage * 3 * by_registers <= kNormSmemPerSm ? 3 : 2;
+    n.smem = stage * n.stages;
+    const int resident = std::max(1, std::min(by_registers, (int)(kNormSmemPerSm / n.smem)));
     n.ctas = (int)std::max<int64_t>(1, std::min<int64_t>(groups, (int64_t)kNormSms * resident / n.cluster));
+}
+
+void forward_shape(const rikfad_residual_norm *p, NormParams &n)
+{
+    const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
+    shape(n, kNormMaxThreads);
+    steps(n, p->dtype, p->residual_dtype, p->gate_dtype);
+    n.units = r + a + (p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
+    n.full = n.cols % 8 == 0 && n.wide_x && n.wide_params && (!p->z.data || n.wide_z) && (!p->gate.data || n.wide_gate) &&
+             (!p->u.data || n.wide_u) && (!p->h.data || n.wide_h);
+    grid(n, kNormForwardThreads, false);
 }
 
 struct Workspace {
@@ -186,21 +214,28 @@ struct Workspace {
 };
 
 // Partial sums: one row of each kind for every cluster, and two of the gate's for
-// every worker whose rows share gates with others.
+// every group whose rows share gates with others.
 Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n)
 {
-    shape(n);
-    n.shared_gate = p->dgate.data && p->gate_rows != 1;
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
-    const int g = p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0;
-    n.units = 2 * a + 2 * r + g;
-    grid(n, kNormBackwardThreads, n.units, 3);
+    n.bias = p->dpre_bias || p->dpost_bias;
+    // Two rows at a time with biases take 168 registers; the widest rows would then
+    // need more than 8 blocks.
+    const bool one = n.bias && p->cols > (int64_t)kNormBackwardThreads<true> * 8 * 8;
+    const int threads = n.bias && !one ? kNormBackwardThreads<true> : kNormBackwardThreads<false>;
+    shape(n, threads);
+    steps(n, p->dtype, p->residual_dtype, p->gate_dtype);
+    n.units = 2 * a + 2 * r + (p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
+    n.full = n.cols % 8 == 0 && n.wide_x && n.wide_params && (!p->z.data || n.wide_z) && (!p->gate.data || n.wide_gate) &&
+             (!p->du.data || n.wide_du) && (!p->dh.data || n.wide_dh) && (!p->dx.data || n.wide_dx) &&
+             (!p->dz.data || n.wide_dz) && (!p->dgate.data || n.wide_dgate);
+    grid(n, threads, one);
     n.sums = 0;
     for (const void *v : {p->dpre_weight, p->dpost_weight, p->dpre_bias, p->dpost_bias})
         n.sums += v != nullptr;
     Workspace w;
     w.weights = (int64_t)n.sums * n.ctas * n.cols;
-    w.gates = n.shared_gate ? (int64_t)2 * n.ctas * n.row_groups * n.cols : 0;
+    w.gates = p->dgate.data && p->gate_rows > 1 ? (int64_t)2 * n.ctas * n.row_groups * n.cols : 0;
     return w;
 }
 
@@ -243,10 +278,7 @@ RIKFAD_API int rikfad_residual_norm_forward(const rikfad_residual_norm *p, void 
     if (p->rows == 0)
         return RIKFAD_OK;
     NormParams n = params(p, false);
-    shape(n);
-    const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
-    n.units = r + (p->z.data ? a : 0) + (p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
-    grid(n, kNormForwardThreads, n.units, 3);
+    forward_shape(p, n);
     e = launch_norm(n, p->dtype, p->residual_dtype, false, (cudaStream_t)stream);
     return e == cudaSuccess ? RIKFAD_OK : report_cuda(e, "launch of a residual norm's forward kernel");
     RK_ENTRY_END

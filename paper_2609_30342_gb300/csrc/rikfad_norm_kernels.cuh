@@ -9,14 +9,17 @@
 // The backward kernel forms u again from x, z and the gate: the same bytes as
 // reading u, without the rounding that a stored u has.
 //
-// Both kernels are bound by memory: every element is read once and written once.
-// A thread owns 8 columns of a row and keeps them in registers from the load to
-// the store; the loads of the next rows are under way meanwhile (cp.async into
-// slots of shared memory that only this thread reads, so no barrier separates a
-// copy from its use).  Sums over a row: shuffles, then one barrier over the row's
-// warps (or the cluster's blocks).  Sums over rows stay in the thread's registers
-// to the end of the launch, leave one partial row per cluster, and a second kernel
-// adds those in order.
+// Both kernels are bound by memory as long as they need few instructions: every
+// element is read once and written once.  A thread owns 8 columns of N rows at a
+// time and keeps them in registers from the load to the store; the rows share its
+// weights' loads, its branches and the barriers of its sums, and hide one another's
+// latencies.  Arithmetic is on pairs of float32 (fma.rn.f32x2).  The copies of the
+// next rows are under way meanwhile (cp.async into slots of shared memory that only
+// this thread reads, so no barrier separates a copy from its use).  Sums over a
+// row: shuffles, and beyond a warp one barrier over the row's warps (or the
+// cluster's blocks).  Sums over rows stay in the thread's registers to the end of
+// the launch, leave one partial row per cluster, and a second kernel adds those in
+// order.
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -27,6 +30,91 @@
 #include "rikfad_types.cuh"
 
 namespace rikfad {
+
+// ------------------------------------------------- pairs of float32
+
+typedef uint64_t f2;        // two float32, the first in the low half
+
+__device__ __forceinline__ f2 pair(float lo, float hi)
+{
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ f2 both(float v) { return pair(v, v); }
+__device__ __forceinline__ float2 halves(f2 v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f2 add(f2 a, f2 b)
+{
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 mul(f2 a, f2 b)
+{
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 fma(f2 a, f2 b, f2 c)
+{
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float total(f2 v)
+{
+    const float2 t = halves(v);
+    return t.x + t.y;
+}
+
+// 8 elements as 4 pairs.
+struct Vec8 {
+    f2 v[4];
+};
+
+template <typename T> __device__ __forceinline__ Vec8 widen(const Raw8<T> &r)
+{
+    float f[8];
+    unpack8(r, f);
+    Vec8 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        o.v[i] = pair(f[2 * i], f[2 * i + 1]);
+    return o;
+}
+
+template <typename T> __device__ __forceinline__ Raw8<T> narrow(const Vec8 &o)
+{
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 t = halves(o.v[i]);
+        f[2 * i] = t.x;
+        f[2 * i + 1] = t.y;
+    }
+    return pack8(f, T());
+}
+
+__device__ __forceinline__ Vec8 splat(float v)
+{
+    const f2 b = both(v);
+    return {{b, b, b, b}};
+}
+
+// Elements n and beyond set to zero.
+__device__ __forceinline__ void cut(Vec8 &o, int n)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 t = halves(o.v[i]);
+        o.v[i] = pair(2 * i < n ? t.x : 0.f, 2 * i + 1 < n ? t.y : 0.f);
+    }
+}
 
 // ------------------------------------------------------------------ staging
 
@@ -61,14 +149,15 @@ __device__ __forceinline__ uint4 smem_get(uint32_t smem)
 // 16-byte units of 8 elements.
 template <typename T> constexpr int kUnits = sizeof(T) / 2;
 
-// Up to n <= 8 elements into this thread's slot, whose units are `stride` bytes
+// n elements (1 to 8) into this thread's slot, whose units are `stride` bytes
 // apart: copies in flight where the row starts on 16 bytes, else element by element.
-template <typename T> __device__ __forceinline__ void stage8(uint32_t slot, uint32_t stride, const T *src, int n, bool wide)
+// FULL: every row starts on 16 bytes and n is 8.
+template <typename T, bool FULL> __device__ __forceinline__ void stage8(uint32_t slot, uint32_t stride, const void *src, int n, bool wide)
 {
-    if (wide && n == 8) {
+    if (FULL || (wide && n == 8)) {
         copy16_async(slot, src);
         if constexpr (sizeof(T) == 4)
-            copy16_async(slot + stride, src + 4);
+            copy16_async(slot + stride, static_cast<const char *>(src) + 16);
         return;
     }
     union {
@@ -81,13 +170,13 @@ template <typename T> __device__ __forceinline__ void stage8(uint32_t slot, uint
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         if (e < n)
-            r.v[e] = src[e];
+            r.v[e] = static_cast<const T *>(src)[e];
 #pragma unroll
     for (int i = 0; i < kUnits<T>; ++i)
         smem_put(slot + i * stride, r.w[i]);
 }
 
-template <typename T> __device__ __forceinline__ void fetch8(uint32_t slot, uint32_t stride, float (&v)[8])
+template <typename T> __device__ __forceinline__ Vec8 fetch8(uint32_t slot, uint32_t stride)
 {
     Raw8<T> r;
     if constexpr (sizeof(T) == 4) {
@@ -97,46 +186,47 @@ template <typename T> __device__ __forceinline__ void fetch8(uint32_t slot, uint
     } else {
         r.w = smem_get(slot);
     }
-    unpack8(r, v);
+    return widen(r);
 }
 
-template <typename T> __device__ __forceinline__ void put8(T *dst, const float (&v)[8], int n, bool wide)
+template <typename T, bool FULL> __device__ __forceinline__ void put8(void *to, const Vec8 &v, int n, bool wide)
 {
-    if (wide && n == 8) {
-        const Raw8<T> r = pack8(v, T());
+    const Raw8<T> r = narrow<T>(v);
+    if (FULL || (wide && n == 8)) {
         if constexpr (sizeof(T) == 4) {
-            reinterpret_cast<float4 *>(dst)[0] = r.a;
-            reinterpret_cast<float4 *>(dst)[1] = r.b;
+            static_cast<float4 *>(to)[0] = r.a;
+            static_cast<float4 *>(to)[1] = r.b;
         } else {
-            *reinterpret_cast<uint4 *>(dst) = r.w;
+            *static_cast<uint4 *>(to) = r.w;
         }
         return;
     }
+    const T *each = reinterpret_cast<const T *>(&r);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         if (e < n)
-            dst[e] = from_f32<T>(v[e]);
+            static_cast<T *>(to)[e] = each[e];
 }
 
-// 8 weights or biases of type A or float32; `absent` where the vector is NULL, 0
-// beyond the row's end.
-template <typename A> __device__ __forceinline__ void param8(const void *p, bool f32, int col, int n, bool wide, float absent,
-                                                             float (&v)[8])
+// Columns [col, col + n) of a weight or bias of type A or float32; `absent` where
+// the vector is NULL, 0 beyond n.
+template <typename A, bool FULL> __device__ __forceinline__ Vec8 param8(const void *p, bool f32, int col, int n, bool wide, float absent)
 {
+    if (n == 0)
+        return splat(0.f);
     if (p == nullptr) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = e < n ? absent : 0.f;
-    } else if (wide && n == 8) {
-        if (f32)
-            unpack8(load_raw8(static_cast<const float *>(p) + col), v);
-        else
-            unpack8(load_raw8(static_cast<const A *>(p) + col), v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = e >= n ? 0.f : f32 ? static_cast<const float *>(p)[col + e] : to_f32(static_cast<const A *>(p)[col + e]);
+        Vec8 o = splat(absent);
+        if (!FULL)
+            cut(o, n);
+        return o;
     }
+    if (FULL || (wide && n == 8))
+        return f32 ? widen(load_raw8(static_cast<const float *>(p) + col)) : widen(load_raw8(static_cast<const A *>(p) + col));
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        f[e] = e >= n ? 0.f : f32 ? static_cast<const float *>(p)[col + e] : to_f32(static_cast<const A *>(p)[col + e]);
+    return widen(Raw8<float>{make_float4(f[0], f[1], f[2], f[3]), make_float4(f[4], f[5], f[6], f[7])});
 }
 
 // ----------------------------------------------------------- sums over a row
@@ -146,33 +236,41 @@ __device__ __forceinline__ uint32_t smem_address(const void *p) { return (uint32
 struct alignas(16) RowSums {
     // [parity][value][warp of the cluster]: a sum's slots are written again two sums
     // later, with a barrier in between that follows every read of the first
-    float slot[2][2][kNormMaxWarps * 8];
+    float slot[2][4][kNormMaxWarps * 8];
 };
+
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 // The sums of N values over a row's threads, in every one of them, always in the
 // same order.
 template <int N> __device__ __forceinline__ void row_sum(const NormParams &p, RowSums &s, int &parity, float (&v)[N])
 {
-    const int width = min(p.lanes, 32);
-    for (int o = width / 2; o > 0; o >>= 1)
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    for (int o = 16; o > 0; o >>= 1)
+        if (o < p.lanes)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
     if (p.lanes <= 32 && p.cluster == 1)
         return;
     parity ^= 1;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = p.threads >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (p.cluster == 1) {
         if (lane == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 s.slot[parity][i][warp] = v[i];
         __syncthreads();
+        // 0 beyond the row's warps
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            v[i] = 0.f;
-            for (int w = 0; w < warps; w += 4) {
-                const float4 f = *reinterpret_cast<const float4 *>(&s.slot[parity][i][w]);     // beyond the warps: 0
+            float4 f = *reinterpret_cast<const float4 *>(&s.slot[parity][i][0]);
+            v[i] = (f.x + f.y) + (f.z + f.w);
+            for (int w = 4; w * 32 < p.threads; w += 4) {
+                f = *reinterpret_cast<const float4 *>(&s.slot[parity][i][w]);
                 v[i] += (f.x + f.y) + (f.z + f.w);
             }
         }
@@ -191,7 +289,7 @@ template <int N> __device__ __forceinline__ void row_sum(const NormParams &p, Ro
             asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote), "f"(v[i]) : "memory");
         }
     }
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_barrier();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         float t = 0.f;
@@ -201,190 +299,290 @@ template <int N> __device__ __forceinline__ void row_sum(const NormParams &p, Ro
     }
 }
 
-// Mean and 1 / deviation (or root mean square) of 8 values a thread.
-__device__ __forceinline__ void row_stats(const NormParams &p, RowSums &s, int &parity, int kind, float eps, int n,
-                                          const float (&v)[8], float &m, float &r)
-{
-    m = 0.f;
-    r = 1.f;
-    if (kind == RIKFAD_NORM_NONE)
-        return;
-    float t[1];
-    if (kind == RIKFAD_NORM_LAYER) {
-        t[0] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-        row_sum(p, s, parity, t);
-        m = t[0] * p.inv_cols;
-    }
-    t[0] = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float d = kind == RIKFAD_NORM_LAYER ? (e < n ? v[e] - m : 0.f) : v[e];
-        t[0] = fmaf(d, d, t[0]);
-    }
-    row_sum(p, s, parity, t);
-    r = rsqrtf(fmaf(t[0], p.inv_cols, eps));
-}
-
 // ------------------------------------------------------------------ geometry
 
-// A thread's columns and a block's share of the rows.
+// A thread's columns and rows, the same in both directions.
 struct Place {
     int col, n;             // first column, how many (0 to 8)
-    int64_t row, step;      // first row and distance to the next
-    int count, rounds;      // rows of this thread's group; rounds of the block
+    int64_t row;            // first row
+    int step;               // distance to the next
+    int count, most;        // rows of this thread's group, and of the block's longest
+
+    __device__ __forceinline__ explicit Place(const NormParams &p)
+    {
+        const int rank = blockIdx.x % p.cluster, id = blockIdx.x / p.cluster;
+        const int lane = threadIdx.x % p.lanes, group = threadIdx.x / p.lanes;
+        const int begin = rank * p.cta_cols, end = min(p.cols, begin + p.cta_cols);
+        col = begin + lane * 8;
+        n = max(0, min(8, end - col));
+        if (p.gate_rows > 1) {
+            // each group walks its own run of rows, so that the rows of a gate stay together
+            const int64_t workers = (int64_t)p.ctas * p.row_groups, me = (int64_t)id * p.row_groups + group;
+            row = p.rows * me / workers;
+            step = 1;
+            count = (int)(p.rows * (me + 1) / workers - row);
+            most = (int)((p.rows + workers - 1) / workers);
+        } else {
+            // a block's groups take neighbouring rows
+            const int64_t from = p.rows * id / p.ctas, to = p.rows * (id + 1) / p.ctas;
+            row = from + group;
+            step = p.row_groups;
+            count = (int)max((int64_t)0, (to - row + p.row_groups - 1) / p.row_groups);
+            most = (int)((to - from + p.row_groups - 1) / p.row_groups);
+        }
+    }
 };
 
-// `contiguous`: each group of lanes walks its own run of rows (sums over the rows
-// of a gate stay with one group); otherwise a block's groups take neighbouring rows.
-__device__ __forceinline__ Place place(const NormParams &p, bool contiguous)
+// Where this thread's columns of its first row are; `step` bytes on is its next.
+__device__ __forceinline__ char *first_row(const NormRows &r, int bytes, const Place &q)
 {
-    Place q;
-    const int rank = blockIdx.x % p.cluster, id = blockIdx.x / p.cluster;
-    const int lane = threadIdx.x % p.lanes, group = threadIdx.x / p.lanes;
-    const int first = rank * p.cta_cols + lane * 8;
-    q.n = lane * 8 < p.cta_cols ? max(0, min(8, p.cols - first)) : 0;
-    q.col = q.n > 0 ? first : 0;
-    if (contiguous) {
-        const int64_t workers = (int64_t)p.ctas * p.row_groups, me = (int64_t)id * p.row_groups + group;
-        q.row = p.rows * me / workers;
-        q.step = 1;
-        q.count = (int)(p.rows * (me + 1) / workers - q.row);
-        q.rounds = (int)((p.rows + workers - 1) / workers);
-    } else {
-        const int64_t begin = p.rows * id / p.ctas, end = p.rows * (id + 1) / p.ctas;
-        q.row = begin + group;
-        q.step = p.row_groups;
-        q.count = (int)max((int64_t)0, (end - q.row + p.row_groups - 1) / p.row_groups);
-        q.rounds = (int)((end - begin + p.row_groups - 1) / p.row_groups);
+    return static_cast<char *>(r.data) + (q.row * r.stride + q.col) * bytes;
+}
+
+// The gate's rows: one for every row, or the same for gate_rows of them.
+struct GateWalk {
+    char *at;
+    int left;               // rows of the gate row to go
+
+    __device__ __forceinline__ GateWalk(const NormParams &p, const NormRows &r, int bytes, const Place &q)
+    {
+        const int64_t row = p.gate_rows > 1 ? q.row / p.gate_rows : q.row;
+        left = p.gate_rows > 1 ? (int)min((row + 1) * p.gate_rows - q.row, (int64_t)INT32_MAX) : 1;
+        at = static_cast<char *>(r.data) + (row * r.stride + q.col) * bytes;
     }
-    return q;
-}
+    __device__ __forceinline__ void next(const NormParams &p, const NormRows &r)
+    {
+        if (--left == 0) {
+            at += r.step;
+            left = p.gate_period;
+        }
+    }
+};
 
-template <typename A> __device__ __forceinline__ void stage_gate(const NormParams &p, uint32_t slot, uint32_t stride, int64_t row,
-                                                                 const Place &q)
+// The head of both kernels: the slots of the sums and of threads without columns
+// are zero.
+__device__ __forceinline__ void prepare(const NormParams &p, RowSums &sums, const Place &q, uint32_t slot, int units)
 {
-    const int64_t at = row / p.gate_rows * p.gate.stride + q.col;
-    if (p.gate_f32)
-        stage8(slot, stride, static_cast<const float *>(p.gate.data) + at, q.n, p.wide_gate);
+    for (int i = threadIdx.x; i < (int)(sizeof sums / 4); i += p.threads)
+        (&sums.slot[0][0][0])[i] = 0.f;
+    if (q.n == 0)
+        for (int i = 0; i < units; ++i)
+            smem_put(slot + i * p.threads * 16, make_uint4(0, 0, 0, 0));
+    if (p.cluster > 1)
+        cluster_barrier();
     else
-        stage8(slot, stride, static_cast<const A *>(p.gate.data) + at, q.n, p.wide_gate);
+        __syncthreads();
+    wait_for_predecessor();
 }
 
-template <typename A> __device__ __forceinline__ void fetch_gate(const NormParams &p, uint32_t slot, uint32_t stride, float (&v)[8])
+// v - m, 0 beyond the row's end.
+template <bool FULL> __device__ __forceinline__ Vec8 centred(const Vec8 &v, float m, int n)
 {
-    if (p.gate_f32)
-        fetch8<float>(slot, stride, v);
-    else
-        fetch8<A>(slot, stride, v);
+    const f2 minus = both(n > 0 ? -m : 0.f);
+    Vec8 d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        d.v[i] = add(v.v[i], minus);
+    if (!FULL)
+        cut(d, n);
+    return d;
 }
 
-__device__ __forceinline__ void clear_slots(const NormParams &p, uint32_t slot, uint32_t stride)
+__device__ __forceinline__ float squares(const Vec8 &v)
 {
-    for (int i = 0; i < p.units * p.stages; ++i)
-        smem_put(slot + i * stride, make_uint4(0, 0, 0, 0));
+    f2 s = mul(v.v[0], v.v[0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i)
+        s = fma(v.v[i], v.v[i], s);
+    return total(s);
+}
+
+__device__ __forceinline__ float elements(const Vec8 &v) { return total(add(add(v.v[0], v.v[1]), add(v.v[2], v.v[3]))); }
+
+// Means and 1 / deviations (or root mean squares) of N rows; v becomes v - m.
+template <int N, bool FULL> __device__ __forceinline__ void row_stats(const NormParams &p, RowSums &s, int &parity, int kind, float eps, int n,
+                                                                      Vec8 (&v)[N], float (&m)[N], float (&r)[N])
+{
+    float t[N];
+    if (kind == RIKFAD_NORM_LAYER) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            t[j] = elements(v[j]);
+        row_sum(p, s, parity, t);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            m[j] = t[j] * p.inv_cols;
+            v[j] = centred<FULL>(v[j], m[j], n);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        t[j] = squares(v[j]);
+    row_sum(p, s, parity, t);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        r[j] = rsqrtf(fmaf(t[j], p.inv_cols, eps));
 }
 
 // ------------------------------------------------------------------- forward
 
-template <typename A, typename R>
-__global__ void __launch_bounds__(kNormMaxThreads, kNormForwardThreads / kNormMaxThreads)
+template <typename A, typename R, int N, bool FULL>
+__global__ void __maxnreg__((65536 / kNormForwardThreads / 8 * 8))
     rikfad_norm_forward_kernel(const __grid_constant__ NormParams p)
 {
     extern __shared__ uint4 stages[];
     __shared__ RowSums sums;
-    const Place q = place(p, false);
+    const Place q(p);
     const uint32_t stride = p.threads * 16, slot = smem_address(stages + threadIdx.x);
-    const uint32_t stage_bytes = stride * p.units;
+    const uint32_t row_bytes = stride * p.units, stage_bytes = row_bytes * N, end = slot + p.stages * stage_bytes;
     const bool branch = p.z.data != nullptr, gated = p.gate.data != nullptr;
+    const bool post = branch && p.post != RIKFAD_NORM_NONE, pre = p.pre != RIKFAD_NORM_NONE;
+    const uint32_t z_at = kUnits<R> * stride, gate_at = z_at + kUnits<A> * stride;
     int parity = 0;
-    for (int i = threadIdx.x; i < (int)(sizeof sums / 4); i += p.threads)
-        (&sums.slot[0][0][0])[i] = 0.f;
-    if (q.n == 0)
-        clear_slots(p, slot, stride);
-    if (p.cluster > 1)
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    else
-        __syncthreads();
-    wait_for_predecessor();
-    auto issue = [&](int k) {
-        if (k < q.count && q.n > 0) {
-            const int64_t row = q.row + k * q.step;
-            uint32_t at = slot + (uint32_t)(k % p.stages) * stage_bytes;
-            stage8(at, stride, static_cast<const R *>(p.x.data) + row * p.x.stride + q.col, q.n, p.wide_x);
-            at += kUnits<R> * stride;
-            if (branch) {
-                stage8(at, stride, static_cast<const A *>(p.z.data) + row * p.z.stride + q.col, q.n, p.wide_z);
-                at += kUnits<A> * stride;
+    prepare(p, sums, q, slot, p.units * N * p.stages);
+    char *x = first_row(p.x, sizeof(R), q), *z = first_row(p.z, sizeof(A), q);
+    char *u_out = first_row(p.u, sizeof(R), q), *h_out = first_row(p.h, sizeof(A), q);
+    GateWalk gate(p, p.gate, p.gate_f32 ? 4 : (int)sizeof(A), q);
+    int ahead = 0;              // rows issued
+    uint32_t issue_at = slot;
+    auto issue = [&]() {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (ahead + j < q.count && q.n > 0) {
+                const uint32_t at = issue_at + j * row_bytes;
+                stage8<R, FULL>(at, stride, x, q.n, p.wide_x);
+                x += p.x.step;
+                if (branch) {
+                    stage8<A, FULL>(at + z_at, stride, z, q.n, p.wide_z);
+                    z += p.z.step;
+                }
+                if (gated) {
+                    if (p.gate_f32)
+                        stage8<float, FULL>(at + gate_at, stride, gate.at, q.n, p.wide_gate);
+                    else
+                        stage8<A, FULL>(at + gate_at, stride, gate.at, q.n, p.wide_gate);
+                    gate.next(p, p.gate);
+                }
             }
-            if (gated)
-                stage_gate<A>(p, at, stride, row, q);
-        }
         commit_copies();
+        ahead += N;
+        issue_at += stage_bytes;
+        if (issue_at == end)
+            issue_at = slot;
     };
     for (int k = 0; k < p.stages - 1; ++k)
-        issue(k);
-    for (int k = 0; k < q.rounds; ++k) {
-        issue(k + p.stages - 1);
+        issue();
+    uint32_t at0 = slot;
+    for (int k = 0; k < q.most; k += N) {
+        issue();
         wait_copies(p.stages);
-        const int64_t row = q.row + k * q.step;
-        const bool live = k < q.count;
-        uint32_t at = slot + (uint32_t)(k % p.stages) * stage_bytes;
-        float u[8], m2 = 0.f, r2 = 1.f, m1, r1;
-        fetch8<R>(at, stride, u);
-        at += kUnits<R> * stride;
+        Vec8 u[N], v[N];
+        float m2[N], r2[N], m1[N], r1[N];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            u[e] *= p.a;
+        for (int j = 0; j < N; ++j) {
+            m2[j] = m1[j] = 0.f;
+            r2[j] = r1[j] = 1.f;
+            u[j] = fetch8<R>(at0 + j * row_bytes, stride);
+        }
+        const f2 a2 = both(p.a);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                u[j].v[i] = mul(u[j].v[i], a2);
         if (branch) {
-            float v[8], w[8];
-            fetch8<A>(at, stride, v);
-            at += kUnits<A> * stride;
-            row_stats(p, sums, parity, p.post, p.post_eps, q.n, v, m2, r2);
-            if (p.post != RIKFAD_NORM_NONE) {
-                param8<A>(p.post_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f, w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[e] = (v[e] - m2) * r2 * w[e];
+            for (int j = 0; j < N; ++j)
+                v[j] = fetch8<A>(at0 + j * row_bytes + z_at, stride);
+            if (post) {
+                row_stats<N, FULL>(p, sums, parity, p.post, p.post_eps, q.n, v, m2, r2);
+                const Vec8 w = param8<A, FULL>(p.post_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const f2 r = both(r2[j]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        v[j].v[i] = mul(mul(v[j].v[i], r), w.v[i]);
+                }
                 if (p.post_bias) {
-                    param8<A>(p.post_bias, p.param_f32, q.col, q.n, p.wide_params, 0.f, w);
+                    const Vec8 b = param8<A, FULL>(p.post_bias, p.param_f32, q.col, q.n, p.wide_params, 0.f);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        v[e] += w[e];
+                    for (int j = 0; j < N; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            v[j].v[i] = add(v[j].v[i], b.v[i]);
                 }
             }
             if (gated) {
-                fetch_gate<A>(p, at, stride, w);
+                if (p.gate_f32) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[e] *= w[e];
-            }
+                    for (int j = 0; j < N; ++j) {
+                        const Vec8 g = fetch8<float>(at0 + j * row_bytes + gate_at, stride);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                u[e] = fmaf(p.b, v[e], u[e]);
-        }
-        row_stats(p, sums, parity, p.pre, p.pre_eps, q.n, u, m1, r1);
-        if (live && q.n > 0) {
-            if (p.u.data)
-                put8(static_cast<R *>(p.u.data) + row * p.u.stride + q.col, u, q.n, p.wide_u);
-            if (p.h.data) {
-                if (p.pre != RIKFAD_NORM_NONE) {
-                    float w[8];
-                    param8<A>(p.pre_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f, w);
+                        for (int i = 0; i < 4; ++i)
+                            v[j].v[i] = mul(v[j].v[i], g.v[i]);
+                    }
+                } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        u[e] = (u[e] - m1) * r1 * w[e];
-                    if (p.pre_bias) {
-                        param8<A>(p.pre_bias, p.param_f32, q.col, q.n, p.wide_params, 0.f, w);
+                    for (int j = 0; j < N; ++j) {
+                        const Vec8 g = fetch8<A>(at0 + j * row_bytes + gate_at, stride);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            u[e] += w[e];
+                        for (int i = 0; i < 4; ++i)
+                            v[j].v[i] = mul(v[j].v[i], g.v[i]);
                     }
                 }
-                put8(static_cast<A *>(p.h.data) + row * p.h.stride + q.col, u, q.n, p.wide_h);
             }
-            if (p.stats && q.col == 0)
-                p.stats[row] = make_float4(m2, r2, m1, r1);
+            const f2 b2 = both(p.b);
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    u[j].v[i] = fma(v[j].v[i], b2, u[j].v[i]);
         }
+        if (p.u.data) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (k + j < q.count && q.n > 0) {
+                    put8<R, FULL>(u_out, u[j], q.n, p.wide_u);
+                    u_out += p.u.step;
+                }
+        }
+        if (pre) {
+            row_stats<N, FULL>(p, sums, parity, p.pre, p.pre_eps, q.n, u, m1, r1);
+            const Vec8 w = param8<A, FULL>(p.pre_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const f2 r = both(r1[j]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    u[j].v[i] = mul(mul(u[j].v[i], r), w.v[i]);
+            }
+            if (p.pre_bias) {
+                const Vec8 b = param8<A, FULL>(p.pre_bias, p.param_f32, q.col, q.n, p.wide_params, 0.f);
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        u[j].v[i] = add(u[j].v[i], b.v[i]);
+            }
+        }
+        if (p.h.data) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (k + j < q.count && q.n > 0) {
+                    put8<A, FULL>(h_out, u[j], q.n, p.wide_h);
+                    h_out += p.h.step;
+                }
+        }
+        if (p.stats && q.col == 0) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (k + j < q.count)
+                    p.stats[q.row + (int64_t)(k + j) * q.step] = make_float4(m2[j], r2[j], m1[j], r1[j]);
+        }
+        at0 += stage_bytes;
+        if (at0 == end)
+            at0 = slot;
     }
     allow_successor_launch();
 }
@@ -392,21 +590,18 @@ __global__ void __launch_bounds__(kNormMaxThreads, kNormForwardThreads / kNormMa
 // ------------------------------------------------------------------ backward
 
 // One partial row of a sum over rows, from the block's groups in order.
-__device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, float *part, int id, float *buffer, const float (&acc)[8])
+__device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, float *part, float *buffer, const Vec8 &acc)
 {
-    float *out = part + (int64_t)id * p.cols;
+    float *out = part + (int64_t)(blockIdx.x / p.cluster) * p.cols;
     if (p.row_groups == 1) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < q.n)
-                out[q.col + e] = acc[e];
+        put8<float, false>(out + q.col, acc, q.n, false);
         return;
     }
     __syncthreads();
     const int group = threadIdx.x / p.lanes, width = p.lanes * 8;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        buffer[group * width + (threadIdx.x % p.lanes) * 8 + e] = acc[e];
+    for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f2 *>(buffer + group * width + q.col + 2 * i) = acc.v[i];
     __syncthreads();
     for (int c = threadIdx.x; c < p.cols; c += p.threads) {
         float t = 0.f;
@@ -416,236 +611,377 @@ __device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, f
     }
 }
 
-template <typename A, typename R, bool BIAS>
-__global__ void __launch_bounds__(kNormMaxThreads, kNormBackwardThreads / kNormMaxThreads)
+// The branch's y2 and n are formed twice from the stages, on both sides of the
+// first sum over the row: the registers go to the sums over rows.
+template <typename A, typename R, int N, bool FULL, bool BIAS>
+__global__ void __maxnreg__((65536 / kNormBackwardThreads<BIAS && (N > 1)> / 8 * 8))
     rikfad_norm_backward_kernel(const __grid_constant__ NormParams p)
 {
     extern __shared__ uint4 stages[];
     __shared__ RowSums sums;
-    const Place q = place(p, p.shared_gate);
+    const Place q(p);
     const uint32_t stride = p.threads * 16, slot = smem_address(stages + threadIdx.x);
-    const uint32_t stage_bytes = stride * p.units;
+    const uint32_t row_bytes = stride * p.units, stage_bytes = row_bytes * N, end = slot + p.stages * stage_bytes;
     const bool branch = p.z.data != nullptr, gated = p.gate.data != nullptr;
     const bool post = branch && p.post != RIKFAD_NORM_NONE, pre = p.pre != RIKFAD_NORM_NONE;
+    const bool shared_gate = p.dgate.data && p.gate_rows > 1;
+    const int gate_bytes = p.gate_f32 ? 4 : (int)sizeof(A);
     int parity = 0;
-    for (int i = threadIdx.x; i < (int)(sizeof sums / 4); i += p.threads)
-        (&sums.slot[0][0][0])[i] = 0.f;
-    if (q.n == 0)
-        clear_slots(p, slot, stride);
-    if (p.cluster > 1)
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    else
-        __syncthreads();
-    wait_for_predecessor();
-    // a thread's slots of a row: x, z, dh, du, gate
+    prepare(p, sums, q, slot, p.units * N * p.stages);
+    // a row's slots: x, z, dh, du, gate
     const uint32_t z_at = kUnits<R> * stride, dh_at = z_at + kUnits<A> * stride, du_at = dh_at + kUnits<A> * stride;
     const uint32_t gate_at = du_at + kUnits<R> * stride;
-    auto issue = [&](int k) {
-        if (k < q.count && q.n > 0) {
-            const int64_t row = q.row + k * q.step;
-            const uint32_t at = slot + (uint32_t)(k % p.stages) * stage_bytes;
-            stage8(at, stride, static_cast<const R *>(p.x.data) + row * p.x.stride + q.col, q.n, p.wide_x);
-            if (branch)
-                stage8(at + z_at, stride, static_cast<const A *>(p.z.data) + row * p.z.stride + q.col, q.n, p.wide_z);
-            if (p.dh.data)
-                stage8(at + dh_at, stride, static_cast<const A *>(p.dh.data) + row * p.dh.stride + q.col, q.n, p.wide_dh);
-            if (p.du.data)
-                stage8(at + du_at, stride, static_cast<const R *>(p.du.data) + row * p.du.stride + q.col, q.n, p.wide_du);
-            if (gated)
-                stage_gate<A>(p, at + gate_at, stride, row, q);
-        }
+    char *x = first_row(p.x, sizeof(R), q), *z = first_row(p.z, sizeof(A), q);
+    char *dh = first_row(p.dh, sizeof(A), q), *du = first_row(p.du, sizeof(R), q);
+    char *dx = first_row(p.dx, sizeof(R), q), *dz = first_row(p.dz, sizeof(A), q);
+    GateWalk gate(p, p.gate, gate_bytes, q);
+    int ahead = 0;
+    uint32_t issue_at = slot;
+    auto issue = [&]() {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (ahead + j < q.count && q.n > 0) {
+                const uint32_t at = issue_at + j * row_bytes;
+                stage8<R, FULL>(at, stride, x, q.n, p.wide_x);
+                x += p.x.step;
+                if (branch) {
+                    stage8<A, FULL>(at + z_at, stride, z, q.n, p.wide_z);
+                    z += p.z.step;
+                }
+                if (p.dh.data) {
+                    stage8<A, FULL>(at + dh_at, stride, dh, q.n, p.wide_dh);
+                    dh += p.dh.step;
+                }
+                if (p.du.data) {
+                    stage8<R, FULL>(at + du_at, stride, du, q.n, p.wide_du);
+                    du += p.du.step;
+                }
+                if (gated) {
+                    if (p.gate_f32)
+                        stage8<float, FULL>(at + gate_at, stride, gate.at, q.n, p.wide_gate);
+                    else
+                        stage8<A, FULL>(at + gate_at, stride, gate.at, q.n, p.wide_gate);
+                    gate.next(p, p.gate);
+                }
+            }
         commit_copies();
+        ahead += N;
+        issue_at += stage_bytes;
+        if (issue_at == end)
+            issue_at = slot;
     };
-    float dw1[8] = {}, dw2[8] = {}, db1[8] = {}, db2[8] = {}, dg[8] = {};
-    int64_t gate_row = q.row / p.gate_rows;     // of the sum in dg
-    int64_t gate_left = p.shared_gate ? (gate_row + 1) * p.gate_rows - q.row : 0;
-    bool gate_whole = q.row % p.gate_rows == 0; // the sum began with the gate's first row
-    int gate_slot = 0;                          // 0: the group's first gate, 1: its last
-    const int64_t worker = (int64_t)(blockIdx.x / p.cluster) * p.row_groups + threadIdx.x / p.lanes;
-    if (p.shared_gate && q.count == 0)          // a group without rows adds nothing to the gate it lies in
-        for (int e = 0; e < q.n; ++e)
-            p.gate_part[2 * worker * p.cols + q.col + e] = 0.f;
+    Vec8 dw1 = splat(0.f), dw2 = dw1, db1 = dw1, db2 = dw1, dg = dw1;
+    // dgate: a row for every row, or the sum over the gate's
+    const int64_t gate_row0 = p.gate_rows > 1 ? q.row / p.gate_rows : q.row;
+    GateWalk dgate(p, p.dgate, gate_bytes, q);
+    bool gate_whole = p.gate_rows * gate_row0 == q.row;     // the sum began with the gate's first row
+    bool gate_first = true;                                 // it is the group's first
+    auto gate_part = [&](const Vec8 &v) {
+        const int64_t worker = (int64_t)(blockIdx.x / p.cluster) * p.row_groups + threadIdx.x / p.lanes;
+        put8<float, false>(p.gate_part + (2 * worker + (gate_first ? 0 : 1)) * p.cols + q.col, v, q.n, false);
+    };
+    auto put_gate = [&](const Vec8 &v) {
+        if (q.n == 0)
+            return;
+        if (p.gate_f32)
+            put8<float, FULL>(dgate.at, v, q.n, p.wide_dgate);
+        else
+            put8<A, FULL>(dgate.at, v, q.n, p.wide_dgate);
+    };
+    if (shared_gate && q.count == 0)            // a group without rows adds nothing to the gate it lies in
+        gate_part(dg);
     for (int k = 0; k < p.stages - 1; ++k)
-        issue(k);
-    float4 next = q.count > 0 ? p.stats[q.row] : make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = 0; k < q.rounds; ++k) {
-        issue(k + p.stages - 1);
-        const int64_t row = q.row + k * q.step;
-        const bool live = k < q.count;
-        const float m2 = next.x, r2 = next.y, m1 = next.z, r1 = next.w;
-        if (k + 1 < q.count)
-            next = p.stats[row + q.step];
+        issue();
+    const float4 *stats = p.stats + q.row;
+    float4 next[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        next[j] = j < q.count ? stats[j * q.step] : make_float4(0.f, 0.f, 0.f, 0.f);
+    uint32_t at0 = slot;
+    for (int k = 0; k < q.most; k += N) {
+        issue();
+        float m2[N], r2[N], m1[N], r1[N];
+        stats += N * q.step;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            m2[j] = next[j].x;
+            r2[j] = next[j].y;
+            m1[j] = next[j].z;
+            r1[j] = next[j].w;
+            if (k + N + j < q.count)
+                next[j] = stats[j * q.step];
+        }
         wait_copies(p.stages);
-        const uint32_t at = slot + (uint32_t)(k % p.stages) * stage_bytes;
-        float y1[8], y2[8], n[8], gate[8], g1[8], w[8];
-        fetch8<R>(at, stride, y1);
+
+        // y2 and n of every row
+        Vec8 e[N], y[N], n[N];
+        auto branch_of = [&](Vec8(&y2)[N]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            y1[e] *= p.a;
-            y2[e] = n[e] = 0.f;
-            gate[e] = 1.f;
-        }
-        if (branch) {
-            fetch8<A>(at + z_at, stride, n);
-            if (post) {
-                param8<A>(p.post_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f, w);
+            for (int j = 0; j < N; ++j)
+                n[j] = fetch8<A>(at0 + j * row_bytes + z_at, stride);
+            if (!post)
+                return;
+            const Vec8 w = param8<A, FULL>(p.post_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    y2[e] = (n[e] - m2) * r2;
-                    n[e] = y2[e] * w[e];
-                }
-                if (p.post_bias) {
-                    param8<A>(p.post_bias, p.param_f32, q.col, q.n, p.wide_params, 0.f, w);
+            for (int j = 0; j < N; ++j) {
+                const f2 minus = both(-m2[j]), r = both(r2[j]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        n[e] += w[e];
+                for (int i = 0; i < 4; ++i) {
+                    y2[j].v[i] = mul(add(n[j].v[i], minus), r);
+                    n[j].v[i] = mul(y2[j].v[i], w.v[i]);
                 }
             }
-            if (gated)
-                fetch_gate<A>(p, at + gate_at, stride, gate);
+            if (p.post_bias) {
+                const Vec8 b = param8<A, FULL>(p.post_bias, p.param_f32, q.col, q.n, p.wide_params, 0.f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                y1[e] = fmaf(p.b, gate[e] * n[e], y1[e]);
-        }
-        float e1[8];            // du, then the gradient of u
-        if (p.du.data)
-            fetch8<R>(at + du_at, stride, e1);
-        else
+                for (int j = 0; j < N; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                e1[e] = 0.f;
-        if (p.dh.data)
-            fetch8<A>(at + dh_at, stride, g1);
-        else
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                g1[e] = 0.f;
-        if (pre) {
-            param8<A>(p.pre_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f, w);
-            float t[2] = {0.f, 0.f};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                y1[e] = (y1[e] - m1) * r1;
-                if (live) {
-                    dw1[e] = fmaf(g1[e], y1[e], dw1[e]);
-                    if (BIAS)
-                        db1[e] += g1[e];
-                }
-                g1[e] *= w[e];
-                t[0] = fmaf(g1[e], y1[e], t[0]);
-                t[1] += g1[e];
+                    for (int i = 0; i < 4; ++i)
+                        n[j].v[i] = add(n[j].v[i], b.v[i]);
             }
-            row_sum(p, sums, parity, t);
-            t[0] *= p.inv_cols;
-            t[1] = p.pre == RIKFAD_NORM_LAYER ? t[1] * p.inv_cols : 0.f;
+        };
+        auto times_gate = [&](Vec8(&v)[N]) {
+            if (p.gate_f32) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                e1[e] = fmaf(r1, (g1[e] - t[1]) - y1[e] * t[0], e1[e]);
-        } else {
+                for (int j = 0; j < N; ++j) {
+                    const Vec8 g = fetch8<float>(at0 + j * row_bytes + gate_at, stride);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                e1[e] += g1[e];
-        }
-        if (live && q.n > 0 && p.dx.data) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                w[e] = p.a * e1[e];
-            put8(static_cast<R *>(p.dx.data) + row * p.dx.stride + q.col, w, q.n, p.wide_dx);
-        }
-        if (branch) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                e1[e] *= p.b;
-            if (p.shared_gate) {
-                if (live)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        dg[e] = fmaf(e1[e], n[e], dg[e]);
-                // The gate's last row, or the group's: a gate that lies within the
-                // group is done, others leave a partial sum.
-                if (live && (--gate_left == 0 || k + 1 == q.count)) {
-                    const bool whole = gate_whole && gate_left == 0;
-                    if (whole) {
-                        const int64_t to = gate_row * p.dgate.stride + q.col;
-                        if (q.n > 0) {
-                            if (p.gate_f32)
-                                put8(static_cast<float *>(p.dgate.data) + to, dg, q.n, p.wide_dgate);
-                            else
-                                put8(static_cast<A *>(p.dgate.data) + to, dg, q.n, p.wide_dgate);
-                        }
-                    } else {
-                        float *part = p.gate_part + (2 * worker + gate_slot) * p.cols + q.col;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (e < q.n)
-                                part[e] = dg[e];
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        dg[e] = 0.f;
-                    ++gate_row;
-                    gate_left = p.gate_rows;
-                    gate_whole = true;
-                    gate_slot = 1;
+                    for (int i = 0; i < 4; ++i)
+                        v[j].v[i] = mul(v[j].v[i], g.v[i]);
                 }
-            } else if (p.dgate.data && live && q.n > 0) {
+            } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    w[e] = e1[e] * n[e];
-                const int64_t to = row * p.dgate.stride + q.col;
-                if (p.gate_f32)
-                    put8(static_cast<float *>(p.dgate.data) + to, w, q.n, p.wide_dgate);
-                else
-                    put8(static_cast<A *>(p.dgate.data) + to, w, q.n, p.wide_dgate);
+                for (int j = 0; j < N; ++j) {
+                    const Vec8 g = fetch8<A>(at0 + j * row_bytes + gate_at, stride);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        v[j].v[i] = mul(v[j].v[i], g.v[i]);
+                }
             }
+        };
+        // -mean(e y) and -mean(e) (a layer norm's) of every row
+        auto means = [&](int kind, float(&t0)[N], float(&t1)[N]) {
+            if (kind == RIKFAD_NORM_LAYER) {
+                float t[2 * N];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                e1[e] *= gate[e];
-            if (post) {
-                param8<A>(p.post_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f, w);
-                float t[2] = {0.f, 0.f};
+                for (int j = 0; j < N; ++j) {
+                    f2 s = mul(e[j].v[0], y[j].v[0]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (live) {
-                        dw2[e] = fmaf(e1[e], y2[e], dw2[e]);
-                        if (BIAS)
-                            db2[e] += e1[e];
-                    }
-                    e1[e] *= w[e];
-                    t[0] = fmaf(e1[e], y2[e], t[0]);
-                    t[1] += e1[e];
+                    for (int i = 1; i < 4; ++i)
+                        s = fma(e[j].v[i], y[j].v[i], s);
+                    t[2 * j] = total(s);
+                    t[2 * j + 1] = elements(e[j]);
                 }
                 row_sum(p, sums, parity, t);
-                t[0] *= p.inv_cols;
-                t[1] = p.post == RIKFAD_NORM_LAYER ? t[1] * p.inv_cols : 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    e1[e] = r2 * ((e1[e] - t[1]) - y2[e] * t[0]);
+                for (int j = 0; j < N; ++j) {
+                    t0[j] = -t[2 * j] * p.inv_cols;
+                    t1[j] = -t[2 * j + 1] * p.inv_cols;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    f2 s = mul(e[j].v[0], y[j].v[0]);
+#pragma unroll
+                    for (int i = 1; i < 4; ++i)
+                        s = fma(e[j].v[i], y[j].v[i], s);
+                    t0[j] = total(s);
+                }
+                row_sum(p, sums, parity, t0);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    t0[j] *= -p.inv_cols;
+                    t1[j] = 0.f;
+                }
             }
-            if (live && q.n > 0 && p.dz.data)
-                put8(static_cast<A *>(p.dz.data) + row * p.dz.stride + q.col, e1, q.n, p.wide_dz);
+        };
+
+        // e: the gradient of h, then of u
+        if (p.dh.data) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                e[j] = fetch8<A>(at0 + j * row_bytes + dh_at, stride);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                e[j] = splat(0.f);
         }
+        float t0[N], t1[N];
+        if (pre) {
+            if (branch) {
+                branch_of(y);
+                if (gated)
+                    times_gate(n);
+            }
+            const f2 a2 = both(p.a), b2 = both(p.b);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                y[j] = fetch8<R>(at0 + j * row_bytes, stride);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    y[j].v[i] = mul(y[j].v[i], a2);
+            }
+            if (branch) {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        y[j].v[i] = fma(n[j].v[i], b2, y[j].v[i]);
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const f2 minus = both(-m1[j]), r = both(r1[j]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    y[j].v[i] = mul(add(y[j].v[i], minus), r);
+                if (k + j < q.count) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        dw1.v[i] = fma(e[j].v[i], y[j].v[i], dw1.v[i]);
+                        if (BIAS)
+                            db1.v[i] = add(e[j].v[i], db1.v[i]);
+                    }
+                }
+            }
+            if (p.pre_weight) {
+                const Vec8 w = param8<A, FULL>(p.pre_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f);
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        e[j].v[i] = mul(e[j].v[i], w.v[i]);
+            }
+            means(p.pre, t0, t1);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const f2 my = both(t0[j]), m = both(t1[j]), r = both(r1[j]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    e[j].v[i] = mul(fma(y[j].v[i], my, add(e[j].v[i], m)), r);
+            }
+        }
+        if (p.du.data) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const Vec8 d = fetch8<R>(at0 + j * row_bytes + du_at, stride);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    e[j].v[i] = add(e[j].v[i], d.v[i]);
+            }
+        }
+        if (p.dx.data) {
+            const f2 a2 = both(p.a);
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (k + j < q.count && q.n > 0) {
+                    Vec8 o;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        o.v[i] = mul(e[j].v[i], a2);
+                    put8<R, FULL>(dx, o, q.n, p.wide_dx);
+                    dx += p.dx.step;
+                }
+        }
+        if (branch) {
+            const f2 b2 = both(p.b);
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    e[j].v[i] = mul(e[j].v[i], b2);
+            if (post || p.dgate.data)
+                branch_of(y);
+            if (shared_gate) {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (k + j < q.count) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            dg.v[i] = fma(e[j].v[i], n[j].v[i], dg.v[i]);
+                        // The gate's last row, or the group's: a gate that lies within
+                        // the group is done, others leave a partial sum (the group's
+                        // first gate in row 0, its last in row 1).
+                        if (dgate.left == 1 || k + j + 1 == q.count) {
+                            if (gate_whole && dgate.left == 1)
+                                put_gate(dg);
+                            else
+                                gate_part(dg);
+                            dg = splat(0.f);
+                            gate_whole = true;
+                            gate_first = false;
+                        }
+                        dgate.next(p, p.dgate);
+                    }
+            } else if (p.dgate.data) {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (k + j < q.count) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            n[j].v[i] = mul(e[j].v[i], n[j].v[i]);
+                        put_gate(n[j]);
+                        dgate.next(p, p.dgate);
+                    }
+            }
+            if (gated)
+                times_gate(e);
+            if (post) {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (k + j < q.count) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            dw2.v[i] = fma(e[j].v[i], y[j].v[i], dw2.v[i]);
+                            if (BIAS)
+                                db2.v[i] = add(e[j].v[i], db2.v[i]);
+                        }
+                    }
+                const Vec8 w = param8<A, FULL>(p.post_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f);
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        e[j].v[i] = mul(e[j].v[i], w.v[i]);
+                means(p.post, t0, t1);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const f2 my = both(t0[j]), m = both(t1[j]), r = both(r2[j]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        e[j].v[i] = mul(fma(y[j].v[i], my, add(e[j].v[i], m)), r);
+                }
+            }
+            if (p.dz.data) {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (k + j < q.count && q.n > 0) {
+                        put8<A, FULL>(dz, e[j], q.n, p.wide_dz);
+                        dz += p.dz.step;
+                    }
+            }
+        }
+        at0 += stage_bytes;
+        if (at0 == end)
+            at0 = slot;
     }
     allow_successor_launch();
     asm volatile("cp.async.wait_all;" ::: "memory");
-    float *part = p.sum_part;
-    float *buffer = reinterpret_cast<float *>(stages);
-    const int id = blockIdx.x / p.cluster;
+    float *part = p.sum_part, *buffer = reinterpret_cast<float *>(stages);
     const int64_t size = (int64_t)p.ctas * p.cols;
     if (p.dpre_weight) {
-        store_sum(p, q, part, id, buffer, dw1);
+        store_sum(p, q, part, buffer, dw1);
         part += size;
     }
     if (p.dpost_weight) {
-        store_sum(p, q, part, id, buffer, dw2);
+        store_sum(p, q, part, buffer, dw2);
         part += size;
     }
     if (BIAS && p.dpre_bias) {
-        store_sum(p, q, part, id, buffer, db1);
+        store_sum(p, q, part, buffer, db1);
         part += size;
     }
     if (BIAS && p.dpost_bias)
-        store_sum(p, q, part, id, buffer, db2);
+        store_sum(p, q, part, buffer, db2);
 }
 
 // ----------------------------------------------------------- sums over rows
@@ -737,16 +1073,26 @@ template <typename K> cudaError_t launch_clustered(K kernel, const NormParams &n
     return cudaLaunchKernelEx(&cfg, kernel, n);
 }
 
-template <typename A, typename R> cudaError_t launch_norm(const NormParams &n, bool backward, cudaStream_t s)
+template <typename A, typename R, bool FULL> cudaError_t launch_rows(const NormParams &n, bool backward, cudaStream_t s)
 {
     if (!backward)
-        return launch_clustered(rikfad_norm_forward_kernel<A, R>, n, s);
-    const bool bias = n.dpre_bias || n.dpost_bias;
-    const cudaError_t e = bias ? launch_clustered(rikfad_norm_backward_kernel<A, R, true>, n, s)
-                               : launch_clustered(rikfad_norm_backward_kernel<A, R, false>, n, s);
-    if (e != cudaSuccess || (n.sums == 0 && !n.shared_gate))
+        return n.at_once == 1 ? launch_clustered(rikfad_norm_forward_kernel<A, R, 1, FULL>, n, s)
+                              : launch_clustered(rikfad_norm_forward_kernel<A, R, kNormRows, FULL>, n, s);
+    if (n.at_once == 1)
+        return launch_clustered(rikfad_norm_backward_kernel<A, R, 1, FULL, true>, n, s);
+    return n.bias ? launch_clustered(rikfad_norm_backward_kernel<A, R, kNormRows, FULL, true>, n, s)
+                  : launch_clustered(rikfad_norm_backward_kernel<A, R, kNormRows, FULL, false>, n, s);
+}
+
+template <typename A, typename R> cudaError_t launch_norm(const NormParams &n, bool backward, cudaStream_t s)
+{
+    const cudaError_t e = n.full ? launch_rows<A, R, true>(n, backward, s) : launch_rows<A, R, false>(n, backward, s);
+    if (!backward)
         return e;
-    const int64_t gates = n.shared_gate ? n.rows / n.gate_rows : 0;
+    const bool shared_gate = n.dgate.data && n.gate_rows > 1;
+    if (e != cudaSuccess || (n.sums == 0 && !shared_gate))
+        return e;
+    const int64_t gates = shared_gate ? n.rows / n.gate_rows : 0;
     const dim3 grid((unsigned)((n.cols + 31) / 32), (unsigned)(n.sums + (gates < 1024 ? gates : 1024)));
     return launch_chained(rikfad_norm_join_kernel<A>, grid, 32 * kJoinRows, 0, s, n);
 }
