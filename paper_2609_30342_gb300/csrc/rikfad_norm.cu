@@ -106,92 +106,104 @@ NormParams params(const rikfad_residual_norm *p, bool backward)
     n.rows = p->rows;
     n.cols = (int32_t)p->cols;
     n.inv_cols = 1.f / (float)p->cols;
-    n.post = p->post;
-    n.pre = p->pre;
     n.a = (float)p->residual_scale;
     n.b = (float)p->branch_scale;
     n.post_eps = (float)p->post_eps;
     n.pre_eps = (float)p->pre_eps;
     n.gate_rows = p->gate.data ? p->gate_rows : 1;
     n.gate_period = (int32_t)std::min<int64_t>(n.gate_rows, INT32_MAX);
-    n.gate_f32 = p->gate_dtype == RIKFAD_F32;
-    n.param_f32 = p->param_dtype == RIKFAD_F32;
-    n.x = {p->x.data, p->x.stride, 0};
-    n.z = {p->z.data, p->z.stride, 0};
-    n.gate = {p->gate.data, p->gate.stride, 0};
     n.post_weight = p->post_weight;
     n.post_bias = p->post_bias;
     n.pre_weight = p->pre_weight;
     n.pre_bias = p->pre_bias;
     n.stats = reinterpret_cast<float4 *>(p->stats);
     const int64_t gates = p->rows / std::max<int64_t>(n.gate_rows, 1);
-    n.wide_x = wide(p->x, p->residual_dtype, p->rows);
-    n.wide_z = wide(p->z, p->dtype, p->rows);
-    n.wide_gate = wide(p->gate, p->gate_dtype, gates);
-    n.wide_params = true;
-    for (const void *v : {p->post_weight, p->post_bias, p->pre_weight, p->pre_bias})
-        n.wide_params = n.wide_params && (uintptr_t)v % 16 == 0;
+    auto flag = [&](bool on, uint32_t bit) { n.flags |= on ? bit : 0; };
+    auto tensor = [&](NormRows &to, const rikfad_rows &r, int dtype, int64_t rows, uint32_t on, uint32_t wide_bit) {
+        to = {r.data, r.data ? r.stride : 0, 0};
+        flag(r.data != nullptr, on);
+        // absent tensors do not matter
+        n.wide |= r.data == nullptr || wide(r, dtype, rows) ? wide_bit : 0;
+    };
+    tensor(n.x, p->x, p->residual_dtype, p->rows, 0, kNormWideX);
+    tensor(n.z, p->z, p->dtype, p->rows, kNormBranch, kNormWideZ);
+    tensor(n.gate, p->gate, p->gate_dtype, gates, kNormGated, kNormWideGate);
+    flag(p->gate_dtype == RIKFAD_F32, kNormGateF32);
+    flag(p->param_dtype == RIKFAD_F32, kNormParamF32);
+    flag(p->z.data && p->post != RIKFAD_NORM_NONE, kNormPost);
+    flag(p->post == RIKFAD_NORM_LAYER, kNormPostLayer);
+    flag(p->pre != RIKFAD_NORM_NONE, kNormPre);
+    flag(p->pre == RIKFAD_NORM_LAYER, kNormPreLayer);
+    const void *const vectors[4] = {p->post_weight, p->post_bias, p->pre_weight, p->pre_bias};
+    const uint32_t bits[4] = {kNormPostWeight, kNormPostBias, kNormPreWeight, kNormPreBias};
+    for (int i = 0; i < 4; ++i)
+        flag(vectors[i] != nullptr, bits[i]);
+    n.general = p->post_bias || p->pre_bias || p->post == RIKFAD_NORM_LAYER || p->pre == RIKFAD_NORM_LAYER;
     if (!backward) {
-        n.u = {p->u.data, p->u.stride, 0};
-        n.h = {p->h.data, p->h.stride, 0};
-        n.wide_u = wide(p->u, p->residual_dtype, p->rows);
-        n.wide_h = wide(p->h, p->dtype, p->rows);
+        tensor(n.u, p->u, p->residual_dtype, p->rows, kNormU, kNormWideU);
+        tensor(n.h, p->h, p->dtype, p->rows, kNormH, kNormWideH);
+        flag(p->stats != nullptr, kNormStats);
+        n.wide |= kNormWideDu | kNormWideDh | kNormWideDx | kNormWideDz | kNormWideDgate;
         return n;
     }
-    n.du = {p->du.data, p->du.stride, 0};
-    n.dh = {p->dh.data, p->dh.stride, 0};
-    n.dx = {p->dx.data, p->dx.stride, 0};
-    n.dz = {p->dz.data, p->dz.stride, 0};
-    n.dgate = {p->dgate.data, p->dgate.stride, 0};
+    n.wide |= kNormWideU | kNormWideH;
+    tensor(n.du, p->du, p->residual_dtype, p->rows, kNormDu, kNormWideDu);
+    tensor(n.dh, p->dh, p->dtype, p->rows, kNormDh, kNormWideDh);
+    tensor(n.dx, p->dx, p->residual_dtype, p->rows, kNormDx, kNormWideDx);
+    tensor(n.dz, p->dz, p->dtype, p->rows, kNormDz, kNormWideDz);
+    tensor(n.dgate, p->dgate, p->gate_dtype, gates, kNormDgate, kNormWideDgate);
+    flag(p->dgate.data && p->gate_rows > 1, kNormSharedGate);
     n.dpost_weight = p->dpost_weight;
     n.dpost_bias = p->dpost_bias;
     n.dpre_weight = p->dpre_weight;
     n.dpre_bias = p->dpre_bias;
-    n.wide_du = wide(p->du, p->residual_dtype, p->rows);
-    n.wide_dh = wide(p->dh, p->dtype, p->rows);
-    n.wide_dx = wide(p->dx, p->residual_dtype, p->rows);
-    n.wide_dz = wide(p->dz, p->dtype, p->rows);
-    n.wide_dgate = wide(p->dgate, p->gate_dtype, gates);
+    flag(p->dpre_weight, kNormDpreWeight);
+    flag(p->dpost_weight, kNormDpostWeight);
+    flag(p->dpre_bias, kNormDpreBias);
+    flag(p->dpost_bias, kNormDpostBias);
+    n.general = n.general || p->dpre_bias || p->dpost_bias;
     return n;
 }
 
-// Threads of a row, columns of a block and blocks of a cluster, from the width
-// and the most threads that a block's registers allow (rikfad_norm.hpp).
-void shape(NormParams &n, int most_threads)
+// Threads of a row, columns of a block and blocks of a cluster, from the width; how
+// far a thread's rows are apart.
+void shape(NormParams &n, const rikfad_residual_norm *p)
 {
     const int vectors = (n.cols + 7) / 8;
     n.cluster = 1;
-    while ((vectors + n.cluster - 1) / n.cluster > most_threads)
+    while ((vectors + n.cluster - 1) / n.cluster > kNormMaxThreads)
         n.cluster *= 2;
     const int here = (vectors + n.cluster - 1) / n.cluster;
     n.cta_cols = here * 8;
-    n.lanes = here <= 8 ? 8 : here <= 16 ? 16 : (here + 31) / 32 * 32;
+    n.lanes = 1;
+    while (n.lanes < 32 && n.lanes < here)
+        n.lanes *= 2;
+    if (here > 32)
+        n.lanes = (here + 31) / 32 * 32;
     n.threads = n.lanes <= 32 ? 128 : n.lanes;
     n.row_groups = n.threads / n.lanes;
-}
-
-// A thread's rows are `row_groups` apart, or neighbours where rows share gates.
-void steps(NormParams &n, int dtype, int residual_dtype, int gate_dtype)
-{
+    n.full = n.cols % 8 == 0 && n.wide == kNormWideAll;
+    // `row_groups` rows, or neighbours where rows share gates
     const int64_t rows = n.gate_rows > 1 ? 1 : n.row_groups;
-    const int64_t a = rows * dtype_bytes(dtype), r = rows * dtype_bytes(residual_dtype), g = rows * dtype_bytes(gate_dtype);
+    const int64_t a = rows * dtype_bytes(p->dtype), r = rows * dtype_bytes(p->residual_dtype);
+    const int64_t g = rows * dtype_bytes(p->gate_dtype);
     for (NormRows *t : {&n.z, &n.h, &n.dh, &n.dz})
         t->step = t->stride * a;
     for (NormRows *t : {&n.x, &n.u, &n.du, &n.dx})
         t->step = t->stride * r;
+    // the rows of a shared gate are counted, so a step there is one gate
     for (NormRows *t : {&n.gate, &n.dgate})
         t->step = t->stride * g;
 }
 
 // Clusters of a launch: as many as are resident at once (`threads_per_sm` by the
 // kernel's register bound, and by the shared memory of their stages), no more than
-// there are rows.  Two rows at a time once every group has them.
-void grid(NormParams &n, int threads_per_sm, bool one_row)
+// there are rows.
+void grid(NormParams &n, int threads_per_sm)
 {
     const int by_registers = std::max(1, threads_per_sm / n.threads);
     const int64_t groups = (n.rows + n.row_groups - 1) / n.row_groups;
-    n.at_once = !one_row && groups >= (int64_t)kNormRows * kNormSms * by_registers / n.cluster ? kNormRows : 1;
-    const size_t stage = (size_t)n.threads * 16 * n.units * n.at_once;
+    const size_t stage = (size_t)n.threads * 16 * n.units;
     n.stages = stage * 3 * by_registers <= kNormSmemPerSm ? 3 : 2;
     n.smem = stage * n.stages;
     const int resident = std::max(1, std::min(by_registers, (int)(kNormSmemPerSm / n.smem)));
@@ -201,12 +213,9 @@ void grid(NormParams &n, int threads_per_sm, bool one_row)
 void forward_shape(const rikfad_residual_norm *p, NormParams &n)
 {
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
-    shape(n, kNormMaxThreads);
-    steps(n, p->dtype, p->residual_dtype, p->gate_dtype);
     n.units = r + a + (p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
-    n.full = n.cols % 8 == 0 && n.wide_x && n.wide_params && (!p->z.data || n.wide_z) && (!p->gate.data || n.wide_gate) &&
-             (!p->u.data || n.wide_u) && (!p->h.data || n.wide_h);
-    grid(n, kNormForwardThreads, false);
+    shape(n, p);
+    grid(n, kNormForwardThreads);
 }
 
 struct Workspace {
@@ -218,18 +227,9 @@ struct Workspace {
 Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n)
 {
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
-    n.bias = p->dpre_bias || p->dpost_bias;
-    // Two rows at a time with biases take 168 registers; the widest rows would then
-    // need more than 8 blocks.
-    const bool one = n.bias && p->cols > (int64_t)kNormBackwardThreads<true> * 8 * 8;
-    const int threads = n.bias && !one ? kNormBackwardThreads<true> : kNormBackwardThreads<false>;
-    shape(n, threads);
-    steps(n, p->dtype, p->residual_dtype, p->gate_dtype);
     n.units = 2 * a + 2 * r + (p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
-    n.full = n.cols % 8 == 0 && n.wide_x && n.wide_params && (!p->z.data || n.wide_z) && (!p->gate.data || n.wide_gate) &&
-             (!p->du.data || n.wide_du) && (!p->dh.data || n.wide_dh) && (!p->dx.data || n.wide_dx) &&
-             (!p->dz.data || n.wide_dz) && (!p->dgate.data || n.wide_dgate);
-    grid(n, threads, one);
+    shape(n, p);
+    grid(n, kNormBackwardThreads);
     n.sums = 0;
     for (const void *v : {p->dpre_weight, p->dpost_weight, p->dpre_bias, p->dpost_bias})
         n.sums += v != nullptr;

@@ -8,19 +8,61 @@
 
 namespace rikfad {
 
-// A row of up to 4096 columns is one block's (or, up to 256 columns, 8, 16 or 32
-// lanes of one): every thread owns 8 neighbouring columns, so that a block of 512
-// threads may use 128 registers each.  Wider rows are split over a cluster of up to
-// 8 blocks, which exchange their sums through distributed shared memory.
+// A row of up to 4096 columns is one block's (or, up to 256 columns, 1 to 32 lanes
+// of one): every thread owns 8 neighbouring columns, so that a block of 512 threads
+// may use 128 registers each.  Wider rows are split over a cluster of up to 8 blocks,
+// which exchange their sums through distributed shared memory.
 constexpr int kNormMaxThreads = 512;
 constexpr int kNormMaxWarps = kNormMaxThreads / 32;
-constexpr int kNormRows = 2;                // rows of a thread at a time (1 where rows are few)
-// Threads of an SM by the kernels' register bounds: 80; 168 with two rows and
-// biases, else 128.
+// Threads of an SM, by the registers that the kernels are given.
 constexpr int kNormForwardThreads = 768;
-template <bool WIDE> constexpr int kNormBackwardThreads = WIDE ? 384 : 512;
+constexpr int kNormBackwardThreads = 512;
+constexpr int norm_registers(int threads) { return 65536 / threads / 8 * 8; }
 constexpr int kNormSms = 152;
-constexpr size_t kNormSmemPerSm = 200 << 10;    // for the stages; a block keeps 4 KB more
+constexpr size_t kNormSmemPerSm = 200 << 10;    // for the stages; a block keeps 1 KB more
+
+enum : uint32_t {
+    kNormBranch = 1u << 0,          // z is there
+    kNormGated = 1u << 1,
+    kNormGateF32 = 1u << 2,
+    kNormParamF32 = 1u << 3,
+    kNormPost = 1u << 4,
+    kNormPostLayer = 1u << 5,
+    kNormPostWeight = 1u << 6,
+    kNormPostBias = 1u << 7,
+    kNormPre = 1u << 8,
+    kNormPreLayer = 1u << 9,
+    kNormPreWeight = 1u << 10,
+    kNormPreBias = 1u << 11,
+    kNormU = 1u << 12,
+    kNormH = 1u << 13,
+    kNormStats = 1u << 14,
+    kNormDu = 1u << 15,
+    kNormDh = 1u << 16,
+    kNormDx = 1u << 17,
+    kNormDz = 1u << 18,
+    kNormDgate = 1u << 19,
+    kNormSharedGate = 1u << 20,     // dgate is a sum over rows
+    kNormDpreWeight = 1u << 21,
+    kNormDpostWeight = 1u << 22,
+    kNormDpreBias = 1u << 23,
+    kNormDpostBias = 1u << 24,
+};
+
+// Tensors whose rows all start on 16 bytes.
+enum : uint32_t {
+    kNormWideX = 1u << 0,
+    kNormWideZ = 1u << 1,
+    kNormWideGate = 1u << 2,
+    kNormWideU = 1u << 3,
+    kNormWideH = 1u << 4,
+    kNormWideDu = 1u << 5,
+    kNormWideDh = 1u << 6,
+    kNormWideDx = 1u << 7,
+    kNormWideDz = 1u << 8,
+    kNormWideDgate = 1u << 9,
+    kNormWideAll = (1u << 10) - 1,
+};
 
 // Rows of `cols` elements, and the bytes from a thread's row to its next one.
 struct NormRows {
@@ -30,7 +72,7 @@ struct NormRows {
 
 struct NormParams {
     int64_t rows, gate_rows;
-    int32_t cols, post, pre;
+    int32_t cols;
     float inv_cols, a, b, post_eps, pre_eps;
     int32_t gate_period;        // gate_rows, within int
     NormRows x, z, gate;
@@ -39,16 +81,13 @@ struct NormParams {
     NormRows u, h;
     NormRows du, dh, dx, dz, dgate;
     void *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;
-    bool gate_f32, param_f32;
-    // rows that start on 16 bytes
-    bool wide_x, wide_z, wide_gate, wide_params, wide_u, wide_h, wide_du, wide_dh, wide_dx, wide_dz, wide_dgate;
+    uint32_t flags, wide;
     // the launch
-    int32_t at_once;                        // rows of a thread: 1 or kNormRows
-    bool full, bias;                        // no ragged row; gradients of biases
+    bool full, general;                     // no ragged row; a layer norm, a bias or its gradient
     int32_t threads, lanes, row_groups;     // of a block; of a row within it; rows of a block at a time
     int32_t cluster, cta_cols;              // blocks of a row; columns of each
     int32_t ctas;                           // clusters of the launch
-    int32_t units, stages;                  // 16-byte units of 8 columns of a row; rounds in flight and in use
+    int32_t units, stages;                  // 16-byte units of a thread's row; rows in flight and in use
     size_t smem;
     // backward: partial sums
     int32_t sums;

@@ -10,16 +10,16 @@
 // reading u, without the rounding that a stored u has.
 //
 // Both kernels are bound by memory as long as they need few instructions: every
-// element is read once and written once.  A thread owns 8 columns of N rows at a
-// time and keeps them in registers from the load to the store; the rows share its
-// weights' loads, its branches and the barriers of its sums, and hide one another's
-// latencies.  Arithmetic is on pairs of float32 (fma.rn.f32x2).  The copies of the
-// next rows are under way meanwhile (cp.async into slots of shared memory that only
-// this thread reads, so no barrier separates a copy from its use).  Sums over a
-// row: shuffles, and beyond a warp one barrier over the row's warps (or the
-// cluster's blocks).  Sums over rows stay in the thread's registers to the end of
-// the launch, leave one partial row per cluster, and a second kernel adds those in
-// order.
+// element is read once and written once.  A thread owns 8 columns and keeps a row's
+// elements there in registers from the load to the store, the weights in registers
+// for the whole launch; arithmetic is on pairs of float32 (fma.rn.f32x2).  The
+// copies of the next rows are under way meanwhile (cp.async into slots of shared
+// memory that only this thread reads, so no barrier separates a copy from its use).
+// What is absent (a tensor, columns beyond the row's end, a last round's rows) is
+// staged as zeros: the arithmetic has no branches for it.  Sums over a row:
+// shuffles, and beyond a warp one barrier over the row's warps (or the cluster's
+// blocks).  Sums over rows stay in the thread's registers to the end of the launch,
+// leave one partial row per cluster, and a second kernel adds those in order.
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -118,9 +118,10 @@ __device__ __forceinline__ void cut(Vec8 &o, int n)
 
 // ------------------------------------------------------------------ staging
 
-__device__ __forceinline__ void copy16_async(uint32_t smem, const void *src)
+// 16 bytes in flight, or 16 bytes of zeros without a read.
+__device__ __forceinline__ void copy16_async(uint32_t smem, const void *src, bool on)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(src) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
 
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -149,15 +150,15 @@ __device__ __forceinline__ uint4 smem_get(uint32_t smem)
 // 16-byte units of 8 elements.
 template <typename T> constexpr int kUnits = sizeof(T) / 2;
 
-// n elements (1 to 8) into this thread's slot, whose units are `stride` bytes
-// apart: copies in flight where the row starts on 16 bytes, else element by element.
-// FULL: every row starts on 16 bytes and n is 8.
+// n elements (0 to 8) into this thread's slot, whose units are `stride` bytes
+// apart, and zeros after them: copies in flight where the row starts on 16 bytes,
+// else element by element.  FULL: every row starts on 16 bytes and n is 0 or 8.
 template <typename T, bool FULL> __device__ __forceinline__ void stage8(uint32_t slot, uint32_t stride, const void *src, int n, bool wide)
 {
-    if (FULL || (wide && n == 8)) {
-        copy16_async(slot, src);
+    if (FULL || (wide && n % 8 == 0)) {
+        copy16_async(slot, src, n);
         if constexpr (sizeof(T) == 4)
-            copy16_async(slot + stride, static_cast<const char *>(src) + 16);
+            copy16_async(slot + stride, static_cast<const char *>(src) + 16, n);
         return;
     }
     union {
@@ -189,10 +190,13 @@ template <typename T> __device__ __forceinline__ Vec8 fetch8(uint32_t slot, uint
     return widen(r);
 }
 
+// Stores n elements (0 to 8).
 template <typename T, bool FULL> __device__ __forceinline__ void put8(void *to, const Vec8 &v, int n, bool wide)
 {
     const Raw8<T> r = narrow<T>(v);
-    if (FULL || (wide && n == 8)) {
+    if (FULL || (wide && n % 8 == 0)) {
+        if (n == 0)
+            return;
         if constexpr (sizeof(T) == 4) {
             static_cast<float4 *>(to)[0] = r.a;
             static_cast<float4 *>(to)[1] = r.b;
@@ -208,25 +212,15 @@ template <typename T, bool FULL> __device__ __forceinline__ void put8(void *to, 
             static_cast<T *>(to)[e] = each[e];
 }
 
-// Columns [col, col + n) of a weight or bias of type A or float32; `absent` where
+// Columns [col, col + n) of a weight or bias of type A or float32, `absent` where
 // the vector is NULL, 0 beyond n.
-template <typename A, bool FULL> __device__ __forceinline__ Vec8 param8(const void *p, bool f32, int col, int n, bool wide, float absent)
+template <typename A> __device__ __forceinline__ Vec8 param8(const void *p, bool f32, int col, int n, float absent)
 {
-    if (n == 0)
-        return splat(0.f);
-    if (p == nullptr) {
-        Vec8 o = splat(absent);
-        if (!FULL)
-            cut(o, n);
-        return o;
-    }
-    if (FULL || (wide && n == 8))
-        return f32 ? widen(load_raw8(static_cast<const float *>(p) + col)) : widen(load_raw8(static_cast<const A *>(p) + col));
     float f[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        f[e] = e >= n ? 0.f : f32 ? static_cast<const float *>(p)[col + e] : to_f32(static_cast<const A *>(p)[col + e]);
-    return widen(Raw8<float>{make_float4(f[0], f[1], f[2], f[3]), make_float4(f[4], f[5], f[6], f[7])});
+        f[e] = e >= n ? 0.f : !p ? absent : f32 ? static_cast<const float *>(p)[col + e] : to_f32(static_cast<const A *>(p)[col + e]);
+    return {{pair(f[0], f[1]), pair(f[2], f[3]), pair(f[4], f[5]), pair(f[6], f[7])}};
 }
 
 // ----------------------------------------------------------- sums over a row
@@ -236,7 +230,7 @@ __device__ __forceinline__ uint32_t smem_address(const void *p) { return (uint32
 struct alignas(16) RowSums {
     // [parity][value][warp of the cluster]: a sum's slots are written again two sums
     // later, with a barrier in between that follows every read of the first
-    float slot[2][4][kNormMaxWarps * 8];
+    float slot[2][2][kNormMaxWarps * 8];
 };
 
 __device__ __forceinline__ void cluster_barrier()
@@ -244,66 +238,101 @@ __device__ __forceinline__ void cluster_barrier()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// The sums of N values over a row's threads, in every one of them, always in the
-// same order.
-template <int N> __device__ __forceinline__ void row_sum(const NormParams &p, RowSums &s, int &parity, float (&v)[N])
-{
+// A row's threads, and where they leave their sums.
+struct Team {
+    RowSums *sums;
+    uint32_t mine, first;       // shared memory: this warp's slot, a row's first slot (of parity 0, value 0)
+    int lanes, threads, cluster;
+    uint32_t rank;              // of this block in its cluster
+    uint32_t parity;            // bytes: 0 or kParity
+
+    static constexpr uint32_t kValue = sizeof(RowSums::slot[0][0]), kParity = sizeof(RowSums::slot[0]);
+
+    __device__ __forceinline__ Team(const NormParams &p, RowSums &s) : sums(&s), lanes(p.lanes), threads(p.threads), cluster(p.cluster), parity(0)
+    {
+        first = smem_address(&s.slot[0][0][0]);
+        mine = first + (threadIdx.x >> 5) * 4;
+        rank = 0;
+        if (cluster > 1)
+            asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    }
+
+    // The sums of N values over a row's threads, in every one of them, always in the
+    // same order.
+    template <int N> __device__ __forceinline__ void sum(float (&v)[N])
+    {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        if (o < p.lanes)
+        for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float t = __shfl_xor_sync(0xffffffffu, v[i], o);
+                v[i] = o < lanes ? v[i] + t : v[i];
+            }
+        if (lanes <= 32 && cluster == 1)
+            return;
+        parity ^= kParity;
+        if (cluster == 1) {
+            if ((threadIdx.x & 31) == 0)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine + parity + i * kValue), "f"(v[i]) : "memory");
+            __syncthreads();
+            // slots beyond the row's warps are 0
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    if (p.lanes <= 32 && p.cluster == 1)
-        return;
-    parity ^= 1;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (p.cluster == 1) {
-        if (lane == 0)
+                v[i] = four(first + parity + i * kValue);
+            if (threads > 128) {
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                s.slot[parity][i][warp] = v[i];
-        __syncthreads();
-        // 0 beyond the row's warps
+                for (int i = 0; i < N; ++i)
+                    v[i] += four(first + parity + i * kValue + 16);
+                if (threads > 256)
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float4 f = *reinterpret_cast<const float4 *>(&s.slot[parity][i][0]);
-            v[i] = (f.x + f.y) + (f.z + f.w);
-            for (int w = 4; w * 32 < p.threads; w += 4) {
-                f = *reinterpret_cast<const float4 *>(&s.slot[parity][i][w]);
-                v[i] += (f.x + f.y) + (f.z + f.w);
+                    for (int i = 0; i < N; ++i)
+                        v[i] += four(first + parity + i * kValue + 32) + four(first + parity + i * kValue + 48);
+            }
+            return;
+        }
+        across(v);
+    }
+
+    __device__ __forceinline__ static float four(uint32_t at)
+    {
+        float4 f;
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(at) : "memory");
+        return (f.x + f.y) + (f.z + f.w);
+    }
+
+    // Over the blocks of a cluster: lane r hands the warp's values to block r.
+    template <int N> __device__ __forceinline__ void across(float (&v)[N])
+    {
+        const int lane = threadIdx.x & 31;
+        if (lane < cluster) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                uint32_t remote;
+                asm("mapa.shared::cluster.u32 %0, %1, %2;"
+                    : "=r"(remote)
+                    : "r"(mine + parity + i * kValue + rank * kNormMaxWarps * 4), "r"(lane));
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote), "f"(v[i]) : "memory");
             }
         }
-        return;
-    }
-    // lane r < cluster hands the warp's values to block r
-    uint32_t rank;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    if (lane < p.cluster) {
+        cluster_barrier();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            uint32_t remote;
-            asm("mapa.shared::cluster.u32 %0, %1, %2;"
-                : "=r"(remote)
-                : "r"(smem_address(&s.slot[parity][i][rank * kNormMaxWarps + warp])), "r"(lane));
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote), "f"(v[i]) : "memory");
+            const float *slots = sums->slot[parity ? 1 : 0][i];
+            float t = 0.f;
+            for (int w = lane; w < cluster * kNormMaxWarps; w += 32)
+                t += slots[w];
+            v[i] = warp_sum(t);
         }
     }
-    cluster_barrier();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float t = 0.f;
-        for (int w = lane; w < p.cluster * kNormMaxWarps; w += 32)
-            t += s.slot[parity][i][w];
-        v[i] = warp_sum(t);
-    }
-}
+};
 
 // ------------------------------------------------------------------ geometry
 
 // A thread's columns and rows, the same in both directions.
 struct Place {
-    int col, n;             // first column, how many (0 to 8)
+    int col, n;             // first column and how many (0 to 8); without any, a column that exists
     int64_t row;            // first row
     int step;               // distance to the next
     int count, most;        // rows of this thread's group, and of the block's longest
@@ -315,6 +344,8 @@ struct Place {
         const int begin = rank * p.cta_cols, end = min(p.cols, begin + p.cta_cols);
         col = begin + lane * 8;
         n = max(0, min(8, end - col));
+        if (n == 0)
+            col = 0;
         if (p.gate_rows > 1) {
             // each group walks its own run of rows, so that the rows of a gate stay together
             const int64_t workers = (int64_t)p.ctas * p.row_groups, me = (int64_t)id * p.row_groups + group;
@@ -330,10 +361,11 @@ struct Place {
             count = (int)max((int64_t)0, (to - row + p.row_groups - 1) / p.row_groups);
             most = (int)((to - from + p.row_groups - 1) / p.row_groups);
         }
+        row = min(row, p.rows - 1);         // a group without rows points at one that exists
     }
 };
 
-// Where this thread's columns of its first row are; `step` bytes on is its next.
+// This thread's columns of its first row; `step` bytes on are its next ones.
 __device__ __forceinline__ char *first_row(const NormRows &r, int bytes, const Place &q)
 {
     return static_cast<char *>(r.data) + (q.row * r.stride + q.col) * bytes;
@@ -359,15 +391,11 @@ struct GateWalk {
     }
 };
 
-// The head of both kernels: the slots of the sums and of threads without columns
-// are zero.
-__device__ __forceinline__ void prepare(const NormParams &p, RowSums &sums, const Place &q, uint32_t slot, int units)
+// The head of both kernels.
+__device__ __forceinline__ void prepare(const NormParams &p, RowSums &sums)
 {
     for (int i = threadIdx.x; i < (int)(sizeof sums / 4); i += p.threads)
         (&sums.slot[0][0][0])[i] = 0.f;
-    if (q.n == 0)
-        for (int i = 0; i < units; ++i)
-            smem_put(slot + i * p.threads * 16, make_uint4(0, 0, 0, 0));
     if (p.cluster > 1)
         cluster_barrier();
     else
@@ -375,214 +403,153 @@ __device__ __forceinline__ void prepare(const NormParams &p, RowSums &sums, cons
     wait_for_predecessor();
 }
 
-// v - m, 0 beyond the row's end.
-template <bool FULL> __device__ __forceinline__ Vec8 centred(const Vec8 &v, float m, int n)
+#define RK_PAIR _Pragma("unroll") for (int i = 0; i < 4; ++i)
+
+__device__ __forceinline__ float dot(const Vec8 &a, const Vec8 &b)
 {
-    const f2 minus = both(n > 0 ? -m : 0.f);
-    Vec8 d;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        d.v[i] = add(v.v[i], minus);
-    if (!FULL)
-        cut(d, n);
-    return d;
+    f2 s = mul(a.v[0], b.v[0]), t = mul(a.v[1], b.v[1]);
+    s = fma(a.v[2], b.v[2], s);
+    t = fma(a.v[3], b.v[3], t);
+    return total(add(s, t));
 }
 
-__device__ __forceinline__ float squares(const Vec8 &v)
-{
-    f2 s = mul(v.v[0], v.v[0]);
-#pragma unroll
-    for (int i = 1; i < 4; ++i)
-        s = fma(v.v[i], v.v[i], s);
-    return total(s);
-}
+__device__ __forceinline__ float elements(const Vec8 &a) { return total(add(add(a.v[0], a.v[1]), add(a.v[2], a.v[3]))); }
 
-__device__ __forceinline__ float elements(const Vec8 &v) { return total(add(add(v.v[0], v.v[1]), add(v.v[2], v.v[3]))); }
-
-// Means and 1 / deviations (or root mean squares) of N rows; v becomes v - m.
-template <int N, bool FULL> __device__ __forceinline__ void row_stats(const NormParams &p, RowSums &s, int &parity, int kind, float eps, int n,
-                                                                      Vec8 (&v)[N], float (&m)[N], float (&r)[N])
+// Mean and 1 / deviation (or root mean square) of a row; v becomes v - m, 0 beyond
+// the row's end.
+template <bool FULL, bool GENERAL>
+__device__ __forceinline__ void row_stats(const NormParams &p, Team &team, bool layer, float eps, int n, Vec8 &v, float &m, float &r)
 {
-    float t[N];
-    if (kind == RIKFAD_NORM_LAYER) {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            t[j] = elements(v[j]);
-        row_sum(p, s, parity, t);
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            m[j] = t[j] * p.inv_cols;
-            v[j] = centred<FULL>(v[j], m[j], n);
-        }
+    if (GENERAL && layer) {
+        float t[1] = {elements(v)};
+        team.sum(t);
+        m = t[0] * p.inv_cols;
+        const f2 minus = both(n > 0 ? -m : 0.f);
+        RK_PAIR v.v[i] = add(v.v[i], minus);
+        if (!FULL)
+            cut(v, n);
     }
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-        t[j] = squares(v[j]);
-    row_sum(p, s, parity, t);
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-        r[j] = rsqrtf(fmaf(t[j], p.inv_cols, eps));
+    float t[1] = {dot(v, v)};
+    team.sum(t);
+    r = rsqrtf(fmaf(t[0], p.inv_cols, eps));
+}
+
+// A thread's ring of stages: where the next row's copies go, and where the present
+// row's are.
+struct Ring {
+    uint32_t begin, end, bytes, put, get;
+
+    __device__ __forceinline__ Ring(const NormParams &p, const void *stages)
+    {
+        begin = smem_address(stages) + threadIdx.x * 16;
+        bytes = p.threads * 16 * p.units;
+        end = begin + bytes * p.stages;
+        put = get = begin;
+    }
+    __device__ __forceinline__ void issued()
+    {
+        commit_copies();
+        put += bytes;
+        if (put == end)
+            put = begin;
+    }
+    __device__ __forceinline__ void used()
+    {
+        get += bytes;
+        if (get == end)
+            get = begin;
+    }
+};
+
+template <typename A, bool FULL> __device__ __forceinline__ void stage_gate(const NormParams &p, uint32_t to, uint32_t stride, const char *at, int n)
+{
+    if (p.flags & kNormGateF32)
+        stage8<float, FULL>(to, stride, at, n, p.wide & kNormWideGate);
+    else
+        stage8<A, FULL>(to, stride, at, n, p.wide & kNormWideGate);
+}
+
+template <typename A> __device__ __forceinline__ Vec8 fetch_gate(const NormParams &p, uint32_t at, uint32_t stride)
+{
+    return p.flags & kNormGateF32 ? fetch8<float>(at, stride) : fetch8<A>(at, stride);
 }
 
 // ------------------------------------------------------------------- forward
 
-template <typename A, typename R, int N, bool FULL>
-__global__ void __maxnreg__((65536 / kNormForwardThreads / 8 * 8))
-    rikfad_norm_forward_kernel(const __grid_constant__ NormParams p)
+template <typename A, typename R, bool FULL, bool POST, bool GENERAL>
+__global__ void __maxnreg__((norm_registers(kNormForwardThreads))) rikfad_norm_forward_kernel(const __grid_constant__ NormParams p)
 {
     extern __shared__ uint4 stages[];
     __shared__ RowSums sums;
     const Place q(p);
-    const uint32_t stride = p.threads * 16, slot = smem_address(stages + threadIdx.x);
-    const uint32_t row_bytes = stride * p.units, stage_bytes = row_bytes * N, end = slot + p.stages * stage_bytes;
-    const bool branch = p.z.data != nullptr, gated = p.gate.data != nullptr;
-    const bool post = branch && p.post != RIKFAD_NORM_NONE, pre = p.pre != RIKFAD_NORM_NONE;
+    const uint32_t f = p.flags;
+    const bool branch = POST || (f & kNormBranch), gated = f & kNormGated;
+    const uint32_t stride = p.threads * 16;
     const uint32_t z_at = kUnits<R> * stride, gate_at = z_at + kUnits<A> * stride;
-    int parity = 0;
-    prepare(p, sums, q, slot, p.units * N * p.stages);
-    char *x = first_row(p.x, sizeof(R), q), *z = first_row(p.z, sizeof(A), q);
+    Ring ring(p, stages);
+    Team team(p, sums);
+    prepare(p, sums);
+    const char *x = first_row(p.x, sizeof(R), q), *z = first_row(p.z, sizeof(A), q);
     char *u_out = first_row(p.u, sizeof(R), q), *h_out = first_row(p.h, sizeof(A), q);
-    GateWalk gate(p, p.gate, p.gate_f32 ? 4 : (int)sizeof(A), q);
-    int ahead = 0;              // rows issued
-    uint32_t issue_at = slot;
+    GateWalk gate(p, p.gate, f & kNormGateF32 ? 4 : (int)sizeof(A), q);
+    int left = q.count;         // rows to issue; the pointers stay on rows that exist
     auto issue = [&]() {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (ahead + j < q.count && q.n > 0) {
-                const uint32_t at = issue_at + j * row_bytes;
-                stage8<R, FULL>(at, stride, x, q.n, p.wide_x);
-                x += p.x.step;
-                if (branch) {
-                    stage8<A, FULL>(at + z_at, stride, z, q.n, p.wide_z);
-                    z += p.z.step;
-                }
-                if (gated) {
-                    if (p.gate_f32)
-                        stage8<float, FULL>(at + gate_at, stride, gate.at, q.n, p.wide_gate);
-                    else
-                        stage8<A, FULL>(at + gate_at, stride, gate.at, q.n, p.wide_gate);
-                    gate.next(p, p.gate);
-                }
-            }
-        commit_copies();
-        ahead += N;
-        issue_at += stage_bytes;
-        if (issue_at == end)
-            issue_at = slot;
+        const int n = left > 0 ? q.n : 0;
+        stage8<R, FULL>(ring.put, stride, x, n, p.wide & kNormWideX);
+        if (branch)
+            stage8<A, FULL>(ring.put + z_at, stride, z, n, p.wide & kNormWideZ);
+        if (gated)
+            stage_gate<A, FULL>(p, ring.put + gate_at, stride, gate.at, n);
+        if (--left > 0) {
+            x += p.x.step;
+            z += p.z.step;
+            gate.next(p, p.gate);
+        }
+        ring.issued();
     };
     for (int k = 0; k < p.stages - 1; ++k)
         issue();
-    uint32_t at0 = slot;
-    for (int k = 0; k < q.most; k += N) {
+    const Vec8 w2 = param8<A>(p.post_weight, f & kNormParamF32, q.col, q.n, 1.f);
+    const Vec8 w1 = param8<A>(p.pre_weight, f & kNormParamF32, q.col, q.n, 1.f);
+    Vec8 b2, b1;
+    if (GENERAL) {
+        b2 = param8<A>(p.post_bias, f & kNormParamF32, q.col, q.n, 0.f);
+        b1 = param8<A>(p.pre_bias, f & kNormParamF32, q.col, q.n, 0.f);
+    }
+    const f2 a = both(p.a), b = both(p.b);
+    const bool keeps = (f & kNormStats) && q.col == 0;
+    for (int k = 0; k < q.most; ++k) {
         issue();
         wait_copies(p.stages);
-        Vec8 u[N], v[N];
-        float m2[N], r2[N], m1[N], r1[N];
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            m2[j] = m1[j] = 0.f;
-            r2[j] = r1[j] = 1.f;
-            u[j] = fetch8<R>(at0 + j * row_bytes, stride);
-        }
-        const f2 a2 = both(p.a);
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                u[j].v[i] = mul(u[j].v[i], a2);
+        float m2 = 0.f, r2 = 1.f, m1 = 0.f, r1 = 1.f;
+        Vec8 u = fetch8<R>(ring.get, stride);
+        RK_PAIR u.v[i] = mul(u.v[i], a);
         if (branch) {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                v[j] = fetch8<A>(at0 + j * row_bytes + z_at, stride);
-            if (post) {
-                row_stats<N, FULL>(p, sums, parity, p.post, p.post_eps, q.n, v, m2, r2);
-                const Vec8 w = param8<A, FULL>(p.post_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f);
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const f2 r = both(r2[j]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        v[j].v[i] = mul(mul(v[j].v[i], r), w.v[i]);
-                }
-                if (p.post_bias) {
-                    const Vec8 b = param8<A, FULL>(p.post_bias, p.param_f32, q.col, q.n, p.wide_params, 0.f);
-#pragma unroll
-                    for (int j = 0; j < N; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            v[j].v[i] = add(v[j].v[i], b.v[i]);
-                }
+            Vec8 v = fetch8<A>(ring.get + z_at, stride);
+            if (POST) {
+                row_stats<FULL, GENERAL>(p, team, f & kNormPostLayer, p.post_eps, q.n, v, m2, r2);
+                const f2 r = both(r2);
+                RK_PAIR v.v[i] = GENERAL ? fma(mul(v.v[i], r), w2.v[i], b2.v[i]) : mul(mul(v.v[i], r), w2.v[i]);
             }
             if (gated) {
-                if (p.gate_f32) {
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const Vec8 g = fetch8<float>(at0 + j * row_bytes + gate_at, stride);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            v[j].v[i] = mul(v[j].v[i], g.v[i]);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const Vec8 g = fetch8<A>(at0 + j * row_bytes + gate_at, stride);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            v[j].v[i] = mul(v[j].v[i], g.v[i]);
-                    }
-                }
+                const Vec8 g = fetch_gate<A>(p, ring.get + gate_at, stride);
+                RK_PAIR v.v[i] = mul(v.v[i], g.v[i]);
             }
-            const f2 b2 = both(p.b);
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    u[j].v[i] = fma(v[j].v[i], b2, u[j].v[i]);
+            RK_PAIR u.v[i] = fma(v.v[i], b, u.v[i]);
         }
-        if (p.u.data) {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (k + j < q.count && q.n > 0) {
-                    put8<R, FULL>(u_out, u[j], q.n, p.wide_u);
-                    u_out += p.u.step;
-                }
+        const int n = k < q.count ? q.n : 0;
+        put8<R, FULL>(u_out, u, f & kNormU ? n : 0, p.wide & kNormWideU);
+        u_out += p.u.step;
+        if (f & kNormPre) {
+            row_stats<FULL, GENERAL>(p, team, f & kNormPreLayer, p.pre_eps, q.n, u, m1, r1);
+            const f2 r = both(r1);
+            RK_PAIR u.v[i] = GENERAL ? fma(mul(u.v[i], r), w1.v[i], b1.v[i]) : mul(mul(u.v[i], r), w1.v[i]);
         }
-        if (pre) {
-            row_stats<N, FULL>(p, sums, parity, p.pre, p.pre_eps, q.n, u, m1, r1);
-            const Vec8 w = param8<A, FULL>(p.pre_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const f2 r = both(r1[j]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    u[j].v[i] = mul(mul(u[j].v[i], r), w.v[i]);
-            }
-            if (p.pre_bias) {
-                const Vec8 b = param8<A, FULL>(p.pre_bias, p.param_f32, q.col, q.n, p.wide_params, 0.f);
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        u[j].v[i] = add(u[j].v[i], b.v[i]);
-            }
-        }
-        if (p.h.data) {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (k + j < q.count && q.n > 0) {
-                    put8<A, FULL>(h_out, u[j], q.n, p.wide_h);
-                    h_out += p.h.step;
-                }
-        }
-        if (p.stats && q.col == 0) {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (k + j < q.count)
-                    p.stats[q.row + (int64_t)(k + j) * q.step] = make_float4(m2[j], r2[j], m1[j], r1[j]);
-        }
-        at0 += stage_bytes;
-        if (at0 == end)
-            at0 = slot;
+        put8<A, FULL>(h_out, u, f & kNormH ? n : 0, p.wide & kNormWideH);
+        h_out += p.h.step;
+        if (keeps && n > 0)
+            p.stats[q.row + (int64_t)k * q.step] = make_float4(m2, r2, m1, r1);
+        ring.used();
     }
     allow_successor_launch();
 }
@@ -599,9 +566,8 @@ __device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, f
     }
     __syncthreads();
     const int group = threadIdx.x / p.lanes, width = p.lanes * 8;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f2 *>(buffer + group * width + q.col + 2 * i) = acc.v[i];
+    if (q.n > 0)
+        RK_PAIR *reinterpret_cast<f2 *>(buffer + group * width + q.col + 2 * i) = acc.v[i];
     __syncthreads();
     for (int c = threadIdx.x; c < p.cols; c += p.threads) {
         float t = 0.f;
@@ -611,376 +577,189 @@ __device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, f
     }
 }
 
-// The branch's y2 and n are formed twice from the stages, on both sides of the
-// first sum over the row: the registers go to the sums over rows.
-template <typename A, typename R, int N, bool FULL, bool BIAS>
-__global__ void __maxnreg__((65536 / kNormBackwardThreads<BIAS && (N > 1)> / 8 * 8))
-    rikfad_norm_backward_kernel(const __grid_constant__ NormParams p)
+template <typename A, typename R, bool FULL, bool POST, bool GENERAL>
+__global__ void __maxnreg__((norm_registers(kNormBackwardThreads))) rikfad_norm_backward_kernel(const __grid_constant__ NormParams p)
 {
     extern __shared__ uint4 stages[];
     __shared__ RowSums sums;
     const Place q(p);
-    const uint32_t stride = p.threads * 16, slot = smem_address(stages + threadIdx.x);
-    const uint32_t row_bytes = stride * p.units, stage_bytes = row_bytes * N, end = slot + p.stages * stage_bytes;
-    const bool branch = p.z.data != nullptr, gated = p.gate.data != nullptr;
-    const bool post = branch && p.post != RIKFAD_NORM_NONE, pre = p.pre != RIKFAD_NORM_NONE;
-    const bool shared_gate = p.dgate.data && p.gate_rows > 1;
-    const int gate_bytes = p.gate_f32 ? 4 : (int)sizeof(A);
-    int parity = 0;
-    prepare(p, sums, q, slot, p.units * N * p.stages);
+    const uint32_t f = p.flags;
+    const bool branch = POST || (f & kNormBranch), gated = f & kNormGated;
+    const uint32_t stride = p.threads * 16;
+    const int gate_bytes = f & kNormGateF32 ? 4 : (int)sizeof(A);
     // a row's slots: x, z, dh, du, gate
     const uint32_t z_at = kUnits<R> * stride, dh_at = z_at + kUnits<A> * stride, du_at = dh_at + kUnits<A> * stride;
     const uint32_t gate_at = du_at + kUnits<R> * stride;
-    char *x = first_row(p.x, sizeof(R), q), *z = first_row(p.z, sizeof(A), q);
-    char *dh = first_row(p.dh, sizeof(A), q), *du = first_row(p.du, sizeof(R), q);
+    Ring ring(p, stages);
+    Team team(p, sums);
+    prepare(p, sums);
+    const char *x = first_row(p.x, sizeof(R), q), *z = first_row(p.z, sizeof(A), q);
+    // absent ones are read nowhere (zeros take their place)
+    const char *dh = f & kNormDh ? first_row(p.dh, sizeof(A), q) : x, *du = f & kNormDu ? first_row(p.du, sizeof(R), q) : x;
     char *dx = first_row(p.dx, sizeof(R), q), *dz = first_row(p.dz, sizeof(A), q);
     GateWalk gate(p, p.gate, gate_bytes, q);
-    int ahead = 0;
-    uint32_t issue_at = slot;
+    int left = q.count;
     auto issue = [&]() {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (ahead + j < q.count && q.n > 0) {
-                const uint32_t at = issue_at + j * row_bytes;
-                stage8<R, FULL>(at, stride, x, q.n, p.wide_x);
-                x += p.x.step;
-                if (branch) {
-                    stage8<A, FULL>(at + z_at, stride, z, q.n, p.wide_z);
-                    z += p.z.step;
-                }
-                if (p.dh.data) {
-                    stage8<A, FULL>(at + dh_at, stride, dh, q.n, p.wide_dh);
-                    dh += p.dh.step;
-                }
-                if (p.du.data) {
-                    stage8<R, FULL>(at + du_at, stride, du, q.n, p.wide_du);
-                    du += p.du.step;
-                }
-                if (gated) {
-                    if (p.gate_f32)
-                        stage8<float, FULL>(at + gate_at, stride, gate.at, q.n, p.wide_gate);
-                    else
-                        stage8<A, FULL>(at + gate_at, stride, gate.at, q.n, p.wide_gate);
-                    gate.next(p, p.gate);
-                }
-            }
-        commit_copies();
-        ahead += N;
-        issue_at += stage_bytes;
-        if (issue_at == end)
-            issue_at = slot;
+        const int n = left > 0 ? q.n : 0;
+        stage8<R, FULL>(ring.put, stride, x, n, p.wide & kNormWideX);
+        if (branch)
+            stage8<A, FULL>(ring.put + z_at, stride, z, n, p.wide & kNormWideZ);
+        stage8<A, FULL>(ring.put + dh_at, stride, dh, f & kNormDh ? n : 0, p.wide & kNormWideDh);
+        stage8<R, FULL>(ring.put + du_at, stride, du, f & kNormDu ? n : 0, p.wide & kNormWideDu);
+        if (gated)
+            stage_gate<A, FULL>(p, ring.put + gate_at, stride, gate.at, n);
+        if (--left > 0) {
+            x += p.x.step;
+            z += p.z.step;
+            dh += p.dh.step;
+            du += p.du.step;
+            gate.next(p, p.gate);
+        }
+        ring.issued();
     };
     Vec8 dw1 = splat(0.f), dw2 = dw1, db1 = dw1, db2 = dw1, dg = dw1;
     // dgate: a row for every row, or the sum over the gate's
-    const int64_t gate_row0 = p.gate_rows > 1 ? q.row / p.gate_rows : q.row;
     GateWalk dgate(p, p.dgate, gate_bytes, q);
-    bool gate_whole = p.gate_rows * gate_row0 == q.row;     // the sum began with the gate's first row
-    bool gate_first = true;                                 // it is the group's first
-    auto gate_part = [&](const Vec8 &v) {
+    bool gate_whole = p.gate_rows <= 1 || q.row % p.gate_rows == 0;     // the sum began with the gate's first row
+    bool gate_first = true;                                             // it is the group's first
+    auto gate_part = [&]() {
         const int64_t worker = (int64_t)(blockIdx.x / p.cluster) * p.row_groups + threadIdx.x / p.lanes;
-        put8<float, false>(p.gate_part + (2 * worker + (gate_first ? 0 : 1)) * p.cols + q.col, v, q.n, false);
+        put8<float, false>(p.gate_part + (2 * worker + (gate_first ? 0 : 1)) * p.cols + q.col, dg, q.n, false);
     };
     auto put_gate = [&](const Vec8 &v) {
-        if (q.n == 0)
-            return;
-        if (p.gate_f32)
-            put8<float, FULL>(dgate.at, v, q.n, p.wide_dgate);
+        if (f & kNormGateF32)
+            put8<float, FULL>(dgate.at, v, q.n, p.wide & kNormWideDgate);
         else
-            put8<A, FULL>(dgate.at, v, q.n, p.wide_dgate);
+            put8<A, FULL>(dgate.at, v, q.n, p.wide & kNormWideDgate);
     };
-    if (shared_gate && q.count == 0)            // a group without rows adds nothing to the gate it lies in
-        gate_part(dg);
+    if ((f & kNormSharedGate) && q.count == 0)  // a group without rows adds nothing to the gate it lies in
+        gate_part();
     for (int k = 0; k < p.stages - 1; ++k)
         issue();
+    const Vec8 w2 = param8<A>(p.post_weight, f & kNormParamF32, q.col, q.n, 1.f);
+    const Vec8 w1 = param8<A>(p.pre_weight, f & kNormParamF32, q.col, q.n, 1.f);
+    Vec8 b2 = param8<A>(p.post_bias, f & kNormParamF32, q.col, q.n, 0.f);
+    const f2 a = both(p.a), b = both(p.b);
     const float4 *stats = p.stats + q.row;
-    float4 next[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-        next[j] = j < q.count ? stats[j * q.step] : make_float4(0.f, 0.f, 0.f, 0.f);
-    uint32_t at0 = slot;
-    for (int k = 0; k < q.most; k += N) {
-        issue();
-        float m2[N], r2[N], m1[N], r1[N];
-        stats += N * q.step;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            m2[j] = next[j].x;
-            r2[j] = next[j].y;
-            m1[j] = next[j].z;
-            r1[j] = next[j].w;
-            if (k + N + j < q.count)
-                next[j] = stats[j * q.step];
+    float4 next = q.count > 0 ? *stats : make_float4(0.f, 0.f, 0.f, 0.f);
+    // e becomes r (e - [mean e] - y mean(e y))
+    auto through_norm = [&](bool layer, float r, Vec8 &e, const Vec8 &y) {
+        float t0, t1 = 0.f;
+        if (GENERAL && layer) {
+            float t[2] = {dot(e, y), elements(e)};
+            team.sum(t);
+            t0 = -t[0] * p.inv_cols;
+            t1 = -t[1] * p.inv_cols;
+        } else {
+            float t[1] = {dot(e, y)};
+            team.sum(t);
+            t0 = -t[0] * p.inv_cols;
         }
+        // columns beyond the row's end stay zero: they add nothing to later sums
+        const f2 my = both(t0), m = both(t1), rr = both(q.n > 0 ? r : 0.f);
+        RK_PAIR e.v[i] = mul(fma(y.v[i], my, add(e.v[i], m)), rr);
+        if (!FULL)
+            cut(e, q.n);
+    };
+    for (int k = 0; k < q.most; ++k) {
+        issue();
+        const int n = k < q.count ? q.n : 0;
+        const float m2 = next.x, r2 = next.y, m1 = next.z, r1 = next.w;
+        stats += q.step;
+        next = k + 1 < q.count ? *stats : make_float4(0.f, 0.f, 0.f, 0.f);
         wait_copies(p.stages);
 
-        // y2 and n of every row
-        Vec8 e[N], y[N], n[N];
-        auto branch_of = [&](Vec8(&y2)[N]) {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                n[j] = fetch8<A>(at0 + j * row_bytes + z_at, stride);
-            if (!post)
-                return;
-            const Vec8 w = param8<A, FULL>(p.post_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const f2 minus = both(-m2[j]), r = both(r2[j]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    y2[j].v[i] = mul(add(n[j].v[i], minus), r);
-                    n[j].v[i] = mul(y2[j].v[i], w.v[i]);
-                }
-            }
-            if (p.post_bias) {
-                const Vec8 b = param8<A, FULL>(p.post_bias, p.param_f32, q.col, q.n, p.wide_params, 0.f);
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        n[j].v[i] = add(n[j].v[i], b.v[i]);
-            }
-        };
-        auto times_gate = [&](Vec8(&v)[N]) {
-            if (p.gate_f32) {
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const Vec8 g = fetch8<float>(at0 + j * row_bytes + gate_at, stride);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        v[j].v[i] = mul(v[j].v[i], g.v[i]);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const Vec8 g = fetch8<A>(at0 + j * row_bytes + gate_at, stride);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        v[j].v[i] = mul(v[j].v[i], g.v[i]);
-                }
-            }
-        };
-        // -mean(e y) and -mean(e) (a layer norm's) of every row
-        auto means = [&](int kind, float(&t0)[N], float(&t1)[N]) {
-            if (kind == RIKFAD_NORM_LAYER) {
-                float t[2 * N];
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    f2 s = mul(e[j].v[0], y[j].v[0]);
-#pragma unroll
-                    for (int i = 1; i < 4; ++i)
-                        s = fma(e[j].v[i], y[j].v[i], s);
-                    t[2 * j] = total(s);
-                    t[2 * j + 1] = elements(e[j]);
-                }
-                row_sum(p, sums, parity, t);
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    t0[j] = -t[2 * j] * p.inv_cols;
-                    t1[j] = -t[2 * j + 1] * p.inv_cols;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    f2 s = mul(e[j].v[0], y[j].v[0]);
-#pragma unroll
-                    for (int i = 1; i < 4; ++i)
-                        s = fma(e[j].v[i], y[j].v[i], s);
-                    t0[j] = total(s);
-                }
-                row_sum(p, sums, parity, t0);
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    t0[j] *= -p.inv_cols;
-                    t1[j] = 0.f;
-                }
-            }
-        };
-
-        // e: the gradient of h, then of u
-        if (p.dh.data) {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                e[j] = fetch8<A>(at0 + j * row_bytes + dh_at, stride);
-        } else {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                e[j] = splat(0.f);
-        }
-        float t0[N], t1[N];
-        if (pre) {
-            if (branch) {
-                branch_of(y);
-                if (gated)
-                    times_gate(n);
-            }
-            const f2 a2 = both(p.a), b2 = both(p.b);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                y[j] = fetch8<R>(at0 + j * row_bytes, stride);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    y[j].v[i] = mul(y[j].v[i], a2);
-            }
-            if (branch) {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        y[j].v[i] = fma(n[j].v[i], b2, y[j].v[i]);
-            }
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const f2 minus = both(-m1[j]), r = both(r1[j]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    y[j].v[i] = mul(add(y[j].v[i], minus), r);
-                if (k + j < q.count) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        dw1.v[i] = fma(e[j].v[i], y[j].v[i], dw1.v[i]);
-                        if (BIAS)
-                            db1.v[i] = add(e[j].v[i], db1.v[i]);
-                    }
-                }
-            }
-            if (p.pre_weight) {
-                const Vec8 w = param8<A, FULL>(p.pre_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f);
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        e[j].v[i] = mul(e[j].v[i], w.v[i]);
-            }
-            means(p.pre, t0, t1);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const f2 my = both(t0[j]), m = both(t1[j]), r = both(r1[j]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    e[j].v[i] = mul(fma(y[j].v[i], my, add(e[j].v[i], m)), r);
-            }
-        }
-        if (p.du.data) {
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const Vec8 d = fetch8<R>(at0 + j * row_bytes + du_at, stride);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    e[j].v[i] = add(e[j].v[i], d.v[i]);
-            }
-        }
-        if (p.dx.data) {
-            const f2 a2 = both(p.a);
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (k + j < q.count && q.n > 0) {
-                    Vec8 o;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        o.v[i] = mul(e[j].v[i], a2);
-                    put8<R, FULL>(dx, o, q.n, p.wide_dx);
-                    dx += p.dx.step;
-                }
-        }
+        Vec8 e = fetch8<A>(ring.get + dh_at, stride);       // the gradient of h, then of u
+        Vec8 y = fetch8<R>(ring.get, stride), y2, nn, g = splat(1.f);
+        RK_PAIR y.v[i] = mul(y.v[i], a);
         if (branch) {
-            const f2 b2 = both(p.b);
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    e[j].v[i] = mul(e[j].v[i], b2);
-            if (post || p.dgate.data)
-                branch_of(y);
-            if (shared_gate) {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (k + j < q.count) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            dg.v[i] = fma(e[j].v[i], n[j].v[i], dg.v[i]);
-                        // The gate's last row, or the group's: a gate that lies within
-                        // the group is done, others leave a partial sum (the group's
-                        // first gate in row 0, its last in row 1).
-                        if (dgate.left == 1 || k + j + 1 == q.count) {
-                            if (gate_whole && dgate.left == 1)
-                                put_gate(dg);
-                            else
-                                gate_part(dg);
-                            dg = splat(0.f);
-                            gate_whole = true;
-                            gate_first = false;
-                        }
-                        dgate.next(p, p.dgate);
-                    }
-            } else if (p.dgate.data) {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (k + j < q.count) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            n[j].v[i] = mul(e[j].v[i], n[j].v[i]);
-                        put_gate(n[j]);
-                        dgate.next(p, p.dgate);
-                    }
+            nn = fetch8<A>(ring.get + z_at, stride);
+            if (POST) {
+                const f2 minus = both(-m2), r = both(r2);
+                RK_PAIR y2.v[i] = mul(add(nn.v[i], minus), r);
+                RK_PAIR nn.v[i] = GENERAL ? fma(y2.v[i], w2.v[i], b2.v[i]) : mul(y2.v[i], w2.v[i]);
             }
             if (gated)
-                times_gate(e);
-            if (post) {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (k + j < q.count) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            dw2.v[i] = fma(e[j].v[i], y[j].v[i], dw2.v[i]);
-                            if (BIAS)
-                                db2.v[i] = add(e[j].v[i], db2.v[i]);
-                        }
-                    }
-                const Vec8 w = param8<A, FULL>(p.post_weight, p.param_f32, q.col, q.n, p.wide_params, 1.f);
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        e[j].v[i] = mul(e[j].v[i], w.v[i]);
-                means(p.post, t0, t1);
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const f2 my = both(t0[j]), m = both(t1[j]), r = both(r2[j]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        e[j].v[i] = mul(fma(y[j].v[i], my, add(e[j].v[i], m)), r);
-                }
-            }
-            if (p.dz.data) {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (k + j < q.count && q.n > 0) {
-                        put8<A, FULL>(dz, e[j], q.n, p.wide_dz);
-                        dz += p.dz.step;
-                    }
-            }
+                g = fetch_gate<A>(p, ring.get + gate_at, stride);
+            RK_PAIR g.v[i] = mul(g.v[i], b);
+            RK_PAIR y.v[i] = fma(nn.v[i], g.v[i], y.v[i]);
         }
-        at0 += stage_bytes;
-        if (at0 == end)
-            at0 = slot;
+        if (f & kNormPre) {
+            const f2 minus = both(-m1), r = both(r1);
+            RK_PAIR
+            {
+                y.v[i] = mul(add(y.v[i], minus), r);
+                dw1.v[i] = fma(e.v[i], y.v[i], dw1.v[i]);
+                if (GENERAL)
+                    db1.v[i] = add(e.v[i], db1.v[i]);
+                e.v[i] = mul(e.v[i], w1.v[i]);
+            }
+            through_norm(f & kNormPreLayer, r1, e, y);
+        }
+        {
+            const Vec8 d = fetch8<R>(ring.get + du_at, stride);
+            RK_PAIR e.v[i] = add(e.v[i], d.v[i]);
+        }
+        Vec8 o;
+        RK_PAIR o.v[i] = mul(e.v[i], a);
+        put8<R, FULL>(dx, o, f & kNormDx ? n : 0, p.wide & kNormWideDx);
+        dx += p.dx.step;
+        if (branch) {
+            if (f & kNormSharedGate) {
+                if (k < q.count) {
+                    RK_PAIR dg.v[i] = fma(mul(e.v[i], b), nn.v[i], dg.v[i]);
+                    // The gate's last row, or the group's: a gate that lies within the
+                    // group is done, others leave a partial sum (the group's first gate
+                    // in row 0, its last in row 1).
+                    if (dgate.left == 1 || k + 1 == q.count) {
+                        if (gate_whole && dgate.left == 1)
+                            put_gate(dg);
+                        else
+                            gate_part();
+                        dg = splat(0.f);
+                        gate_whole = true;
+                        gate_first = false;
+                    }
+                    dgate.next(p, p.dgate);
+                }
+            } else if ((f & kNormDgate) && k < q.count) {
+                RK_PAIR nn.v[i] = mul(mul(e.v[i], b), nn.v[i]);
+                put_gate(nn);
+                dgate.next(p, p.dgate);
+            }
+            RK_PAIR e.v[i] = mul(e.v[i], g.v[i]);
+            if (POST) {
+                RK_PAIR
+                {
+                    dw2.v[i] = fma(e.v[i], y2.v[i], dw2.v[i]);
+                    if (GENERAL)
+                        db2.v[i] = add(e.v[i], db2.v[i]);
+                    e.v[i] = mul(e.v[i], w2.v[i]);
+                }
+                through_norm(f & kNormPostLayer, r2, e, y2);
+            }
+            put8<A, FULL>(dz, e, f & kNormDz ? n : 0, p.wide & kNormWideDz);
+            dz += p.dz.step;
+        }
+        ring.used();
     }
     allow_successor_launch();
     asm volatile("cp.async.wait_all;" ::: "memory");
     float *part = p.sum_part, *buffer = reinterpret_cast<float *>(stages);
     const int64_t size = (int64_t)p.ctas * p.cols;
-    if (p.dpre_weight) {
+    if (f & kNormDpreWeight) {
         store_sum(p, q, part, buffer, dw1);
         part += size;
     }
-    if (p.dpost_weight) {
+    if (f & kNormDpostWeight) {
         store_sum(p, q, part, buffer, dw2);
         part += size;
     }
-    if (BIAS && p.dpre_bias) {
+    if (GENERAL && (f & kNormDpreBias)) {
         store_sum(p, q, part, buffer, db1);
         part += size;
     }
-    if (BIAS && p.dpost_bias)
+    if (GENERAL && (f & kNormDpostBias))
         store_sum(p, q, part, buffer, db2);
 }
 
@@ -1030,7 +809,7 @@ template <typename A> __global__ void __launch_bounds__(32 * kJoinRows) rikfad_n
                 dst = each[i];
         const float t = join_column(p.sum_part + (int64_t)blockIdx.y * p.ctas * p.cols + c, p.ctas, p.cols, c < p.cols, red);
         if (x == 0 && out < p.cols)
-            store_as<A>(dst, p.param_f32, out, t);
+            store_as<A>(dst, p.flags & kNormParamF32, out, t);
         return;
     }
     const int64_t gates = p.rows / p.gate_rows, workers = (int64_t)p.ctas * p.row_groups;
@@ -1045,7 +824,7 @@ template <typename A> __global__ void __launch_bounds__(32 * kJoinRows) rikfad_n
         const float *first = p.gate_part + (2 * w0 + (head ? 0 : 1)) * p.cols;
         float t = join_column(p.gate_part + 2 * (w0 + 1) * p.cols + c, w1 - w0, (int64_t)2 * p.cols, c < p.cols, red);
         if (x == 0 && out < p.cols)
-            store_as<A>(p.dgate.data, p.gate_f32, g * p.dgate.stride + out, __ldcg(first + out) + t);
+            store_as<A>(p.dgate.data, p.flags & kNormGateF32, g * p.dgate.stride + out, __ldcg(first + out) + t);
     }
 }
 
@@ -1073,15 +852,18 @@ template <typename K> cudaError_t launch_clustered(K kernel, const NormParams &n
     return cudaLaunchKernelEx(&cfg, kernel, n);
 }
 
+template <typename A, typename R, bool FULL, bool POST, bool GENERAL>
+cudaError_t launch_rows(const NormParams &n, bool backward, cudaStream_t s)
+{
+    return backward ? launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL>, n, s)
+                    : launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL>, n, s);
+}
+
 template <typename A, typename R, bool FULL> cudaError_t launch_rows(const NormParams &n, bool backward, cudaStream_t s)
 {
-    if (!backward)
-        return n.at_once == 1 ? launch_clustered(rikfad_norm_forward_kernel<A, R, 1, FULL>, n, s)
-                              : launch_clustered(rikfad_norm_forward_kernel<A, R, kNormRows, FULL>, n, s);
-    if (n.at_once == 1)
-        return launch_clustered(rikfad_norm_backward_kernel<A, R, 1, FULL, true>, n, s);
-    return n.bias ? launch_clustered(rikfad_norm_backward_kernel<A, R, kNormRows, FULL, true>, n, s)
-                  : launch_clustered(rikfad_norm_backward_kernel<A, R, kNormRows, FULL, false>, n, s);
+    if (n.flags & kNormPost)
+        return n.general ? launch_rows<A, R, FULL, true, true>(n, backward, s) : launch_rows<A, R, FULL, true, false>(n, backward, s);
+    return n.general ? launch_rows<A, R, FULL, false, true>(n, backward, s) : launch_rows<A, R, FULL, false, false>(n, backward, s);
 }
 
 template <typename A, typename R> cudaError_t launch_norm(const NormParams &n, bool backward, cudaStream_t s)
