@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <cstdlib>
 #include <new>
 #include <string>
 
@@ -165,22 +166,38 @@ NormParams params(const rikfad_residual_norm *p, bool backward)
     return n;
 }
 
-// Threads of a row, columns of a block and blocks of a cluster, from the width; how
-// far a thread's rows are apart.
-void shape(NormParams &n, const rikfad_residual_norm *p)
+// Threads of a row that has `vectors` vectors, `v` of them a thread's.
+int row_threads(int vectors, int v)
+{
+    const int threads = (vectors + v - 1) / v;
+    int lanes = 1;
+    while (lanes < 32 && lanes < threads)
+        lanes *= 2;
+    return threads <= 32 ? lanes : (threads + 31) / 32 * 32;
+}
+
+// Vectors of a thread, threads of a row, columns of a block and blocks of a
+// cluster, from the width; how far a thread's rows are apart.  A block has at most
+// `most_threads` threads of `most_vectors` vectors each.
+void shape(NormParams &n, const rikfad_residual_norm *p, int most_vectors, int most_threads)
 {
     const int vectors = (n.cols + 7) / 8;
-    n.cluster = 1;
-    while ((vectors + n.cluster - 1) / n.cluster > kNormMaxThreads)
+    n.cluster = getenv("RK_C") ? atoi(getenv("RK_C")) : 1;
+    while ((vectors + n.cluster - 1) / n.cluster > most_threads * most_vectors)
         n.cluster *= 2;
     const int here = (vectors + n.cluster - 1) / n.cluster;
     n.cta_cols = here * 8;
-    n.lanes = 1;
-    while (n.lanes < 32 && n.lanes < here)
-        n.lanes *= 2;
-    if (here > 32)
-        n.lanes = (here + 31) / 32 * 32;
-    n.threads = n.lanes <= 32 ? 128 : n.lanes;
+    // A row's fixed work costs a thread about as much as one vector does.
+    int best = 0;
+    for (int v = 1; v <= most_vectors; ++v) {
+        const int threads = n.cluster > 1 ? (row_threads(here, v) + 31) / 32 * 32 : row_threads(here, v);
+        if (threads <= most_threads && (best == 0 || threads * (v + 1) < best)) {
+            best = threads * (v + 1);
+            n.vectors = v;
+            n.lanes = threads;
+        }
+    }
+    n.threads = n.lanes <= 32 && n.cluster == 1 ? 128 : n.lanes;
     n.row_groups = n.threads / n.lanes;
     n.full = n.cols % 8 == 0 && n.wide == kNormWideAll;
     // `row_groups` rows, or neighbours where rows share gates
@@ -203,7 +220,7 @@ void grid(NormParams &n, int threads_per_sm)
 {
     const int by_registers = std::max(1, threads_per_sm / n.threads);
     const int64_t groups = (n.rows + n.row_groups - 1) / n.row_groups;
-    const size_t stage = (size_t)n.threads * 16 * n.units;
+    const size_t stage = (size_t)n.threads * 16 * n.units * n.vectors;
     n.stages = stage * 3 * by_registers <= kNormSmemPerSm ? 3 : 2;
     n.smem = stage * n.stages;
     const int resident = std::max(1, std::min(by_registers, (int)(kNormSmemPerSm / n.smem)));
@@ -214,7 +231,7 @@ void forward_shape(const rikfad_residual_norm *p, NormParams &n)
 {
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
     n.units = r + a + (p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
-    shape(n, p);
+    shape(n, p, 1, kNormMaxThreads);
     grid(n, kNormForwardThreads);
 }
 
@@ -228,8 +245,13 @@ Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n)
 {
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
     n.units = 2 * a + 2 * r + (p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
-    shape(n, p);
-    grid(n, kNormBackwardThreads);
+    const bool shared = p->dgate.data && p->gate_rows > 1, post = n.flags & kNormPost;
+    const int one = post && n.general ? kNormBackwardThreads<true, true, 1> : kNormBackwardThreads<false, false, 1>;
+    const int two = !post ? kNormBackwardThreads<false, false, 2> : n.general ? kNormBackwardThreads<true, true, 2> : kNormBackwardThreads<true, false, 2>;
+    const char *ev = getenv("RK_V");
+    const int mv = ev ? atoi(ev) : 2;
+    shape(n, p, shared ? 1 : mv, shared || mv == 1 ? one : 256);
+    grid(n, n.vectors == 1 ? one : two);
     n.sums = 0;
     for (const void *v : {p->dpre_weight, p->dpost_weight, p->dpre_bias, p->dpost_bias})
         n.sums += v != nullptr;

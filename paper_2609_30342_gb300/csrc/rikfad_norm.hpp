@@ -8,16 +8,17 @@
 
 namespace rikfad {
 
-// A row of up to 4096 columns is one block's (or, up to 256 columns, 1 to 32 lanes
-// of one): every thread owns 8 neighbouring columns, so that a block of 512 threads
-// may use 128 registers each.  Wider rows are split over a cluster of up to 8 blocks,
-// which exchange their sums through distributed shared memory.
+// A thread owns 8 neighbouring columns of a row, or up to three times 8 in the
+// backward pass.  A row is one to 32 lanes', then up to 16 warps' (a block's), then a
+// cluster's of up to 8 blocks, which exchange their sums through distributed shared
+// memory.
 constexpr int kNormMaxThreads = 512;
 constexpr int kNormMaxWarps = kNormMaxThreads / 32;
 // Threads of an SM, by the registers that the kernels are given.
 constexpr int kNormForwardThreads = 768;
-constexpr int kNormBackwardThreads = 512;
-constexpr int norm_registers(int threads) { return 65536 / threads / 8 * 8; }
+template <bool POST, bool GENERAL, int V>
+constexpr int kNormBackwardThreads = V == 1 ? (POST && GENERAL ? 384 : 512) : !POST ? 384 : GENERAL ? 256 : 320;
+constexpr int norm_registers(int threads) { return threads <= 256 ? 248 : 65536 / threads / 8 * 8; }
 constexpr int kNormSms = 152;
 constexpr size_t kNormSmemPerSm = 200 << 10;    // for the stages; a block keeps 1 KB more
 
@@ -84,10 +85,11 @@ struct NormParams {
     uint32_t flags, wide;
     // the launch
     bool full, general;                     // no ragged row; a layer norm, a bias or its gradient
+    int32_t vectors;                        // of a thread
     int32_t threads, lanes, row_groups;     // of a block; of a row within it; rows of a block at a time
     int32_t cluster, cta_cols;              // blocks of a row; columns of each
     int32_t ctas;                           // clusters of the launch
-    int32_t units, stages;                  // 16-byte units of a thread's row; rows in flight and in use
+    int32_t units, stages;                  // 16-byte units of a vector; rows in flight and in use
     size_t smem;
     // backward: partial sums
     int32_t sums;

@@ -241,58 +241,65 @@ __device__ __forceinline__ void cluster_barrier()
 // A row's threads, and where they leave their sums.
 struct Team {
     RowSums *sums;
-    uint32_t mine, first;       // shared memory: this warp's slot, a row's first slot (of parity 0, value 0)
-    int lanes, threads, cluster;
-    uint32_t rank;              // of this block in its cluster
+    uint32_t first;             // shared memory: a row's first slot (of parity 0, value 0)
+    uint32_t warp, lane;
+    int lanes, warps, cluster;
     uint32_t parity;            // bytes: 0 or kParity
 
     static constexpr uint32_t kValue = sizeof(RowSums::slot[0][0]), kParity = sizeof(RowSums::slot[0]);
 
-    __device__ __forceinline__ Team(const NormParams &p, RowSums &s) : sums(&s), lanes(p.lanes), threads(p.threads), cluster(p.cluster), parity(0)
+    __device__ __forceinline__ Team(const NormParams &p, RowSums &s)
+        : sums(&s), first(smem_address(&s.slot[0][0][0])), warp(threadIdx.x >> 5), lane(threadIdx.x & 31), lanes(p.lanes),
+          warps(p.threads >> 5), cluster(p.cluster), parity(0)
     {
-        first = smem_address(&s.slot[0][0][0]);
-        mine = first + (threadIdx.x >> 5) * 4;
-        rank = 0;
-        if (cluster > 1)
-            asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     }
 
     // The sums of N values over a row's threads, in every one of them, always in the
     // same order.
     template <int N> __device__ __forceinline__ void sum(float (&v)[N])
     {
+        if (lanes < 32) {           // several rows a warp
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float t = __shfl_xor_sync(0xffffffffu, v[i], o);
+                    v[i] = o < lanes ? v[i] + t : v[i];
+                }
+            return;
+        }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float t = __shfl_xor_sync(0xffffffffu, v[i], o);
-                v[i] = o < lanes ? v[i] + t : v[i];
-            }
-        if (lanes <= 32 && cluster == 1)
+            for (int i = 0; i < N; ++i)
+                v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        if (cluster > 1) {
+            across(v);
+            return;
+        }
+        if (lanes == 32)
             return;
         parity ^= kParity;
-        if (cluster == 1) {
-            if ((threadIdx.x & 31) == 0)
+        if (lane == 0)
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine + parity + i * kValue), "f"(v[i]) : "memory");
-            __syncthreads();
-            // slots beyond the row's warps are 0
+            for (int i = 0; i < N; ++i)
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(first + parity + i * kValue + warp * 4), "f"(v[i]) : "memory");
+        __syncthreads();
+        // slots beyond the row's warps are 0
+        if (warps <= 4) {
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 v[i] = four(first + parity + i * kValue);
-            if (threads > 128) {
+        } else if (warps <= 8) {
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    v[i] += four(first + parity + i * kValue + 16);
-                if (threads > 256)
+            for (int i = 0; i < N; ++i)
+                v[i] = four(first + parity + i * kValue) + four(first + parity + i * kValue + 16);
+        } else {
 #pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        v[i] += four(first + parity + i * kValue + 32) + four(first + parity + i * kValue + 48);
-            }
-            return;
+            for (int i = 0; i < N; ++i)
+                v[i] = (four(first + parity + i * kValue) + four(first + parity + i * kValue + 16)) +
+                       (four(first + parity + i * kValue + 32) + four(first + parity + i * kValue + 48));
         }
-        across(v);
     }
 
     __device__ __forceinline__ static float four(uint32_t at)
@@ -305,14 +312,16 @@ struct Team {
     // Over the blocks of a cluster: lane r hands the warp's values to block r.
     template <int N> __device__ __forceinline__ void across(float (&v)[N])
     {
-        const int lane = threadIdx.x & 31;
+        parity ^= kParity;
+        uint32_t rank;
+        asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
         if (lane < cluster) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 uint32_t remote;
                 asm("mapa.shared::cluster.u32 %0, %1, %2;"
                     : "=r"(remote)
-                    : "r"(mine + parity + i * kValue + rank * kNormMaxWarps * 4), "r"(lane));
+                    : "r"(first + parity + i * kValue + (rank * kNormMaxWarps + warp) * 4), "r"(lane));
                 asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote), "f"(v[i]) : "memory");
             }
         }
@@ -337,11 +346,17 @@ struct Place {
     int step;               // distance to the next
     int count, most;        // rows of this thread's group, and of the block's longest
 
+    int end;                // of the block's columns
+
+    // columns (0 to 8) of this thread's vector j, `apart` columns after the one before
+    __device__ __forceinline__ int columns(int j, int apart) const { return n > 0 ? max(0, min(8, end - col - j * apart)) : 0; }
+
     __device__ __forceinline__ explicit Place(const NormParams &p)
     {
         const int rank = blockIdx.x % p.cluster, id = blockIdx.x / p.cluster;
         const int lane = threadIdx.x % p.lanes, group = threadIdx.x / p.lanes;
-        const int begin = rank * p.cta_cols, end = min(p.cols, begin + p.cta_cols);
+        const int begin = rank * p.cta_cols;
+        end = min(p.cols, begin + p.cta_cols);
         col = begin + lane * 8;
         n = max(0, min(8, end - col));
         if (n == 0)
@@ -404,6 +419,7 @@ __device__ __forceinline__ void prepare(const NormParams &p, RowSums &sums)
 }
 
 #define RK_PAIR _Pragma("unroll") for (int i = 0; i < 4; ++i)
+#define RK_EACH _Pragma("unroll") for (int j = 0; j < V; ++j)
 
 __device__ __forceinline__ float dot(const Vec8 &a, const Vec8 &b)
 {
@@ -439,10 +455,10 @@ __device__ __forceinline__ void row_stats(const NormParams &p, Team &team, bool 
 struct Ring {
     uint32_t begin, end, bytes, put, get;
 
-    __device__ __forceinline__ Ring(const NormParams &p, const void *stages)
+    __device__ __forceinline__ Ring(const NormParams &p, const void *stages, int vectors = 1)
     {
         begin = smem_address(stages) + threadIdx.x * 16;
-        bytes = p.threads * 16 * p.units;
+        bytes = p.threads * 16 * p.units * vectors;
         end = begin + bytes * p.stages;
         put = get = begin;
     }
@@ -482,7 +498,8 @@ __global__ void __maxnreg__((norm_registers(kNormForwardThreads))) rikfad_norm_f
     extern __shared__ uint4 stages[];
     __shared__ RowSums sums;
     const Place q(p);
-    const uint32_t f = p.flags;
+    uint32_t f = p.flags;
+    asm volatile("" : "+r"(f));        // in a register: its tests need no constant loads
     const bool branch = POST || (f & kNormBranch), gated = f & kNormGated;
     const uint32_t stride = p.threads * 16;
     const uint32_t z_at = kUnits<R> * stride, gate_at = z_at + kUnits<A> * stride;
@@ -556,41 +573,49 @@ __global__ void __maxnreg__((norm_registers(kNormForwardThreads))) rikfad_norm_f
 
 // ------------------------------------------------------------------ backward
 
-// One partial row of a sum over rows, from the block's groups in order.
-__device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, float *part, float *buffer, const Vec8 &acc)
+// n columns of one partial row of a sum over rows, from the block's groups in order.
+__device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, float *part, float *buffer, const Vec8 &acc, int off, int n)
 {
     float *out = part + (int64_t)(blockIdx.x / p.cluster) * p.cols;
     if (p.row_groups == 1) {
-        put8<float, false>(out + q.col, acc, q.n, false);
+        put8<float, false>(out + q.col + off, acc, n, false);
         return;
     }
+    // the vectors of all lanes, then those `off` columns on
     __syncthreads();
     const int group = threadIdx.x / p.lanes, width = p.lanes * 8;
-    if (q.n > 0)
+    if (n > 0)
         RK_PAIR *reinterpret_cast<f2 *>(buffer + group * width + q.col + 2 * i) = acc.v[i];
     __syncthreads();
-    for (int c = threadIdx.x; c < p.cols; c += p.threads) {
+    for (int c = threadIdx.x; c < min(width, p.cols - off); c += p.threads) {
         float t = 0.f;
         for (int g = 0; g < p.row_groups; ++g)
             t += buffer[g * width + c];
-        out[c] = t;
+        out[off + c] = t;
     }
 }
 
-template <typename A, typename R, bool FULL, bool POST, bool GENERAL>
-__global__ void __maxnreg__((norm_registers(kNormBackwardThreads))) rikfad_norm_backward_kernel(const __grid_constant__ NormParams p)
+// V vectors of 8 columns a thread, `lanes` vectors apart.  With V > 1 a row's fixed
+// work (addresses, branches, sums) is shared by 8 V elements; a gate shared by rows is
+// summed (SHARED) with V = 1 only.
+template <typename A, typename R, bool FULL, bool POST, bool GENERAL, int V, bool SHARED>
+__global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, V>))) rikfad_norm_backward_kernel(const __grid_constant__ NormParams p)
 {
     extern __shared__ uint4 stages[];
     __shared__ RowSums sums;
     const Place q(p);
-    const uint32_t f = p.flags;
-    const bool branch = POST || (f & kNormBranch), gated = f & kNormGated;
+    uint32_t f = p.flags;
+    asm volatile("" : "+r"(f));        // in a register: its tests need no constant loads
+    const bool branch = POST || (f & kNormBranch), gated = f & kNormGated, shared_gate = SHARED;
     const uint32_t stride = p.threads * 16;
     const int gate_bytes = f & kNormGateF32 ? 4 : (int)sizeof(A);
-    // a row's slots: x, z, dh, du, gate
+    // a vector's slots: x, z, dh, du, gate
     const uint32_t z_at = kUnits<R> * stride, dh_at = z_at + kUnits<A> * stride, du_at = dh_at + kUnits<A> * stride;
-    const uint32_t gate_at = du_at + kUnits<R> * stride;
-    Ring ring(p, stages);
+    const uint32_t gate_at = du_at + kUnits<R> * stride, next_at = stride * p.units;
+    const int apart = p.lanes * 8;
+    int cols[V];                // columns of each vector: 0 to 8
+    RK_EACH cols[j] = q.columns(j, apart);
+    Ring ring(p, stages, V);
     Team team(p, sums);
     prepare(p, sums);
     const char *x = first_row(p.x, sizeof(R), q), *z = first_row(p.z, sizeof(A), q);
@@ -598,16 +623,21 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads))) rikfad_norm_
     const char *dh = f & kNormDh ? first_row(p.dh, sizeof(A), q) : x, *du = f & kNormDu ? first_row(p.du, sizeof(R), q) : x;
     char *dx = first_row(p.dx, sizeof(R), q), *dz = first_row(p.dz, sizeof(A), q);
     GateWalk gate(p, p.gate, gate_bytes, q);
-    int left = q.count;
+    int left = q.count;         // rows to issue; the pointers stay on rows that exist
     auto issue = [&]() {
-        const int n = left > 0 ? q.n : 0;
-        stage8<R, FULL>(ring.put, stride, x, n, p.wide & kNormWideX);
-        if (branch)
-            stage8<A, FULL>(ring.put + z_at, stride, z, n, p.wide & kNormWideZ);
-        stage8<A, FULL>(ring.put + dh_at, stride, dh, f & kNormDh ? n : 0, p.wide & kNormWideDh);
-        stage8<R, FULL>(ring.put + du_at, stride, du, f & kNormDu ? n : 0, p.wide & kNormWideDu);
-        if (gated)
-            stage_gate<A, FULL>(p, ring.put + gate_at, stride, gate.at, n);
+        RK_EACH
+        {
+            // a vector that this thread lacks reads nowhere, from its first one's address
+            const int n = left > 0 ? cols[j] : 0, off = cols[j] > 0 ? j * apart : 0;
+            const uint32_t to = ring.put + j * next_at;
+            stage8<R, FULL>(to, stride, x + off * (int)sizeof(R), n, p.wide & kNormWideX);
+            if (branch)
+                stage8<A, FULL>(to + z_at, stride, z + off * (int)sizeof(A), n, p.wide & kNormWideZ);
+            stage8<A, FULL>(to + dh_at, stride, dh + off * (int)sizeof(A), f & kNormDh ? n : 0, p.wide & kNormWideDh);
+            stage8<R, FULL>(to + du_at, stride, du + off * (int)sizeof(R), f & kNormDu ? n : 0, p.wide & kNormWideDu);
+            if (gated)
+                stage_gate<A, FULL>(p, to + gate_at, stride, gate.at + off * gate_bytes, n);
+        }
         if (--left > 0) {
             x += p.x.step;
             z += p.z.step;
@@ -617,7 +647,8 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads))) rikfad_norm_
         }
         ring.issued();
     };
-    Vec8 dw1 = splat(0.f), dw2 = dw1, db1 = dw1, db2 = dw1, dg = dw1;
+    Vec8 dw1[V], dw2[V], db1[V], db2[V], dg = splat(0.f);
+    RK_EACH dw1[j] = dw2[j] = db1[j] = db2[j] = splat(0.f);
     // dgate: a row for every row, or the sum over the gate's
     GateWalk dgate(p, p.dgate, gate_bytes, q);
     bool gate_whole = p.gate_rows <= 1 || q.row % p.gate_rows == 0;     // the sum began with the gate's first row
@@ -626,94 +657,121 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads))) rikfad_norm_
         const int64_t worker = (int64_t)(blockIdx.x / p.cluster) * p.row_groups + threadIdx.x / p.lanes;
         put8<float, false>(p.gate_part + (2 * worker + (gate_first ? 0 : 1)) * p.cols + q.col, dg, q.n, false);
     };
-    auto put_gate = [&](const Vec8 &v) {
+    auto put_gate = [&](const Vec8 &v, int j, int n) {
         if (f & kNormGateF32)
-            put8<float, FULL>(dgate.at, v, q.n, p.wide & kNormWideDgate);
+            put8<float, FULL>(dgate.at + j * apart * 4, v, n, p.wide & kNormWideDgate);
         else
-            put8<A, FULL>(dgate.at, v, q.n, p.wide & kNormWideDgate);
+            put8<A, FULL>(dgate.at + j * apart * (int)sizeof(A), v, n, p.wide & kNormWideDgate);
     };
-    if ((f & kNormSharedGate) && q.count == 0)  // a group without rows adds nothing to the gate it lies in
+    if (shared_gate && q.count == 0)            // a group without rows adds nothing to the gate it lies in
         gate_part();
     for (int k = 0; k < p.stages - 1; ++k)
         issue();
-    const Vec8 w2 = param8<A>(p.post_weight, f & kNormParamF32, q.col, q.n, 1.f);
-    const Vec8 w1 = param8<A>(p.pre_weight, f & kNormParamF32, q.col, q.n, 1.f);
-    Vec8 b2 = param8<A>(p.post_bias, f & kNormParamF32, q.col, q.n, 0.f);
+    Vec8 w2[V], w1[V], b2[V];
+    RK_EACH
+    {
+        w2[j] = param8<A>(p.post_weight, f & kNormParamF32, q.col + j * apart, cols[j], 1.f);
+        w1[j] = param8<A>(p.pre_weight, f & kNormParamF32, q.col + j * apart, cols[j], 1.f);
+        b2[j] = param8<A>(p.post_bias, f & kNormParamF32, q.col + j * apart, cols[j], 0.f);
+    }
     const f2 a = both(p.a), b = both(p.b);
     const float4 *stats = p.stats + q.row;
     float4 next = q.count > 0 ? *stats : make_float4(0.f, 0.f, 0.f, 0.f);
     // e becomes r (e - [mean e] - y mean(e y))
-    auto through_norm = [&](bool layer, float r, Vec8 &e, const Vec8 &y) {
-        float t0, t1 = 0.f;
+    auto through_norm = [&](bool layer, float r, Vec8(&e)[V], const Vec8(&y)[V]) {
+        float t0 = 0.f, t1 = 0.f;
+        RK_EACH t0 += dot(e[j], y[j]);
         if (GENERAL && layer) {
-            float t[2] = {dot(e, y), elements(e)};
+            RK_EACH t1 += elements(e[j]);
+            float t[2] = {t0, t1};
             team.sum(t);
             t0 = -t[0] * p.inv_cols;
             t1 = -t[1] * p.inv_cols;
         } else {
-            float t[1] = {dot(e, y)};
+            float t[1] = {t0};
             team.sum(t);
             t0 = -t[0] * p.inv_cols;
         }
-        // columns beyond the row's end stay zero: they add nothing to later sums
-        const f2 my = both(t0), m = both(t1), rr = both(q.n > 0 ? r : 0.f);
-        RK_PAIR e.v[i] = mul(fma(y.v[i], my, add(e.v[i], m)), rr);
-        if (!FULL)
-            cut(e, q.n);
+        const f2 my = both(t0), m = both(t1);
+        RK_EACH
+        {
+            // columns beyond the row's end stay zero: they add nothing to later sums
+            const f2 rr = both(cols[j] > 0 ? r : 0.f);
+            RK_PAIR e[j].v[i] = mul(GENERAL ? fma(y[j].v[i], my, add(e[j].v[i], m)) : fma(y[j].v[i], my, e[j].v[i]), rr);
+            if (!FULL)
+                cut(e[j], cols[j]);
+        }
     };
     for (int k = 0; k < q.most; ++k) {
         issue();
-        const int n = k < q.count ? q.n : 0;
+        const bool live = k < q.count;
         const float m2 = next.x, r2 = next.y, m1 = next.z, r1 = next.w;
         stats += q.step;
         next = k + 1 < q.count ? *stats : make_float4(0.f, 0.f, 0.f, 0.f);
         wait_copies(p.stages);
 
-        Vec8 e = fetch8<A>(ring.get + dh_at, stride);       // the gradient of h, then of u
-        Vec8 y = fetch8<R>(ring.get, stride), y2, nn, g = splat(1.f);
-        RK_PAIR y.v[i] = mul(y.v[i], a);
+        Vec8 e[V], y[V], y2[V], nn[V], g[V];
+        RK_EACH
+        {
+            e[j] = fetch8<A>(ring.get + j * next_at + dh_at, stride);       // the gradient of h, then of u
+            y[j] = fetch8<R>(ring.get + j * next_at, stride);
+            RK_PAIR y[j].v[i] = mul(y[j].v[i], a);
+        }
         if (branch) {
-            nn = fetch8<A>(ring.get + z_at, stride);
-            if (POST) {
-                const f2 minus = both(-m2), r = both(r2);
-                RK_PAIR y2.v[i] = mul(add(nn.v[i], minus), r);
-                RK_PAIR nn.v[i] = GENERAL ? fma(y2.v[i], w2.v[i], b2.v[i]) : mul(y2.v[i], w2.v[i]);
+            RK_EACH
+            {
+                nn[j] = fetch8<A>(ring.get + j * next_at + z_at, stride);
+                if (POST) {
+                    const f2 minus = both(-m2 * r2), r = both(r2);
+                    RK_PAIR y2[j].v[i] = GENERAL ? mul(add(nn[j].v[i], both(-m2)), r) : mul(nn[j].v[i], r);
+                    RK_PAIR nn[j].v[i] = GENERAL ? fma(y2[j].v[i], w2[j].v[i], b2[j].v[i]) : mul(y2[j].v[i], w2[j].v[i]);
+                }
+                g[j] = splat(p.b);
             }
             if (gated)
-                g = fetch_gate<A>(p, ring.get + gate_at, stride);
-            RK_PAIR g.v[i] = mul(g.v[i], b);
-            RK_PAIR y.v[i] = fma(nn.v[i], g.v[i], y.v[i]);
+                RK_EACH
+                {
+                    g[j] = fetch_gate<A>(p, ring.get + j * next_at + gate_at, stride);
+                    RK_PAIR g[j].v[i] = mul(g[j].v[i], b);
+                }
+            RK_EACH
+                RK_PAIR y[j].v[i] = fma(nn[j].v[i], g[j].v[i], y[j].v[i]);
         }
         if (f & kNormPre) {
             const f2 minus = both(-m1), r = both(r1);
-            RK_PAIR
-            {
-                y.v[i] = mul(add(y.v[i], minus), r);
-                dw1.v[i] = fma(e.v[i], y.v[i], dw1.v[i]);
-                if (GENERAL)
-                    db1.v[i] = add(e.v[i], db1.v[i]);
-                e.v[i] = mul(e.v[i], w1.v[i]);
-            }
+            RK_EACH
+                RK_PAIR
+                {
+                    y[j].v[i] = GENERAL ? mul(add(y[j].v[i], minus), r) : mul(y[j].v[i], r);
+                    dw1[j].v[i] = fma(e[j].v[i], y[j].v[i], dw1[j].v[i]);
+                    if (GENERAL)
+                        db1[j].v[i] = add(e[j].v[i], db1[j].v[i]);
+                    e[j].v[i] = mul(e[j].v[i], w1[j].v[i]);
+                }
             through_norm(f & kNormPreLayer, r1, e, y);
         }
+        RK_EACH
         {
-            const Vec8 d = fetch8<R>(ring.get + du_at, stride);
-            RK_PAIR e.v[i] = add(e.v[i], d.v[i]);
+            const Vec8 d = fetch8<R>(ring.get + j * next_at + du_at, stride);
+            RK_PAIR e[j].v[i] = add(e[j].v[i], d.v[i]);
         }
-        Vec8 o;
-        RK_PAIR o.v[i] = mul(e.v[i], a);
-        put8<R, FULL>(dx, o, f & kNormDx ? n : 0, p.wide & kNormWideDx);
+        RK_EACH
+        {
+            Vec8 o;
+            RK_PAIR o.v[i] = mul(e[j].v[i], a);
+            put8<R, FULL>(dx + j * apart * (int)sizeof(R), o, live && (f & kNormDx) ? cols[j] : 0, p.wide & kNormWideDx);
+        }
         dx += p.dx.step;
         if (branch) {
-            if (f & kNormSharedGate) {
-                if (k < q.count) {
-                    RK_PAIR dg.v[i] = fma(mul(e.v[i], b), nn.v[i], dg.v[i]);
+            if (shared_gate) {
+                if (live) {
+                    RK_PAIR dg.v[i] = fma(mul(e[0].v[i], b), nn[0].v[i], dg.v[i]);
                     // The gate's last row, or the group's: a gate that lies within the
                     // group is done, others leave a partial sum (the group's first gate
                     // in row 0, its last in row 1).
                     if (dgate.left == 1 || k + 1 == q.count) {
                         if (gate_whole && dgate.left == 1)
-                            put_gate(dg);
+                            put_gate(dg, 0, q.n);
                         else
                             gate_part();
                         dg = splat(0.f);
@@ -722,23 +780,29 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads))) rikfad_norm_
                     }
                     dgate.next(p, p.dgate);
                 }
-            } else if ((f & kNormDgate) && k < q.count) {
-                RK_PAIR nn.v[i] = mul(mul(e.v[i], b), nn.v[i]);
-                put_gate(nn);
+            } else if (f & kNormDgate) {
+                RK_EACH
+                {
+                    RK_PAIR nn[j].v[i] = mul(mul(e[j].v[i], b), nn[j].v[i]);
+                    put_gate(nn[j], j, live ? cols[j] : 0);
+                }
                 dgate.next(p, p.dgate);
             }
-            RK_PAIR e.v[i] = mul(e.v[i], g.v[i]);
+            RK_EACH
+                RK_PAIR e[j].v[i] = mul(e[j].v[i], g[j].v[i]);
             if (POST) {
-                RK_PAIR
-                {
-                    dw2.v[i] = fma(e.v[i], y2.v[i], dw2.v[i]);
-                    if (GENERAL)
-                        db2.v[i] = add(e.v[i], db2.v[i]);
-                    e.v[i] = mul(e.v[i], w2.v[i]);
-                }
+                RK_EACH
+                    RK_PAIR
+                    {
+                        dw2[j].v[i] = fma(e[j].v[i], y2[j].v[i], dw2[j].v[i]);
+                        if (GENERAL)
+                            db2[j].v[i] = add(e[j].v[i], db2[j].v[i]);
+                        e[j].v[i] = mul(e[j].v[i], w2[j].v[i]);
+                    }
                 through_norm(f & kNormPostLayer, r2, e, y2);
             }
-            put8<A, FULL>(dz, e, f & kNormDz ? n : 0, p.wide & kNormWideDz);
+            RK_EACH
+                put8<A, FULL>(dz + j * apart * (int)sizeof(A), e[j], live && (f & kNormDz) ? cols[j] : 0, p.wide & kNormWideDz);
             dz += p.dz.step;
         }
         ring.used();
@@ -747,20 +811,18 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads))) rikfad_norm_
     asm volatile("cp.async.wait_all;" ::: "memory");
     float *part = p.sum_part, *buffer = reinterpret_cast<float *>(stages);
     const int64_t size = (int64_t)p.ctas * p.cols;
-    if (f & kNormDpreWeight) {
-        store_sum(p, q, part, buffer, dw1);
-        part += size;
+    auto store = [&](uint32_t flag, const Vec8(&acc)[V]) {
+        if (f & flag) {
+            RK_EACH store_sum(p, q, part, buffer, acc[j], j * apart, cols[j]);
+            part += size;
+        }
+    };
+    store(kNormDpreWeight, dw1);
+    store(kNormDpostWeight, dw2);
+    if (GENERAL) {
+        store(kNormDpreBias, db1);
+        store(kNormDpostBias, db2);
     }
-    if (f & kNormDpostWeight) {
-        store_sum(p, q, part, buffer, dw2);
-        part += size;
-    }
-    if (GENERAL && (f & kNormDpreBias)) {
-        store_sum(p, q, part, buffer, db1);
-        part += size;
-    }
-    if (GENERAL && (f & kNormDpostBias))
-        store_sum(p, q, part, buffer, db2);
 }
 
 // ----------------------------------------------------------- sums over rows
@@ -855,8 +917,13 @@ template <typename K> cudaError_t launch_clustered(K kernel, const NormParams &n
 template <typename A, typename R, bool FULL, bool POST, bool GENERAL>
 cudaError_t launch_rows(const NormParams &n, bool backward, cudaStream_t s)
 {
-    return backward ? launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL>, n, s)
-                    : launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL>, n, s);
+    if (!backward)
+        return launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL>, n, s);
+    if (n.flags & kNormSharedGate)
+        return launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 1, true>, n, s);
+    if (n.vectors == 1)
+        return launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 1, false>, n, s);
+    return launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 2, false>, n, s);
 }
 
 template <typename A, typename R, bool FULL> cudaError_t launch_rows(const NormParams &n, bool backward, cudaStream_t s)

@@ -99,13 +99,11 @@ class GradientClipper:
         device = ptrs.device
         total = torch.empty((), dtype=torch.float32, device=device)
         norms = torch.empty(len(self.numels), dtype=torch.float32, device=device)
-        if stream is None:
-            stream = torch.cuda.current_stream(device)
-        elif not isinstance(stream, int):
+        if stream is not None and not isinstance(stream, int):
             total.record_stream(stream)
             norms.record_stream(stream)
         rikfad._check(rikfad.lib().rikfad_clip_run(self.handle, ptrs.grads, out, max_norm, norms.data_ptr(),
-                                                   total.data_ptr(), rikfad._stream_ptr(stream)))
+                                                   total.data_ptr(), rikfad._raw_stream(stream, device.index)))
         return total, norms
 
     def norm(self, grads=None, stream=None, ptrs=None):

@@ -26,36 +26,36 @@ _NORM = struct.Struct("=3q 4i 2i 4d 6q 4q 4q q 4q 6q 4q qQ")
 # struct rikfad_rotary: sizes, types, pointers, magnitude, two sets of heads
 _ROTARY = struct.Struct("=2q 4i qq2q 2i 2i d 18q")
 
+_NO_BACKWARD = (0,) * 16
+_NO_HEADS = (0,) * 9
+
 ResidualNormGrads = namedtuple("ResidualNormGrads", "x z gate post_weight post_bias pre_weight pre_bias")
 
 
-def _rows(name, t, cols, dtype, device, rows=None):
-    """A tensor as rows of ``cols`` contiguous elements: (pointer, row stride, number of rows)."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
-        raise ValueError("%s must be a CUDA tensor on the device of x" % name)
+def _rows(name, t, cols, dtype, device, rows):
+    """A tensor as ``rows`` rows of ``cols`` contiguous elements: (pointer, row stride)."""
     if t.dtype is not dtype:
         raise ValueError("%s must be %s, not %s" % (name, dtype, t.dtype))
-    shape = t.shape
-    if len(shape) == 0 or shape[-1] != cols:
-        raise ValueError("%s must have %d columns" % (name, cols))
+    if t.get_device() != device:
+        raise ValueError("%s must be a CUDA tensor on the device of x" % name)
     if t.dim() != 2:
-        try:
-            t = t.view(-1, cols)
-        except RuntimeError:
-            raise ValueError("the rows of %s must be evenly spaced" % name) from None
-    n = t.shape[0]
-    if rows is not None and n != rows:
-        raise ValueError("%s has %d rows, expected %d" % (name, n, rows))
-    stride = t.stride()
-    if cols > 1 and stride[1] != 1:
-        raise ValueError("the rows of %s must be contiguous" % name)
-    if n > 1 and stride[0] < cols:
-        raise ValueError("the rows of %s must not overlap" % name)
-    return t.data_ptr(), (stride[0] if n > 1 else cols), n
+        t = _matrix(name, t, cols)
+    n, c = t.shape
+    if c != cols or n != rows:
+        raise ValueError("%s is %d rows of %d columns, expected %d of %d" % (name, n, c, rows, cols))
+    s0, s1 = t.stride()
+    if s1 != 1 and cols > 1 or s0 < cols and n > 1:
+        raise ValueError("the rows of %s must be contiguous and not overlap" % name)
+    return t.data_ptr(), s0 if n > 1 else cols
 
 
-def _stream(stream, device):
-    return torch.cuda.current_stream(device).cuda_stream if stream is None else rikfad._stream_ptr(stream)
+def _matrix(name, t, cols):
+    if t.dim() == 0 or t.shape[-1] != cols:
+        raise ValueError("%s must have %d columns" % (name, cols))
+    try:
+        return t.view(-1, cols)
+    except RuntimeError:
+        raise ValueError("the rows of %s must be evenly spaced" % name) from None
 
 
 class ResidualNorm:
@@ -79,71 +79,80 @@ class ResidualNorm:
         self.cols, self.post, self.pre = int(cols), post, pre
         self.post_eps, self.pre_eps = float(post_eps), float(pre_eps)
         self.residual_scale, self.branch_scale = float(residual_scale), float(branch_scale)
+        self._kinds = (_KINDS[post], _KINDS[pre])
+        self._scales = (self.post_eps, self.pre_eps, self.residual_scale, self.branch_scale)
+        self._workspace = {}        # bytes by sizes, types and what is there
 
     def _vector(self, name, v, dtype, device):
         if v is None:
             return 0
-        if not isinstance(v, torch.Tensor) or v.device != device:
-            raise ValueError("%s must be a CUDA tensor on the device of x" % name)
-        if v.dtype is not dtype or v.dim() != 1 or v.shape[0] != self.cols or not v.is_contiguous():
-            raise ValueError("%s must be %d contiguous elements of %s" % (name, self.cols, dtype))
+        if v.dtype is not dtype or v.get_device() != device or v.dim() != 1 or v.shape[0] != self.cols or \
+                not v.is_contiguous():
+            raise ValueError("%s must be %d contiguous elements of %s on the device of x" % (name, self.cols, dtype))
         return v.data_ptr()
 
     def _inputs(self, x, z, gate, weights, dtype):
-        """The head of the parameter block up to the weights, and (rows, types)."""
+        """The head of the parameter block up to the weights, and (rows, type of z, device)."""
         cols = self.cols
-        if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        for t in (x, z, gate) + weights:
+            if t is not None and not isinstance(t, torch.Tensor):
+                raise ValueError("inputs must be tensors")
+        device = x.get_device()
+        if device < 0:
             raise ValueError("x must be a CUDA tensor")
-        device = x.device
-        dt = z.dtype if z is not None else (x.dtype if dtype is None else dtype)
+        rt = x.dtype
+        dt = z.dtype if z is not None else (rt if dtype is None else dtype)
+        w2, b2, w1, b1 = weights
+        first = w2 if w2 is not None else w1 if w1 is not None else b2 if b2 is not None else b1
+        pt = _F32 if first is None else first.dtype
+        gt = _F32 if gate is None else gate.dtype
         if dt not in _TORCH:
             raise ValueError("z must be float32, bfloat16 or float16")
-        rt = x.dtype
-        pt = next((w.dtype for w in weights if w is not None), _F32)
-        gt = _F32 if gate is None else gate.dtype
-        for name, t in (("x", rt), ("weights and biases", pt), ("gate", gt)):
-            if t is not _F32 and t is not dt:
-                raise ValueError("%s must be float32 or %s" % (name, dt))
-        px, sx, rows = _rows("x", x, cols, rt, device)
-        pz, sz, _ = (0, 0, 0) if z is None else _rows("z", z, cols, dt, device, rows)
-        pg, sg, per = 0, 0, 1
+        if (rt is not _F32 and rt is not dt) or (pt is not _F32 and pt is not dt) or (gt is not _F32 and gt is not dt):
+            raise ValueError("x, weights, biases and gate must be float32 or %s" % dt)
+        rows = x.shape[0] if x.dim() == 2 else _matrix("x", x, cols).shape[0]
+        px, sx = _rows("x", x, cols, rt, device, rows)
+        pz = sz = pg = sg = 0
+        per = 1
+        if z is not None:
+            pz, sz = _rows("z", z, cols, dt, device, rows)
+        elif gate is not None or self.post is not None:
+            raise ValueError("a post norm or a gate needs z")
         if gate is not None:
-            if z is None:
-                raise ValueError("a gate needs z")
-            pg, sg, n = _rows("gate", gate, cols, gt, device)
+            n = gate.shape[0] if gate.dim() == 2 else _matrix("gate", gate, cols).shape[0]
             if n == 0 and rows or n and rows % n:
                 raise ValueError("the gate's rows must divide those of x")
+            pg, sg = _rows("gate", gate, cols, gt, device, n)
             per = rows // n if n and rows else 1
-        if z is None and (self.post is not None or weights[0] is not None or weights[1] is not None):
-            raise ValueError("a post norm needs z")
-        if self.post is None and (weights[0] is not None or weights[1] is not None):
+        if self.post is None and (w2 is not None or b2 is not None):
             raise ValueError("post_weight and post_bias need a post norm")
-        if self.pre is None and (weights[2] is not None or weights[3] is not None):
+        if self.pre is None and (w1 is not None or b1 is not None):
             raise ValueError("pre_weight and pre_bias need a pre norm")
-        names = ("post_weight", "post_bias", "pre_weight", "pre_bias")
-        head = (rows, cols, per, _TORCH[dt], _TORCH[rt], _TORCH[pt], _TORCH[gt], _KINDS[self.post], _KINDS[self.pre],
-                self.post_eps, self.pre_eps, self.residual_scale, self.branch_scale, px, sx, pz, sz, pg, sg,
-                *(self._vector(n, w, pt, device) for n, w in zip(names, weights)))
-        return head, rows, dt, pt
+        vector = self._vector
+        head = (rows, cols, per, _TORCH[dt], _TORCH[rt], _TORCH[pt], _TORCH[gt], *self._kinds, *self._scales,
+                px, sx, pz, sz, pg, sg, vector("post_weight", w2, pt, device), vector("post_bias", b2, pt, device),
+                vector("pre_weight", w1, pt, device), vector("pre_bias", b1, pt, device))
+        return head, rows, dt, device
 
     def forward(self, x, z=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None,
                 need_stats=True, dtype=None, out=None, stream=None):
         """(u, h, stats).  ``stats`` (None without ``need_stats``) is what ``backward`` needs besides the inputs.
         Without z, u = residual_scale x and ``dtype`` gives h's type (default x's).  ``out``: (u, h) to write to; u may
         be x and h may be z; None for one that is not wanted."""
-        head, rows, dt, _ = self._inputs(x, z, gate, (post_weight, post_bias, pre_weight, pre_bias), dtype)
-        device, cols = x.device, self.cols
+        head, rows, dt, device = self._inputs(x, z, gate, (post_weight, post_bias, pre_weight, pre_bias), dtype)
+        cols = self.cols
         if out is None:
-            u = torch.empty(x.shape, dtype=x.dtype, device=device)
-            h = torch.empty(x.shape, dtype=dt, device=device)
+            u = torch.empty_like(x, memory_format=torch.contiguous_format)
+            h = torch.empty_like(x, dtype=dt, memory_format=torch.contiguous_format)
+            pu, ph = u.data_ptr(), h.data_ptr()
+            su = sh = cols
         else:
             u, h = out
-        pu, su, _ = (0, 0, 0) if u is None else _rows("u", u, cols, x.dtype, device, rows)
-        ph, sh, _ = (0, 0, 0) if h is None else _rows("h", h, cols, dt, device, rows)
-        stats = torch.empty(rows, 4, dtype=_F32, device=device) if need_stats else None
-        block = _NORM.pack(*head, pu, su, ph, sh, 0 if stats is None else stats.data_ptr(), *([0] * 16))
-        with torch.cuda.device(device):
-            rikfad._check(rikfad.lib().rikfad_residual_norm_forward(block, _stream(stream, device)))
+            pu, su = (0, 0) if u is None else _rows("u", u, cols, x.dtype, device, rows)
+            ph, sh = (0, 0) if h is None else _rows("h", h, cols, dt, device, rows)
+        stats = torch.empty(rows, 4, dtype=_F32, device=x.device) if need_stats else None
+        block = _NORM.pack(*head, pu, su, ph, sh, 0 if stats is None else stats.data_ptr(), *_NO_BACKWARD)
+        rikfad._call_on(device, rikfad.lib().rikfad_residual_norm_forward, block, rikfad._raw_stream(stream, device))
         return u, h, stats
 
     def backward(self, du, dh, x, z=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None,
@@ -151,29 +160,38 @@ class ResidualNorm:
         """``ResidualNormGrads`` of the forward call's inputs (None where the input is None), from the gradients of u
         and h (either may be None)."""
         weights = (post_weight, post_bias, pre_weight, pre_bias)
-        dt = dh.dtype if dh is not None else None
-        head, rows, dt, pt = self._inputs(x, z, gate, weights, dt)
-        device, cols = x.device, self.cols
-        pdu, sdu, _ = (0, 0, 0) if du is None else _rows("du", du, cols, x.dtype, device, rows)
-        pdh, sdh, _ = (0, 0, 0) if dh is None else _rows("dh", dh, cols, dt, device, rows)
-        if stats is None or stats.dtype is not _F32 or tuple(stats.shape) != (rows, 4) or not stats.is_contiguous() \
-                or stats.device != device:
+        head, rows, dt, device = self._inputs(x, z, gate, weights, dh.dtype if dh is not None else None)
+        cols = self.cols
+        pdu, sdu = (0, 0) if du is None else _rows("du", du, cols, x.dtype, device, rows)
+        pdh, sdh = (0, 0) if dh is None else _rows("dh", dh, cols, dt, device, rows)
+        if stats is None or stats.dtype is not _F32 or stats.shape != (rows, 4) or not stats.is_contiguous() \
+                or stats.get_device() != device:
             raise ValueError("stats must be what forward returned for these inputs")
-        dx = torch.empty(x.shape, dtype=x.dtype, device=device)
-        dz = None if z is None else torch.empty(z.shape, dtype=dt, device=device)
-        dgate = None if gate is None else torch.empty(gate.shape, dtype=gate.dtype, device=device)
-        dw = [None if w is None else torch.empty(cols, dtype=pt, device=device) for w in weights]
-        tail = [dx.data_ptr(), cols, 0 if z is None else dz.data_ptr(), cols, 0 if gate is None else dgate.data_ptr(), cols]
-        tail += [0 if w is None else w.data_ptr() for w in dw]
-        body = (*head, 0, 0, 0, 0, stats.data_ptr(), pdu, sdu, pdh, sdh, *tail)
-        L = rikfad.lib()
-        with torch.cuda.device(device):
-            nbytes = L.rikfad_residual_norm_workspace(_NORM.pack(*body, 0, 0))
-            work = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-            if stream is not None and not isinstance(stream, int) and work is not None:
+        dense = torch.contiguous_format
+        dx = torch.empty_like(x, memory_format=dense)
+        dz = None if z is None else torch.empty_like(z, memory_format=dense)
+        dgate = None if gate is None else torch.empty_like(gate, memory_format=dense)
+        dw = [None if w is None else torch.empty_like(w) for w in weights]
+        outputs = (dx.data_ptr(), cols, 0 if z is None else dz.data_ptr(), cols, 0 if gate is None else dgate.data_ptr(),
+                   cols, *[0 if w is None else w.data_ptr() for w in dw])
+        body = (*head, 0, 0, 0, 0, stats.data_ptr(), pdu, sdu, pdh, sdh, *outputs)
+        lib = rikfad.lib()
+        # the size of the workspace goes by sizes, types and what is there alone
+        shape = (*head[:9], z is None, du is None, dh is None, *[w is None for w in dw])
+        nbytes = self._workspace.get(shape)
+        if nbytes is None:
+            nbytes = lib.rikfad_residual_norm_workspace(_NORM.pack(*body, 0, 0))
+            if len(self._workspace) >= 64:
+                self._workspace.clear()
+            self._workspace[shape] = nbytes
+        pw = 0
+        if nbytes:
+            work = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+            pw = work.data_ptr()
+            if stream is not None and not isinstance(stream, int):
                 work.record_stream(stream)
-            rikfad._check(L.rikfad_residual_norm_backward(_NORM.pack(*body, work.data_ptr() if nbytes else 0, nbytes),
-                                                          _stream(stream, device)))
+        rikfad._call_on(device, lib.rikfad_residual_norm_backward, _NORM.pack(*body, pw, nbytes),
+                        rikfad._raw_stream(stream, device))
         return ResidualNormGrads(dx, dz, dgate, *dw)
 
     def __call__(self, x, z=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None,
@@ -263,63 +281,75 @@ class Rotary:
         self.frequencies = frequencies
         signed = [v - (1 << 64) if v >= 1 << 63 else v for v in turns[:n]]
         self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
+        self._turns, self._layout = self.turns.data_ptr(), 0 if layout == "half" else 1
 
-    def _heads(self, name, t, shape, dtype, device):
-        """(batch, token, head) strides of a [tokens, heads, head_dim] or [batch, tokens, heads, head_dim] tensor."""
-        if not isinstance(t, torch.Tensor) or t.device != device:
-            raise ValueError("%s must be a CUDA tensor on the device of q" % name)
+    def _heads(self, name, t, lead, dtype, device):
+        """(pointer, heads, batch, token and head strides) of a [tokens, heads, head_dim] or
+        [batch, tokens, heads, head_dim] tensor."""
         if t.dtype is not dtype:
             raise ValueError("%s must be %s, not %s" % (name, dtype, t.dtype))
-        if t.shape[:-2] != shape or t.shape[-1] != self.head_dim:
+        if t.get_device() != device:
+            raise ValueError("%s must be a CUDA tensor on the device of q" % name)
+        shape, s = t.shape, t.stride()
+        if shape[:-2] != lead or shape[-1] != self.head_dim:
             raise ValueError("%s must be [tokens, heads, %d] or [batch, tokens, heads, %d], with the tokens of q"
                              % (name, self.head_dim, self.head_dim))
-        s = t.stride()
         if s[-1] != 1 and self.head_dim > 1:
             raise ValueError("the heads of %s must be contiguous" % name)
-        return (0, *s[:2]) if len(s) == 3 else s[:3]
+        if len(s) == 3:
+            return t.data_ptr(), shape[1], 0, s[0], s[1]
+        return t.data_ptr(), shape[2], s[0], s[1], s[2]
 
     def rotate(self, q, k=None, positions=None, start=0, inverse=False, out=None, stream=None):
         """(q', k') of queries and keys [tokens, heads, head_dim] or [batch, tokens, heads, head_dim] (k' None without
         k).  ``positions``: int32 or int64 CUDA tensor [tokens] or [batch, tokens]; default ``start`` + 0, 1, ...
         ``inverse`` turns back: the gradient of the rotation.  ``out``: (q', k') to write to; q and k themselves
         rotate in place."""
-        if not isinstance(q, torch.Tensor) or not q.is_cuda:
-            raise ValueError("q must be a CUDA tensor")
-        if q.dtype not in _TORCH:
-            raise ValueError("q must be float32, bfloat16 or float16")
-        if q.dim() not in (3, 4):
-            raise ValueError("q must be [tokens, heads, head_dim] or [batch, tokens, heads, head_dim]")
-        device, lead = q.device, q.shape[:-2]
-        if self.turns.device != device:
+        for t in (q, k, positions):
+            if t is not None and not isinstance(t, torch.Tensor):
+                raise ValueError("inputs must be tensors")
+        device, dtype = q.get_device(), q.dtype
+        if device < 0 or device != self.turns.get_device():
             raise ValueError("q must be on %s, the device of the frequencies" % self.turns.device)
-        batch, tokens = (1, lead[0]) if len(lead) == 1 else lead
+        if dtype not in _TORCH:
+            raise ValueError("q must be float32, bfloat16 or float16")
+        lead = q.shape[:-2]
+        if len(lead) == 1:
+            batch, tokens = 1, lead[0]
+        elif len(lead) == 2:
+            batch, tokens = lead
+        else:
+            raise ValueError("q must be [tokens, heads, head_dim] or [batch, tokens, heads, head_dim]")
         pp, pb, width = 0, 0, 8
         if positions is not None:
-            if not isinstance(positions, torch.Tensor) or positions.device != device or \
-                    positions.dtype not in (torch.int32, torch.int64):
+            width = 4 if positions.dtype is torch.int32 else 8
+            if positions.get_device() != device or width == 8 and positions.dtype is not torch.int64:
                 raise ValueError("positions must be an int32 or int64 CUDA tensor on the device of q")
-            if positions.shape == lead and len(lead) == 2:
+            if len(lead) == 2 and positions.shape == lead:
                 pb = positions.stride(0)
-            elif tuple(positions.shape) != (tokens,):
+            elif positions.shape != (tokens,):
                 raise ValueError("positions must be [tokens] or [batch, tokens]")
             if tokens > 1 and positions.stride(-1) != 1:
                 raise ValueError("positions must be contiguous along the tokens")
-            pp, width = positions.data_ptr(), positions.element_size()
+            pp = positions.data_ptr()
         if out is None:
-            out = (torch.empty(q.shape, dtype=q.dtype, device=device),
-                   None if k is None else torch.empty(k.shape, dtype=q.dtype, device=device))
-        lists, sets = [], [("q", q, out[0])] + ([] if k is None else [("k", k, out[1])])
-        for name, src, dst in sets:
-            strides = self._heads(name, src, lead, q.dtype, device)
-            if dst.shape != src.shape:
+            dense = torch.contiguous_format
+            out = (torch.empty_like(q, memory_format=dense),
+                   None if k is None else torch.empty_like(k, memory_format=dense))
+        lists = []
+        for name, src, dst in (("q", q, out[0]), ("k", k, out[1])):
+            if src is None:
+                lists += _NO_HEADS
+                continue
+            ps, heads, *from_ = self._heads(name, src, lead, dtype, device)
+            pd, to_heads, *to = self._heads(name, dst, lead, dtype, device)
+            if to_heads != heads:
                 raise ValueError("the output of %s must have its shape" % name)
-            lists += [src.data_ptr(), dst.data_ptr(), src.shape[-2], *strides,
-                      *self._heads("the output of " + name, dst, lead, q.dtype, device)]
-        block = _ROTARY.pack(batch, tokens, self.head_dim, self.rotary_dim, 0 if self.layout == "half" else 1,
-                             _TORCH[q.dtype], self.turns.data_ptr(), pp, pb, int(start), width, 1 if inverse else 0,
-                             len(sets), 0, self.magnitude, *lists, *([0] * (18 - len(lists))))
-        with torch.cuda.device(device):
-            rikfad._check(rikfad.lib().rikfad_rotary_apply(block, _stream(stream, device)))
+            lists += (ps, pd, heads, *from_, *to)
+        block = _ROTARY.pack(batch, tokens, self.head_dim, self.rotary_dim, self._layout, _TORCH[dtype],
+                             self._turns, pp, pb, start, width, 1 if inverse else 0, 1 if k is None else 2, 0,
+                             self.magnitude, *lists)
+        rikfad._call_on(device, rikfad.lib().rikfad_rotary_apply, block, rikfad._raw_stream(stream, device))
         return out[0], (None if k is None else out[1])
 
     def __call__(self, q, k, positions=None, start=0):

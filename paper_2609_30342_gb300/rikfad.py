@@ -152,6 +152,25 @@ def _stream_ptr(stream):
     return stream.cuda_stream
 
 
+def _raw_stream(stream, index):
+    """The cudaStream_t of ``stream`` (a torch stream or an integer), or of the
+    current stream of device ``index``."""
+    if stream is None:
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # a tenth of current_stream's time
+        return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _call_on(index, function, *args):
+    """``function(*args)``, checked, with device ``index`` current."""
+    import torch
+    if torch.cuda.current_device() == index:
+        return _check(function(*args))
+    with torch.cuda.device(index):
+        return _check(function(*args))
+
+
 def _ptr(t):
     if t is None:
         return None
