@@ -7,7 +7,6 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
-#include <cstdlib>
 #include <new>
 #include <string>
 
@@ -112,7 +111,6 @@ NormParams params(const rikfad_residual_norm *p, bool backward)
     n.post_eps = (float)p->post_eps;
     n.pre_eps = (float)p->pre_eps;
     n.gate_rows = p->gate.data ? p->gate_rows : 1;
-    n.gate_period = (int32_t)std::min<int64_t>(n.gate_rows, INT32_MAX);
     n.post_weight = p->post_weight;
     n.post_bias = p->post_bias;
     n.pre_weight = p->pre_weight;
@@ -130,6 +128,7 @@ NormParams params(const rikfad_residual_norm *p, bool backward)
     tensor(n.z, p->z, p->dtype, p->rows, kNormBranch, kNormWideZ);
     tensor(n.gate, p->gate, p->gate_dtype, gates, kNormGated, kNormWideGate);
     flag(p->gate_dtype == RIKFAD_F32, kNormGateF32);
+    flag(p->gate.data && p->gate_rows > 1, kNormSharedGate);
     flag(p->param_dtype == RIKFAD_F32, kNormParamF32);
     flag(p->z.data && p->post != RIKFAD_NORM_NONE, kNormPost);
     flag(p->post == RIKFAD_NORM_LAYER, kNormPostLayer);
@@ -153,7 +152,6 @@ NormParams params(const rikfad_residual_norm *p, bool backward)
     tensor(n.dx, p->dx, p->residual_dtype, p->rows, kNormDx, kNormWideDx);
     tensor(n.dz, p->dz, p->dtype, p->rows, kNormDz, kNormWideDz);
     tensor(n.dgate, p->dgate, p->gate_dtype, gates, kNormDgate, kNormWideDgate);
-    flag(p->dgate.data && p->gate_rows > 1, kNormSharedGate);
     n.dpost_weight = p->dpost_weight;
     n.dpost_bias = p->dpost_bias;
     n.dpre_weight = p->dpre_weight;
@@ -176,13 +174,44 @@ int row_threads(int vectors, int v)
     return threads <= 32 ? lanes : (threads + 31) / 32 * 32;
 }
 
+// Rows of odd widths: if every tensor's rows drift by the same number of elements
+// from 16 bytes, from an aligned start, rows that drift equally far make a class
+// with aligned vectors.  Otherwise (and where a shared gate's sums over rows would
+// need too many partial rows) each tensor's own rows decide.
+void drifting(NormParams &n, const rikfad_residual_norm *p)
+{
+    if (n.wide == kNormWideAll || p->rows <= 1)
+        return;
+    const NormRows *const all[] = {&n.x, &n.z, &n.u, &n.h, &n.du, &n.dh, &n.dx, &n.dz,
+                                   p->gate_rows > 1 ? nullptr : &n.gate, p->gate_rows > 1 ? nullptr : &n.dgate};
+    int drift = -1;
+    for (const NormRows *t : all) {
+        if (t == nullptr || t->data == nullptr)
+            continue;
+        if ((uintptr_t)t->data % 16 || (drift >= 0 && t->stride % 8 != drift))
+            return;
+        drift = (int)(t->stride % 8);
+    }
+    if (drift <= 0)
+        return;
+    n.drift = drift;
+    n.classes = drift % 4 == 0 ? 2 : drift % 2 == 0 ? 4 : 8;
+    n.wide |= kNormWideAll & ~(p->gate_rows > 1 ? kNormWideGate | kNormWideDgate : 0u);
+    if (p->gate_rows > 1)
+        n.wide &= ~(kNormWideGate | kNormWideDgate);
+}
+
 // Vectors of a thread, threads of a row, columns of a block and blocks of a
 // cluster, from the width; how far a thread's rows are apart.  A block has at most
 // `most_threads` threads of `most_vectors` vectors each.
-void shape(NormParams &n, const rikfad_residual_norm *p, int most_vectors, int most_threads)
+void shape(NormParams &n, const rikfad_residual_norm *p, int most_vectors, int most_threads, bool classes = true)
 {
-    const int vectors = (n.cols + 7) / 8;
-    n.cluster = getenv("RK_C") ? atoi(getenv("RK_C")) : 1;
+    n.classes = 1;
+    n.drift = 0;
+    if (classes)
+        drifting(n, p);
+    const int vectors = (n.cols + (n.classes > 1 ? 7 : 0) + 7) / 8;     // a shifted row may begin within one
+    n.cluster = 1;
     while ((vectors + n.cluster - 1) / n.cluster > most_threads * most_vectors)
         n.cluster *= 2;
     const int here = (vectors + n.cluster - 1) / n.cluster;
@@ -199,9 +228,9 @@ void shape(NormParams &n, const rikfad_residual_norm *p, int most_vectors, int m
     }
     n.threads = n.lanes <= 32 && n.cluster == 1 ? 128 : n.lanes;
     n.row_groups = n.threads / n.lanes;
-    n.full = n.cols % 8 == 0 && n.wide == kNormWideAll;
-    // `row_groups` rows, or neighbours where rows share gates
-    const int64_t rows = n.gate_rows > 1 ? 1 : n.row_groups;
+    n.full = n.cols % 8 == 0 && n.wide == kNormWideAll && n.classes == 1;
+    // `row_groups` rows of a class, or neighbours where rows share gates
+    const int64_t rows = n.classes * (int64_t)(n.gate_rows > 1 ? 1 : n.row_groups);
     const int64_t a = rows * dtype_bytes(p->dtype), r = rows * dtype_bytes(p->residual_dtype);
     const int64_t g = rows * dtype_bytes(p->gate_dtype);
     for (NormRows *t : {&n.z, &n.h, &n.dh, &n.dz})
@@ -210,7 +239,8 @@ void shape(NormParams &n, const rikfad_residual_norm *p, int most_vectors, int m
         t->step = t->stride * r;
     // the rows of a shared gate are counted, so a step there is one gate
     for (NormRows *t : {&n.gate, &n.dgate})
-        t->step = t->stride * g;
+        t->step = n.gate_rows > 1 ? t->stride * dtype_bytes(p->gate_dtype) : t->stride * g;
+    n.flags |= p->gate.data && n.gate_rows >= 16 ? kNormGateHeld : 0;
 }
 
 // Clusters of a launch: as many as are resident at once (`threads_per_sm` by the
@@ -225,12 +255,13 @@ void grid(NormParams &n, int threads_per_sm)
     n.smem = stage * n.stages;
     const int resident = std::max(1, std::min(by_registers, (int)(kNormSmemPerSm / n.smem)));
     n.ctas = (int)std::max<int64_t>(1, std::min<int64_t>(groups, (int64_t)kNormSms * resident / n.cluster));
+    n.ctas = (n.ctas + n.classes - 1) / n.classes * n.classes;      // as many for each class
 }
 
 void forward_shape(const rikfad_residual_norm *p, NormParams &n)
 {
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
-    n.units = r + a + (p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
+    n.units = r + a + (p->gate.data && p->gate_rows < 16 ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
     shape(n, p, 1, kNormMaxThreads);
     grid(n, kNormForwardThreads);
 }
@@ -241,23 +272,31 @@ struct Workspace {
 
 // Partial sums: one row of each kind for every cluster, and two of the gate's for
 // every group whose rows share gates with others.
-Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n)
+Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n, bool classes = true)
 {
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
-    n.units = 2 * a + 2 * r + (p->gate.data ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
-    const bool shared = p->dgate.data && p->gate_rows > 1, post = n.flags & kNormPost;
+    n.units = 2 * a + 2 * r + (p->gate.data && p->gate_rows < 16 ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
+    const bool gated = n.flags & kNormSharedGate, shared = gated && p->dgate.data, post = n.flags & kNormPost;
     const int one = post && n.general ? kNormBackwardThreads<true, true, 1> : kNormBackwardThreads<false, false, 1>;
     const int two = !post ? kNormBackwardThreads<false, false, 2> : n.general ? kNormBackwardThreads<true, true, 2> : kNormBackwardThreads<true, false, 2>;
-    const char *ev = getenv("RK_V");
-    const int mv = ev ? atoi(ev) : 2;
-    shape(n, p, shared ? 1 : mv, shared || mv == 1 ? one : 256);
+    shape(n, p, gated ? 1 : 2, gated ? one : kNormMaxThreads / 2, classes);
     grid(n, n.vectors == 1 ? one : two);
     n.sums = 0;
     for (const void *v : {p->dpre_weight, p->dpost_weight, p->dpre_bias, p->dpost_bias})
         n.sums += v != nullptr;
+    // A group leaves partial sums of two gates at most; where its rows of a class reach
+    // over more, every tensor's own rows decide.
+    if (shared && n.classes > 1) {
+        const int64_t workers = (int64_t)(n.ctas / n.classes) * n.row_groups;
+        const int64_t rows = (p->rows + n.classes - 1) / n.classes;
+        if ((rows + workers - 1) / workers * n.classes > p->gate_rows) {
+            NormParams again = params(p, true);
+            return backward_shape(p, n = again, false);
+        }
+    }
     Workspace w;
     w.weights = (int64_t)n.sums * n.ctas * n.cols;
-    w.gates = p->dgate.data && p->gate_rows > 1 ? (int64_t)2 * n.ctas * n.row_groups * n.cols : 0;
+    w.gates = shared ? (int64_t)2 * n.ctas * n.row_groups * n.cols : 0;
     return w;
 }
 

@@ -43,14 +43,15 @@ enum : uint32_t {
     kNormDx = 1u << 17,
     kNormDz = 1u << 18,
     kNormDgate = 1u << 19,
-    kNormSharedGate = 1u << 20,     // dgate is a sum over rows
+    kNormSharedGate = 1u << 20,     // a gate serves several rows
     kNormDpreWeight = 1u << 21,
     kNormDpostWeight = 1u << 22,
     kNormDpreBias = 1u << 23,
     kNormDpostBias = 1u << 24,
+    kNormGateHeld = 1u << 25,       // a gate lasts so long that it is kept in registers
 };
 
-// Tensors whose rows all start on 16 bytes.
+// Tensors whose vectors all start on 16 bytes.
 enum : uint32_t {
     kNormWideX = 1u << 0,
     kNormWideZ = 1u << 1,
@@ -75,7 +76,8 @@ struct NormParams {
     int64_t rows, gate_rows;
     int32_t cols;
     float inv_cols, a, b, post_eps, pre_eps;
-    int32_t gate_period;        // gate_rows, within int
+    // Rows of class c (c, c + classes, ...) start c * drift % 8 elements after a vector.
+    int32_t classes, drift;
     NormRows x, z, gate;
     const void *post_weight, *post_bias, *pre_weight, *pre_bias;
     float4 *stats;              // mean, 1/deviation of post; the same of pre
@@ -84,7 +86,7 @@ struct NormParams {
     void *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;
     uint32_t flags, wide;
     // the launch
-    bool full, general;                     // no ragged row; a layer norm, a bias or its gradient
+    bool full, general;                     // only whole vectors; a layer norm, a bias or its gradient
     int32_t vectors;                        // of a thread
     int32_t threads, lanes, row_groups;     // of a block; of a row within it; rows of a block at a time
     int32_t cluster, cta_cols;              // blocks of a row; columns of each

@@ -16,7 +16,10 @@
 // copies of the next rows are under way meanwhile (cp.async into slots of shared
 // memory that only this thread reads, so no barrier separates a copy from its use).
 // What is absent (a tensor, columns beyond the row's end, a last round's rows) is
-// staged as zeros: the arithmetic has no branches for it.  Sums over a row:
+// staged as zeros: the arithmetic has no branches for it.  Rows that do not start on
+// 16 bytes (an odd width) are read in aligned vectors all the same: rows whose starts
+// are equally far from 16 bytes (every P-th, P = 2, 4 or 8) go to the same block,
+// whose columns are shifted by that much.  Sums over a row:
 // shuffles, and beyond a warp one barrier over the row's warps (or the cluster's
 // blocks).  Sums over rows stay in the thread's registers to the end of the launch,
 // leave one partial row per cluster, and a second kernel adds those in order.
@@ -106,22 +109,29 @@ __device__ __forceinline__ Vec8 splat(float v)
     return {{b, b, b, b}};
 }
 
-// Elements n and beyond set to zero.
-__device__ __forceinline__ void cut(Vec8 &o, int n)
+// The elements of a vector that a row has: [lo, hi).
+struct Span {
+    int lo, hi;
+};
+
+// The other elements set to zero.
+__device__ __forceinline__ void cut(Vec8 &o, const Span &n)
 {
+    if (n.lo == 0 && n.hi == 8)
+        return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 t = halves(o.v[i]);
-        o.v[i] = pair(2 * i < n ? t.x : 0.f, 2 * i + 1 < n ? t.y : 0.f);
+        o.v[i] = pair(2 * i >= n.lo && 2 * i < n.hi ? t.x : 0.f, 2 * i + 1 >= n.lo && 2 * i + 1 < n.hi ? t.y : 0.f);
     }
 }
 
 // ------------------------------------------------------------------ staging
 
-// 16 bytes in flight, or 16 bytes of zeros without a read.
-__device__ __forceinline__ void copy16_async(uint32_t smem, const void *src, bool on)
+// The first `bytes` (0 to 16) of 16 in flight, and zeros after them.
+__device__ __forceinline__ void copy16_async(uint32_t smem, const void *src, int bytes)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(src), "r"(on ? 16 : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(src), "r"(bytes) : "memory");
 }
 
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -150,15 +160,19 @@ __device__ __forceinline__ uint4 smem_get(uint32_t smem)
 // 16-byte units of 8 elements.
 template <typename T> constexpr int kUnits = sizeof(T) / 2;
 
-// n elements (0 to 8) into this thread's slot, whose units are `stride` bytes
-// apart, and zeros after them: copies in flight where the row starts on 16 bytes,
-// else element by element.  FULL: every row starts on 16 bytes and n is 0 or 8.
-template <typename T, bool FULL> __device__ __forceinline__ void stage8(uint32_t slot, uint32_t stride, const void *src, int n, bool wide)
+// Elements [lo, hi) of a vector into this thread's slot, whose units are `stride`
+// bytes apart, with zeros after them.  `wide`: the vector starts on 16 bytes; then
+// the copies are in flight, and the elements before lo are the row's before
+// (fetch8 clears them).  FULL: every vector is wide, all of a row's or none.
+template <typename T, bool FULL> __device__ __forceinline__ void stage8(uint32_t slot, uint32_t stride, const void *src, const Span &n, bool wide)
 {
-    if (FULL || (wide && n % 8 == 0)) {
-        copy16_async(slot, src, n);
-        if constexpr (sizeof(T) == 4)
-            copy16_async(slot + stride, static_cast<const char *>(src) + 16, n);
+    if (FULL || wide) {
+        if constexpr (sizeof(T) == 4) {
+            copy16_async(slot, src, FULL ? n.hi * 2 : min(n.hi, 4) * 4);
+            copy16_async(slot + stride, static_cast<const char *>(src) + 16, FULL ? n.hi * 2 : max(n.hi - 4, 0) * 4);
+        } else {
+            copy16_async(slot, src, n.hi * 2);
+        }
         return;
     }
     union {
@@ -170,14 +184,14 @@ template <typename T, bool FULL> __device__ __forceinline__ void stage8(uint32_t
         r.w[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        if (e < n)
+        if (e >= n.lo && e < n.hi)
             r.v[e] = static_cast<const T *>(src)[e];
 #pragma unroll
     for (int i = 0; i < kUnits<T>; ++i)
         smem_put(slot + i * stride, r.w[i]);
 }
 
-template <typename T> __device__ __forceinline__ Vec8 fetch8(uint32_t slot, uint32_t stride)
+template <typename T, bool FULL> __device__ __forceinline__ Vec8 fetch8(uint32_t slot, uint32_t stride, const Span &n)
 {
     Raw8<T> r;
     if constexpr (sizeof(T) == 4) {
@@ -187,15 +201,18 @@ template <typename T> __device__ __forceinline__ Vec8 fetch8(uint32_t slot, uint
     } else {
         r.w = smem_get(slot);
     }
-    return widen(r);
+    Vec8 v = widen(r);
+    if (!FULL && n.lo > 0)
+        cut(v, {n.lo, 8});
+    return v;
 }
 
-// Stores n elements (0 to 8).
-template <typename T, bool FULL> __device__ __forceinline__ void put8(void *to, const Vec8 &v, int n, bool wide)
+// Stores elements [lo, hi) of a vector.
+template <typename T, bool FULL> __device__ __forceinline__ void put8(void *to, const Vec8 &v, const Span &n, bool wide)
 {
     const Raw8<T> r = narrow<T>(v);
-    if (FULL || (wide && n % 8 == 0)) {
-        if (n == 0)
+    if (FULL || (wide && n.hi - n.lo == 8)) {
+        if (FULL && n.hi == 0)
             return;
         if constexpr (sizeof(T) == 4) {
             static_cast<float4 *>(to)[0] = r.a;
@@ -208,18 +225,21 @@ template <typename T, bool FULL> __device__ __forceinline__ void put8(void *to, 
     const T *each = reinterpret_cast<const T *>(&r);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        if (e < n)
+        if (e >= n.lo && e < n.hi)
             static_cast<T *>(to)[e] = each[e];
 }
 
-// Columns [col, col + n) of a weight or bias of type A or float32, `absent` where
-// the vector is NULL, 0 beyond n.
-template <typename A> __device__ __forceinline__ Vec8 param8(const void *p, bool f32, int col, int n, float absent)
+// Columns col + [lo, hi) of a vector of type A or float32, `absent` where it is
+// NULL, 0 beyond.
+template <typename A> __device__ __forceinline__ Vec8 param8(const void *p, bool f32, int64_t col, const Span &n, float absent)
 {
     float f[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        f[e] = e >= n ? 0.f : !p ? absent : f32 ? static_cast<const float *>(p)[col + e] : to_f32(static_cast<const A *>(p)[col + e]);
+        f[e] = e < n.lo || e >= n.hi ? 0.f
+               : !p                  ? absent
+               : f32                 ? static_cast<const float *>(p)[col + e]
+                                     : to_f32(static_cast<const A *>(p)[col + e]);
     return {{pair(f[0], f[1]), pair(f[2], f[3]), pair(f[4], f[5]), pair(f[6], f[7])}};
 }
 
@@ -339,70 +359,95 @@ struct Team {
 
 // ------------------------------------------------------------------ geometry
 
+// The rows of one class (every p.classes-th row, from `first`): how many there are,
+// and where worker w of n begins, counted within the class.
+__device__ __forceinline__ int64_t class_rows(const NormParams &p, int first) { return (p.rows - first + p.classes - 1) / p.classes; }
+__device__ __forceinline__ int64_t worker_begin(int64_t rows, int64_t w, int64_t n) { return rows * w / n; }
+
 // A thread's columns and rows, the same in both directions.
 struct Place {
-    int col, n;             // first column and how many (0 to 8); without any, a column that exists
+    int col;                // of its first vector; negative where the row starts within it
+    int end;                // of the block's columns
+    Span n;                 // of its first vector; without columns, {0, 0} where the row's first vector starts
     int64_t row;            // first row
-    int step;               // distance to the next
+    int64_t step;           // distance to the next
     int count, most;        // rows of this thread's group, and of the block's longest
 
-    int end;                // of the block's columns
-
-    // columns (0 to 8) of this thread's vector j, `apart` columns after the one before
-    __device__ __forceinline__ int columns(int j, int apart) const { return n > 0 ? max(0, min(8, end - col - j * apart)) : 0; }
+    // the span of this thread's vector j, `apart` columns after the one before
+    __device__ __forceinline__ Span span(int j, int apart) const
+    {
+        return j == 0 ? n : Span{0, n.hi > 0 ? max(0, min(8, end - col - j * apart)) : 0};
+    }
 
     __device__ __forceinline__ explicit Place(const NormParams &p)
     {
         const int rank = blockIdx.x % p.cluster, id = blockIdx.x / p.cluster;
         const int lane = threadIdx.x % p.lanes, group = threadIdx.x / p.lanes;
-        const int begin = rank * p.cta_cols;
-        end = min(p.cols, begin + p.cta_cols);
-        col = begin + lane * 8;
-        n = max(0, min(8, end - col));
-        if (n == 0)
-            col = 0;
+        const int first = id % p.classes, block = id / p.classes, blocks = p.ctas / p.classes;
+        const int shift = first * p.drift % 8;
+        col = rank * p.cta_cols + lane * 8 - shift;
+        end = min(p.cols, (rank + 1) * p.cta_cols - shift);
+        n.lo = max(0, -col);
+        n.hi = min(8, end - col);
+        if (n.hi <= n.lo) {
+            col = -shift;       // an aligned start, as for every copy, those of no bytes too
+            n = {0, 0};
+        }
+        const int64_t rows = class_rows(p, first);
         if (p.gate_rows > 1) {
             // each group walks its own run of rows, so that the rows of a gate stay together
-            const int64_t workers = (int64_t)p.ctas * p.row_groups, me = (int64_t)id * p.row_groups + group;
-            row = p.rows * me / workers;
-            step = 1;
-            count = (int)(p.rows * (me + 1) / workers - row);
-            most = (int)((p.rows + workers - 1) / workers);
+            const int64_t workers = (int64_t)blocks * p.row_groups, me = (int64_t)block * p.row_groups + group;
+            const int64_t begin = worker_begin(rows, me, workers);
+            row = first + p.classes * begin;
+            step = p.classes;
+            count = (int)(worker_begin(rows, me + 1, workers) - begin);
+            most = (int)((rows + workers - 1) / workers);
         } else {
             // a block's groups take neighbouring rows
-            const int64_t from = p.rows * id / p.ctas, to = p.rows * (id + 1) / p.ctas;
-            row = from + group;
-            step = p.row_groups;
-            count = (int)max((int64_t)0, (to - row + p.row_groups - 1) / p.row_groups);
+            const int64_t from = worker_begin(rows, block, blocks), to = worker_begin(rows, block + 1, blocks);
+            row = first + p.classes * (from + group);
+            step = (int64_t)p.classes * p.row_groups;
+            count = (int)max((int64_t)0, (to - from - group + p.row_groups - 1) / p.row_groups);
             most = (int)((to - from + p.row_groups - 1) / p.row_groups);
         }
         row = min(row, p.rows - 1);         // a group without rows points at one that exists
     }
 };
 
-// This thread's columns of its first row; `step` bytes on are its next ones.
+// This thread's columns of its first row (without rows, the tensor's start); `step`
+// bytes on are its next ones.
 __device__ __forceinline__ char *first_row(const NormRows &r, int bytes, const Place &q)
 {
-    return static_cast<char *>(r.data) + (q.row * r.stride + q.col) * bytes;
+    return static_cast<char *>(r.data) + (q.count > 0 ? (q.row * r.stride + q.col) * bytes : 0);
 }
 
-// The gate's rows: one for every row, or the same for gate_rows of them.
-struct GateWalk {
+// The gate's rows: one for every row, or (SHARED) the same for gate_rows of them.
+template <bool SHARED> struct GateWalk {
     char *at;
-    int left;               // rows of the gate row to go
+    int64_t into;           // rows of the gate before the present one
+    bool first;             // the present row is the first that this group has of the gate
 
-    __device__ __forceinline__ GateWalk(const NormParams &p, const NormRows &r, int bytes, const Place &q)
+    __device__ __forceinline__ GateWalk(const NormParams &p, const NormRows &r, int bytes, const Place &q) : into(0), first(true)
     {
-        const int64_t row = p.gate_rows > 1 ? q.row / p.gate_rows : q.row;
-        left = p.gate_rows > 1 ? (int)min((row + 1) * p.gate_rows - q.row, (int64_t)INT32_MAX) : 1;
-        at = static_cast<char *>(r.data) + (row * r.stride + q.col) * bytes;
-    }
-    __device__ __forceinline__ void next(const NormParams &p, const NormRows &r)
-    {
-        if (--left == 0) {
-            at += r.step;
-            left = p.gate_period;
+        if (!SHARED) {
+            at = first_row(r, bytes, q);
+            return;
         }
+        const int64_t row = q.row / p.gate_rows;
+        into = q.row - row * p.gate_rows;
+        at = static_cast<char *>(r.data) + (q.count > 0 ? (row * r.stride + q.col) * bytes : 0);
+    }
+    // the present row is this group's last of the gate
+    __device__ __forceinline__ bool last(const NormParams &p, const Place &q) const { return into + q.step >= p.gate_rows; }
+    __device__ __forceinline__ void next(const NormParams &p, const NormRows &r, const Place &q)
+    {
+        if (!SHARED) {
+            at += r.step;
+            return;
+        }
+        first = last(p, q);
+        for (into += q.step; into >= p.gate_rows; into -= p.gate_rows)
+            at += r.step;
     }
 };
 
@@ -434,13 +479,13 @@ __device__ __forceinline__ float elements(const Vec8 &a) { return total(add(add(
 // Mean and 1 / deviation (or root mean square) of a row; v becomes v - m, 0 beyond
 // the row's end.
 template <bool FULL, bool GENERAL>
-__device__ __forceinline__ void row_stats(const NormParams &p, Team &team, bool layer, float eps, int n, Vec8 &v, float &m, float &r)
+__device__ __forceinline__ void row_stats(const NormParams &p, Team &team, bool layer, float eps, const Span &n, Vec8 &v, float &m, float &r)
 {
     if (GENERAL && layer) {
         float t[1] = {elements(v)};
         team.sum(t);
         m = t[0] * p.inv_cols;
-        const f2 minus = both(n > 0 ? -m : 0.f);
+        const f2 minus = both(n.hi > 0 ? -m : 0.f);
         RK_PAIR v.v[i] = add(v.v[i], minus);
         if (!FULL)
             cut(v, n);
@@ -477,7 +522,7 @@ struct Ring {
     }
 };
 
-template <typename A, bool FULL> __device__ __forceinline__ void stage_gate(const NormParams &p, uint32_t to, uint32_t stride, const char *at, int n)
+template <typename A, bool FULL> __device__ __forceinline__ void stage_gate(const NormParams &p, uint32_t to, uint32_t stride, const char *at, const Span &n)
 {
     if (p.flags & kNormGateF32)
         stage8<float, FULL>(to, stride, at, n, p.wide & kNormWideGate);
@@ -485,14 +530,14 @@ template <typename A, bool FULL> __device__ __forceinline__ void stage_gate(cons
         stage8<A, FULL>(to, stride, at, n, p.wide & kNormWideGate);
 }
 
-template <typename A> __device__ __forceinline__ Vec8 fetch_gate(const NormParams &p, uint32_t at, uint32_t stride)
+template <typename A, bool FULL> __device__ __forceinline__ Vec8 fetch_gate(const NormParams &p, uint32_t at, uint32_t stride, const Span &n)
 {
-    return p.flags & kNormGateF32 ? fetch8<float>(at, stride) : fetch8<A>(at, stride);
+    return p.flags & kNormGateF32 ? fetch8<float, FULL>(at, stride, n) : fetch8<A, FULL>(at, stride, n);
 }
 
 // ------------------------------------------------------------------- forward
 
-template <typename A, typename R, bool FULL, bool POST, bool GENERAL>
+template <typename A, typename R, bool FULL, bool POST, bool GENERAL, bool SHARED>
 __global__ void __maxnreg__((norm_registers(kNormForwardThreads))) rikfad_norm_forward_kernel(const __grid_constant__ NormParams p)
 {
     extern __shared__ uint4 stages[];
@@ -503,24 +548,26 @@ __global__ void __maxnreg__((norm_registers(kNormForwardThreads))) rikfad_norm_f
     const bool branch = POST || (f & kNormBranch), gated = f & kNormGated;
     const uint32_t stride = p.threads * 16;
     const uint32_t z_at = kUnits<R> * stride, gate_at = z_at + kUnits<A> * stride;
+    const bool staged = gated && !(SHARED && (f & kNormGateHeld));      // else held in registers while it lasts
     Ring ring(p, stages);
     Team team(p, sums);
     prepare(p, sums);
     const char *x = first_row(p.x, sizeof(R), q), *z = first_row(p.z, sizeof(A), q);
     char *u_out = first_row(p.u, sizeof(R), q), *h_out = first_row(p.h, sizeof(A), q);
-    GateWalk gate(p, p.gate, f & kNormGateF32 ? 4 : (int)sizeof(A), q);
+    GateWalk<SHARED> gate(p, p.gate, f & kNormGateF32 ? 4 : (int)sizeof(A), q);
     int left = q.count;         // rows to issue; the pointers stay on rows that exist
     auto issue = [&]() {
-        const int n = left > 0 ? q.n : 0;
+        const Span n = left > 0 ? q.n : Span{0, 0};
         stage8<R, FULL>(ring.put, stride, x, n, p.wide & kNormWideX);
         if (branch)
             stage8<A, FULL>(ring.put + z_at, stride, z, n, p.wide & kNormWideZ);
-        if (gated)
+        if (staged)
             stage_gate<A, FULL>(p, ring.put + gate_at, stride, gate.at, n);
         if (--left > 0) {
             x += p.x.step;
             z += p.z.step;
-            gate.next(p, p.gate);
+            if (staged)
+                gate.next(p, p.gate, q);
         }
         ring.issued();
     };
@@ -528,44 +575,50 @@ __global__ void __maxnreg__((norm_registers(kNormForwardThreads))) rikfad_norm_f
         issue();
     const Vec8 w2 = param8<A>(p.post_weight, f & kNormParamF32, q.col, q.n, 1.f);
     const Vec8 w1 = param8<A>(p.pre_weight, f & kNormParamF32, q.col, q.n, 1.f);
-    Vec8 b2, b1;
+    Vec8 b2, b1, held = splat(1.f);
     if (GENERAL) {
         b2 = param8<A>(p.post_bias, f & kNormParamF32, q.col, q.n, 0.f);
         b1 = param8<A>(p.pre_bias, f & kNormParamF32, q.col, q.n, 0.f);
     }
     const f2 a = both(p.a), b = both(p.b);
-    const bool keeps = (f & kNormStats) && q.col == 0;
+    const bool keeps = (f & kNormStats) && q.col <= 0;
     for (int k = 0; k < q.most; ++k) {
         issue();
+        const Span n = k < q.count ? q.n : Span{0, 0};
+        if (SHARED && gated && !staged) {
+            if (gate.first)
+                held = param8<A>(gate.at, f & kNormGateF32, 0, n, 1.f);
+            if (k + 1 < q.count)
+                gate.next(p, p.gate, q);
+        }
         wait_copies(p.stages);
         float m2 = 0.f, r2 = 1.f, m1 = 0.f, r1 = 1.f;
-        Vec8 u = fetch8<R>(ring.get, stride);
+        Vec8 u = fetch8<R, FULL>(ring.get, stride, q.n);
         RK_PAIR u.v[i] = mul(u.v[i], a);
         if (branch) {
-            Vec8 v = fetch8<A>(ring.get + z_at, stride);
+            Vec8 v = fetch8<A, FULL>(ring.get + z_at, stride, q.n);
             if (POST) {
                 row_stats<FULL, GENERAL>(p, team, f & kNormPostLayer, p.post_eps, q.n, v, m2, r2);
                 const f2 r = both(r2);
                 RK_PAIR v.v[i] = GENERAL ? fma(mul(v.v[i], r), w2.v[i], b2.v[i]) : mul(mul(v.v[i], r), w2.v[i]);
             }
             if (gated) {
-                const Vec8 g = fetch_gate<A>(p, ring.get + gate_at, stride);
+                const Vec8 g = !SHARED || staged ? fetch_gate<A, FULL>(p, ring.get + gate_at, stride, q.n) : held;
                 RK_PAIR v.v[i] = mul(v.v[i], g.v[i]);
             }
             RK_PAIR u.v[i] = fma(v.v[i], b, u.v[i]);
         }
-        const int n = k < q.count ? q.n : 0;
-        put8<R, FULL>(u_out, u, f & kNormU ? n : 0, p.wide & kNormWideU);
+        put8<R, FULL>(u_out, u, f & kNormU ? n : Span{0, 0}, p.wide & kNormWideU);
         u_out += p.u.step;
         if (f & kNormPre) {
             row_stats<FULL, GENERAL>(p, team, f & kNormPreLayer, p.pre_eps, q.n, u, m1, r1);
             const f2 r = both(r1);
             RK_PAIR u.v[i] = GENERAL ? fma(mul(u.v[i], r), w1.v[i], b1.v[i]) : mul(mul(u.v[i], r), w1.v[i]);
         }
-        put8<A, FULL>(h_out, u, f & kNormH ? n : 0, p.wide & kNormWideH);
+        put8<A, FULL>(h_out, u, f & kNormH ? n : Span{0, 0}, p.wide & kNormWideH);
         h_out += p.h.step;
-        if (keeps && n > 0)
-            p.stats[q.row + (int64_t)k * q.step] = make_float4(m2, r2, m1, r1);
+        if (keeps && n.hi > 0)
+            p.stats[q.row + k * q.step] = make_float4(m2, r2, m1, r1);
         ring.used();
     }
     allow_successor_launch();
@@ -573,8 +626,11 @@ __global__ void __maxnreg__((norm_registers(kNormForwardThreads))) rikfad_norm_f
 
 // ------------------------------------------------------------------ backward
 
-// n columns of one partial row of a sum over rows, from the block's groups in order.
-__device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, float *part, float *buffer, const Vec8 &acc, int off, int n)
+// How far a block's columns are shifted (Place).
+__device__ __forceinline__ int id_shift(const NormParams &p) { return (blockIdx.x / p.cluster) % p.classes * p.drift % 8; }
+
+// Elements n of one partial row of a sum over rows, from the block's groups in order.
+__device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, float *part, float *buffer, const Vec8 &acc, int off, const Span &n)
 {
     float *out = part + (int64_t)(blockIdx.x / p.cluster) * p.cols;
     if (p.row_groups == 1) {
@@ -584,14 +640,18 @@ __device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, f
     // the vectors of all lanes, then those `off` columns on
     __syncthreads();
     const int group = threadIdx.x / p.lanes, width = p.lanes * 8;
-    if (n > 0)
-        RK_PAIR *reinterpret_cast<f2 *>(buffer + group * width + q.col + 2 * i) = acc.v[i];
+    if (n.hi > 0)
+        RK_PAIR *reinterpret_cast<f2 *>(buffer + group * width + (threadIdx.x % p.lanes) * 8 + 2 * i) = acc.v[i];
     __syncthreads();
-    for (int c = threadIdx.x; c < min(width, p.cols - off); c += p.threads) {
+    // column `first` + c is at c
+    const int first = off - id_shift(p);
+    for (int c = threadIdx.x; c < width; c += p.threads) {
+        if (first + c < 0 || first + c >= p.cols)
+            continue;
         float t = 0.f;
         for (int g = 0; g < p.row_groups; ++g)
             t += buffer[g * width + c];
-        out[off + c] = t;
+        out[first + c] = t;
     }
 }
 
@@ -606,15 +666,17 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
     const Place q(p);
     uint32_t f = p.flags;
     asm volatile("" : "+r"(f));        // in a register: its tests need no constant loads
-    const bool branch = POST || (f & kNormBranch), gated = f & kNormGated, shared_gate = SHARED;
+    const bool branch = POST || (f & kNormBranch), gated = f & kNormGated, shared_gate = SHARED && (f & kNormDgate);
     const uint32_t stride = p.threads * 16;
     const int gate_bytes = f & kNormGateF32 ? 4 : (int)sizeof(A);
     // a vector's slots: x, z, dh, du, gate
     const uint32_t z_at = kUnits<R> * stride, dh_at = z_at + kUnits<A> * stride, du_at = dh_at + kUnits<A> * stride;
     const uint32_t gate_at = du_at + kUnits<R> * stride, next_at = stride * p.units;
     const int apart = p.lanes * 8;
-    int cols[V];                // columns of each vector: 0 to 8
-    RK_EACH cols[j] = q.columns(j, apart);
+    Span cols[V];               // of each vector
+    RK_EACH cols[j] = q.span(j, apart);
+    const Span none{0, 0};
+    const bool staged = gated && !(SHARED && (f & kNormGateHeld));      // else held in registers while it lasts
     Ring ring(p, stages, V);
     Team team(p, sums);
     prepare(p, sums);
@@ -622,20 +684,21 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
     // absent ones are read nowhere (zeros take their place)
     const char *dh = f & kNormDh ? first_row(p.dh, sizeof(A), q) : x, *du = f & kNormDu ? first_row(p.du, sizeof(R), q) : x;
     char *dx = first_row(p.dx, sizeof(R), q), *dz = first_row(p.dz, sizeof(A), q);
-    GateWalk gate(p, p.gate, gate_bytes, q);
+    GateWalk<SHARED> gate(p, p.gate, gate_bytes, q);
     int left = q.count;         // rows to issue; the pointers stay on rows that exist
     auto issue = [&]() {
         RK_EACH
         {
             // a vector that this thread lacks reads nowhere, from its first one's address
-            const int n = left > 0 ? cols[j] : 0, off = cols[j] > 0 ? j * apart : 0;
+            const Span n = left > 0 ? cols[j] : none;
+            const int off = cols[j].hi > 0 ? j * apart : 0;
             const uint32_t to = ring.put + j * next_at;
             stage8<R, FULL>(to, stride, x + off * (int)sizeof(R), n, p.wide & kNormWideX);
             if (branch)
                 stage8<A, FULL>(to + z_at, stride, z + off * (int)sizeof(A), n, p.wide & kNormWideZ);
-            stage8<A, FULL>(to + dh_at, stride, dh + off * (int)sizeof(A), f & kNormDh ? n : 0, p.wide & kNormWideDh);
-            stage8<R, FULL>(to + du_at, stride, du + off * (int)sizeof(R), f & kNormDu ? n : 0, p.wide & kNormWideDu);
-            if (gated)
+            stage8<A, FULL>(to + dh_at, stride, dh + off * (int)sizeof(A), f & kNormDh ? n : none, p.wide & kNormWideDh);
+            stage8<R, FULL>(to + du_at, stride, du + off * (int)sizeof(R), f & kNormDu ? n : none, p.wide & kNormWideDu);
+            if (staged)
                 stage_gate<A, FULL>(p, to + gate_at, stride, gate.at + off * gate_bytes, n);
         }
         if (--left > 0) {
@@ -643,21 +706,21 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
             z += p.z.step;
             dh += p.dh.step;
             du += p.du.step;
-            gate.next(p, p.gate);
+            if (staged)
+                gate.next(p, p.gate, q);
         }
         ring.issued();
     };
     Vec8 dw1[V], dw2[V], db1[V], db2[V], dg = splat(0.f);
     RK_EACH dw1[j] = dw2[j] = db1[j] = db2[j] = splat(0.f);
     // dgate: a row for every row, or the sum over the gate's
-    GateWalk dgate(p, p.dgate, gate_bytes, q);
-    bool gate_whole = p.gate_rows <= 1 || q.row % p.gate_rows == 0;     // the sum began with the gate's first row
-    bool gate_first = true;                                             // it is the group's first
+    GateWalk<SHARED> dgate(p, p.dgate, gate_bytes, q);
+    bool gate_first = true;                     // the sum is of the group's first gate
+    const int64_t worker = (int64_t)(blockIdx.x / p.cluster) * p.row_groups + threadIdx.x / p.lanes;
     auto gate_part = [&]() {
-        const int64_t worker = (int64_t)(blockIdx.x / p.cluster) * p.row_groups + threadIdx.x / p.lanes;
         put8<float, false>(p.gate_part + (2 * worker + (gate_first ? 0 : 1)) * p.cols + q.col, dg, q.n, false);
     };
-    auto put_gate = [&](const Vec8 &v, int j, int n) {
+    auto put_gate = [&](const Vec8 &v, int j, const Span &n) {
         if (f & kNormGateF32)
             put8<float, FULL>(dgate.at + j * apart * 4, v, n, p.wide & kNormWideDgate);
         else
@@ -665,6 +728,9 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
     };
     if (shared_gate && q.count == 0)            // a group without rows adds nothing to the gate it lies in
         gate_part();
+    bool gate_whole = p.classes == 1 && dgate.into == 0;    // the sum began with the gate's first row
+    Vec8 held[V];
+    RK_EACH held[j] = splat(1.f);
     for (int k = 0; k < p.stages - 1; ++k)
         issue();
     Vec8 w2[V], w1[V], b2[V];
@@ -696,7 +762,7 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
         RK_EACH
         {
             // columns beyond the row's end stay zero: they add nothing to later sums
-            const f2 rr = both(cols[j] > 0 ? r : 0.f);
+            const f2 rr = both(cols[j].hi > 0 ? r : 0.f);
             RK_PAIR e[j].v[i] = mul(GENERAL ? fma(y[j].v[i], my, add(e[j].v[i], m)) : fma(y[j].v[i], my, e[j].v[i]), rr);
             if (!FULL)
                 cut(e[j], cols[j]);
@@ -708,19 +774,25 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
         const float m2 = next.x, r2 = next.y, m1 = next.z, r1 = next.w;
         stats += q.step;
         next = k + 1 < q.count ? *stats : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (SHARED && gated && !staged) {
+            if (gate.first)
+                RK_EACH held[j] = param8<A>(gate.at, f & kNormGateF32, j * apart, live ? cols[j] : none, 1.f);
+            if (k + 1 < q.count)
+                gate.next(p, p.gate, q);
+        }
         wait_copies(p.stages);
 
         Vec8 e[V], y[V], y2[V], nn[V], g[V];
         RK_EACH
         {
-            e[j] = fetch8<A>(ring.get + j * next_at + dh_at, stride);       // the gradient of h, then of u
-            y[j] = fetch8<R>(ring.get + j * next_at, stride);
+            e[j] = fetch8<A, FULL>(ring.get + j * next_at + dh_at, stride, cols[j]);       // the gradient of h, then of u
+            y[j] = fetch8<R, FULL>(ring.get + j * next_at, stride, cols[j]);
             RK_PAIR y[j].v[i] = mul(y[j].v[i], a);
         }
         if (branch) {
             RK_EACH
             {
-                nn[j] = fetch8<A>(ring.get + j * next_at + z_at, stride);
+                nn[j] = fetch8<A, FULL>(ring.get + j * next_at + z_at, stride, cols[j]);
                 if (POST) {
                     const f2 minus = both(-m2 * r2), r = both(r2);
                     RK_PAIR y2[j].v[i] = GENERAL ? mul(add(nn[j].v[i], both(-m2)), r) : mul(nn[j].v[i], r);
@@ -731,7 +803,7 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
             if (gated)
                 RK_EACH
                 {
-                    g[j] = fetch_gate<A>(p, ring.get + j * next_at + gate_at, stride);
+                    g[j] = !SHARED || staged ? fetch_gate<A, FULL>(p, ring.get + j * next_at + gate_at, stride, cols[j]) : held[j];
                     RK_PAIR g[j].v[i] = mul(g[j].v[i], b);
                 }
             RK_EACH
@@ -752,41 +824,42 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
         }
         RK_EACH
         {
-            const Vec8 d = fetch8<R>(ring.get + j * next_at + du_at, stride);
+            const Vec8 d = fetch8<R, FULL>(ring.get + j * next_at + du_at, stride, cols[j]);
             RK_PAIR e[j].v[i] = add(e[j].v[i], d.v[i]);
         }
         RK_EACH
         {
             Vec8 o;
             RK_PAIR o.v[i] = mul(e[j].v[i], a);
-            put8<R, FULL>(dx + j * apart * (int)sizeof(R), o, live && (f & kNormDx) ? cols[j] : 0, p.wide & kNormWideDx);
+            put8<R, FULL>(dx + j * apart * (int)sizeof(R), o, live && (f & kNormDx) ? cols[j] : none, p.wide & kNormWideDx);
         }
         dx += p.dx.step;
         if (branch) {
             if (shared_gate) {
                 if (live) {
                     RK_PAIR dg.v[i] = fma(mul(e[0].v[i], b), nn[0].v[i], dg.v[i]);
-                    // The gate's last row, or the group's: a gate that lies within the
-                    // group is done, others leave a partial sum (the group's first gate
-                    // in row 0, its last in row 1).
-                    if (dgate.left == 1 || k + 1 == q.count) {
-                        if (gate_whole && dgate.left == 1)
+                    // The group's last row of the gate, or of all: a gate that lies within
+                    // the group is done, others leave a partial sum (the group's first
+                    // gate in row 0, its last in row 1).
+                    const bool last = dgate.last(p, q);
+                    if (last || k + 1 == q.count) {
+                        if (gate_whole && last)
                             put_gate(dg, 0, q.n);
                         else
                             gate_part();
                         dg = splat(0.f);
-                        gate_whole = true;
+                        gate_whole = p.classes == 1;
                         gate_first = false;
                     }
-                    dgate.next(p, p.dgate);
+                    dgate.next(p, p.dgate, q);
                 }
-            } else if (f & kNormDgate) {
+            } else if (!SHARED && (f & kNormDgate)) {
                 RK_EACH
                 {
                     RK_PAIR nn[j].v[i] = mul(mul(e[j].v[i], b), nn[j].v[i]);
-                    put_gate(nn[j], j, live ? cols[j] : 0);
+                    put_gate(nn[j], j, live ? cols[j] : none);
                 }
-                dgate.next(p, p.dgate);
+                dgate.next(p, p.dgate, q);
             }
             RK_EACH
                 RK_PAIR e[j].v[i] = mul(e[j].v[i], g[j].v[i]);
@@ -802,7 +875,7 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
                 through_norm(f & kNormPostLayer, r2, e, y2);
             }
             RK_EACH
-                put8<A, FULL>(dz + j * apart * (int)sizeof(A), e[j], live && (f & kNormDz) ? cols[j] : 0, p.wide & kNormWideDz);
+                put8<A, FULL>(dz + j * apart * (int)sizeof(A), e[j], live && (f & kNormDz) ? cols[j] : none, p.wide & kNormWideDz);
             dz += p.dz.step;
         }
         ring.used();
@@ -874,19 +947,39 @@ template <typename A> __global__ void __launch_bounds__(32 * kJoinRows) rikfad_n
             store_as<A>(dst, p.flags & kNormParamF32, out, t);
         return;
     }
-    const int64_t gates = p.rows / p.gate_rows, workers = (int64_t)p.ctas * p.row_groups;
+    const int64_t gates = p.rows / p.gate_rows, workers = (int64_t)(p.ctas / p.classes) * p.row_groups;   // of a class
     for (int64_t g = blockIdx.y - p.sums; g < gates; g += gridDim.y - p.sums) {
-        // worker w has rows [rows w / workers, rows (w + 1) / workers)
         const int64_t begin = g * p.gate_rows, end = begin + p.gate_rows;
-        const int64_t w0 = ((begin + 1) * workers - 1) / p.rows, w1 = (end * workers - 1) / p.rows;
-        if (w0 == w1)
-            continue;       // written by its only worker
-        // the first worker's sum is of its last gate, unless that is its first as well
-        const bool head = p.rows * w0 / workers / p.gate_rows == g;
-        const float *first = p.gate_part + (2 * w0 + (head ? 0 : 1)) * p.cols;
-        float t = join_column(p.gate_part + 2 * (w0 + 1) * p.cols + c, w1 - w0, (int64_t)2 * p.cols, c < p.cols, red);
+        float t = 0.f;
+        bool done = false;
+        for (int first = 0; first < p.classes; ++first) {
+            // the class's rows of the gate, [i0, i1] of its own, and their workers
+            const int64_t rows = class_rows(p, first);
+            const int64_t i0 = begin <= first ? 0 : (begin - first + p.classes - 1) / p.classes;
+            const int64_t i1 = end - 1 < first ? -1 : (end - 1 - first) / p.classes;
+            if (i1 < i0)
+                continue;
+            const int64_t w0 = ((i0 + 1) * workers - 1) / rows, w1 = ((i1 + 1) * workers - 1) / rows;
+            if (p.classes == 1 && w0 == w1) {
+                done = true;        // written by its only worker
+                break;
+            }
+            if (c < p.cols)
+                for (int64_t w = w0 + y; w <= w1; w += kJoinRows) {
+                    const int64_t row = first + p.classes * worker_begin(rows, w, workers);     // the worker's first
+                    // block (w / row_groups) of the class has number (w / row_groups) classes + first
+                    const int64_t worker = (w / p.row_groups * p.classes + first) * p.row_groups + w % p.row_groups;
+                    t += __ldcg(p.gate_part + (2 * worker + (row / p.gate_rows == g ? 0 : 1)) * p.cols + c);
+                }
+        }
+        if (done)
+            continue;
+        __syncthreads();
+        red[y][x] = t;
+        __syncthreads();
+        t = warp_sum(red[x][y]);
         if (x == 0 && out < p.cols)
-            store_as<A>(p.dgate.data, p.flags & kNormGateF32, g * p.dgate.stride + out, __ldcg(first + out) + t);
+            store_as<A>(p.dgate.data, p.flags & kNormGateF32, g * p.dgate.stride + out, t);
     }
 }
 
@@ -918,7 +1011,8 @@ template <typename A, typename R, bool FULL, bool POST, bool GENERAL>
 cudaError_t launch_rows(const NormParams &n, bool backward, cudaStream_t s)
 {
     if (!backward)
-        return launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL>, n, s);
+        return n.flags & kNormSharedGate ? launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, true>, n, s)
+                                         : launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, false>, n, s);
     if (n.flags & kNormSharedGate)
         return launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 1, true>, n, s);
     if (n.vectors == 1)
