@@ -1,7 +1,7 @@
 // rikfad_norm.cu -- residual sum of a transformer block with the norms around it:
 // argument checks, workspace and launch shapes.  The mathematics and the kernels
-// are in rikfad_norm_kernels.cuh, instantiated per element type in
-// rikfad_norm_f32.cu, rikfad_norm_bf16.cu and rikfad_norm_f16.cu.
+// are in rikfad_norm_kernels.cuh, instantiated per direction and element types in
+// rikfad_norm_forward_*.cu and rikfad_norm_backward_*.cu.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -183,7 +183,7 @@ void drifting(NormParams &n, const rikfad_residual_norm *p)
     if (n.wide == kNormWideAll || p->rows <= 1)
         return;
     const NormRows *const all[] = {&n.x, &n.z, &n.u, &n.h, &n.du, &n.dh, &n.dx, &n.dz,
-                                   p->gate_rows > 1 ? nullptr : &n.gate, p->gate_rows > 1 ? nullptr : &n.dgate};
+                                   n.gate_rows > 1 ? nullptr : &n.gate, n.gate_rows > 1 ? nullptr : &n.dgate};
     int drift = -1;
     for (const NormRows *t : all) {
         if (t == nullptr || t->data == nullptr)
@@ -196,8 +196,8 @@ void drifting(NormParams &n, const rikfad_residual_norm *p)
         return;
     n.drift = drift;
     n.classes = drift % 4 == 0 ? 2 : drift % 2 == 0 ? 4 : 8;
-    n.wide |= kNormWideAll & ~(p->gate_rows > 1 ? kNormWideGate | kNormWideDgate : 0u);
-    if (p->gate_rows > 1)
+    n.wide |= kNormWideAll & ~(n.gate_rows > 1 ? kNormWideGate | kNormWideDgate : 0u);
+    if (n.gate_rows > 1)
         n.wide &= ~(kNormWideGate | kNormWideDgate);
 }
 
@@ -240,7 +240,7 @@ void shape(NormParams &n, const rikfad_residual_norm *p, int most_vectors, int m
     // the rows of a shared gate are counted, so a step there is one gate
     for (NormRows *t : {&n.gate, &n.dgate})
         t->step = n.gate_rows > 1 ? t->stride * dtype_bytes(p->gate_dtype) : t->stride * g;
-    n.flags |= p->gate.data && n.gate_rows >= 16 ? kNormGateHeld : 0;
+    n.flags |= p->gate.data && n.gate_rows >= kNormHeldRows ? kNormGateHeld : 0;
 }
 
 // Clusters of a launch: as many as are resident at once (`threads_per_sm` by the
@@ -261,9 +261,10 @@ void grid(NormParams &n, int threads_per_sm)
 void forward_shape(const rikfad_residual_norm *p, NormParams &n)
 {
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
-    n.units = r + a + (p->gate.data && p->gate_rows < 16 ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
-    shape(n, p, 1, kNormMaxThreads);
-    grid(n, kNormForwardThreads);
+    n.units = r + a + (p->gate.data && p->gate_rows < kNormHeldRows ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
+    const int most = n.flags & kNormSharedGate ? 1 : 2;
+    shape(n, p, most, kNormMaxThreads / most);
+    grid(n, n.vectors == 1 ? kNormForwardThreads<1> : kNormForwardThreads<2>);
 }
 
 struct Workspace {
@@ -275,7 +276,7 @@ struct Workspace {
 Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n, bool classes = true)
 {
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
-    n.units = 2 * a + 2 * r + (p->gate.data && p->gate_rows < 16 ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
+    n.units = 2 * a + 2 * r + (p->gate.data && p->gate_rows < kNormHeldRows ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
     const bool gated = n.flags & kNormSharedGate, shared = gated && p->dgate.data, post = n.flags & kNormPost;
     const int one = post && n.general ? kNormBackwardThreads<true, true, 1> : kNormBackwardThreads<false, false, 1>;
     const int two = !post ? kNormBackwardThreads<false, false, 2> : n.general ? kNormBackwardThreads<true, true, 2> : kNormBackwardThreads<true, false, 2>;
@@ -300,12 +301,17 @@ Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n, bool clas
     return w;
 }
 
+using Launch = cudaError_t (*)(const NormParams &, cudaStream_t);
+
 cudaError_t launch_norm(const NormParams &n, int dtype, int residual_dtype, bool backward, cudaStream_t s)
 {
-    const bool f32 = residual_dtype == RIKFAD_F32;
-    return dtype == RIKFAD_F32 ? launch_norm_f32(n, backward, s)
-           : dtype == RIKFAD_BF16 ? launch_norm_bf16(n, f32, backward, s)
-                                  : launch_norm_f16(n, f32, backward, s);
+    // by dtype, residual_dtype == RIKFAD_F32 and direction
+    static const Launch table[3][2][2] = {
+        {{norm_forward_f32_f32, norm_backward_f32_f32}, {norm_forward_f32_f32, norm_backward_f32_f32}},
+        {{norm_forward_bf16_bf16, norm_backward_bf16_bf16}, {norm_forward_bf16_f32, norm_backward_bf16_f32}},
+        {{norm_forward_f16_f16, norm_backward_f16_f16}, {norm_forward_f16_f32, norm_backward_f16_f32}},
+    };
+    return table[dtype][residual_dtype == RIKFAD_F32][backward](n, s);
 }
 
 }  // namespace

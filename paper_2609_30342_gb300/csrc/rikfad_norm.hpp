@@ -15,10 +15,11 @@ namespace rikfad {
 constexpr int kNormMaxThreads = 512;
 constexpr int kNormMaxWarps = kNormMaxThreads / 32;
 // Threads of an SM, by the registers that the kernels are given.
-constexpr int kNormForwardThreads = 768;
+template <int V> constexpr int kNormForwardThreads = V == 1 ? 768 : 512;
 template <bool POST, bool GENERAL, int V>
 constexpr int kNormBackwardThreads = V == 1 ? (POST && GENERAL ? 384 : 512) : !POST ? 384 : GENERAL ? 256 : 320;
 constexpr int norm_registers(int threads) { return threads <= 256 ? 248 : 65536 / threads / 8 * 8; }
+constexpr int64_t kNormHeldRows = 16;           // rows of a gate from which it is kept in registers
 constexpr int kNormSms = 152;
 constexpr size_t kNormSmemPerSm = 200 << 10;    // for the stages; a block keeps 1 KB more
 
@@ -99,8 +100,16 @@ struct NormParams {
     float *gate_part;           // ctas x row_groups x 2 x cols
 };
 
-cudaError_t launch_norm_f32(const NormParams &n, bool backward, cudaStream_t s);
-cudaError_t launch_norm_bf16(const NormParams &n, bool residual_f32, bool backward, cudaStream_t s);
-cudaError_t launch_norm_f16(const NormParams &n, bool residual_f32, bool backward, cudaStream_t s);
+// One translation unit each (types of the activations and of the residual stream).
+cudaError_t norm_forward_f32_f32(const NormParams &n, cudaStream_t s);
+cudaError_t norm_backward_f32_f32(const NormParams &n, cudaStream_t s);
+cudaError_t norm_forward_bf16_bf16(const NormParams &n, cudaStream_t s);
+cudaError_t norm_backward_bf16_bf16(const NormParams &n, cudaStream_t s);
+cudaError_t norm_forward_bf16_f32(const NormParams &n, cudaStream_t s);
+cudaError_t norm_backward_bf16_f32(const NormParams &n, cudaStream_t s);
+cudaError_t norm_forward_f16_f16(const NormParams &n, cudaStream_t s);
+cudaError_t norm_backward_f16_f16(const NormParams &n, cudaStream_t s);
+cudaError_t norm_forward_f16_f32(const NormParams &n, cudaStream_t s);
+cudaError_t norm_backward_f16_f32(const NormParams &n, cudaStream_t s);
 
 }  // namespace rikfad

@@ -1,0 +1,8 @@
+// The residual norm's backward kernels for bf16 activations and a bf16 residual stream.
+#include "rikfad_norm_kernels.cuh"
+
+namespace rikfad {
+
+cudaError_t norm_backward_bf16_bf16(const NormParams &n, cudaStream_t s) { return norm_backward<__nv_bfloat16, __nv_bfloat16>(n, s); }
+
+}  // namespace rikfad

@@ -478,19 +478,25 @@ __device__ __forceinline__ float elements(const Vec8 &a) { return total(add(add(
 
 // Mean and 1 / deviation (or root mean square) of a row; v becomes v - m, 0 beyond
 // the row's end.
-template <bool FULL, bool GENERAL>
-__device__ __forceinline__ void row_stats(const NormParams &p, Team &team, bool layer, float eps, const Span &n, Vec8 &v, float &m, float &r)
+template <bool FULL, bool GENERAL, int V>
+__device__ __forceinline__ void row_stats(const NormParams &p, Team &team, bool layer, float eps, const Span (&n)[V], Vec8 (&v)[V], float &m,
+                                          float &r)
 {
     if (GENERAL && layer) {
-        float t[1] = {elements(v)};
+        float t[1] = {0.f};
+        RK_EACH t[0] += elements(v[j]);
         team.sum(t);
         m = t[0] * p.inv_cols;
-        const f2 minus = both(n.hi > 0 ? -m : 0.f);
-        RK_PAIR v.v[i] = add(v.v[i], minus);
-        if (!FULL)
-            cut(v, n);
+        RK_EACH
+        {
+            const f2 minus = both(n[j].hi > 0 ? -m : 0.f);
+            RK_PAIR v[j].v[i] = add(v[j].v[i], minus);
+            if (!FULL)
+                cut(v[j], n[j]);
+        }
     }
-    float t[1] = {dot(v, v)};
+    float t[1] = {0.f};
+    RK_EACH t[0] += dot(v[j], v[j]);
     team.sum(t);
     r = rsqrtf(fmaf(t[0], p.inv_cols, eps));
 }
@@ -537,8 +543,8 @@ template <typename A, bool FULL> __device__ __forceinline__ Vec8 fetch_gate(cons
 
 // ------------------------------------------------------------------- forward
 
-template <typename A, typename R, bool FULL, bool POST, bool GENERAL, bool SHARED>
-__global__ void __maxnreg__((norm_registers(kNormForwardThreads))) rikfad_norm_forward_kernel(const __grid_constant__ NormParams p)
+template <typename A, typename R, bool FULL, bool POST, bool GENERAL, bool SHARED, int V>
+__global__ void __maxnreg__((norm_registers(kNormForwardThreads<V>))) rikfad_norm_forward_kernel(const __grid_constant__ NormParams p)
 {
     extern __shared__ uint4 stages[];
     __shared__ RowSums sums;
@@ -547,22 +553,32 @@ __global__ void __maxnreg__((norm_registers(kNormForwardThreads))) rikfad_norm_f
     asm volatile("" : "+r"(f));        // in a register: its tests need no constant loads
     const bool branch = POST || (f & kNormBranch), gated = f & kNormGated;
     const uint32_t stride = p.threads * 16;
-    const uint32_t z_at = kUnits<R> * stride, gate_at = z_at + kUnits<A> * stride;
+    const uint32_t z_at = kUnits<R> * stride, gate_at = z_at + kUnits<A> * stride, next_at = stride * p.units;
     const bool staged = gated && !(SHARED && (f & kNormGateHeld));      // else held in registers while it lasts
-    Ring ring(p, stages);
+    const int apart = p.lanes * 8, gate_bytes = f & kNormGateF32 ? 4 : (int)sizeof(A);
+    Span cols[V];               // of each vector
+    RK_EACH cols[j] = q.span(j, apart);
+    const Span none{0, 0};
+    Ring ring(p, stages, V);
     Team team(p, sums);
     prepare(p, sums);
     const char *x = first_row(p.x, sizeof(R), q), *z = first_row(p.z, sizeof(A), q);
     char *u_out = first_row(p.u, sizeof(R), q), *h_out = first_row(p.h, sizeof(A), q);
-    GateWalk<SHARED> gate(p, p.gate, f & kNormGateF32 ? 4 : (int)sizeof(A), q);
+    GateWalk<SHARED> gate(p, p.gate, gate_bytes, q);
     int left = q.count;         // rows to issue; the pointers stay on rows that exist
     auto issue = [&]() {
-        const Span n = left > 0 ? q.n : Span{0, 0};
-        stage8<R, FULL>(ring.put, stride, x, n, p.wide & kNormWideX);
-        if (branch)
-            stage8<A, FULL>(ring.put + z_at, stride, z, n, p.wide & kNormWideZ);
-        if (staged)
-            stage_gate<A, FULL>(p, ring.put + gate_at, stride, gate.at, n);
+        RK_EACH
+        {
+            // a vector that this thread lacks reads nowhere, from its first one's address
+            const Span n = left > 0 ? cols[j] : none;
+            const int off = cols[j].hi > 0 ? j * apart : 0;
+            const uint32_t to = ring.put + j * next_at;
+            stage8<R, FULL>(to, stride, x + off * (int)sizeof(R), n, p.wide & kNormWideX);
+            if (branch)
+                stage8<A, FULL>(to + z_at, stride, z + off * (int)sizeof(A), n, p.wide & kNormWideZ);
+            if (staged)
+                stage_gate<A, FULL>(p, to + gate_at, stride, gate.at + off * gate_bytes, n);
+        }
         if (--left > 0) {
             x += p.x.step;
             z += p.z.step;
@@ -573,51 +589,66 @@ __global__ void __maxnreg__((norm_registers(kNormForwardThreads))) rikfad_norm_f
     };
     for (int k = 0; k < p.stages - 1; ++k)
         issue();
-    const Vec8 w2 = param8<A>(p.post_weight, f & kNormParamF32, q.col, q.n, 1.f);
-    const Vec8 w1 = param8<A>(p.pre_weight, f & kNormParamF32, q.col, q.n, 1.f);
-    Vec8 b2, b1, held = splat(1.f);
-    if (GENERAL) {
-        b2 = param8<A>(p.post_bias, f & kNormParamF32, q.col, q.n, 0.f);
-        b1 = param8<A>(p.pre_bias, f & kNormParamF32, q.col, q.n, 0.f);
+    Vec8 w2[V], w1[V], b2[V], b1[V], held[V];
+    RK_EACH
+    {
+        w2[j] = param8<A>(p.post_weight, f & kNormParamF32, q.col + j * apart, cols[j], 1.f);
+        w1[j] = param8<A>(p.pre_weight, f & kNormParamF32, q.col + j * apart, cols[j], 1.f);
+        if (GENERAL) {
+            b2[j] = param8<A>(p.post_bias, f & kNormParamF32, q.col + j * apart, cols[j], 0.f);
+            b1[j] = param8<A>(p.pre_bias, f & kNormParamF32, q.col + j * apart, cols[j], 0.f);
+        }
+        held[j] = splat(1.f);
     }
     const f2 a = both(p.a), b = both(p.b);
     const bool keeps = (f & kNormStats) && q.col <= 0;
     for (int k = 0; k < q.most; ++k) {
         issue();
-        const Span n = k < q.count ? q.n : Span{0, 0};
+        const bool live = k < q.count;
         if (SHARED && gated && !staged) {
             if (gate.first)
-                held = param8<A>(gate.at, f & kNormGateF32, 0, n, 1.f);
+                RK_EACH held[j] = param8<A>(gate.at, f & kNormGateF32, j * apart, live ? cols[j] : none, 1.f);
             if (k + 1 < q.count)
                 gate.next(p, p.gate, q);
         }
         wait_copies(p.stages);
         float m2 = 0.f, r2 = 1.f, m1 = 0.f, r1 = 1.f;
-        Vec8 u = fetch8<R, FULL>(ring.get, stride, q.n);
-        RK_PAIR u.v[i] = mul(u.v[i], a);
-        if (branch) {
-            Vec8 v = fetch8<A, FULL>(ring.get + z_at, stride, q.n);
-            if (POST) {
-                row_stats<FULL, GENERAL>(p, team, f & kNormPostLayer, p.post_eps, q.n, v, m2, r2);
-                const f2 r = both(r2);
-                RK_PAIR v.v[i] = GENERAL ? fma(mul(v.v[i], r), w2.v[i], b2.v[i]) : mul(mul(v.v[i], r), w2.v[i]);
-            }
-            if (gated) {
-                const Vec8 g = !SHARED || staged ? fetch_gate<A, FULL>(p, ring.get + gate_at, stride, q.n) : held;
-                RK_PAIR v.v[i] = mul(v.v[i], g.v[i]);
-            }
-            RK_PAIR u.v[i] = fma(v.v[i], b, u.v[i]);
+        Vec8 u[V], v[V];
+        RK_EACH
+        {
+            u[j] = fetch8<R, FULL>(ring.get + j * next_at, stride, cols[j]);
+            RK_PAIR u[j].v[i] = mul(u[j].v[i], a);
         }
-        put8<R, FULL>(u_out, u, f & kNormU ? n : Span{0, 0}, p.wide & kNormWideU);
+        if (branch) {
+            RK_EACH v[j] = fetch8<A, FULL>(ring.get + j * next_at + z_at, stride, cols[j]);
+            if (POST) {
+                row_stats<FULL, GENERAL>(p, team, f & kNormPostLayer, p.post_eps, cols, v, m2, r2);
+                const f2 r = both(r2);
+                RK_EACH
+                    RK_PAIR v[j].v[i] = GENERAL ? fma(mul(v[j].v[i], r), w2[j].v[i], b2[j].v[i]) : mul(mul(v[j].v[i], r), w2[j].v[i]);
+            }
+            if (gated)
+                RK_EACH
+                {
+                    const Vec8 g = !SHARED || staged ? fetch_gate<A, FULL>(p, ring.get + j * next_at + gate_at, stride, cols[j]) : held[j];
+                    RK_PAIR v[j].v[i] = mul(v[j].v[i], g.v[i]);
+                }
+            RK_EACH
+                RK_PAIR u[j].v[i] = fma(v[j].v[i], b, u[j].v[i]);
+        }
+        RK_EACH
+            put8<R, FULL>(u_out + j * apart * (int)sizeof(R), u[j], live && (f & kNormU) ? cols[j] : none, p.wide & kNormWideU);
         u_out += p.u.step;
         if (f & kNormPre) {
-            row_stats<FULL, GENERAL>(p, team, f & kNormPreLayer, p.pre_eps, q.n, u, m1, r1);
+            row_stats<FULL, GENERAL>(p, team, f & kNormPreLayer, p.pre_eps, cols, u, m1, r1);
             const f2 r = both(r1);
-            RK_PAIR u.v[i] = GENERAL ? fma(mul(u.v[i], r), w1.v[i], b1.v[i]) : mul(mul(u.v[i], r), w1.v[i]);
+            RK_EACH
+                RK_PAIR u[j].v[i] = GENERAL ? fma(mul(u[j].v[i], r), w1[j].v[i], b1[j].v[i]) : mul(mul(u[j].v[i], r), w1[j].v[i]);
         }
-        put8<A, FULL>(h_out, u, f & kNormH ? n : Span{0, 0}, p.wide & kNormWideH);
+        RK_EACH
+            put8<A, FULL>(h_out + j * apart * (int)sizeof(A), u[j], live && (f & kNormH) ? cols[j] : none, p.wide & kNormWideH);
         h_out += p.h.step;
-        if (keeps && n.hi > 0)
+        if (keeps && live && q.n.hi > 0)
             p.stats[q.row + k * q.step] = make_float4(m2, r2, m1, r1);
         ring.used();
     }
@@ -901,21 +932,17 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
 // ----------------------------------------------------------- sums over rows
 
 constexpr int kJoinRows = 32;       // rows of partial sums read at a time, by 32 columns
+constexpr int kJoinThreads = 32 * kJoinRows;
 
-// Column blockIdx.x * 32 + x of `count` partial rows, `stride` apart, in thread row
-// 0: a fixed tree.
-__device__ __forceinline__ float join_column(const float *part, int64_t count, int64_t stride, bool live, float (&red)[kJoinRows][33])
+// The block's total of its threads' `t` by column (threadIdx.x % 32): a fixed tree;
+// that of column y in every lane of warp y.
+__device__ __forceinline__ float join_rows(float t, float (&red)[kJoinRows][33])
 {
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    float t = 0.f;
-    if (live)
-#pragma unroll 8
-        for (int64_t i = y; i < count; i += kJoinRows)
-            t += __ldcg(part + i * stride);
     __syncthreads();
     red[y][x] = t;
     __syncthreads();
-    return warp_sum(red[x][y]);     // of column y, in every lane
+    return warp_sum(red[x][y]);
 }
 
 template <typename A> __device__ __forceinline__ void store_as(void *p, bool f32, int64_t i, float v)
@@ -928,13 +955,14 @@ template <typename A> __device__ __forceinline__ void store_as(void *p, bool f32
 
 // blockIdx.y below p.sums: a weight's or bias's gradient; beyond: gates whose rows
 // several groups share.
-template <typename A> __global__ void __launch_bounds__(32 * kJoinRows) rikfad_norm_join_kernel(const __grid_constant__ NormParams p)
+template <typename A> __global__ void __launch_bounds__(kJoinThreads) rikfad_norm_join_kernel(const __grid_constant__ NormParams p)
 {
     __shared__ float red[kJoinRows][33];
     wait_for_predecessor();
     allow_successor_launch();
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + x, out = (int64_t)blockIdx.x * 32 + y;
+    const bool writes = x == 0 && out < p.cols;
     if ((int)blockIdx.y < p.sums) {
         void *const each[4] = {p.dpre_weight, p.dpost_weight, p.dpre_bias, p.dpost_bias};
         int at = blockIdx.y;
@@ -942,43 +970,41 @@ template <typename A> __global__ void __launch_bounds__(32 * kJoinRows) rikfad_n
         for (int i = 0; i < 4; ++i)
             if (each[i] && at-- == 0)
                 dst = each[i];
-        const float t = join_column(p.sum_part + (int64_t)blockIdx.y * p.ctas * p.cols + c, p.ctas, p.cols, c < p.cols, red);
-        if (x == 0 && out < p.cols)
+        const float *part = p.sum_part + (int64_t)blockIdx.y * p.ctas * p.cols + c;
+        float t = 0.f;
+        if (c < p.cols)
+#pragma unroll 16
+            for (int i = y; i < p.ctas; i += kJoinRows)
+                t += __ldcg(part + (int64_t)i * p.cols);
+        t = join_rows(t, red);
+        if (writes)
             store_as<A>(dst, p.flags & kNormParamF32, out, t);
         return;
     }
     const int64_t gates = p.rows / p.gate_rows, workers = (int64_t)(p.ctas / p.classes) * p.row_groups;   // of a class
     for (int64_t g = blockIdx.y - p.sums; g < gates; g += gridDim.y - p.sums) {
         const int64_t begin = g * p.gate_rows, end = begin + p.gate_rows;
+        // Thread row y takes every (kJoinRows / classes)-th worker of class y % classes:
+        // the class's rows of the gate are [i0, i1] of its own.
+        const int first = y % p.classes;
+        const int64_t rows = class_rows(p, first);
+        const int64_t i0 = begin <= first ? 0 : (begin - first + p.classes - 1) / p.classes;
+        const int64_t i1 = end - 1 < first ? -1 : (end - 1 - first) / p.classes;
         float t = 0.f;
-        bool done = false;
-        for (int first = 0; first < p.classes; ++first) {
-            // the class's rows of the gate, [i0, i1] of its own, and their workers
-            const int64_t rows = class_rows(p, first);
-            const int64_t i0 = begin <= first ? 0 : (begin - first + p.classes - 1) / p.classes;
-            const int64_t i1 = end - 1 < first ? -1 : (end - 1 - first) / p.classes;
-            if (i1 < i0)
-                continue;
+        if (i0 <= i1) {
             const int64_t w0 = ((i0 + 1) * workers - 1) / rows, w1 = ((i1 + 1) * workers - 1) / rows;
-            if (p.classes == 1 && w0 == w1) {
-                done = true;        // written by its only worker
-                break;
-            }
+            if (p.classes == 1 && w0 == w1)
+                continue;           // written by its only worker
             if (c < p.cols)
-                for (int64_t w = w0 + y; w <= w1; w += kJoinRows) {
+                for (int64_t w = w0 + y / p.classes; w <= w1; w += kJoinRows / p.classes) {
                     const int64_t row = first + p.classes * worker_begin(rows, w, workers);     // the worker's first
-                    // block (w / row_groups) of the class has number (w / row_groups) classes + first
+                    // block b of the class has number b classes + first
                     const int64_t worker = (w / p.row_groups * p.classes + first) * p.row_groups + w % p.row_groups;
                     t += __ldcg(p.gate_part + (2 * worker + (row / p.gate_rows == g ? 0 : 1)) * p.cols + c);
                 }
         }
-        if (done)
-            continue;
-        __syncthreads();
-        red[y][x] = t;
-        __syncthreads();
-        t = warp_sum(red[x][y]);
-        if (x == 0 && out < p.cols)
+        t = join_rows(t, red);
+        if (writes)
             store_as<A>(p.dgate.data, p.flags & kNormGateF32, g * p.dgate.stride + out, t);
     }
 }
@@ -1007,37 +1033,49 @@ template <typename K> cudaError_t launch_clustered(K kernel, const NormParams &n
     return cudaLaunchKernelEx(&cfg, kernel, n);
 }
 
-template <typename A, typename R, bool FULL, bool POST, bool GENERAL>
-cudaError_t launch_rows(const NormParams &n, bool backward, cudaStream_t s)
+template <typename A, typename R, bool FULL, bool POST, bool GENERAL> cudaError_t launch_forward(const NormParams &n, cudaStream_t s)
 {
-    if (!backward)
-        return n.flags & kNormSharedGate ? launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, true>, n, s)
-                                         : launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, false>, n, s);
+    if (n.flags & kNormSharedGate)
+        return launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, true, 1>, n, s);
+    return n.vectors == 1 ? launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, false, 1>, n, s)
+                          : launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, false, 2>, n, s);
+}
+
+template <typename A, typename R, bool FULL, bool POST, bool GENERAL> cudaError_t launch_backward(const NormParams &n, cudaStream_t s)
+{
     if (n.flags & kNormSharedGate)
         return launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 1, true>, n, s);
-    if (n.vectors == 1)
-        return launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 1, false>, n, s);
-    return launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 2, false>, n, s);
+    return n.vectors == 1 ? launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 1, false>, n, s)
+                          : launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 2, false>, n, s);
 }
 
-template <typename A, typename R, bool FULL> cudaError_t launch_rows(const NormParams &n, bool backward, cudaStream_t s)
+// The kernels of one pair of types; a translation unit instantiates one of the two.
+template <typename A, typename R> cudaError_t norm_forward(const NormParams &n, cudaStream_t s)
 {
-    if (n.flags & kNormPost)
-        return n.general ? launch_rows<A, R, FULL, true, true>(n, backward, s) : launch_rows<A, R, FULL, true, false>(n, backward, s);
-    return n.general ? launch_rows<A, R, FULL, false, true>(n, backward, s) : launch_rows<A, R, FULL, false, false>(n, backward, s);
+    const bool post = n.flags & kNormPost;
+    if (n.full)
+        return post ? (n.general ? launch_forward<A, R, true, true, true>(n, s) : launch_forward<A, R, true, true, false>(n, s))
+                    : (n.general ? launch_forward<A, R, true, false, true>(n, s) : launch_forward<A, R, true, false, false>(n, s));
+    return post ? (n.general ? launch_forward<A, R, false, true, true>(n, s) : launch_forward<A, R, false, true, false>(n, s))
+                : (n.general ? launch_forward<A, R, false, false, true>(n, s) : launch_forward<A, R, false, false, false>(n, s));
 }
 
-template <typename A, typename R> cudaError_t launch_norm(const NormParams &n, bool backward, cudaStream_t s)
+template <typename A, typename R> cudaError_t norm_backward(const NormParams &n, cudaStream_t s)
 {
-    const cudaError_t e = n.full ? launch_rows<A, R, true>(n, backward, s) : launch_rows<A, R, false>(n, backward, s);
-    if (!backward)
-        return e;
+    const bool post = n.flags & kNormPost;
+    cudaError_t e;
+    if (n.full)
+        e = post ? (n.general ? launch_backward<A, R, true, true, true>(n, s) : launch_backward<A, R, true, true, false>(n, s))
+                 : (n.general ? launch_backward<A, R, true, false, true>(n, s) : launch_backward<A, R, true, false, false>(n, s));
+    else
+        e = post ? (n.general ? launch_backward<A, R, false, true, true>(n, s) : launch_backward<A, R, false, true, false>(n, s))
+                 : (n.general ? launch_backward<A, R, false, false, true>(n, s) : launch_backward<A, R, false, false, false>(n, s));
     const bool shared_gate = n.dgate.data && n.gate_rows > 1;
     if (e != cudaSuccess || (n.sums == 0 && !shared_gate))
         return e;
     const int64_t gates = shared_gate ? n.rows / n.gate_rows : 0;
     const dim3 grid((unsigned)((n.cols + 31) / 32), (unsigned)(n.sums + (gates < 1024 ? gates : 1024)));
-    return launch_chained(rikfad_norm_join_kernel<A>, grid, 32 * kJoinRows, 0, s, n);
+    return launch_chained(rikfad_norm_join_kernel<A>, grid, kJoinThreads, 0, s, n);
 }
 
 }  // namespace rikfad
