@@ -190,6 +190,49 @@ def test_many_rows(rows, gate_rows, gate):
     run(op, _inputs(rows, 96, "bf16", post="rms", pre="layer", gate=gate, gate_rows=gate_rows), gate_rows)
 
 
+@pytest.mark.parametrize("rows,gate_rows", [(1400, 1400), (1400, 700), (1400, 28), (1400, 7), (1398, 3), (1398, 1), (40, 20)])
+@pytest.mark.parametrize("cols", [37, 129, 1001, 1002, 1004, 2500])
+@pytest.mark.parametrize("gate", ["rows", "shared"])
+def test_odd_widths_and_gates(rows, gate_rows, cols, gate):
+    """Rows that start anywhere, with sums over the rows of gates that last short and long."""
+    if gate == "rows":
+        gate_rows = 1
+    op = ResidualNorm(cols, post="rms", pre="layer")
+    run(op, _inputs(rows, cols, "f16", "f32", post="rms", pre="layer", gate=gate, gate_rows=gate_rows), gate_rows)
+
+
+@pytest.mark.parametrize("cols", [129, 1001, 4104, 9001, 20003])
+def test_odd_widths_in_wider_rows(cols):
+    """Row strides that drift by the same number of elements, and by different ones."""
+    op = ResidualNorm(cols, post="layer", pre="rms")
+    for pads in ((3, 3, 3, 3, 3), (0, 8, 16, 0, 8), (0, 1, 2, 3, 4)):
+        t = _inputs(21, cols, "bf16", post="layer", pre="rms", gate="rows", bias=True)
+        for k, pad in zip(("x", "z", "gate", "du", "dh"), pads):
+            wide = torch.full((21, cols + pad), float("nan"), dtype=t[k].dtype, device="cuda")
+            wide[:, :cols] = t[k]
+            t[k] = wide[:, :cols]
+        run(op, t)
+
+
+@pytest.mark.parametrize("cols", [72, 1001])
+def test_a_shared_gate_without_its_gradient(cols):
+    """Through the C entry: dgate and other outputs may be left out."""
+    from paper_2609_30342_gb300 import layers
+    op = ResidualNorm(cols, post="rms", pre="rms")
+    t = _inputs(60, cols, "bf16", gate="shared", gate_rows=20)
+    weights = {k: t[k] for k in NAMES}
+    _, _, stats = op.forward(t["x"], t["z"], **weights)
+    full = op.backward(t["du"], t["dh"], t["x"], t["z"], stats=stats, **weights)
+    head = op._inputs(t["x"], t["z"], t["gate"], tuple(t[k] for k in NAMES[1:]), None)[0]
+    dz = torch.zeros_like(t["z"])
+    block = layers._NORM.pack(*head, 0, 0, 0, 0, stats.data_ptr(), t["du"].data_ptr(), cols, t["dh"].data_ptr(), cols,
+                              0, 0, dz.data_ptr(), cols, 0, 0, 0, 0, 0, 0, 0, 0)
+    assert rikfad.lib().rikfad_residual_norm_workspace(block) == 0
+    assert rikfad.lib().rikfad_residual_norm_backward(block, torch.cuda.current_stream().cuda_stream) == rikfad.OK
+    torch.cuda.synchronize()
+    assert torch.equal(dz, full.z)
+
+
 @pytest.mark.parametrize("pre", KINDS)
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_without_a_branch(pre, dtype):
