@@ -16,6 +16,7 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <cstring>
 #include <new>
 #include <string>
 #include <vector>
@@ -358,12 +359,8 @@ struct rikfad_clip_s {
     std::vector<Part> parts;
     std::vector<const void *> seen_grad;    // addresses that passed check_address
     std::vector<void *> seen_out;
-    Segment *d_segments = nullptr;
-    int32_t *d_block_segment = nullptr;
-    double *d_partial = nullptr;
-    double *d_tensor_sum = nullptr;
-    unsigned int *d_tensor_done = nullptr;
-    ClipResult *d_result = nullptr;
+    void *memory = nullptr;                 // the plan and what the kernels leave in it, one allocation
+    ClipParams params{};                    // pointers into it
     size_t workspace = 0;
 };
 
@@ -371,24 +368,16 @@ namespace {
 
 void release(rikfad_clip c)
 {
-    for (void *p : {(void *)c->d_segments, (void *)c->d_block_segment, (void *)c->d_partial,
-                    (void *)c->d_tensor_sum, (void *)c->d_tensor_done, (void *)c->d_result})
-        counted_free(p);
+    counted_free(c->memory);
     delete c;
 }
 
-template <typename T> int allocate(rikfad_clip c, T **dst, size_t count, const T *src)
+// Where `count` elements of T go in an image of the plan's memory, 16-byte aligned.
+template <typename T> size_t place(size_t &bytes, size_t count)
 {
-    const size_t bytes = sizeof(T) * std::max<size_t>(count, 1);
-    cudaError_t e = counted_malloc((void **)dst, bytes);
-    if (e == cudaErrorMemoryAllocation)
-        return report_error(RIKFAD_ERR_OOM, "cudaMalloc of a clipping plan failed: out of memory");
-    if (e != cudaSuccess)
-        return report_cuda(e, "cudaMalloc of a clipping plan");
-    c->workspace += bytes;
-    if (src && count && (e = cudaMemcpy(*dst, src, sizeof(T) * count, cudaMemcpyHostToDevice)) != cudaSuccess)
-        return report_cuda(e, "cudaMemcpy of a clipping plan");
-    return RIKFAD_OK;
+    const size_t at = bytes;
+    bytes += (sizeof(T) * count + 15) / 16 * 16;
+    return at;
 }
 
 // Cuts tensors [t0, t1) into at most `most` shares of equal size.
@@ -454,16 +443,35 @@ int create(rikfad_clip c, const int64_t *numel, const int *grad_dtype, const int
     }
     c->blocks = (int)block_segment.size();
     block_segment.push_back((int32_t)segments.size());
-    int rc = allocate(c, &c->d_segments, segments.size(), segments.data());
-    if (!rc) rc = allocate(c, &c->d_block_segment, block_segment.size(), block_segment.data());
-    if (!rc) rc = allocate<double>(c, &c->d_partial, segments.size(), nullptr);
-    const std::vector<double> zeros(ntensors, 0.0);
-    if (!rc) rc = allocate(c, &c->d_tensor_sum, zeros.size(), zeros.data());
-    const std::vector<unsigned int> none_done(ntensors, 0u);
-    if (!rc) rc = allocate(c, &c->d_tensor_done, none_done.size(), none_done.data());
-    const ClipResult none = {1.f, 0u};
-    if (!rc) rc = allocate(c, &c->d_result, 1, &none);
-    return rc;
+    size_t bytes = 0;
+    const size_t at_segments = place<Segment>(bytes, segments.size());
+    const size_t at_blocks = place<int32_t>(bytes, block_segment.size());
+    const size_t at_partial = place<double>(bytes, segments.size());
+    const size_t at_sum = place<double>(bytes, ntensors);
+    const size_t at_done = place<unsigned int>(bytes, ntensors);
+    const size_t at_result = place<ClipResult>(bytes, 1);
+    std::vector<char> image(bytes, 0);          // sums and counters start at zero
+    if (!segments.empty())
+        std::memcpy(&image[at_segments], segments.data(), sizeof(Segment) * segments.size());
+    std::memcpy(&image[at_blocks], block_segment.data(), sizeof(int32_t) * block_segment.size());
+    e = counted_malloc(&c->memory, bytes);
+    if (e == cudaErrorMemoryAllocation)
+        return report_error(RIKFAD_ERR_OOM, "cudaMalloc of a clipping plan failed: out of memory");
+    if (e == cudaSuccess)
+        e = cudaMemcpy(c->memory, image.data(), bytes, cudaMemcpyHostToDevice);
+    if (e != cudaSuccess)
+        return report_cuda(e, "memory of a clipping plan");
+    c->workspace = bytes;
+    char *const base = static_cast<char *>(c->memory);
+    c->params.segments = reinterpret_cast<const Segment *>(base + at_segments);
+    c->params.block_segment = reinterpret_cast<const int32_t *>(base + at_blocks);
+    c->params.partial = reinterpret_cast<double *>(base + at_partial);
+    c->params.tensor_sum = reinterpret_cast<double *>(base + at_sum);
+    c->params.tensor_done = reinterpret_cast<unsigned int *>(base + at_done);
+    c->params.result = reinterpret_cast<ClipResult *>(base + at_result);
+    c->params.ntensors = ntensors;
+    c->params.total_blocks = c->blocks;
+    return RIKFAD_OK;
 }
 
 template <int CAP> int launch(rikfad_clip c, const Part &part, const ClipParams &a, const void *const *grad,
@@ -599,15 +607,7 @@ RIKFAD_API int rikfad_clip_run(rikfad_clip c, const void *const *grad, void *con
     if ((e = cudaPeekAtLastError()) != cudaSuccess)
         return report_cuda(e, "earlier CUDA error");
     const cudaStream_t s = (cudaStream_t)stream;
-    ClipParams a{};
-    a.segments = c->d_segments;
-    a.block_segment = c->d_block_segment;
-    a.partial = c->d_partial;
-    a.result = c->d_result;
-    a.tensor_sum = c->d_tensor_sum;
-    a.tensor_done = c->d_tensor_done;
-    a.ntensors = c->ntensors;
-    a.total_blocks = c->blocks;
+    ClipParams a = c->params;
     a.max_norm = max_norm;
     a.norms = norms;
     a.total = total;

@@ -176,12 +176,11 @@ int row_threads(int vectors, int v)
 
 // Rows of odd widths: if every tensor's rows drift by the same number of elements
 // from 16 bytes, from an aligned start, rows that drift equally far make a class
-// with aligned vectors.  Otherwise (and where a shared gate's sums over rows would
-// need too many partial rows) each tensor's own rows decide.
-void drifting(NormParams &n, const rikfad_residual_norm *p)
+// with aligned vectors.  0: there is no such drift, each tensor's own rows decide.
+int drift_of(const NormParams &n)
 {
-    if (n.wide == kNormWideAll || p->rows <= 1)
-        return;
+    if (n.wide == kNormWideAll || n.rows <= 1)
+        return 0;
     const NormRows *const all[] = {&n.x, &n.z, &n.u, &n.h, &n.du, &n.dh, &n.dx, &n.dz,
                                    n.gate_rows > 1 ? nullptr : &n.gate, n.gate_rows > 1 ? nullptr : &n.dgate};
     int drift = -1;
@@ -189,27 +188,29 @@ void drifting(NormParams &n, const rikfad_residual_norm *p)
         if (t == nullptr || t->data == nullptr)
             continue;
         if ((uintptr_t)t->data % 16 || (drift >= 0 && t->stride % 8 != drift))
-            return;
+            return 0;
         drift = (int)(t->stride % 8);
     }
-    if (drift <= 0)
-        return;
+    return std::max(drift, 0);
+}
+
+void set_drift(NormParams &n, int drift)
+{
     n.drift = drift;
-    n.classes = drift % 4 == 0 ? 2 : drift % 2 == 0 ? 4 : 8;
-    n.wide |= kNormWideAll & ~(n.gate_rows > 1 ? kNormWideGate | kNormWideDgate : 0u);
-    if (n.gate_rows > 1)
+    n.classes = drift == 0 ? 1 : drift % 4 == 0 ? 2 : drift % 2 == 0 ? 4 : 8;
+    if (drift == 0)
+        return;
+    n.wide = kNormWideAll;
+    if (n.gate_rows > 1)            // their rows are others than the rest's
         n.wide &= ~(kNormWideGate | kNormWideDgate);
 }
 
 // Vectors of a thread, threads of a row, columns of a block and blocks of a
 // cluster, from the width; how far a thread's rows are apart.  A block has at most
 // `most_threads` threads of `most_vectors` vectors each.
-void shape(NormParams &n, const rikfad_residual_norm *p, int most_vectors, int most_threads, bool classes = true)
+void shape(NormParams &n, const rikfad_residual_norm *p, int most_vectors, int most_threads, int drift)
 {
-    n.classes = 1;
-    n.drift = 0;
-    if (classes)
-        drifting(n, p);
+    set_drift(n, drift);
     const int vectors = (n.cols + (n.classes > 1 ? 7 : 0) + 7) / 8;     // a shifted row may begin within one
     n.cluster = 1;
     while ((vectors + n.cluster - 1) / n.cluster > most_threads * most_vectors)
@@ -263,7 +264,7 @@ void forward_shape(const rikfad_residual_norm *p, NormParams &n)
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
     n.units = r + a + (p->gate.data && p->gate_rows < kNormHeldRows ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
     const int most = n.flags & kNormSharedGate ? 1 : 2;
-    shape(n, p, most, kNormMaxThreads / most);
+    shape(n, p, most, kNormMaxThreads / most, drift_of(n));
     grid(n, n.vectors == 1 ? kNormForwardThreads<1> : kNormForwardThreads<2>);
 }
 
@@ -273,14 +274,14 @@ struct Workspace {
 
 // Partial sums: one row of each kind for every cluster, and two of the gate's for
 // every group whose rows share gates with others.
-Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n, bool classes = true)
+Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n, int drift)
 {
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
     n.units = 2 * a + 2 * r + (p->gate.data && p->gate_rows < kNormHeldRows ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
     const bool gated = n.flags & kNormSharedGate, shared = gated && p->dgate.data, post = n.flags & kNormPost;
     const int one = post && n.general ? kNormBackwardThreads<true, true, 1> : kNormBackwardThreads<false, false, 1>;
     const int two = !post ? kNormBackwardThreads<false, false, 2> : n.general ? kNormBackwardThreads<true, true, 2> : kNormBackwardThreads<true, false, 2>;
-    shape(n, p, gated ? 1 : 2, gated ? one : kNormMaxThreads / 2, classes);
+    shape(n, p, gated ? 1 : 2, gated ? one : kNormMaxThreads / 2, drift);
     grid(n, n.vectors == 1 ? one : two);
     n.sums = 0;
     for (const void *v : {p->dpre_weight, p->dpost_weight, p->dpre_bias, p->dpost_bias})
@@ -292,7 +293,7 @@ Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n, bool clas
         const int64_t rows = (p->rows + n.classes - 1) / n.classes;
         if ((rows + workers - 1) / workers * n.classes > p->gate_rows) {
             NormParams again = params(p, true);
-            return backward_shape(p, n = again, false);
+            return backward_shape(p, n = again, 0);
         }
     }
     Workspace w;
@@ -325,9 +326,14 @@ RIKFAD_API size_t rikfad_residual_norm_workspace(const rikfad_residual_norm *p)
     report_error(RIKFAD_OK, "");
     if (p->rows == 0)
         return 0;
-    NormParams n = params(p, true);
-    const Workspace w = backward_shape(p, n);
-    return (size_t)(w.weights + w.gates) * sizeof(float);
+    // enough for rows that start anywhere
+    int64_t floats = 0;
+    for (const int drift : {0, 1, 2, 4}) {
+        NormParams n = params(p, true);
+        const Workspace w = backward_shape(p, n, drift);
+        floats = std::max(floats, w.weights + w.gates);
+    }
+    return (size_t)floats * sizeof(float);
 }
 
 RIKFAD_API int rikfad_residual_norm_forward(const rikfad_residual_norm *p, void *stream)
@@ -380,7 +386,7 @@ RIKFAD_API int rikfad_residual_norm_backward(const rikfad_residual_norm *p, void
     if (p->rows > 0 && p->stats == nullptr)
         return bad("stats is NULL");
     NormParams n = params(p, true);
-    const Workspace w = p->rows > 0 ? backward_shape(p, n) : Workspace();
+    const Workspace w = p->rows > 0 ? backward_shape(p, n, drift_of(n)) : Workspace();
     const int64_t floats = w.weights + w.gates;
     if (p->workspace_bytes / sizeof(float) < (size_t)floats || (floats > 0 && p->workspace == nullptr))
         return bad("the workspace is smaller than rikfad_residual_norm_workspace");
