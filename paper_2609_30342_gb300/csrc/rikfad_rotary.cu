@@ -24,6 +24,7 @@ namespace {
 
 constexpr int kRotaryThreads = 256;
 constexpr int kSms = 152;
+constexpr int kRotaryBlocksPerSm = 5;
 constexpr int kTableFloats = 8192;      // cosines and sines of a tile of tokens: 32 KB at most
 
 struct RotaryParams {
@@ -44,8 +45,61 @@ template <> struct Word<16> { using type = uint4; };
 
 template <typename T, int V> union Vec {
     typename Word<V * sizeof(T)>::type word;
+    uint32_t pairs[V * sizeof(T) >= 4 ? V * sizeof(T) / 4 : 1];
     T v[V];
     __device__ __forceinline__ Vec() {}
+};
+
+template <typename T, int V> __device__ __forceinline__ void widen(const Vec<T, V> &r, float (&f)[V])
+{
+    if constexpr (sizeof(T) == 2 && V > 1) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i)
+            unpack2(r.pairs[i], f[2 * i], f[2 * i + 1], T());
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            f[i] = to_f32(r.v[i]);
+    }
+}
+
+template <typename T, int V> __device__ __forceinline__ void narrow(const float (&f)[V], Vec<T, V> &r)
+{
+    if constexpr (sizeof(T) == 2 && V > 1) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i)
+            r.pairs[i] = pack2(f[2 * i], f[2 * i + 1], T());
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            r.v[i] = from_f32<T>(f[i]);
+    }
+}
+
+// Where a thread is in its tile, and how it goes on: divisions once, not per unit.
+struct Walk {
+    int slot, head, unit;       // token within the tile, head of both lists, unit of the head
+    int slots, heads, units;    // of one step
+
+    __device__ __forceinline__ Walk(const RotaryParams &p, int w, int step)
+    {
+        unit = w % p.units;
+        head = w / p.units % p.heads;
+        slot = w / p.units / p.heads;
+        units = step % p.units;
+        heads = step / p.units % p.heads;
+        slots = step / p.units / p.heads;
+    }
+    __device__ __forceinline__ void next(const RotaryParams &p)
+    {
+        unit += units;
+        const int carry = unit >= p.units;
+        unit -= carry ? p.units : 0;
+        head += heads + carry;
+        const int over = head >= p.heads;
+        head -= over ? p.heads : 0;
+        slot += slots + over;
+    }
 };
 
 // A unit is V pairs of one head, as two vectors of V elements: in the half layout
@@ -58,25 +112,22 @@ template <typename T, int V> struct Unit {
     int pair;               // first pair, in the tile's table; < 0: copy
     Vec<T, V> a, b;
 
-    __device__ __forceinline__ void locate(const RotaryParams &p, int64_t token0, int w)
+    __device__ __forceinline__ void locate(const RotaryParams &p, int64_t token0, const Walk &w)
     {
-        const int u = w % p.units, rest = w / p.units;
-        int head = rest % p.heads;
-        const int slot = rest / p.heads;                        // token within the tile
-        const int64_t at = token0 + slot;
+        const int64_t at = token0 + w.slot;
         const int64_t batch = p.d.batch == 1 ? 0 : at / p.d.tokens, token = at - batch * p.d.tokens;
-        const int list = head >= (int)p.d.lists[0].heads;
-        head -= list ? (int)p.d.lists[0].heads : 0;
+        const int list = w.head >= (int)p.d.lists[0].heads;
+        const int head = w.head - (list ? (int)p.d.lists[0].heads : 0);
         const rikfad_rotary_heads &l = p.d.lists[list];
         src = static_cast<const T *>(l.src) + batch * l.src_batch + token * l.src_token + head * l.src_head;
         dst = static_cast<T *>(l.dst) + batch * l.dst_batch + token * l.dst_token + head * l.dst_head;
-        if (u < p.turn_units) {
+        if (w.unit < p.turn_units) {
             const bool half = p.d.layout == RIKFAD_ROTARY_HALF;
-            first = half ? u * V : 2 * u * V;
+            first = half ? w.unit * V : 2 * w.unit * V;
             second = first + (half ? p.d.rotary_dim / 2 : V);
-            pair = slot * (p.d.rotary_dim / 2) + u * V;
+            pair = w.slot * (p.d.rotary_dim / 2) + w.unit * V;
         } else {
-            first = p.d.rotary_dim + 2 * (u - p.turn_units) * V;
+            first = p.d.rotary_dim + 2 * (w.unit - p.turn_units) * V;
             second = first + V < p.d.head_dim ? first + V : -1;
             pair = -1;
         }
@@ -93,17 +144,30 @@ template <typename T, int V> struct Unit {
     {
         if (pair < 0)
             return;
-        const bool half = p.d.layout == RIKFAD_ROTARY_HALF;
+        float x[V], y[V];
+        widen(a, x);
+        widen(b, y);
+        if (p.d.layout == RIKFAD_ROTARY_HALF) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float2 cs = table[pair + e];
-            // interleaved: pair e is elements 2 e and 2 e + 1 of the two vectors together
-            T &x = half ? a.v[e] : (2 * e < V ? a.v[2 * e % V] : b.v[2 * e % V]);
-            T &y = half ? b.v[e] : (2 * e + 1 < V ? a.v[(2 * e + 1) % V] : b.v[(2 * e + 1) % V]);
-            const float fx = to_f32(x), fy = to_f32(y);
-            x = from_f32<T>(fmaf(fx, cs.x, -fy * cs.y));
-            y = from_f32<T>(fmaf(fy, cs.x, fx * cs.y));
+            for (int e = 0; e < V; ++e)
+                turn(x[e], y[e], table[pair + e]);
+        } else {                // pair e is elements 2 e and 2 e + 1 of the two vectors together
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float &even = 2 * e < V ? x[2 * e % V] : y[2 * e % V];
+                float &odd = 2 * e + 1 < V ? x[(2 * e + 1) % V] : y[(2 * e + 1) % V];
+                turn(even, odd, table[pair + e]);
+            }
         }
+        narrow(x, a);
+        narrow(y, b);
+    }
+
+    __device__ __forceinline__ static void turn(float &x, float &y, const float2 &cs)
+    {
+        const float u = x, v = y;
+        x = fmaf(u, cs.x, -v * cs.y);
+        y = fmaf(v, cs.x, u * cs.y);
     }
 
     __device__ __forceinline__ void store() const
@@ -126,10 +190,11 @@ __global__ void __launch_bounds__(kRotaryThreads) rikfad_rotary_kernel(const __g
     const int here = (int)min((int64_t)p.tile, tokens - token0);
     const int work = here * p.heads * p.units, step = kRotaryThreads * gridDim.y;
     int w = blockIdx.y * kRotaryThreads + threadIdx.x;
+    Walk walk(p, w, step);
     wait_for_predecessor();
     Unit<T, V> unit;
     if (w < work) {
-        unit.locate(p, token0, w);
+        unit.locate(p, token0, walk);
         unit.load();
     }
     const int pairs = p.d.rotary_dim / 2;
@@ -154,7 +219,8 @@ __global__ void __launch_bounds__(kRotaryThreads) rikfad_rotary_kernel(const __g
         Unit<T, V> next;
         w += step;
         if (w < work) {
-            next.locate(p, token0, w);
+            walk.next(p);
+            next.locate(p, token0, walk);
             next.load();
         }
         unit.turn(p, table);
@@ -235,9 +301,13 @@ template <typename T, int V> cudaError_t launch(RotaryParams p, cudaStream_t s)
     const int64_t per_token = (int64_t)p.heads * p.units, tokens = p.d.batch * p.d.tokens;
     if (per_token == 0 || tokens == 0)
         return cudaSuccess;
-    // About four units for each thread, within the table's size.
+    // Units of a thread: 2 to 16, so that a launch has a dozen rounds of blocks where it
+    // can (16384 tokens of 24 x 64: 45 us for two calls with 2, 77 with 16; 131072 tokens of
+    // 40 x 128: 448 us with 16, 530 with 2), within the table's size.
+    const int64_t share = tokens * per_token / ((int64_t)12 * kRotaryBlocksPerSm * kSms * kRotaryThreads);
+    const int64_t each = std::max<int64_t>(2, std::min<int64_t>(16, share));
     const int64_t most = pairs ? std::max(1, kTableFloats / 2 / pairs) : 1 << 10;
-    p.tile = (int32_t)std::max<int64_t>(1, std::min(most, 4 * kRotaryThreads / per_token));
+    p.tile = (int32_t)std::max<int64_t>(1, std::min(most, each * kRotaryThreads / per_token));
     // Few tokens: smaller tiles, then several blocks for a tile, until the SMs have work.
     while (p.tile > 1 && (tokens + p.tile - 1) / p.tile < 2 * kSms)
         p.tile /= 2;
