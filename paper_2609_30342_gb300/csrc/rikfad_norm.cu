@@ -249,6 +249,7 @@ void shape(NormParams &n, const rikfad_residual_norm *p, int most_vectors, int m
 // there are rows.
 void grid(NormParams &n, int threads_per_sm)
 {
+    n.threads_per_sm = threads_per_sm;
     const int by_registers = std::max(1, threads_per_sm / n.threads);
     const int64_t groups = (n.rows + n.row_groups - 1) / n.row_groups;
     const size_t stage = (size_t)n.threads * 16 * n.units * n.vectors;
@@ -278,11 +279,11 @@ Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n, int drift
 {
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
     n.units = 2 * a + 2 * r + (p->gate.data && p->gate_rows < kNormHeldRows ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
-    const bool gated = n.flags & kNormSharedGate, shared = gated && p->dgate.data, post = n.flags & kNormPost;
-    const int one = post && n.general ? kNormBackwardThreads<true, true, 1> : kNormBackwardThreads<false, false, 1>;
-    const int two = !post ? kNormBackwardThreads<false, false, 2> : n.general ? kNormBackwardThreads<true, true, 2> : kNormBackwardThreads<true, false, 2>;
-    shape(n, p, gated ? 1 : 2, gated ? one : kNormMaxThreads / 2, drift);
-    grid(n, n.vectors == 1 ? one : two);
+    const bool shared = (n.flags & kNormSharedGate) && p->dgate.data, post = n.flags & kNormPost;
+    const bool narrow = p->cols <= 8 * kNormGeneralThreads - 8;        // a shifted row may need one vector more
+    const int threads = post && n.general && narrow ? kNormGeneralThreads : kNormBackwardThreads;
+    shape(n, p, 1, threads, drift);
+    grid(n, threads);
     n.sums = 0;
     for (const void *v : {p->dpre_weight, p->dpost_weight, p->dpre_bias, p->dpost_bias})
         n.sums += v != nullptr;

@@ -8,16 +8,19 @@
 
 namespace rikfad {
 
-// A thread owns 8 neighbouring columns of a row, or up to three times 8 in the
-// backward pass.  A row is one to 32 lanes', then up to 16 warps' (a block's), then a
+// A thread owns 8 neighbouring columns of a row (two times 8 forward, where a row has
+// enough of them).  A row is one to 32 lanes', then up to 16 warps' (a block's), then a
 // cluster's of up to 8 blocks, which exchange their sums through distributed shared
 // memory.
 constexpr int kNormMaxThreads = 512;
 constexpr int kNormMaxWarps = kNormMaxThreads / 32;
 // Threads of an SM, by the registers that the kernels are given.
 template <int V> constexpr int kNormForwardThreads = V == 1 ? 768 : 512;
-template <bool POST, bool GENERAL, int V>
-constexpr int kNormBackwardThreads = V == 1 ? (POST && GENERAL ? 384 : 512) : !POST ? 384 : GENERAL ? 256 : 320;
+constexpr int kNormBackwardThreads = 512;
+// Backward with a post norm and layer norms or biases, rows of up to 384 threads: 168
+// registers instead of 128 (8192 x 1600: 91 us instead of 99; 4096 x 4096, two blocks a
+// row then: 189 us instead of 120).
+constexpr int kNormGeneralThreads = 384;
 constexpr int norm_registers(int threads) { return threads <= 256 ? 248 : 65536 / threads / 8 * 8; }
 constexpr int64_t kNormHeldRows = 16;           // rows of a gate from which it is kept in registers
 constexpr int kNormSms = 152;
@@ -92,6 +95,7 @@ struct NormParams {
     int32_t threads, lanes, row_groups;     // of a block; of a row within it; rows of a block at a time
     int32_t cluster, cta_cols;              // blocks of a row; columns of each
     int32_t ctas;                           // clusters of the launch
+    int32_t threads_per_sm;                 // by the kernel's registers
     int32_t units, stages;                  // 16-byte units of a vector; rows in flight and in use
     size_t smem;
     // backward: partial sums

@@ -660,37 +660,34 @@ __global__ void __maxnreg__((norm_registers(kNormForwardThreads<V>))) rikfad_nor
 // How far a block's columns are shifted (Place).
 __device__ __forceinline__ int id_shift(const NormParams &p) { return (blockIdx.x / p.cluster) % p.classes * p.drift % 8; }
 
-// Elements n of one partial row of a sum over rows, from the block's groups in order.
-__device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, float *part, float *buffer, const Vec8 &acc, int off, const Span &n)
+// One partial row of a sum over rows, from the block's groups in order.
+__device__ __forceinline__ void store_sum(const NormParams &p, const Place &q, float *part, float *buffer, const Vec8 &acc)
 {
     float *out = part + (int64_t)(blockIdx.x / p.cluster) * p.cols;
     if (p.row_groups == 1) {
-        put8<float, false>(out + q.col + off, acc, n, false);
+        put8<float, false>(out + q.col, acc, q.n, false);
         return;
     }
-    // the vectors of all lanes, then those `off` columns on
     __syncthreads();
     const int group = threadIdx.x / p.lanes, width = p.lanes * 8;
-    if (n.hi > 0)
+    if (q.n.hi > 0)
         RK_PAIR *reinterpret_cast<f2 *>(buffer + group * width + (threadIdx.x % p.lanes) * 8 + 2 * i) = acc.v[i];
     __syncthreads();
-    // column `first` + c is at c
-    const int first = off - id_shift(p);
-    for (int c = threadIdx.x; c < width; c += p.threads) {
-        if (first + c < 0 || first + c >= p.cols)
-            continue;
+    const int shift = id_shift(p);          // column c is at c + shift
+    for (int c = threadIdx.x; c < p.cols; c += p.threads) {
         float t = 0.f;
         for (int g = 0; g < p.row_groups; ++g)
-            t += buffer[g * width + c];
-        out[first + c] = t;
+            t += buffer[g * width + c + shift];
+        out[c] = t;
     }
 }
 
-// V vectors of 8 columns a thread, `lanes` vectors apart.  With V > 1 a row's fixed
-// work (addresses, branches, sums) is shared by 8 V elements; a gate shared by rows is
-// summed (SHARED) with V = 1 only.
-template <typename A, typename R, bool FULL, bool POST, bool GENERAL, int V, bool SHARED>
-__global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, V>))) rikfad_norm_backward_kernel(const __grid_constant__ NormParams p)
+// One vector of 8 columns a thread: with two, the accumulators, weights and elements
+// of both do not fit the registers of two blocks an SM (32768 x 4096: 631 us with the
+// weights read for every row and the branch formed twice, 456 so).  SHARED: a gate
+// serves several rows.  THREADS: of an SM, by the registers that the kernel is given.
+template <typename A, typename R, bool FULL, bool POST, bool GENERAL, bool SHARED, int THREADS>
+__global__ void __maxnreg__((norm_registers(THREADS))) rikfad_norm_backward_kernel(const __grid_constant__ NormParams p)
 {
     extern __shared__ uint4 stages[];
     __shared__ RowSums sums;
@@ -702,13 +699,10 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
     const int gate_bytes = f & kNormGateF32 ? 4 : (int)sizeof(A);
     // a vector's slots: x, z, dh, du, gate
     const uint32_t z_at = kUnits<R> * stride, dh_at = z_at + kUnits<A> * stride, du_at = dh_at + kUnits<A> * stride;
-    const uint32_t gate_at = du_at + kUnits<R> * stride, next_at = stride * p.units;
-    const int apart = p.lanes * 8;
-    Span cols[V];               // of each vector
-    RK_EACH cols[j] = q.span(j, apart);
+    const uint32_t gate_at = du_at + kUnits<R> * stride;
     const Span none{0, 0};
     const bool staged = gated && !(SHARED && (f & kNormGateHeld));      // else held in registers while it lasts
-    Ring ring(p, stages, V);
+    Ring ring(p, stages);
     Team team(p, sums);
     prepare(p, sums);
     const char *x = first_row(p.x, sizeof(R), q), *z = first_row(p.z, sizeof(A), q);
@@ -718,20 +712,14 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
     GateWalk<SHARED> gate(p, p.gate, gate_bytes, q);
     int left = q.count;         // rows to issue; the pointers stay on rows that exist
     auto issue = [&]() {
-        RK_EACH
-        {
-            // a vector that this thread lacks reads nowhere, from its first one's address
-            const Span n = left > 0 ? cols[j] : none;
-            const int off = cols[j].hi > 0 ? j * apart : 0;
-            const uint32_t to = ring.put + j * next_at;
-            stage8<R, FULL>(to, stride, x + off * (int)sizeof(R), n, p.wide & kNormWideX);
-            if (branch)
-                stage8<A, FULL>(to + z_at, stride, z + off * (int)sizeof(A), n, p.wide & kNormWideZ);
-            stage8<A, FULL>(to + dh_at, stride, dh + off * (int)sizeof(A), f & kNormDh ? n : none, p.wide & kNormWideDh);
-            stage8<R, FULL>(to + du_at, stride, du + off * (int)sizeof(R), f & kNormDu ? n : none, p.wide & kNormWideDu);
-            if (staged)
-                stage_gate<A, FULL>(p, to + gate_at, stride, gate.at + off * gate_bytes, n);
-        }
+        const Span n = left > 0 ? q.n : none;
+        stage8<R, FULL>(ring.put, stride, x, n, p.wide & kNormWideX);
+        if (branch)
+            stage8<A, FULL>(ring.put + z_at, stride, z, n, p.wide & kNormWideZ);
+        stage8<A, FULL>(ring.put + dh_at, stride, dh, f & kNormDh ? n : none, p.wide & kNormWideDh);
+        stage8<R, FULL>(ring.put + du_at, stride, du, f & kNormDu ? n : none, p.wide & kNormWideDu);
+        if (staged)
+            stage_gate<A, FULL>(p, ring.put + gate_at, stride, gate.at, n);
         if (--left > 0) {
             x += p.x.step;
             z += p.z.step;
@@ -742,8 +730,7 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
         }
         ring.issued();
     };
-    Vec8 dw1[V], dw2[V], db1[V], db2[V], dg = splat(0.f);
-    RK_EACH dw1[j] = dw2[j] = db1[j] = db2[j] = splat(0.f);
+    Vec8 dw1 = splat(0.f), dw2 = dw1, db1 = dw1, db2 = dw1, dg = dw1;
     // dgate: a row for every row, or the sum over the gate's
     GateWalk<SHARED> dgate(p, p.dgate, gate_bytes, q);
     bool gate_first = true;                     // the sum is of the group's first gate
@@ -751,131 +738,105 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
     auto gate_part = [&]() {
         put8<float, false>(p.gate_part + (2 * worker + (gate_first ? 0 : 1)) * p.cols + q.col, dg, q.n, false);
     };
-    auto put_gate = [&](const Vec8 &v, int j, const Span &n) {
+    auto put_gate = [&](const Vec8 &v, const Span &n) {
         if (f & kNormGateF32)
-            put8<float, FULL>(dgate.at + j * apart * 4, v, n, p.wide & kNormWideDgate);
+            put8<float, FULL>(dgate.at, v, n, p.wide & kNormWideDgate);
         else
-            put8<A, FULL>(dgate.at + j * apart * (int)sizeof(A), v, n, p.wide & kNormWideDgate);
+            put8<A, FULL>(dgate.at, v, n, p.wide & kNormWideDgate);
     };
     if (shared_gate && q.count == 0)            // a group without rows adds nothing to the gate it lies in
         gate_part();
     bool gate_whole = p.classes == 1 && dgate.into == 0;    // the sum began with the gate's first row
-    Vec8 held[V];
-    RK_EACH held[j] = splat(1.f);
+    Vec8 held = splat(1.f);
     for (int k = 0; k < p.stages - 1; ++k)
         issue();
-    Vec8 w2[V], w1[V], b2[V];
-    RK_EACH
-    {
-        w2[j] = param8<A>(p.post_weight, f & kNormParamF32, q.col + j * apart, cols[j], 1.f);
-        w1[j] = param8<A>(p.pre_weight, f & kNormParamF32, q.col + j * apart, cols[j], 1.f);
-        b2[j] = param8<A>(p.post_bias, f & kNormParamF32, q.col + j * apart, cols[j], 0.f);
-    }
+    const Vec8 w2 = param8<A>(p.post_weight, f & kNormParamF32, q.col, q.n, 1.f);
+    const Vec8 w1 = param8<A>(p.pre_weight, f & kNormParamF32, q.col, q.n, 1.f);
+    const Vec8 b2 = param8<A>(p.post_bias, f & kNormParamF32, q.col, q.n, 0.f);
     const f2 a = both(p.a), b = both(p.b);
     const float4 *stats = p.stats + q.row;
     float4 next = q.count > 0 ? *stats : make_float4(0.f, 0.f, 0.f, 0.f);
     // e becomes r (e - [mean e] - y mean(e y))
-    auto through_norm = [&](bool layer, float r, Vec8(&e)[V], const Vec8(&y)[V]) {
-        float t0 = 0.f, t1 = 0.f;
-        RK_EACH t0 += dot(e[j], y[j]);
+    auto through_norm = [&](bool layer, float r, Vec8 &e, const Vec8 &y) {
+        float t0, t1 = 0.f;
         if (GENERAL && layer) {
-            RK_EACH t1 += elements(e[j]);
-            float t[2] = {t0, t1};
+            float t[2] = {dot(e, y), elements(e)};
             team.sum(t);
             t0 = -t[0] * p.inv_cols;
             t1 = -t[1] * p.inv_cols;
         } else {
-            float t[1] = {t0};
+            float t[1] = {dot(e, y)};
             team.sum(t);
             t0 = -t[0] * p.inv_cols;
         }
-        const f2 my = both(t0), m = both(t1);
-        RK_EACH
-        {
-            // columns beyond the row's end stay zero: they add nothing to later sums
-            const f2 rr = both(cols[j].hi > 0 ? r : 0.f);
-            RK_PAIR e[j].v[i] = mul(GENERAL ? fma(y[j].v[i], my, add(e[j].v[i], m)) : fma(y[j].v[i], my, e[j].v[i]), rr);
-            if (!FULL)
-                cut(e[j], cols[j]);
-        }
+        // columns beyond the row's end stay zero: they add nothing to later sums
+        const f2 my = both(t0), m = both(t1), rr = both(q.n.hi > 0 ? r : 0.f);
+        RK_PAIR e.v[i] = mul(GENERAL ? fma(y.v[i], my, add(e.v[i], m)) : fma(y.v[i], my, e.v[i]), rr);
+        if (!FULL)
+            cut(e, q.n);
     };
     for (int k = 0; k < q.most; ++k) {
         issue();
         const bool live = k < q.count;
+        const Span n = live ? q.n : none;
         const float m2 = next.x, r2 = next.y, m1 = next.z, r1 = next.w;
         stats += q.step;
         next = k + 1 < q.count ? *stats : make_float4(0.f, 0.f, 0.f, 0.f);
         if (SHARED && gated && !staged) {
             if (gate.first)
-                RK_EACH held[j] = param8<A>(gate.at, f & kNormGateF32, j * apart, live ? cols[j] : none, 1.f);
+                held = param8<A>(gate.at, f & kNormGateF32, 0, n, 1.f);
             if (k + 1 < q.count)
                 gate.next(p, p.gate, q);
         }
         wait_copies(p.stages);
 
-        Vec8 e[V], y[V], y2[V], nn[V], g[V];
-        RK_EACH
-        {
-            e[j] = fetch8<A, FULL>(ring.get + j * next_at + dh_at, stride, cols[j]);       // the gradient of h, then of u
-            y[j] = fetch8<R, FULL>(ring.get + j * next_at, stride, cols[j]);
-            RK_PAIR y[j].v[i] = mul(y[j].v[i], a);
-        }
+        Vec8 e = fetch8<A, FULL>(ring.get + dh_at, stride, q.n);        // the gradient of h, then of u
+        Vec8 y = fetch8<R, FULL>(ring.get, stride, q.n), y2, nn, g;     // nn: n, g: b gate
+        RK_PAIR y.v[i] = mul(y.v[i], a);
         if (branch) {
-            RK_EACH
-            {
-                nn[j] = fetch8<A, FULL>(ring.get + j * next_at + z_at, stride, cols[j]);
-                if (POST) {
-                    const f2 minus = both(-m2 * r2), r = both(r2);
-                    RK_PAIR y2[j].v[i] = GENERAL ? mul(add(nn[j].v[i], both(-m2)), r) : mul(nn[j].v[i], r);
-                    RK_PAIR nn[j].v[i] = GENERAL ? fma(y2[j].v[i], w2[j].v[i], b2[j].v[i]) : mul(y2[j].v[i], w2[j].v[i]);
-                }
-                g[j] = splat(p.b);
+            nn = fetch8<A, FULL>(ring.get + z_at, stride, q.n);
+            if (POST) {
+                const f2 minus = both(-m2), r = both(r2);
+                RK_PAIR y2.v[i] = GENERAL ? mul(add(nn.v[i], minus), r) : mul(nn.v[i], r);
+                RK_PAIR nn.v[i] = GENERAL ? fma(y2.v[i], w2.v[i], b2.v[i]) : mul(y2.v[i], w2.v[i]);
             }
-            if (gated)
-                RK_EACH
-                {
-                    g[j] = !SHARED || staged ? fetch_gate<A, FULL>(p, ring.get + j * next_at + gate_at, stride, cols[j]) : held[j];
-                    RK_PAIR g[j].v[i] = mul(g[j].v[i], b);
-                }
-            RK_EACH
-                RK_PAIR y[j].v[i] = fma(nn[j].v[i], g[j].v[i], y[j].v[i]);
+            g = splat(p.b);
+            if (gated) {
+                g = !SHARED || staged ? fetch_gate<A, FULL>(p, ring.get + gate_at, stride, q.n) : held;
+                RK_PAIR g.v[i] = mul(g.v[i], b);
+            }
+            RK_PAIR y.v[i] = fma(nn.v[i], g.v[i], y.v[i]);
         }
         if (f & kNormPre) {
             const f2 minus = both(-m1), r = both(r1);
-            RK_EACH
-                RK_PAIR
-                {
-                    y[j].v[i] = GENERAL ? mul(add(y[j].v[i], minus), r) : mul(y[j].v[i], r);
-                    dw1[j].v[i] = fma(e[j].v[i], y[j].v[i], dw1[j].v[i]);
-                    if (GENERAL)
-                        db1[j].v[i] = add(e[j].v[i], db1[j].v[i]);
-                    e[j].v[i] = mul(e[j].v[i], w1[j].v[i]);
-                }
+            RK_PAIR
+            {
+                y.v[i] = GENERAL ? mul(add(y.v[i], minus), r) : mul(y.v[i], r);
+                dw1.v[i] = fma(e.v[i], y.v[i], dw1.v[i]);
+                if (GENERAL)
+                    db1.v[i] = add(e.v[i], db1.v[i]);
+                e.v[i] = mul(e.v[i], w1.v[i]);
+            }
             through_norm(f & kNormPreLayer, r1, e, y);
         }
-        RK_EACH
         {
-            const Vec8 d = fetch8<R, FULL>(ring.get + j * next_at + du_at, stride, cols[j]);
-            RK_PAIR e[j].v[i] = add(e[j].v[i], d.v[i]);
+            Vec8 o = fetch8<R, FULL>(ring.get + du_at, stride, q.n);
+            RK_PAIR e.v[i] = add(e.v[i], o.v[i]);
+            RK_PAIR o.v[i] = mul(e.v[i], a);
+            put8<R, FULL>(dx, o, f & kNormDx ? n : none, p.wide & kNormWideDx);
+            dx += p.dx.step;
         }
-        RK_EACH
-        {
-            Vec8 o;
-            RK_PAIR o.v[i] = mul(e[j].v[i], a);
-            put8<R, FULL>(dx + j * apart * (int)sizeof(R), o, live && (f & kNormDx) ? cols[j] : none, p.wide & kNormWideDx);
-        }
-        dx += p.dx.step;
         if (branch) {
             if (shared_gate) {
                 if (live) {
-                    RK_PAIR dg.v[i] = fma(mul(e[0].v[i], b), nn[0].v[i], dg.v[i]);
+                    RK_PAIR dg.v[i] = fma(mul(e.v[i], b), nn.v[i], dg.v[i]);
                     // The group's last row of the gate, or of all: a gate that lies within
                     // the group is done, others leave a partial sum (the group's first
                     // gate in row 0, its last in row 1).
                     const bool last = dgate.last(p, q);
                     if (last || k + 1 == q.count) {
                         if (gate_whole && last)
-                            put_gate(dg, 0, q.n);
+                            put_gate(dg, q.n);
                         else
                             gate_part();
                         dg = splat(0.f);
@@ -885,28 +846,22 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
                     dgate.next(p, p.dgate, q);
                 }
             } else if (!SHARED && (f & kNormDgate)) {
-                RK_EACH
-                {
-                    RK_PAIR nn[j].v[i] = mul(mul(e[j].v[i], b), nn[j].v[i]);
-                    put_gate(nn[j], j, live ? cols[j] : none);
-                }
+                RK_PAIR nn.v[i] = mul(mul(e.v[i], b), nn.v[i]);
+                put_gate(nn, n);
                 dgate.next(p, p.dgate, q);
             }
-            RK_EACH
-                RK_PAIR e[j].v[i] = mul(e[j].v[i], g[j].v[i]);
+            RK_PAIR e.v[i] = mul(e.v[i], g.v[i]);
             if (POST) {
-                RK_EACH
-                    RK_PAIR
-                    {
-                        dw2[j].v[i] = fma(e[j].v[i], y2[j].v[i], dw2[j].v[i]);
-                        if (GENERAL)
-                            db2[j].v[i] = add(e[j].v[i], db2[j].v[i]);
-                        e[j].v[i] = mul(e[j].v[i], w2[j].v[i]);
-                    }
+                RK_PAIR
+                {
+                    dw2.v[i] = fma(e.v[i], y2.v[i], dw2.v[i]);
+                    if (GENERAL)
+                        db2.v[i] = add(e.v[i], db2.v[i]);
+                    e.v[i] = mul(e.v[i], w2.v[i]);
+                }
                 through_norm(f & kNormPostLayer, r2, e, y2);
             }
-            RK_EACH
-                put8<A, FULL>(dz + j * apart * (int)sizeof(A), e[j], live && (f & kNormDz) ? cols[j] : none, p.wide & kNormWideDz);
+            put8<A, FULL>(dz, e, f & kNormDz ? n : none, p.wide & kNormWideDz);
             dz += p.dz.step;
         }
         ring.used();
@@ -915,9 +870,9 @@ __global__ void __maxnreg__((norm_registers(kNormBackwardThreads<POST, GENERAL, 
     asm volatile("cp.async.wait_all;" ::: "memory");
     float *part = p.sum_part, *buffer = reinterpret_cast<float *>(stages);
     const int64_t size = (int64_t)p.ctas * p.cols;
-    auto store = [&](uint32_t flag, const Vec8(&acc)[V]) {
+    auto store = [&](uint32_t flag, const Vec8 &acc) {
         if (f & flag) {
-            RK_EACH store_sum(p, q, part, buffer, acc[j], j * apart, cols[j]);
+            store_sum(p, q, part, buffer, acc);
             part += size;
         }
     };
@@ -1043,10 +998,13 @@ template <typename A, typename R, bool FULL, bool POST, bool GENERAL> cudaError_
 
 template <typename A, typename R, bool FULL, bool POST, bool GENERAL> cudaError_t launch_backward(const NormParams &n, cudaStream_t s)
 {
-    if (n.flags & kNormSharedGate)
-        return launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 1, true>, n, s);
-    return n.vectors == 1 ? launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 1, false>, n, s)
-                          : launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, 2, false>, n, s);
+    const bool shared = n.flags & kNormSharedGate;
+    if constexpr (POST && GENERAL)
+        if (n.threads_per_sm == kNormGeneralThreads)
+            return shared ? launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, true, kNormGeneralThreads>, n, s)
+                          : launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, false, kNormGeneralThreads>, n, s);
+    return shared ? launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, true, kNormBackwardThreads>, n, s)
+                  : launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, false, kNormBackwardThreads>, n, s);
 }
 
 // The kernels of one pair of types; a translation unit instantiates one of the two.
