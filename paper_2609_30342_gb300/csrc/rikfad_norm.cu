@@ -253,8 +253,7 @@ void grid(NormParams &n, int threads_per_sm)
     const int by_registers = std::max(1, threads_per_sm / n.threads);
     const int64_t groups = (n.rows + n.row_groups - 1) / n.row_groups;
     const size_t stage = (size_t)n.threads * 16 * n.units * n.vectors;
-    n.stages = stage * 3 * by_registers <= kNormSmemPerSm ? 3 : 2;
-    n.smem = stage * n.stages;
+    n.smem = 2 * stage;
     const int resident = std::max(1, std::min(by_registers, (int)(kNormSmemPerSm / n.smem)));
     n.ctas = (int)std::max<int64_t>(1, std::min<int64_t>(groups, (int64_t)kNormSms * resident / n.cluster));
     n.ctas = (n.ctas + n.classes - 1) / n.classes * n.classes;      // as many for each class

@@ -96,7 +96,7 @@ struct NormParams {
     int32_t cluster, cta_cols;              // blocks of a row; columns of each
     int32_t ctas;                           // clusters of the launch
     int32_t threads_per_sm;                 // by the kernel's registers
-    int32_t units, stages;                  // 16-byte units of a vector; rows in flight and in use
+    int32_t units;                          // 16-byte units of a vector
     size_t smem;
     // backward: partial sums
     int32_t sums;
