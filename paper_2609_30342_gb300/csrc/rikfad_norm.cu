@@ -265,7 +265,10 @@ void forward_shape(const rikfad_residual_norm *p, NormParams &n)
     n.units = r + a + (p->gate.data && p->gate_rows < kNormHeldRows ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
     const int most = n.flags & kNormSharedGate ? 1 : 2;
     shape(n, p, most, kNormMaxThreads / most, drift_of(n));
-    grid(n, n.vectors == 1 ? kNormForwardThreads<1> : kNormForwardThreads<2>);
+    const bool heavy = (n.flags & kNormPost) && n.general;
+    grid(n, n.vectors == 1                         ? (heavy ? kNormHeavyForwardThreads1 : kNormForwardThreads1)
+            : heavy && p->cols <= kNormHeavyCols ? kNormHeavyThreads
+                                                 : kNormForwardThreads2);
 }
 
 struct Workspace {
@@ -278,9 +281,8 @@ Workspace backward_shape(const rikfad_residual_norm *p, NormParams &n, int drift
 {
     const int a = p->dtype == RIKFAD_F32 ? 2 : 1, r = p->residual_dtype == RIKFAD_F32 ? 2 : 1;
     n.units = 2 * a + 2 * r + (p->gate.data && p->gate_rows < kNormHeldRows ? (p->gate_dtype == RIKFAD_F32 ? 2 : a) : 0);
-    const bool shared = (n.flags & kNormSharedGate) && p->dgate.data, post = n.flags & kNormPost;
-    const bool narrow = p->cols <= 8 * kNormGeneralThreads - 8;        // a shifted row may need one vector more
-    const int threads = post && n.general && narrow ? kNormGeneralThreads : kNormBackwardThreads;
+    const bool shared = (n.flags & kNormSharedGate) && p->dgate.data, heavy = (n.flags & kNormPost) && n.general;
+    const int threads = heavy && p->cols <= kNormHeavyCols ? kNormHeavyThreads : kNormBackwardThreads;
     shape(n, p, 1, threads, drift);
     grid(n, threads);
     n.sums = 0;

@@ -531,8 +531,8 @@ template <typename A, bool FULL> __device__ __forceinline__ Vec8 fetch_gate(cons
 
 // ------------------------------------------------------------------- forward
 
-template <typename A, typename R, bool FULL, bool POST, bool GENERAL, bool SHARED, int V>
-__global__ void __maxnreg__((norm_registers(kNormForwardThreads<V>))) rikfad_norm_forward_kernel(const __grid_constant__ NormParams p)
+template <typename A, typename R, bool FULL, bool POST, bool GENERAL, bool SHARED, int V, int THREADS>
+__global__ void __maxnreg__((norm_registers(THREADS))) rikfad_norm_forward_kernel(const __grid_constant__ NormParams p)
 {
     extern __shared__ uint4 stages[];
     __shared__ RowSums sums;
@@ -752,7 +752,7 @@ __global__ void __maxnreg__((norm_registers(THREADS))) rikfad_norm_backward_kern
     constexpr bool TOGETHER = POST && !SHARED && (FULL || GENERAL);
     // The normalised branch is formed again from its stage, except where the registers
     // hold it (8192 x 1600 of two layer norms: 72 us, 83 formed again).
-    constexpr bool KEEP = POST && GENERAL && !SHARED && THREADS == kNormGeneralThreads;
+    constexpr bool KEEP = POST && GENERAL && !SHARED && THREADS == kNormHeavyThreads;
     Vec8 e, y, kept;
     float r1 = 0.f, r2 = 0.f, m2 = 0.f, t[2];
     auto gate_of = [&](uint32_t at) {
@@ -1050,19 +1050,24 @@ template <typename K> cudaError_t launch_clustered(K kernel, const NormParams &n
 
 template <typename A, typename R, bool FULL, bool POST, bool GENERAL> cudaError_t launch_forward(const NormParams &n, cudaStream_t s)
 {
+    constexpr int kOne = POST && GENERAL ? kNormHeavyForwardThreads1 : kNormForwardThreads1;
     if (n.flags & kNormSharedGate)
-        return launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, true, 1>, n, s);
-    return n.vectors == 1 ? launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, false, 1>, n, s)
-                          : launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, false, 2>, n, s);
+        return launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, true, 1, kOne>, n, s);
+    if (n.vectors == 1)
+        return launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, false, 1, kOne>, n, s);
+    if constexpr (POST && GENERAL)
+        if (n.threads_per_sm == kNormHeavyThreads)
+            return launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, false, 2, kNormHeavyThreads>, n, s);
+    return launch_clustered(rikfad_norm_forward_kernel<A, R, FULL, POST, GENERAL, false, 2, kNormForwardThreads2>, n, s);
 }
 
 template <typename A, typename R, bool FULL, bool POST, bool GENERAL> cudaError_t launch_backward(const NormParams &n, cudaStream_t s)
 {
     const bool shared = n.flags & kNormSharedGate;
     if constexpr (POST && GENERAL)
-        if (n.threads_per_sm == kNormGeneralThreads)
-            return shared ? launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, true, kNormGeneralThreads>, n, s)
-                          : launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, false, kNormGeneralThreads>, n, s);
+        if (n.threads_per_sm == kNormHeavyThreads)
+            return shared ? launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, true, kNormHeavyThreads>, n, s)
+                          : launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, false, kNormHeavyThreads>, n, s);
     return shared ? launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, true, kNormBackwardThreads>, n, s)
                   : launch_clustered(rikfad_norm_backward_kernel<A, R, FULL, POST, GENERAL, false, kNormBackwardThreads>, n, s);
 }
