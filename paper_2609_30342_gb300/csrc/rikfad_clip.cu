@@ -11,6 +11,12 @@
 // microseconds after the others.  The second kernel scales.  It walks
 // every share from its end, so that what the first one read last is read from the
 // L2 cache.
+//
+// Memory bounds both: every gradient is read twice (the factor is known only when
+// all of them have been read once) and written once.  124.4M float32 gradients to
+// bfloat16 in 196 tensors take 197 us (1.24 GB, 6.3 TB/s), 1557.6M of bfloat16 in
+// 772 tensors 1484 us (9.3 GB, 6.3 TB/s), 30.1M of bfloat16 36 us (the second read
+// from L2); a few kilobytes 7 us on the device and twice that on the host.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -282,7 +288,8 @@ template <typename T, typename U> __device__ __forceinline__ void scale8(const R
     store_raw8_cs(out, pack8(v, U()));
 }
 
-// out = c g over a segment, from its end.
+// out = c g over a segment, from its end.  The loads and stores are streaming: nothing
+// is read again.
 template <typename T, typename U> __device__ void scale_segment(const T *g, U *out, int n, float c)
 {
     const bool wide = aligned16(g) && aligned16(out);
@@ -357,7 +364,7 @@ struct rikfad_clip_s {
     std::vector<int64_t> numel;
     std::vector<int> grad_dtype, out_dtype;
     std::vector<Part> parts;
-    std::vector<const void *> seen_grad;    // addresses that passed check_address
+    std::vector<const void *> seen_grad;    // addresses that passed check_address, as in a step's pointer table
     std::vector<void *> seen_out;
     void *memory = nullptr;                 // the plan and what the kernels leave in it, one allocation
     ClipParams params{};                    // pointers into it
@@ -611,8 +618,13 @@ RIKFAD_API int rikfad_clip_run(rikfad_clip c, const void *const *grad, void *con
     a.max_norm = max_norm;
     a.norms = norms;
     a.total = total;
-    if ((rc = launch_parts(c, a, grad, out, false, s)))
+    if ((rc = launch_parts(c, a, grad, out, false, s))) {
+        // the parts that were launched have left their counts
+        const char *const end = static_cast<const char *>(c->memory) + c->workspace;
+        cudaMemsetAsync(a.tensor_done, 0, (size_t)(end - reinterpret_cast<const char *>(a.tensor_done)), s);
+        cudaGetLastError();
         return rc;
+    }
     return out ? launch_parts(c, a, grad, out, true, s) : RIKFAD_OK;
     RK_ENTRY_END
 }

@@ -5,6 +5,11 @@
 // The angle is t times f_i / (2 pi) in 64-bit fixed point: the integer product
 // wraps at whole turns, so its high half is the fraction of a turn to 2^-32 at
 // any position (a float32 product is off by 0.06 rad at position 1e6).
+//
+// Memory bounds it: every element is read once and written once, and the cosines
+// and sines of a token are formed once for all heads of queries and keys.  131072
+// tokens of 40 heads of 128 take 430 us (2.7 GB, 6.2 TB/s), 16384 tokens of 24 heads
+// of 64 about 23 us (101 MB, 4.3 TB/s; a copy of as many bytes takes 22).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -257,6 +262,10 @@ int check(const rikfad_rotary *p)
         const rikfad_rotary_heads &l = p->lists[i];
         if (l.heads < 0 || l.heads > (int64_t)1 << 16)
             return bad("heads is out of range");
+        if (l.heads == 0 || p->tokens == 0 || p->batch == 0)
+            continue;
+        if ((l.heads > 1 && l.dst_head == 0) || (p->tokens > 1 && l.dst_token == 0) || (p->batch > 1 && l.dst_batch == 0))
+            return bad("a stride of 0 would write several heads, tokens or sequences to one place");
     }
     int device = -1;
     const cudaError_t e = cudaGetDevice(&device);

@@ -97,13 +97,13 @@ class GradientClipper:
 
     def _run(self, ptrs, out, max_norm, stream):
         device = ptrs.device
+        if stream is not None:
+            with rikfad._streaming(stream, device.index):
+                return self._run(ptrs, out, max_norm, None)
         total = torch.empty((), dtype=torch.float32, device=device)
         norms = torch.empty(len(self.numels), dtype=torch.float32, device=device)
-        if stream is not None and not isinstance(stream, int):
-            total.record_stream(stream)
-            norms.record_stream(stream)
         rikfad._check(rikfad.lib().rikfad_clip_run(self.handle, ptrs.grads, out, max_norm, norms.data_ptr(),
-                                                   total.data_ptr(), rikfad._raw_stream(stream, device.index)))
+                                                   total.data_ptr(), rikfad._raw_stream(device.index)))
         return total, norms
 
     def norm(self, grads=None, stream=None, ptrs=None):

@@ -6,7 +6,7 @@
 Each has explicit calls on CUDA tensors (``forward``/``backward``, ``rotate``) and is callable inside autograd.
 Argument checks and marshalling only: the work runs in the kernels behind ``rikfad_residual_norm_forward``,
 ``rikfad_residual_norm_backward`` and ``rikfad_rotary_apply``, enqueued on the current stream of the tensors' device (or
-``stream``).
+``stream``, to which what the call allocates then belongs; the inputs have to be ready on it).
 """
 import ctypes
 import math
@@ -30,6 +30,12 @@ _NO_BACKWARD = (0,) * 16
 _NO_HEADS = (0,) * 9
 
 ResidualNormGrads = namedtuple("ResidualNormGrads", "x z gate post_weight post_bias pre_weight pre_bias")
+
+
+def _streaming(stream, t):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("inputs must be CUDA tensors")
+    return rikfad._streaming(stream, t.get_device())
 
 
 def _rows(name, t, cols, dtype, device, rows):
@@ -139,7 +145,11 @@ class ResidualNorm:
         """(u, h, stats).  ``stats`` (None without ``need_stats``) is what ``backward`` needs besides the inputs.
         Without z, u = residual_scale x and ``dtype`` gives h's type (default x's).  ``out``: (u, h) to write to; u may
         be x and h may be z; None for one that is not wanted."""
-        head, rows, dt, device = self._inputs(x, z, gate, (post_weight, post_bias, pre_weight, pre_bias), dtype)
+        weights = (post_weight, post_bias, pre_weight, pre_bias)
+        if stream is not None:
+            with _streaming(stream, x):
+                return self.forward(x, z, gate, *weights, need_stats=need_stats, dtype=dtype, out=out)
+        head, rows, dt, device = self._inputs(x, z, gate, weights, dtype)
         cols = self.cols
         if out is None:
             u = torch.empty_like(x, memory_format=torch.contiguous_format)
@@ -152,7 +162,7 @@ class ResidualNorm:
             ph, sh = (0, 0) if h is None else _rows("h", h, cols, dt, device, rows)
         stats = torch.empty(rows, 4, dtype=_F32, device=x.device) if need_stats else None
         block = _NORM.pack(*head, pu, su, ph, sh, 0 if stats is None else stats.data_ptr(), *_NO_BACKWARD)
-        rikfad._call_on(device, rikfad.lib().rikfad_residual_norm_forward, block, rikfad._raw_stream(stream, device))
+        rikfad._call_on(device, rikfad.lib().rikfad_residual_norm_forward, block, rikfad._raw_stream(device))
         return u, h, stats
 
     def backward(self, du, dh, x, z=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None,
@@ -160,6 +170,9 @@ class ResidualNorm:
         """``ResidualNormGrads`` of the forward call's inputs (None where the input is None), from the gradients of u
         and h (either may be None)."""
         weights = (post_weight, post_bias, pre_weight, pre_bias)
+        if stream is not None:
+            with _streaming(stream, x):
+                return self.backward(du, dh, x, z, gate, *weights, stats=stats)
         head, rows, dt, device = self._inputs(x, z, gate, weights, dh.dtype if dh is not None else None)
         cols = self.cols
         pdu, sdu = (0, 0) if du is None else _rows("du", du, cols, x.dtype, device, rows)
@@ -188,10 +201,8 @@ class ResidualNorm:
         if nbytes:
             work = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
             pw = work.data_ptr()
-            if stream is not None and not isinstance(stream, int):
-                work.record_stream(stream)
         rikfad._call_on(device, lib.rikfad_residual_norm_backward, _NORM.pack(*body, pw, nbytes),
-                        rikfad._raw_stream(stream, device))
+                        rikfad._raw_stream(device))
         return ResidualNormGrads(dx, dz, dgate, *dw)
 
     def __call__(self, x, z=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None,
@@ -305,6 +316,9 @@ class Rotary:
         k).  ``positions``: int32 or int64 CUDA tensor [tokens] or [batch, tokens]; default ``start`` + 0, 1, ...
         ``inverse`` turns back: the gradient of the rotation.  ``out``: (q', k') to write to; q and k themselves
         rotate in place."""
+        if stream is not None:
+            with _streaming(stream, q):
+                return self.rotate(q, k, positions, start, inverse, out)
         for t in (q, k, positions):
             if t is not None and not isinstance(t, torch.Tensor):
                 raise ValueError("inputs must be tensors")
@@ -349,7 +363,7 @@ class Rotary:
         block = _ROTARY.pack(batch, tokens, self.head_dim, self.rotary_dim, self._layout, _TORCH[dtype],
                              self._turns, pp, pb, start, width, 1 if inverse else 0, 1 if k is None else 2, 0,
                              self.magnitude, *lists)
-        rikfad._call_on(device, rikfad.lib().rikfad_rotary_apply, block, rikfad._raw_stream(stream, device))
+        rikfad._call_on(device, rikfad.lib().rikfad_rotary_apply, block, rikfad._raw_stream(device))
         return out[0], (None if k is None else out[1])
 
     def __call__(self, q, k, positions=None, start=0):

@@ -152,14 +152,22 @@ def _stream_ptr(stream):
     return stream.cuda_stream
 
 
-def _raw_stream(stream, index):
-    """The cudaStream_t of ``stream`` (a torch stream or an integer), or of the
-    current stream of device ``index``."""
-    if stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # a tenth of current_stream's time
-        return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
-    return stream if isinstance(stream, int) else stream.cuda_stream
+def _raw_stream(index):
+    """The cudaStream_t of the current stream of device ``index``."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # a tenth of current_stream's time
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+
+
+def _streaming(stream, index):
+    """A context in which ``stream`` is the current stream of device ``index``, so that what is allocated for a call
+    belongs to the stream that the call is enqueued on: a block that another stream still uses is not taken."""
+    import torch
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=index)
+    if stream.device.index != index:
+        raise ValueError("the stream belongs to another device")
+    return torch.cuda.stream(stream)
 
 
 def _call_on(index, function, *args):

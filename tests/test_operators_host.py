@@ -80,6 +80,16 @@ def test_rotary_arguments_are_refused(kw):
     assert rikfad.lib().rikfad_rotary_apply(None, None) == rikfad.ERR_ARG
 
 
+@pytest.mark.parametrize("batch,tokens,heads,zero", [(1, 1, 2, 5), (1, 2, 1, 4), (2, 1, 1, 3)])
+def test_rotary_outputs_that_overlap_themselves_are_refused(batch, tokens, heads, zero):
+    strides = [64] * 6
+    strides[zero] = 0
+    block = layers._ROTARY.pack(batch, tokens, 64, 64, 0, 1, 256, 0, 0, 0, 8, 0, 1, 0, 1.0, 256, 512, heads, *strides,
+                                *([0] * 9))
+    assert rikfad.lib().rikfad_rotary_apply(block, None) == rikfad.ERR_ARG
+    assert b"stride of 0" in rikfad.lib().rikfad_last_error()
+
+
 def test_turns():
     L = rikfad.lib()
     values = [0.0, math.pi, 2 * math.pi, -math.pi / 2, 1.0, 1e-4, 7.0, 1e300]
