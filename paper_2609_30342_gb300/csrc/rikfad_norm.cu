@@ -323,6 +323,7 @@ extern "C" {
 
 RIKFAD_API size_t rikfad_residual_norm_workspace(const rikfad_residual_norm *p)
 {
+    RK_ENTRY_BEGIN
     if (check_sizes(p))
         return 0;
     report_error(RIKFAD_OK, "");
@@ -336,6 +337,11 @@ RIKFAD_API size_t rikfad_residual_norm_workspace(const rikfad_residual_norm *p)
         floats = std::max(floats, w.weights + w.gates);
     }
     return (size_t)floats * sizeof(float);
+    }
+    catch (...)
+    {
+        return 0;
+    }
 }
 
 RIKFAD_API int rikfad_residual_norm_forward(const rikfad_residual_norm *p, void *stream)

@@ -365,6 +365,7 @@ extern "C" {
 
 RIKFAD_API int rikfad_rotary_turns(const double *radians, int64_t n, uint64_t *turns)
 {
+    RK_ENTRY_BEGIN
     if (n < 0 || (n > 0 && (radians == nullptr || turns == nullptr)))
         return bad("need n >= 0, radians and turns");
     for (int64_t i = 0; i < n; ++i) {
@@ -375,6 +376,7 @@ RIKFAD_API int rikfad_rotary_turns(const double *radians, int64_t n, uint64_t *t
         turns[i] = f < 0x1p64 ? (uint64_t)f : 0;
     }
     return RIKFAD_OK;
+    RK_ENTRY_END
 }
 
 RIKFAD_API int rikfad_rotary_apply(const rikfad_rotary *p, void *stream)

@@ -221,6 +221,7 @@ class _ResidualNormFunction(torch.autograd.Function):
         return u, h
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, du, dh):
         x, *rest, stats = ctx.saved_tensors
         du, dh = (None if g is None else g.contiguous() for g in (du, dh))
@@ -380,6 +381,7 @@ class _RotaryFunction(torch.autograd.Function):
         return op.rotate(q, k, positions=positions, start=start)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dq, dk):
         positions = ctx.saved_tensors[0] if ctx.saved_tensors else None
         if dq is None:
