@@ -28,6 +28,7 @@ constexpr int norm_registers(int threads) { return threads <= 256 ? 248 : 65536 
 constexpr int64_t kNormHeldRows = 16;           // rows of a gate from which it is kept in registers
 constexpr int kNormSms = 152;
 constexpr size_t kNormSmemPerSm = 200 << 10;    // for the stages; a block keeps 1 KB more
+constexpr size_t kNormSmemDefault = 40 << 10;   // a block may have as much unasked (48 KB, less the row sums' slots)
 
 enum : uint32_t {
     kNormBranch = 1u << 0,          // z is there

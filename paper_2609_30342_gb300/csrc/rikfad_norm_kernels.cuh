@@ -1042,9 +1042,11 @@ template <typename A> __global__ void __launch_bounds__(kJoinThreads) rikfad_nor
 
 template <typename K> cudaError_t launch_clustered(K kernel, const NormParams &n, cudaStream_t s)
 {
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kNormSmemPerSm);
-    if (e != cudaSuccess)
-        return e;
+    if (n.smem > kNormSmemDefault) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kNormSmemPerSm);
+        if (e != cudaSuccess)
+            return e;
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(n.ctas * n.cluster));
     cfg.blockDim = dim3((unsigned)n.threads);
