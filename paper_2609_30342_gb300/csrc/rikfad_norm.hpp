@@ -19,9 +19,9 @@ constexpr int kNormMaxWarps = kNormMaxThreads / 32;
 constexpr int kNormForwardThreads1 = 768, kNormForwardThreads2 = 512, kNormBackwardThreads = 512;
 // With a post norm and layer norms or biases ("heavy"), fewer threads with more
 // registers: 128 with one vector forward (8192 x 1600 with a shared gate: 47 us, 60 with
-// 80), 168 with two (8192 x 1600: 36 us, 42 with 128) and backward (91 us, 99 with 128) for
+// 80), 168 with two (8192 x 1600: 36 us, 42 with 128) and backward (72 us, 99 with 128) for
 // rows of up to kNormHeavyCols columns.  Wider ones would leave an SM one block, or take
-// two blocks a row (4096 x 4096: forward 52 us instead of 47, backward 189 instead of 120).
+// two blocks a row (4096 x 4096: forward 52 us instead of 47, backward 141 instead of 117).
 constexpr int kNormHeavyForwardThreads1 = 512, kNormHeavyThreads = 384;
 constexpr int kNormHeavyCols = 8 * kNormHeavyThreads - 8;      // a shifted row may need one vector more
 constexpr int norm_registers(int threads) { return threads <= 256 ? 248 : 65536 / threads / 8 * 8; }

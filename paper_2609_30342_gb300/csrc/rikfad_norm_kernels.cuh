@@ -503,8 +503,8 @@ __device__ __forceinline__ void row_stats(const NormParams &p, Team &team, bool 
 }
 
 // A thread's two stages: where the next row's copies go, and where the present row's
-// are.  (Three to five stages are no faster: 56 to 59 us instead of 56 for 8192 x 1600
-// backward; forward, 32768 x 4096 takes 233 us with three, 206 with two.)
+// are.  (Three to five stages were no faster at any size; forward, 32768 x 4096 takes
+// 233 us with three, 206 with two.)
 struct Ring {
     uint32_t put, get, other;       // other: put ^ get
 
