@@ -25,7 +25,9 @@ constexpr int kNormForwardThreads1 = 768, kNormForwardThreads2 = 512, kNormBackw
 constexpr int kNormHeavyForwardThreads1 = 512, kNormHeavyThreads = 384;
 constexpr int kNormHeavyCols = 8 * kNormHeavyThreads - 8;      // a shifted row may need one vector more
 constexpr int norm_registers(int threads) { return threads <= 256 ? 248 : 65536 / threads / 8 * 8; }
-constexpr int64_t kNormHeldRows = 16;           // rows of a gate from which it is kept in registers
+// Rows of a gate from which it is kept in registers, not staged for every row (8192 x
+// 1600, 1024 rows a gate: forward 30 us, 50 staged; 16 rows: 30 and 33; 4 rows: 33 both).
+constexpr int64_t kNormHeldRows = 16;
 constexpr int kNormSms = 152;
 constexpr size_t kNormSmemPerSm = 200 << 10;    // for the stages; a block keeps 1 KB more
 constexpr size_t kNormSmemDefault = 40 << 10;   // a block may have as much unasked (48 KB, less the row sums' slots)
@@ -101,6 +103,8 @@ struct NormParams {
     int32_t ctas;                           // clusters of the launch
     int32_t threads_per_sm;                 // by the kernel's registers
     int32_t units;                          // 16-byte units of a vector
+    int32_t join_rows;                      // of the join kernel (join_gate)
+    bool join_bounds;
     size_t smem;
     // backward: partial sums
     int32_t sums;

@@ -980,62 +980,84 @@ template <typename A> __device__ __forceinline__ void store_as(void *p, bool f32
         static_cast<A *>(p)[i] = from_f32<A>(v);
 }
 
-// Adds the partial rows of a sum in order, 32 columns a block: a few megabytes that
+// A gate whose rows several groups share: the sum of their partial rows in order.
+// Item i is gate i, or with p.join_bounds the gate in which worker i + 1 begins (there
+// are fewer of those where gates serve few rows).  join_rows partial rows are read at a
+// time, by kJoinThreads / join_rows columns.
+template <typename A> __device__ void join_gate(const NormParams &p, float *red, int item, int columns)
+{
+    const int64_t workers = (int64_t)(p.ctas / p.classes) * p.row_groups;       // of a class
+    const int width = kJoinThreads / p.join_rows, x = threadIdx.x % width, y = threadIdx.x / width;
+    const int64_t c = (int64_t)columns * width + x;
+    int64_t g = item;
+    if (p.join_bounds) {
+        // each gate once: the first worker that begins after its first row
+        const int64_t row = worker_begin(p.rows, item + 1, workers), before = worker_begin(p.rows, item, workers);
+        g = row / p.gate_rows;
+        if (row >= p.rows || row == g * p.gate_rows || before > g * p.gate_rows)
+            return;
+    }
+    const int64_t begin = g * p.gate_rows, end = begin + p.gate_rows;
+    // Thread row y takes every (join_rows / classes)-th worker of class y % classes:
+    // the class's rows of the gate are [i0, i1] of its own.
+    const int first = y % p.classes;
+    const int64_t rows = class_rows(p, first);
+    const int64_t i0 = begin <= first ? 0 : (begin - first + p.classes - 1) / p.classes;
+    const int64_t i1 = end - 1 < first ? -1 : (end - 1 - first) / p.classes;
+    float t = 0.f;
+    if (i0 <= i1) {
+        const int64_t w0 = ((i0 + 1) * workers - 1) / rows, w1 = ((i1 + 1) * workers - 1) / rows;
+        if (p.classes == 1 && w0 == w1)
+            return;             // written by its only worker
+        if (c < p.cols)
+            for (int64_t w = w0 + y / p.classes; w <= w1; w += p.join_rows / p.classes) {
+                const int64_t row = first + p.classes * worker_begin(rows, w, workers);     // the worker's first
+                // block b of the class has number b classes + first
+                const int64_t worker = (w / p.row_groups * p.classes + first) * p.row_groups + w % p.row_groups;
+                t += __ldcg(p.gate_part + (2 * worker + (row / p.gate_rows == g ? 0 : 1)) * p.cols + c);
+            }
+    }
+    red[y * (width + 1) + x] = t;
+    __syncthreads();
+    if (y == 0 && c < p.cols) {
+        t = red[x];
+        for (int i = 1; i < p.join_rows; ++i)
+            t += red[i * (width + 1) + x];
+        store_as<A>(p.dgate.data, p.flags & kNormGateF32, g * p.dgate.stride + c, t);
+    }
+}
+
+// Adds the partial rows of the sums in order, 32 columns a block: a few megabytes that
 // the kernel before has left in L2 (8192 x 1600: 3.9 MB; 10 us alone with cold caches).
-// blockIdx.y below p.sums: a weight's or bias's gradient; beyond: gates whose rows
-// several groups share.
+// The first blocks: a weight's or bias's gradient each; beyond: gates.
 template <typename A> __global__ void __launch_bounds__(kJoinThreads) rikfad_norm_join_kernel(const __grid_constant__ NormParams p)
 {
     __shared__ float red[kJoinRows][33];
     wait_for_predecessor();
     allow_successor_launch();
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + x, out = (int64_t)blockIdx.x * 32 + y;
-    const bool writes = x == 0 && out < p.cols;
-    if ((int)blockIdx.y < p.sums) {
-        void *const each[4] = {p.dpre_weight, p.dpost_weight, p.dpre_bias, p.dpost_bias};
-        int at = blockIdx.y;
-        void *dst = nullptr;
-        for (int i = 0; i < 4; ++i)
-            if (each[i] && at-- == 0)
-                dst = each[i];
-        const float *part = p.sum_part + (int64_t)blockIdx.y * p.ctas * p.cols + c;
-        float t = 0.f;
-        if (c < p.cols)
-#pragma unroll 16
-            for (int i = y; i < p.ctas; i += kJoinRows)
-                t += __ldcg(part + (int64_t)i * p.cols);
-        t = join_rows(t, red);
-        if (writes)
-            store_as<A>(dst, p.flags & kNormParamF32, out, t);
+    const int strips = (p.cols + 31) / 32, sum = blockIdx.x / strips;
+    if (sum >= p.sums) {
+        const int id = blockIdx.x - strips * p.sums, columns = (p.cols + kJoinThreads / p.join_rows - 1) / (kJoinThreads / p.join_rows);
+        join_gate<A>(p, &red[0][0], id / columns, id % columns);
         return;
     }
-    const int64_t gates = p.rows / p.gate_rows, workers = (int64_t)(p.ctas / p.classes) * p.row_groups;   // of a class
-    for (int64_t g = blockIdx.y - p.sums; g < gates; g += gridDim.y - p.sums) {
-        const int64_t begin = g * p.gate_rows, end = begin + p.gate_rows;
-        // Thread row y takes every (kJoinRows / classes)-th worker of class y % classes:
-        // the class's rows of the gate are [i0, i1] of its own.
-        const int first = y % p.classes;
-        const int64_t rows = class_rows(p, first);
-        const int64_t i0 = begin <= first ? 0 : (begin - first + p.classes - 1) / p.classes;
-        const int64_t i1 = end - 1 < first ? -1 : (end - 1 - first) / p.classes;
-        float t = 0.f;
-        if (i0 <= i1) {
-            const int64_t w0 = ((i0 + 1) * workers - 1) / rows, w1 = ((i1 + 1) * workers - 1) / rows;
-            if (p.classes == 1 && w0 == w1)
-                continue;           // written by its only worker
-            if (c < p.cols)
-                for (int64_t w = w0 + y / p.classes; w <= w1; w += kJoinRows / p.classes) {
-                    const int64_t row = first + p.classes * worker_begin(rows, w, workers);     // the worker's first
-                    // block b of the class has number b classes + first
-                    const int64_t worker = (w / p.row_groups * p.classes + first) * p.row_groups + w % p.row_groups;
-                    t += __ldcg(p.gate_part + (2 * worker + (row / p.gate_rows == g ? 0 : 1)) * p.cols + c);
-                }
-        }
-        t = join_rows(t, red);
-        if (writes)
-            store_as<A>(p.dgate.data, p.flags & kNormGateF32, g * p.dgate.stride + out, t);
-    }
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t strip = blockIdx.x % strips, c = strip * 32 + x, out = strip * 32 + y;
+    void *const each[4] = {p.dpre_weight, p.dpost_weight, p.dpre_bias, p.dpost_bias};
+    int at = sum;
+    void *dst = nullptr;
+    for (int i = 0; i < 4; ++i)
+        if (each[i] && at-- == 0)
+            dst = each[i];
+    const float *part = p.sum_part + (int64_t)sum * p.ctas * p.cols + c;
+    float t = 0.f;
+    if (c < p.cols)
+#pragma unroll 16
+        for (int i = y; i < p.ctas; i += kJoinRows)
+            t += __ldcg(part + (int64_t)i * p.cols);
+    t = join_rows(t, red);
+    if (x == 0 && out < p.cols)
+        store_as<A>(dst, p.flags & kNormParamF32, out, t);
 }
 
 // ------------------------------------------------------------------- launch
@@ -1109,12 +1131,30 @@ template <typename A, typename R> cudaError_t norm_backward(const NormParams &n,
     else
         e = post ? (n.general ? launch_backward<A, R, false, true, true>(n, s) : launch_backward<A, R, false, true, false>(n, s))
                  : (n.general ? launch_backward<A, R, false, false, true>(n, s) : launch_backward<A, R, false, false, false>(n, s));
-    const bool shared_gate = n.dgate.data && n.gate_rows > 1;
+    const bool shared_gate = n.dgate.data && n.gate_rows > 1 && n.rows > 0;
     if (e != cudaSuccess || (n.sums == 0 && !shared_gate))
         return e;
-    const int64_t gates = shared_gate ? n.rows / n.gate_rows : 0;
-    const dim3 grid((unsigned)((n.cols + 31) / 32), (unsigned)(n.sums + (gates < 1024 ? gates : 1024)));
-    return launch_chained(rikfad_norm_join_kernel<A>, grid, kJoinThreads, 0, s, n);
+    NormParams j = n;
+    int64_t blocks = (int64_t)n.sums * ((n.cols + 31) / 32);
+    j.join_rows = kJoinRows;
+    if (shared_gate) {
+        // Gates, or the places where workers begin, whichever are fewer; and thread rows
+        // for the partial rows that a gate has, at least one for each class (8192 x 1600
+        // backward, 16 rows a gate: 99 us, 487 with all gates and 32 thread rows).
+        const int64_t gates = n.rows / n.gate_rows, workers = (int64_t)(n.ctas / n.classes) * n.row_groups;
+        const int64_t parts = n.classes * (n.gate_rows * workers / n.rows + 2);
+        j.join_bounds = n.classes == 1 && gates >= workers;
+        for (j.join_rows = n.classes; j.join_rows < kJoinRows && j.join_rows < parts;)
+            j.join_rows *= 2;
+        const int width = kJoinThreads / j.join_rows;
+        blocks += (j.join_bounds ? workers - 1 : gates) * ((n.cols + width - 1) / width);
+    }
+    if (blocks == 0)
+        return cudaSuccess;
+    if (blocks > INT32_MAX)
+        return cudaErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks);
+    return launch_chained(rikfad_norm_join_kernel<A>, grid, kJoinThreads, 0, s, j);
 }
 
 }  // namespace rikfad
