@@ -149,6 +149,10 @@ NormParams params(const rikfad_residual_norm *p, bool backward)
     n.wide |= kNormWideU | kNormWideH;
     tensor(n.du, p->du, p->residual_dtype, p->rows, kNormDu, kNormWideDu);
     tensor(n.dh, p->dh, p->dtype, p->rows, kNormDh, kNormWideDh);
+    // An absent gradient's copies of no bytes start where x's do, and on 16 bytes they
+    // have to start as well.
+    if (!(n.wide & kNormWideX))
+        n.wide &= ~((p->du.data ? 0 : kNormWideDu) | (p->dh.data ? 0 : kNormWideDh));
     tensor(n.dx, p->dx, p->residual_dtype, p->rows, kNormDx, kNormWideDx);
     tensor(n.dz, p->dz, p->dtype, p->rows, kNormDz, kNormWideDz);
     tensor(n.dgate, p->dgate, p->gate_dtype, gates, kNormDgate, kNormWideDgate);
