@@ -467,6 +467,10 @@ int create(rikfad_clip c, const int64_t *numel, const int *grad_dtype, const int
         return report_error(RIKFAD_ERR_OOM, "cudaMalloc of a clipping plan failed: out of memory");
     if (e == cudaSuccess)
         e = cudaMemcpy(c->memory, image.data(), bytes, cudaMemcpyHostToDevice);
+    // From pageable memory the copy returns when its bytes are staged, and a stream that
+    // does not wait for the legacy one may run the plan at once.
+    if (e == cudaSuccess)
+        e = cudaStreamSynchronize(cudaStreamLegacy);
     if (e != cudaSuccess)
         return report_cuda(e, "memory of a clipping plan");
     c->workspace = bytes;
