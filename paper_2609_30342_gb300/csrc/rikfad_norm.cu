@@ -214,6 +214,10 @@ void set_drift(NormParams &n, int drift)
 // `most_threads` threads of `most_vectors` vectors each.
 void shape(NormParams &n, const rikfad_residual_norm *p, int most_vectors, int most_threads, int drift)
 {
+    // A shifted row may need a vector more.  Where a cluster has no room for it (rows of
+    // more than 32761 columns), every tensor's own rows decide.
+    if ((n.cols + 7 + 7) / 8 > kNormMaxCluster * most_threads * most_vectors)
+        drift = 0;
     set_drift(n, drift);
     const int vectors = (n.cols + (n.classes > 1 ? 7 : 0) + 7) / 8;     // a shifted row may begin within one
     n.cluster = 1;

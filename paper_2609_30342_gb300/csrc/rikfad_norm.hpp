@@ -14,6 +14,7 @@ namespace rikfad {
 // memory.
 constexpr int kNormMaxThreads = 512;
 constexpr int kNormMaxWarps = kNormMaxThreads / 32;
+constexpr int kNormMaxCluster = 8;              // what every launch may ask for
 // Threads of an SM, by the registers that the kernels are given: 80 with one vector
 // forward, 128 with two and backward.
 constexpr int kNormForwardThreads1 = 768, kNormForwardThreads2 = 512, kNormBackwardThreads = 512;

@@ -251,7 +251,7 @@ __device__ __forceinline__ uint32_t smem_address(const void *p) { return (uint32
 struct alignas(16) RowSums {
     // [parity][value][warp of the cluster]: a sum's slots are written again two sums
     // later, with a barrier in between that follows every read of the first
-    float slot[2][4][kNormMaxWarps * 8];
+    float slot[2][4][kNormMaxWarps * kNormMaxCluster];
 };
 
 __device__ __forceinline__ void cluster_barrier()

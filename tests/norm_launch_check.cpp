@@ -1,9 +1,11 @@
 // Host-side check of the residual norm's launches: the C entries' host code with the
-// kernels' launches replaced by a look at the parameters they would get.  Compiled
-// by tests/test_norm_launch.py; the argument names the check.  Prints "OK" or the
-// first violation.
+// kernels' launches replaced by a look at the parameters they would get and the CUDA
+// runtime by host memory (tests/host_runtime.cpp).  Compiled by
+// tests/test_norm_launch.py; the argument names the check.  Prints "OK" or the first
+// violation.
 //
 //   copies  every 16-byte asynchronous copy, those of no bytes too, starts on 16 bytes
+//   shapes  every width at every drift of its rows has a launch that the kernels run
 #include "rikfad_norm.cu"
 
 #include <cstdio>
@@ -38,19 +40,6 @@ STUB(f16_f16)
 STUB(f16_f32)
 
 }  // namespace rikfad
-
-extern "C" {
-cudaError_t cudaGetDevice(int *device)
-{
-    *device = 0;
-    return cudaSuccess;
-}
-cudaError_t cudaPeekAtLastError() { return cudaSuccess; }
-cudaError_t cudaGetLastError() { return cudaSuccess; }
-cudaError_t cudaMemsetAsync(void *, int, size_t, cudaStream_t) { return cudaSuccess; }
-const char *cudaGetErrorName(cudaError_t) { return ""; }
-const char *cudaGetErrorString(cudaError_t) { return ""; }
-}
 
 static uint64_t g_random = 88172645463325252ull;
 static int64_t below(int64_t n)
@@ -175,18 +164,86 @@ static int copies()
         const bool backward = below(3) > 0;
         rikfad_residual_norm p = draw(backward);
         const int before = g_launches;
-        if (p.cols <= 32761 && (run(p, backward) || g_launches != before + 1))
+        if (run(p, backward) || g_launches != before + 1)
             return fail(p, g_error.c_str(), i, 0);
-        if (g_launches != before && check_copies(p, g_launched, backward))
+        if (check_copies(p, g_launched, backward))
             return 1;
     }
+    return 0;
+}
+
+// What the kernels take: up to 8 blocks of a cluster of up to 16 warps each, whole
+// rows of a warp or warps of a row, and columns for every element of a row wherever
+// it starts.
+static int check_shape(const rikfad_residual_norm &p, const NormParams &n)
+{
+    if (n.cluster != 1 && n.cluster != 2 && n.cluster != 4 && n.cluster != 8)
+        return fail(p, "blocks of a cluster", n.cluster, n.drift);
+    if (n.threads < 32 || n.threads > kNormMaxThreads || n.threads % 32 || n.threads > n.threads_per_sm)
+        return fail(p, "threads of a block", n.threads, n.threads_per_sm);
+    if (n.row_groups * n.lanes != n.threads || (n.lanes < 32 ? 32 % n.lanes : n.lanes % 32) ||
+        (n.row_groups > 1 && (n.lanes > 32 || n.cluster > 1)))
+        return fail(p, "lanes of a row", n.lanes, n.row_groups);
+    const int most_shift = n.classes > 1 ? 7 : 0;
+    if (n.vectors < 1 || n.vectors > 2 || n.lanes * n.vectors * 8 < n.cta_cols || n.cta_cols % 8 ||
+        (int64_t)n.cta_cols * n.cluster < n.cols + most_shift)
+        return fail(p, "columns of a block", n.cta_cols, n.cluster);
+    if (n.classes > 1 && (n.classes * n.drift % 8 || n.drift < 1 || n.drift > 7))
+        return fail(p, "classes of rows", n.classes, n.drift);
+    if (n.full && (n.cols % 8 || n.classes > 1 || n.wide != kNormWideAll))
+        return fail(p, "whole vectors", n.classes, n.wide);
+    if (n.smem != (size_t)2 * n.threads * 16 * n.units * n.vectors || n.smem > kNormSmemPerSm)
+        return fail(p, "shared memory", (long long)n.smem, n.units);
+    if (n.ctas < 1 || n.ctas % n.classes || (int64_t)n.ctas * n.cluster > kNormSms * 64 + 8)
+        return fail(p, "clusters of a launch", n.ctas, n.classes);
+    return 0;
+}
+
+static int shapes()
+{
+    const int64_t some_rows[] = {1, 2, 5, 4096};
+    for (int64_t cols = 1; cols <= 32768; ++cols)
+        for (int pad = 0; pad < 8; ++pad)
+            for (int kind = 0; kind < 8; ++kind) {
+                const bool backward = kind & 1, general = kind & 2, shared = kind & 4;
+                rikfad_residual_norm p{};
+                p.dtype = (int)below(3);
+                p.residual_dtype = chance() ? RIKFAD_F32 : p.dtype;
+                p.rows = some_rows[below(4)] * (shared ? 3 : 1);
+                p.cols = cols;
+                p.gate_rows = shared ? 3 : 1;
+                p.post = general ? RIKFAD_NORM_LAYER : RIKFAD_NORM_RMS;
+                p.pre = RIKFAD_NORM_RMS;
+                const int64_t stride = cols + pad;
+                p.x = somewhere(0, stride, p.residual_dtype, 0);
+                p.z = somewhere(1, stride, p.dtype, 0);
+                p.gate = somewhere(2, stride, p.gate_dtype, 0);
+                void *const vec = reinterpret_cast<void *>((uintptr_t)1 << 50);
+                p.stats = static_cast<float *>(vec);
+                p.pre_weight = p.post_weight = vec;
+                if (backward) {
+                    p.du = somewhere(3, stride, p.residual_dtype, 0);
+                    p.dh = somewhere(4, stride, p.dtype, 0);
+                    p.dx = somewhere(5, stride, p.residual_dtype, 0);
+                    p.dz = somewhere(6, stride, p.dtype, 0);
+                    p.dgate = somewhere(7, stride, p.gate_dtype, 0);
+                    p.dpre_weight = p.dpost_weight = vec;
+                } else {
+                    p.u = somewhere(3, stride, p.residual_dtype, 0);
+                    p.h = somewhere(4, stride, p.dtype, 0);
+                }
+                if (run(p, backward))
+                    return fail(p, g_error.c_str(), pad, kind);
+                if (check_shape(p, g_launched) || check_copies(p, g_launched, backward))
+                    return 1;
+            }
     return 0;
 }
 
 int main(int argc, char **argv)
 {
     const char *what = argc > 1 ? argv[1] : "";
-    const int rc = !std::strcmp(what, "copies") ? copies() : 2;
+    const int rc = !std::strcmp(what, "copies") ? copies() : !std::strcmp(what, "shapes") ? shapes() : 2;
     if (rc == 0)
         std::printf("OK\n");
     return rc;
