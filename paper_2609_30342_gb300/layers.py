@@ -50,7 +50,7 @@ def _rows(name, t, cols, dtype, device, rows):
     if c != cols or n != rows:
         raise ValueError("%s is %d rows of %d columns, expected %d of %d" % (name, n, c, rows, cols))
     s0, s1 = t.stride()
-    if s1 != 1 and cols > 1 or s0 < cols and n > 1:
+    if n and s1 != 1 and cols > 1 or s0 < cols and n > 1:       # without elements strides say nothing
         raise ValueError("the rows of %s must be contiguous and not overlap" % name)
     return t.data_ptr(), s0 if n > 1 else cols
 
@@ -306,7 +306,7 @@ class Rotary:
         if shape[:-2] != lead or shape[-1] != self.head_dim:
             raise ValueError("%s must be [tokens, heads, %d] or [batch, tokens, heads, %d], with the tokens of q"
                              % (name, self.head_dim, self.head_dim))
-        if s[-1] != 1 and self.head_dim > 1:
+        if s[-1] != 1 and self.head_dim > 1 and t.numel():      # without elements strides say nothing
             raise ValueError("the heads of %s must be contiguous" % name)
         if len(s) == 3:
             return t.data_ptr(), shape[1], 0, s[0], s[1]
