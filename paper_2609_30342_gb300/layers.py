@@ -183,7 +183,8 @@ class ResidualNorm:
         dense = torch.contiguous_format
         dx = torch.empty_like(x, memory_format=dense)
         dz = None if z is None else torch.empty_like(z, memory_format=dense)
-        dgate = None if gate is None else torch.empty_like(gate, memory_format=dense)
+        # a gate of no rows of x gets no gradient from them
+        dgate = None if gate is None else (torch.empty_like if rows else torch.zeros_like)(gate, memory_format=dense)
         dw = [None if w is None else torch.empty_like(w) for w in weights]
         outputs = (dx.data_ptr(), cols, 0 if z is None else dz.data_ptr(), cols, 0 if gate is None else dgate.data_ptr(),
                    cols, *[0 if w is None else w.data_ptr() for w in dw])
