@@ -166,14 +166,14 @@ class ResidualNorm:
         return u, h, stats
 
     def backward(self, du, dh, x, z=None, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None,
-                 stats=None, stream=None):
+                 stats=None, stream=None, dtype=None):
         """``ResidualNormGrads`` of the forward call's inputs (None where the input is None), from the gradients of u
-        and h (either may be None)."""
+        and h (either may be None).  Without z and dh, ``dtype`` is h's type as in the forward call (default x's)."""
         weights = (post_weight, post_bias, pre_weight, pre_bias)
         if stream is not None:
             with _streaming(stream, x):
-                return self.backward(du, dh, x, z, gate, *weights, stats=stats)
-        head, rows, dt, device = self._inputs(x, z, gate, weights, dh.dtype if dh is not None else None)
+                return self.backward(du, dh, x, z, gate, *weights, stats=stats, dtype=dtype)
+        head, rows, dt, device = self._inputs(x, z, gate, weights, dtype if dtype is not None or dh is None else dh.dtype)
         cols = self.cols
         pdu, sdu = (0, 0) if du is None else _rows("du", du, cols, x.dtype, device, rows)
         pdh, sdh = (0, 0) if dh is None else _rows("dh", dh, cols, dt, device, rows)
@@ -216,7 +216,7 @@ class _ResidualNormFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, op, dtype, x, *rest):
         u, h, stats = op.forward(x, *rest, dtype=dtype)
-        ctx.op = op
+        ctx.op, ctx.dtype = op, h.dtype
         ctx.set_materialize_grads(False)
         ctx.save_for_backward(x, *rest, stats)
         return u, h
@@ -226,7 +226,7 @@ class _ResidualNormFunction(torch.autograd.Function):
     def backward(ctx, du, dh):
         x, *rest, stats = ctx.saved_tensors
         du, dh = (None if g is None else g.contiguous() for g in (du, dh))
-        return (None, None, *ctx.op.backward(du, dh, x, *rest, stats=stats))
+        return (None, None, *ctx.op.backward(du, dh, x, *rest, stats=stats, dtype=ctx.dtype))
 
 
 def rotary_frequencies(rotary_dim, base=10000.0, scaling=None):
