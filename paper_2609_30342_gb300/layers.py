@@ -294,7 +294,7 @@ class Rotary:
         self.frequencies = frequencies
         signed = [v - (1 << 64) if v >= 1 << 63 else v for v in turns[:n]]
         self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
-        self._turns, self._layout = self.turns.data_ptr(), 0 if layout == "half" else 1
+        self._layout = 0 if layout == "half" else 1
 
     def _heads(self, name, t, lead, dtype, device):
         """(pointer, heads, batch, token and head strides) of a [tokens, heads, head_dim] or
@@ -324,9 +324,11 @@ class Rotary:
         for t in (q, k, positions):
             if t is not None and not isinstance(t, torch.Tensor):
                 raise ValueError("inputs must be tensors")
-        device, dtype = q.get_device(), q.dtype
-        if device < 0 or device != self.turns.get_device():
-            raise ValueError("q must be on %s, the device of the frequencies" % self.turns.device)
+        device, dtype, turns = q.get_device(), q.dtype, self.turns
+        if device < 0 or device != turns.get_device():
+            raise ValueError("q must be on %s, the device of the frequencies" % turns.device)
+        if turns.dtype is not torch.int64 or turns.numel() != self.rotary_dim // 2 or not turns.is_contiguous():
+            raise ValueError("turns must be rotary_dim / 2 contiguous int64 values")
         if dtype not in _TORCH:
             raise ValueError("q must be float32, bfloat16 or float16")
         lead = q.shape[:-2]
@@ -363,7 +365,7 @@ class Rotary:
                 raise ValueError("the output of %s must have its shape" % name)
             lists += (ps, pd, heads, *from_, *to)
         block = _ROTARY.pack(batch, tokens, self.head_dim, self.rotary_dim, self._layout, _TORCH[dtype],
-                             self._turns, pp, pb, start, width, 1 if inverse else 0, 1 if k is None else 2, 0,
+                             turns.data_ptr(), pp, pb, start, width, 1 if inverse else 0, 1 if k is None else 2, 0,
                              self.magnitude, *lists)
         rikfad._call_on(device, rikfad.lib().rikfad_rotary_apply, block, rikfad._raw_stream(device))
         return out[0], (None if k is None else out[1])
