@@ -25,6 +25,8 @@ from . import gradients, rikfad
 # of these keep it within a small model's kernel time.
 _grad, _dtype, _momentum = attrgetter("grad"), attrgetter("dtype"), itemgetter("momentum")
 
+CLIP_PLANS = 16         # a list of 200 tensors plans about 100 KB of GPU memory
+
 
 class RIKFADOptimizer(torch.optim.Optimizer):
     def __init__(self, params, lr, alpha, mu, gamma=0.0, eps_stab=1e-16):
@@ -33,7 +35,7 @@ class RIKFADOptimizer(torch.optim.Optimizer):
         defaults = dict(lr=lr, alpha=alpha, mu=mu, gamma=gamma, eps_stab=eps_stab)
         super().__init__(params, defaults)
         self._groups = {}     # group index -> (handle, parameter list, zero gradients)
-        self._clipper = None  # plan of the last clip_grad_norm's list of sizes
+        self._clippers = {}   # clip_grad_norm's plans by sizes, the last used one last
 
     @staticmethod
     def _shape(p):
@@ -87,18 +89,24 @@ class RIKFADOptimizer(torch.optim.Optimizer):
     @torch.no_grad()
     def clip_grad_norm(self, max_norm):
         """Scale the gradients of every group in place so that their global 2-norm is at most ``max_norm``, and return
-        the norm before (a scalar CUDA tensor; nothing waits).  A norm that is not finite scales nothing."""
+        the norm before (a scalar CUDA tensor).  A norm that is not finite scales nothing.
+
+        The first call for a list of sizes plans it, which allocates and waits for the GPU; the plans of the last
+        ``CLIP_PLANS`` lists are kept (a model whose set of gradients changes from step to step), and with them nothing
+        waits.  A captured graph needs its list's plan as long as it is replayed."""
         grads = [p.grad for group in self.param_groups for p in group["params"] if p.grad is not None]
         if not (all(map(torch.Tensor.is_contiguous, grads)) and set(map(_dtype, grads)) <= {torch.float32}):
             raise ValueError("gradients must be contiguous float32 tensors")
         if len({g.device for g in grads}) > 1:
             raise ValueError("gradients must share one device")
-        sizes = list(map(torch.Tensor.numel, grads))
-        if self._clipper is None or self._clipper.numels != sizes:
-            if self._clipper is not None:
-                self._clipper.close()
-            self._clipper = gradients.GradientClipper(sizes, "f32")
-        return self._clipper.clip(max_norm, grads)[0]
+        key = tuple(map(torch.Tensor.numel, grads))
+        clipper = self._clippers.pop(key, None)
+        if clipper is None:
+            if len(self._clippers) >= CLIP_PLANS:
+                self._clippers.pop(next(iter(self._clippers))).close()
+            clipper = gradients.GradientClipper(key, "f32")
+        self._clippers[key] = clipper
+        return clipper.clip(max_norm, grads)[0]
 
     @torch.no_grad()
     def materialize(self):
@@ -143,6 +151,6 @@ class RIKFADOptimizer(torch.optim.Optimizer):
         for handle, _, _ in self._groups.values():
             handle.close()
         self._groups.clear()
-        if self._clipper is not None:
-            self._clipper.close()
-            self._clipper = None
+        for clipper in self._clippers.values():
+            clipper.close()
+        self._clippers.clear()
