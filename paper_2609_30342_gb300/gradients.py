@@ -5,6 +5,7 @@
 into other tensors, of another type if need be (fp32 gradients summed over micro-batches to the bf16 ones that a handle
 takes).  Argument marshalling only: the work runs in the kernels behind ``rikfad_clip_run``.
 """
+import contextlib
 import ctypes
 
 import torch
@@ -38,18 +39,20 @@ class ClipPointers:
 
 class GradientClipper:
     """``numels``: elements of each tensor; ``dtypes``: "f32", "bf16" or "f16", one for all or one each;
-    ``out_dtypes``: those of the clipped gradients (default: the same)."""
+    ``out_dtypes``: those of the clipped gradients (default: the same); ``device``: where the gradients are (default: the
+    current device)."""
 
-    def __init__(self, numels, dtypes="bf16", out_dtypes=None):
+    def __init__(self, numels, dtypes="bf16", out_dtypes=None, device=None):
         self.numels = [int(n) for n in numels]
         n = len(self.numels)
         self._in = _codes(dtypes, n)
         self._out = self._in if out_dtypes is None else _codes(out_dtypes, n)
         h = ctypes.c_void_p()
         self._h = None
-        rikfad._check(rikfad.lib().rikfad_clip_create((ctypes.c_int64 * max(n, 1))(*self.numels),
-                                                      (ctypes.c_int * max(n, 1))(*self._in),
-                                                      (ctypes.c_int * max(n, 1))(*self._out), n, ctypes.byref(h)))
+        with contextlib.nullcontext() if device is None else torch.cuda.device(device):
+            rikfad._check(rikfad.lib().rikfad_clip_create((ctypes.c_int64 * max(n, 1))(*self.numels),
+                                                          (ctypes.c_int * max(n, 1))(*self._in),
+                                                          (ctypes.c_int * max(n, 1))(*self._out), n, ctypes.byref(h)))
         self._h = h
 
     @property
@@ -102,8 +105,8 @@ class GradientClipper:
                 return self._run(ptrs, out, max_norm, None)
         total = torch.empty((), dtype=torch.float32, device=device)
         norms = torch.empty(len(self.numels), dtype=torch.float32, device=device)
-        rikfad._check(rikfad.lib().rikfad_clip_run(self.handle, ptrs.grads, out, max_norm, norms.data_ptr(),
-                                                   total.data_ptr(), rikfad._raw_stream(device.index)))
+        rikfad._call_on(device.index, rikfad.lib().rikfad_clip_run, self.handle, ptrs.grads, out, max_norm,
+                        norms.data_ptr(), total.data_ptr(), rikfad._raw_stream(device.index))
         return total, norms
 
     def norm(self, grads=None, stream=None, ptrs=None):

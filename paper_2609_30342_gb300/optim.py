@@ -35,7 +35,7 @@ class RIKFADOptimizer(torch.optim.Optimizer):
         defaults = dict(lr=lr, alpha=alpha, mu=mu, gamma=gamma, eps_stab=eps_stab)
         super().__init__(params, defaults)
         self._groups = {}     # group index -> (handle, parameter list, zero gradients)
-        self._clippers = {}   # clip_grad_norm's plans by sizes, the last used one last
+        self._clippers = {}   # clip_grad_norm's plans by device and sizes, the last used one last
 
     @staticmethod
     def _shape(p):
@@ -99,12 +99,12 @@ class RIKFADOptimizer(torch.optim.Optimizer):
             raise ValueError("gradients must be contiguous float32 tensors")
         if len({g.device for g in grads}) > 1:
             raise ValueError("gradients must share one device")
-        key = tuple(map(torch.Tensor.numel, grads))
+        key = (grads[0].device if grads else None, *map(torch.Tensor.numel, grads))
         clipper = self._clippers.pop(key, None)
         if clipper is None:
             if len(self._clippers) >= CLIP_PLANS:
                 self._clippers.pop(next(iter(self._clippers))).close()
-            clipper = gradients.GradientClipper(key, "f32")
+            clipper = gradients.GradientClipper(key[1:], "f32", device=key[0])
         self._clippers[key] = clipper
         return clipper.clip(max_norm, grads)[0]
 
