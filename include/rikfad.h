@@ -430,7 +430,8 @@ enum rikfad_dtype { RIKFAD_F32 = 0, RIKFAD_BF16 = 1, RIKFAD_F16 = 2 };
  *   out_t = c g_t,  c = max_norm / total if max_norm < total < inf, else 1
  * A total that is not finite scales nothing: the gradients stay as they are and
  * the step's non-finite guard names the tensor.  Squares that leave float32's
- * range do not spoil a norm within it.  The sums' order is fixed by the list
+ * range do not spoil a norm within it; a total beyond it is stored as infinity, and
+ * c is formed before it is rounded.  The sums' order is fixed by the list
  * and the GPU, so equal gradients give equal results.
  *
  *   numel      host array, elements (>= 0) of each of the ntensors >= 0 tensors

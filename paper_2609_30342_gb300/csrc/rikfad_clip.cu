@@ -58,9 +58,12 @@ struct Segment {
     int32_t unused;                 // to 48 bytes
 };
 
-// What the kernels of a call leave for one another.
+// What the kernels of a call leave for one another.  The factor is shift times scale:
+// shift is 1, or for factors near the end of float32's range a power of two that keeps
+// scale's 24 bits (an element below 2^-62, whose product with it loses bits, is below
+// the range once scaled).
 struct ClipResult {
-    float scale;
+    float scale, shift;
     unsigned int blocks_done;       // of this call; the last block leaves 0
 };
 
@@ -196,7 +199,10 @@ __device__ void finish_list(const ClipParams &a)
     if (lane == 0) {
         total = sqrt(total);
         *a.total = (float)total;
-        a.result->scale = total > a.max_norm && total < (double)INFINITY ? (float)(a.max_norm / total) : 1.f;
+        const double c = total > a.max_norm && total < (double)INFINITY ? a.max_norm / total : 1.0;
+        const bool low = c < 0x1p-100;
+        a.result->scale = (float)(low ? c * 0x1p64 : c);
+        a.result->shift = low ? 0x1p-64f : 1.f;
     }
 }
 
@@ -279,24 +285,29 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm)
     }
 }
 
-template <typename T, typename U> __device__ __forceinline__ void scale8(const Raw8<T> &r, U *out, float c)
+struct Factor {
+    float scale, shift;
+    __device__ __forceinline__ float operator()(float v) const { return v * shift * scale; }
+};
+
+template <typename T, typename U> __device__ __forceinline__ void scale8(const Raw8<T> &r, U *out, const Factor &c)
 {
     float v[8];
     unpack8(r, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        v[e] *= c;
+        v[e] = c(v[e]);
     store_raw8_cs(out, pack8(v, U()));
 }
 
 // out = c g over a segment, from its end.  The loads and stores are streaming: nothing
 // is read again.
-template <typename T, typename U> __device__ void scale_segment(const T *g, U *out, int n, float c)
+template <typename T, typename U> __device__ void scale_segment(const T *g, U *out, int n, const Factor &c)
 {
     const bool wide = aligned16(g) && aligned16(out);
     const int chunks = wide ? n / 8 : 0;
     for (int i = n - 1 - (int)threadIdx.x; i >= chunks * 8; i -= kClipThreads)
-        out[i] = from_f32<U>(to_f32(g[i]) * c);
+        out[i] = from_f32<U>(c(to_f32(g[i])));
     g += (int64_t)(chunks - 1 - (int)threadIdx.x) * 8;
     out += (int64_t)(chunks - 1 - (int)threadIdx.x) * 8;
     int left = chunks - (int)threadIdx.x;
@@ -318,7 +329,7 @@ template <typename T, typename U> __device__ void scale_segment(const T *g, U *o
     }
 }
 
-template <typename T> __device__ void scale_segment(const T *g, void *out, const Segment &s, float c)
+template <typename T> __device__ void scale_segment(const T *g, void *out, const Segment &s, const Factor &c)
 {
     const int n = (int)(s.end - s.begin);
     if (s.out_dtype == RIKFAD_F32)
@@ -334,13 +345,13 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm)
     rikfad_clip_scale_kernel(const __grid_constant__ ClipParams a, const __grid_constant__ ClipPointers<CAP> ptrs)
 {
     wait_for_predecessor();
-    const float c = a.result->scale;
+    const Factor c{a.result->scale, a.result->shift};
     const int block = a.block0 + blockIdx.x;
     for (int q = a.block_segment[block + 1] - 1; q >= a.block_segment[block]; --q) {
         const Segment s = a.segments[q];
         const void *g = ptrs.grad[s.tensor];
         void *out = ptrs.out[s.tensor];
-        if (c == 1.f && g == out)
+        if (c.scale == 1.f && c.shift == 1.f && g == out)
             continue;
         if (s.grad_dtype == RIKFAD_F32)
             scale_segment(static_cast<const float *>(g), out, s, c);
