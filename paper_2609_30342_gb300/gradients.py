@@ -105,8 +105,14 @@ class GradientClipper:
                 return self._run(ptrs, out, max_norm, None)
         total = torch.empty((), dtype=torch.float32, device=device)
         norms = torch.empty(len(self.numels), dtype=torch.float32, device=device)
-        rikfad._call_on(device.index, rikfad.lib().rikfad_clip_run, self.handle, ptrs.grads, out, max_norm,
-                        norms.data_ptr(), total.data_ptr(), rikfad._raw_stream(device.index))
+        run = rikfad.lib().rikfad_clip_run
+        args = (self.handle, ptrs.grads, out, max_norm, norms.data_ptr(), total.data_ptr(),
+                rikfad._raw_stream(device.index))
+        code = run(*args)
+        if code == rikfad.ERR_STATE:        # another device is current: nothing was enqueued
+            with torch.cuda.device(device):
+                code = run(*args)
+        rikfad._check(code)
         return total, norms
 
     def norm(self, grads=None, stream=None, ptrs=None):

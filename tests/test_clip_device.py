@@ -8,7 +8,7 @@ from paper_2609_30342_gb300.optim import RIKFADOptimizer
 
 
 class _Machine:
-    """Two devices, the first one current; the calls and the device that each found current."""
+    """Two devices, the first one current; the calls that went through and the device that each found current."""
 
     def __init__(self, monkeypatch):
         self.current, self.calls = 0, []
@@ -27,6 +27,10 @@ class _Machine:
         class Library:
             def __getattr__(self, name):
                 def call(*args):
+                    if name == "rikfad_clip_create":
+                        machine.plan = machine.current
+                    elif machine.current != machine.plan:
+                        return rikfad.ERR_STATE
                     machine.calls.append((name, machine.current))
                     return 0
                 return call
@@ -52,6 +56,19 @@ def test_plan_and_call(monkeypatch, index):
     clipper = gradients.GradientClipper([3], "f32", device=torch.device("cuda", index))
     clipper.norm(ptrs=_Pointers(index))
     assert machine.calls == [("rikfad_clip_create", index), ("rikfad_clip_run", index)] and machine.current == 0
+
+
+def test_a_plan_of_another_device_is_refused(monkeypatch):
+    _Machine(monkeypatch)
+    clipper = gradients.GradientClipper([3], "f32", device=torch.device("cuda", 1))
+    monkeypatch.setattr(rikfad, "_check", _raise)
+    with pytest.raises(RuntimeError):
+        clipper.norm(ptrs=_Pointers(0))
+
+
+def _raise(code):
+    if code:
+        raise RuntimeError(code)
 
 
 def test_the_optimiser_plans_where_the_gradients_are(monkeypatch):
