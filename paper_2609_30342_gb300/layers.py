@@ -296,6 +296,17 @@ class Rotary:
         self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
         self._layout = 0 if layout == "half" else 1
 
+    @property
+    def turns(self):
+        """The frequencies as the kernel takes them: turns per position in units of 2^-64, int64 bits."""
+        return self._turns
+
+    @turns.setter
+    def turns(self, turns):
+        if turns.dtype is not torch.int64 or turns.shape != (self.rotary_dim // 2,) or not turns.is_contiguous():
+            raise ValueError("turns must be rotary_dim / 2 contiguous int64 values")
+        self._turns = turns
+
     def _heads(self, name, t, lead, dtype, device):
         """(pointer, heads, batch, token and head strides) of a [tokens, heads, head_dim] or
         [batch, tokens, heads, head_dim] tensor."""
@@ -324,11 +335,9 @@ class Rotary:
         for t in (q, k, positions):
             if t is not None and not isinstance(t, torch.Tensor):
                 raise ValueError("inputs must be tensors")
-        device, dtype, turns = q.get_device(), q.dtype, self.turns
+        device, dtype, turns = q.get_device(), q.dtype, self._turns
         if device < 0 or device != turns.get_device():
             raise ValueError("q must be on %s, the device of the frequencies" % turns.device)
-        if turns.dtype is not torch.int64 or turns.numel() != self.rotary_dim // 2 or not turns.is_contiguous():
-            raise ValueError("turns must be rotary_dim / 2 contiguous int64 values")
         if dtype not in _TORCH:
             raise ValueError("q must be float32, bfloat16 or float16")
         lead = q.shape[:-2]

@@ -48,6 +48,6 @@ def test_frequencies_may_be_replaced():
     op.turns = other.turns.clone()
     assert torch.equal(op.rotate(q)[0], want)
     for wrong in (op.turns[:8], op.turns.int(), op.turns.repeat(2)[::2]):
-        op.turns = wrong
         with pytest.raises(ValueError):
-            op.rotate(q)
+            op.turns = wrong
+    assert torch.equal(op.rotate(q)[0], want)
