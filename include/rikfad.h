@@ -497,7 +497,8 @@ RIKFAD_API int rikfad_clip_run(rikfad_clip c, const void *const *grad, void *con
  *              weights as well
  *   workspace  device memory of rikfad_residual_norm_workspace bytes, 16-byte
  *              aligned: partial sums of the backward call, nothing kept
- * Squares of elements beyond float32's range (above about 1e19) are infinite.
+ * Squares of elements beyond float32's range (above about 1e19) are infinite;
+ * those below it (under about 1e-19) lose bits, which shows with an eps as small.
  * With rows = 0 the backward call writes zeros to the gradients of weights and
  * biases.  Nothing is synchronised or allocated.
  */
