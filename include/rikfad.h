@@ -583,6 +583,40 @@ RIKFAD_API int rikfad_rotary_apply(const rikfad_rotary *p, void *stream);
 RIKFAD_API int rikfad_rotary_turns(const double *radians, int64_t n, uint64_t *turns);
 
 /*
+ * Token embedding: out_t = scale W[id_t] for `tokens` ids, a row of zeros for an
+ * id outside [0, vocab) (padding), and the dense gradient of the table,
+ *   dW_v = scale sum over the tokens t with id_t = v of dout_t,
+ * zeros where there is none.  The sum's order is the tokens', whatever the GPU:
+ * equal inputs give equal results.
+ *   ids        device, id_bytes (4 or 8) bytes each, signed
+ *   table      forward: W; backward: dW, written, or with accumulate != 0 added to
+ *              (rows without a token are then left alone).  `vocab` rows of
+ *              table_dtype
+ *   rows       forward: out, written; backward: dout.  `tokens` rows of dtype
+ *   workspace  backward: device memory of rikfad_embedding_workspace bytes, 16-byte
+ *              aligned; nothing kept
+ * Any two of the element types.  Rows are `width` contiguous elements, `stride`
+ * apart; 0 <= tokens <= 2^30, 0 <= vocab <= 2^30, 1 <= width <= 2^20.  Nothing is
+ * synchronised or allocated.
+ */
+typedef struct {
+    int64_t tokens, vocab, width;
+    int32_t table_dtype, dtype, id_bytes, accumulate;
+    double scale;
+    const void *ids;
+    rikfad_rows table, rows;
+    void *workspace;
+    size_t workspace_bytes;
+} rikfad_embedding;
+
+RIKFAD_API int rikfad_embedding_forward(const rikfad_embedding *p, void *stream);
+RIKFAD_API int rikfad_embedding_backward(const rikfad_embedding *p, void *stream);
+
+/* Workspace bytes of the backward call for p's sizes; 0 with a message in
+ * rikfad_last_error for sizes out of range. */
+RIKFAD_API size_t rikfad_embedding_workspace(const rikfad_embedding *p);
+
+/*
  * Testing hooks.  These have no counterpart in the paper.
  *
  * rikfad_debug_check_failures: a library compiled with -DRIKFAD_CHECKED

@@ -35,7 +35,7 @@ def nvcc():
 
 
 # Sources without device-side plan checks: both builds link the same objects.
-UNCHECKED = ("rikfad_norm", "rikfad_clip", "rikfad_rotary")
+UNCHECKED = ("rikfad_norm", "rikfad_clip", "rikfad_rotary", "rikfad_embed", "rikfad_distill")
 
 
 def sources():

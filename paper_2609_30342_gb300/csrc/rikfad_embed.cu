@@ -1,0 +1,745 @@
+// rikfad_embed.cu -- token embedding: out_t = scale W[id_t], and the table's
+// gradient dW_v = scale sum_{t: id_t = v} dout_t.
+//
+// Forward is a copy of rows.  Backward sorts the tokens by id (stable, so a row's
+// tokens stay in order) and sums runs of equal ids, `chunk` sorted tokens a warp,
+// in float32 registers.  A run within its chunk is written at once; a run over
+// several leaves a partial row in each, joined by a second kernel in the chunks'
+// order.  Nothing depends on which block is first.
+//
+// Memory bounds both: dout is read once, every row of dW written once (rows without
+// a token as zeros, by the same launch).
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <string>
+
+#include "rikfad.h"
+#include "rikfad_host.hpp"
+#include "rikfad_kernels.cuh"
+#include "rikfad_types.cuh"
+
+using namespace rikfad;
+
+namespace {
+
+constexpr int kSms = 152;
+constexpr int kForwardThreads = 256, kForwardRows = 4;
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortCtas = 8, kSortItems = 4;
+constexpr int kSortTile = kSortThreads * kSortItems;
+constexpr int kSortBits = 9;            // of a pass: the warps' counts of 2^9 digits take 32 KB
+constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32, kSumAhead = 8;
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+
+struct EmbedParams {
+    const void *ids;
+    void *table, *rows;
+    int64_t table_stride, row_stride;
+    int64_t tokens, vocab;
+    int32_t width, units;               // units: vectors of a row
+    int32_t id_bytes, accumulate;
+    float scale;
+    // backward
+    uint2 *order;                       // (id, token), sorted; ids outside the table last, as vocab
+    float *head, *tail;                 // partial rows of chunks, `pitch` floats apart
+    int64_t pitch, chunks;
+    int32_t chunk, slabs;               // tokens of a chunk; warps side by side over a row
+    int64_t sum_blocks;
+};
+
+// An id outside the table as vocab.
+__device__ __forceinline__ uint32_t id_at(const void *ids, int id_bytes, int64_t i, int64_t vocab)
+{
+    const int64_t id = id_bytes == 4 ? (int64_t)static_cast<const int32_t *>(ids)[i] : static_cast<const int64_t *>(ids)[i];
+    return (uint32_t)(id >= 0 && id < vocab ? id : vocab);
+}
+
+template <typename T, int V> __device__ __forceinline__ void load(Vec<T, V> &r, const T *p)
+{
+    r.word = *reinterpret_cast<const decltype(r.word) *>(p);
+}
+template <typename T, int V> __device__ __forceinline__ void load_once(Vec<T, V> &r, const T *p)
+{
+    r.word = __ldcs(reinterpret_cast<const decltype(r.word) *>(p));
+}
+template <typename T, int V> __device__ __forceinline__ void store(const Vec<T, V> &r, T *p)
+{
+    *reinterpret_cast<decltype(r.word) *>(p) = r.word;
+}
+
+// A block's threads are `lanes` across a row (blockDim.x) and blockDim.y rows; a
+// thread has kForwardRows rows under way.
+template <typename W, typename O, int V>
+__global__ void __launch_bounds__(kForwardThreads) rikfad_embed_forward_kernel(const __grid_constant__ EmbedParams p)
+{
+    wait_for_predecessor();
+    allow_successor_launch();
+    const W *table = static_cast<const W *>(p.table);
+    const int64_t first = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * kForwardRows;
+    const W *from[kForwardRows];
+    O *to[kForwardRows];
+    bool inside[kForwardRows];
+#pragma unroll
+    for (int r = 0; r < kForwardRows; ++r) {
+        const int64_t t = first + r;
+        const uint32_t id = t < p.tokens ? id_at(p.ids, p.id_bytes, t, p.vocab) : (uint32_t)p.vocab;
+        inside[r] = id < p.vocab;
+        from[r] = table + id * p.table_stride;
+        to[r] = t < p.tokens ? static_cast<O *>(p.rows) + t * p.row_stride : nullptr;
+    }
+    for (int u = blockIdx.y * blockDim.x + threadIdx.x; u < p.units; u += blockDim.x * gridDim.y) {
+        Vec<W, V> in[kForwardRows];
+#pragma unroll
+        for (int r = 0; r < kForwardRows; ++r)
+            if (inside[r])
+                load(in[r], from[r] + (int64_t)u * V);
+#pragma unroll
+        for (int r = 0; r < kForwardRows; ++r) {
+            float f[V];
+            widen(in[r], f);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                f[e] = inside[r] ? f[e] * p.scale : 0.f;
+            Vec<O, V> out;
+            narrow(f, out);
+            if (to[r])
+                store(out, to[r] + (int64_t)u * V);
+        }
+    }
+}
+
+// --------------------------------------------------------------- sorted tokens
+
+struct SortParams {
+    const void *ids;
+    uint2 *from, *to;               // of the passes in turn; the last one writes to `to`
+    int64_t vocab;
+    int32_t tokens, id_bytes, passes, bits;
+};
+
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ uint32_t cluster_read(const uint32_t *mine, int rank)
+{
+    uint32_t at, v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+
+// Exclusive sum over the block's threads.
+__device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t *sums)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t s = v;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const uint32_t o = __shfl_up_sync(~0u, s, d);
+        s += lane >= d ? o : 0;
+    }
+    if (lane == 31)
+        sums[warp] = s;
+    __syncthreads();
+    uint32_t w = lane < kSortWarps ? sums[lane] : 0;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const uint32_t o = __shfl_up_sync(~0u, w, d);
+        w += lane >= d ? o : 0;
+    }
+    const uint32_t before = __shfl_sync(~0u, w, max(warp - 1, 0));
+    return s - v + (warp ? before : 0);
+}
+
+// One cluster of 8 blocks sorts the tokens by id, `bits` bits a pass, the lowest
+// first.  Every block has a run of the pass's input: it counts its digits, learns the
+// other blocks' counts through their shared memory, and moves its entries, a tile
+// at a time, each warp's 32 neighbours in turn, so that equal digits keep their order.
+__global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const __grid_constant__ SortParams p)
+{
+    extern __shared__ uint32_t smem[];
+    const int bins = 1 << p.bits;
+    uint32_t *total = smem, *base = total + bins, *start = base + bins, *sums = start + bins;
+    uint16_t *counts = reinterpret_cast<uint16_t *>(sums + 32);     // [warp][digit]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t rank;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const int64_t share = ((int64_t)p.tokens + kSortCtas - 1) / kSortCtas;
+    const int begin = (int)min(share * rank, (int64_t)p.tokens), end = (int)min(share * (rank + 1), (int64_t)p.tokens);
+    wait_for_predecessor();
+    allow_successor_launch();
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const uint2 *from = (p.passes - pass) % 2 ? p.from : p.to;
+        uint2 *to = (p.passes - pass) % 2 ? p.to : p.from;
+        const int shift = pass * p.bits;
+        auto entry = [&](int i) {
+            return pass == 0 ? make_uint2(id_at(p.ids, p.id_bytes, i, p.vocab), (uint32_t)i) : __ldcg(from + i);
+        };
+        for (int b = threadIdx.x; b < bins; b += kSortThreads)
+            total[b] = 0;
+        __syncthreads();
+        for (int i = begin + threadIdx.x; i < end; i += kSortThreads)
+            atomicAdd(total + (entry(i).x >> shift & (bins - 1)), 1u);      // integers: any order
+        cluster_barrier();
+        {
+            uint32_t before = 0, all = 0;
+            if (threadIdx.x < bins)
+                for (int r = 0; r < kSortCtas; ++r) {
+                    const uint32_t n = cluster_read(total + threadIdx.x, r);
+                    before += r < rank ? n : 0;
+                    all += n;
+                }
+            const uint32_t first = block_exclusive(all, sums);
+            if (threadIdx.x < bins)
+                base[threadIdx.x] = first + before;
+        }
+        for (int tile = begin; tile < end; tile += kSortTile) {
+            for (int b = threadIdx.x; b < bins * kSortWarps / 2; b += kSortThreads)
+                reinterpret_cast<uint32_t *>(counts)[b] = 0;
+            __syncthreads();
+            uint2 e[kSortItems];
+            uint32_t place[kSortItems];
+            uint16_t *mine = counts + warp * bins;
+#pragma unroll
+            for (int k = 0; k < kSortItems; ++k) {
+                const int i = tile + (warp * kSortItems + k) * 32 + lane;
+                e[k] = i < end ? entry(i) : make_uint2(0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < kSortItems; ++k) {
+                const int i = tile + (warp * kSortItems + k) * 32 + lane;
+                const uint32_t digit = e[k].x >> shift & (bins - 1);
+                const uint32_t same = __match_any_sync(~0u, i < end ? digit : ~0u);
+                const int leader = __ffs(same) - 1;
+                uint32_t old = 0;
+                if (lane == leader && i < end) {
+                    old = mine[digit];
+                    mine[digit] = (uint16_t)(old + __popc(same));
+                }
+                __syncwarp();
+                place[k] = __shfl_sync(~0u, old, leader) + __popc(same & ((1u << lane) - 1));
+            }
+            __syncthreads();
+            if (threadIdx.x < bins) {
+                uint32_t n = 0;
+                for (int w = 0; w < kSortWarps; ++w) {
+                    const uint32_t here = counts[w * bins + threadIdx.x];
+                    counts[w * bins + threadIdx.x] = (uint16_t)n;
+                    n += here;
+                }
+                start[threadIdx.x] = base[threadIdx.x];
+                base[threadIdx.x] += n;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kSortItems; ++k) {
+                const int i = tile + (warp * kSortItems + k) * 32 + lane;
+                const uint32_t digit = e[k].x >> shift & (bins - 1);
+                if (i < end)
+                    to[start[digit] + mine[digit] + place[k]] = e[k];
+            }
+            __syncthreads();
+        }
+        cluster_barrier();          // the next pass reads what every block wrote
+    }
+}
+
+// -------------------------------------------------------------------- the sums
+
+// The first of the n sorted entries whose id is at least `id`.
+__device__ __forceinline__ int64_t lower_bound(const uint2 *order, int64_t n, uint32_t id)
+{
+    int64_t lo = 0;
+    while (n > 0) {
+        const int64_t half = n / 2;
+        const bool less = order[lo + half].x < id;
+        lo = less ? lo + half + 1 : lo;
+        n = less ? n - half - 1 : half;
+    }
+    return lo;
+}
+
+template <typename W, int V>
+__device__ __forceinline__ void write_row(const EmbedParams &p, uint32_t id, int unit, float (&sum)[V])
+{
+    W *at = static_cast<W *>(p.table) + id * p.table_stride + (int64_t)unit * V;
+    Vec<W, V> r;
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        sum[e] *= p.scale;
+    if (p.accumulate) {
+        float old[V];
+        load(r, at);
+        widen(r, old);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            sum[e] += old[e];
+    }
+    narrow(sum, r);
+    store(r, at);
+}
+
+// The first sum_blocks blocks sum chunks of sorted tokens, a warp 32 vectors of the
+// row; the others write zeros to the rows without a token, 32 rows a warp.
+template <typename W, typename O, int V>
+__global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __grid_constant__ EmbedParams p)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    wait_for_predecessor();
+    allow_successor_launch();
+    if (blockIdx.x >= p.sum_blocks) {
+        const int64_t row0 = ((blockIdx.x - p.sum_blocks) * kSumWarps + warp) * 32, row = row0 + lane;
+        bool absent = false;
+        if (row < p.vocab) {
+            const int64_t at = lower_bound(p.order, p.tokens, (uint32_t)row);
+            absent = at == p.tokens || p.order[at].x != row;
+        }
+        uint32_t todo = __ballot_sync(~0u, absent);
+        float zero[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            zero[e] = 0.f;
+        Vec<W, V> r;
+        narrow(zero, r);
+        while (todo) {
+            W *at = static_cast<W *>(p.table) + (row0 + __ffs(todo) - 1) * p.table_stride;
+            todo &= todo - 1;
+            for (int u = lane; u < p.units; u += 32)
+                store(r, at + (int64_t)u * V);
+        }
+        return;
+    }
+    const int64_t item = blockIdx.x * kSumWarps + warp, chunk = item / p.slabs;
+    if (chunk >= p.chunks)
+        return;
+    const int unit = (int)(item % p.slabs) * 32 + lane;
+    const bool active = unit < p.units;
+    const int64_t first = chunk * p.chunk, last = min(first + p.chunk, p.tokens);
+    const O *rows = static_cast<const O *>(p.rows) + (int64_t)unit * V;
+    uint32_t run = p.order[first].x;
+    bool from_before = first > 0 && p.order[first - 1].x == run;
+    const uint32_t after = last < p.tokens ? p.order[last].x : ~0u;
+    float sum[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        sum[e] = 0.f;
+    auto finish = [&](bool goes_on) {
+        if (active && run < p.vocab) {
+            if (from_before || goes_on) {
+                float *part = (from_before ? p.head : p.tail) + chunk * p.pitch + (int64_t)unit * V;
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    part[e] = sum[e];
+            } else
+                write_row<W, V>(p, run, unit, sum);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            sum[e] = 0.f;
+        from_before = false;
+    };
+    for (int64_t base = first; base < last; base += 32) {
+        const uint2 mine = base + lane < last ? p.order[base + lane] : make_uint2(~0u, 0);
+        const int here = (int)min((int64_t)32, last - base);
+        for (int j = 0; j < here; j += kSumAhead) {
+            Vec<O, V> in[kSumAhead];
+#pragma unroll
+            for (int k = 0; k < kSumAhead; ++k) {
+                const uint32_t id = __shfl_sync(~0u, mine.x, j + k), token = __shfl_sync(~0u, mine.y, j + k);
+                if (active && id < p.vocab)
+                    load_once(in[k], rows + token * p.row_stride);
+            }
+#pragma unroll
+            for (int k = 0; k < kSumAhead; ++k) {
+                const uint32_t id = __shfl_sync(~0u, mine.x, j + k);
+                if (j + k >= here)
+                    break;
+                if (id != run) {
+                    finish(false);
+                    run = id;
+                }
+                if (active && id < p.vocab) {
+                    float f[V];
+                    widen(in[k], f);
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        sum[e] += f[e];
+                }
+            }
+        }
+    }
+    finish(run == after);
+}
+
+// Runs over several chunks: the partial row of the chunk where one starts, then those
+// of the chunks that it goes on in.  A block has 128 columns of 32 chunks that may
+// start such a run; runs of up to 32 more chunks are a warp's, longer ones the block's.
+template <typename W> __global__ void __launch_bounds__(kJoinThreads) rikfad_embed_join_kernel(const __grid_constant__ EmbedParams p)
+{
+    __shared__ float4 part[kJoinWarps][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    wait_for_predecessor();
+    allow_successor_launch();
+    const int64_t mine = (int64_t)lane * gridDim.x + blockIdx.x;     // neighbours, often of one run, to different blocks
+    bool starts = false;
+    if (mine + 1 < p.chunks) {
+        const int64_t next = (mine + 1) * p.chunk;
+        const uint32_t id = p.order[next].x;
+        starts = id < p.vocab && p.order[next - 1].x == id && (mine == 0 || p.order[mine * p.chunk - 1].x != id);
+    }
+    const uint32_t owners = __ballot_sync(~0u, starts);
+    const int64_t column = (int64_t)blockIdx.y * 128 + lane * 4;
+    const bool active = column < p.pitch;
+    auto add = [&](float4 &s, const float *row) {
+        if (active) {
+            const float4 v = __ldcs(reinterpret_cast<const float4 *>(row + column));
+            s.x += v.x;
+            s.y += v.y;
+            s.z += v.z;
+            s.w += v.w;
+        }
+    };
+    auto write = [&](uint32_t id, const float4 &s) {
+        const float v[4] = {s.x, s.y, s.z, s.w};
+        for (int e = 0; e < 4; ++e)
+            if (column + e < p.width) {
+                float one[1] = {v[e]};
+                write_row<W, 1>(p, id, (int)(column + e), one);
+            }
+    };
+    uint32_t longer = 0;
+    int turn = 0;
+    for (uint32_t left = owners; left; left &= left - 1, ++turn) {
+        const int64_t chunk = (int64_t)(__ffs(left) - 1) * gridDim.x + blockIdx.x;
+        const uint32_t id = p.order[(chunk + 1) * p.chunk].x;
+        const int64_t c = chunk + 1 + lane;
+        const uint32_t more = __ballot_sync(~0u, c < p.chunks && p.order[c * p.chunk].x == id);
+        if (more == ~0u) {
+            longer |= left & -left;
+            continue;
+        }
+        if (turn % kJoinWarps != warp)
+            continue;
+        const int n = __ffs(~more) - 1;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        add(s, p.tail + chunk * p.pitch);
+        for (int j = 0; j < n; ++j)
+            add(s, p.head + (chunk + 1 + j) * p.pitch);
+        write(id, s);
+    }
+    for (; longer; longer &= longer - 1) {
+        const int64_t chunk = (int64_t)(__ffs(longer) - 1) * gridDim.x + blockIdx.x;
+        const uint32_t id = p.order[(chunk + 1) * p.chunk].x;
+        int64_t lo = chunk + 33, n = p.chunks - lo;        // the first chunk that does not start with id
+        while (n > 0) {
+            const int64_t half = n / 2;
+            const bool same = p.order[(lo + half) * p.chunk].x == id;
+            lo = same ? lo + half + 1 : lo;
+            n = same ? n - half - 1 : half;
+        }
+        const int64_t count = lo - chunk - 1, share = (count + kJoinWarps - 1) / kJoinWarps;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (warp == 0)
+            add(s, p.tail + chunk * p.pitch);
+        const int64_t to = min(count, share * (warp + 1));
+#pragma unroll 8
+        for (int64_t j = share * warp; j < to; ++j)
+            add(s, p.head + (chunk + 1 + j) * p.pitch);
+        part[warp][lane] = s;
+        __syncthreads();
+        if (warp == 0) {
+            for (int w = 1; w < kJoinWarps; ++w) {
+                const float4 v = part[w][lane];
+                s.x += v.x;
+                s.y += v.y;
+                s.z += v.z;
+                s.w += v.w;
+            }
+            write(id, s);
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------------ host
+
+int bad(const std::string &msg) { return report_error(RIKFAD_ERR_ARG, msg); }
+
+int check_sizes(const rikfad_embedding *p)
+{
+    if (p == nullptr)
+        return bad("p is NULL");
+    if (p->tokens < 0 || p->tokens > (int64_t)1 << 30 || p->vocab < 0 || p->vocab > (int64_t)1 << 30)
+        return bad("tokens and vocab must be in [0, 2^30]");
+    if (p->width < 1 || p->width > 1 << 20)
+        return bad("width must be in [1, 2^20]");
+    if (!dtype_ok(p->table_dtype) || !dtype_ok(p->dtype))
+        return bad("table_dtype and dtype must be a rikfad_dtype");
+    if (p->id_bytes != 4 && p->id_bytes != 8)
+        return bad("id_bytes must be 4 or 8");
+    if (!std::isfinite(p->scale) || !std::isfinite((float)p->scale))
+        return bad("scale must be finite");
+    return RIKFAD_OK;
+}
+
+int check_rows(const rikfad_rows &r, const char *name, int dtype, int64_t rows, int64_t width, int device)
+{
+    if (rows == 0)
+        return RIKFAD_OK;
+    if (r.data == nullptr)
+        return bad(std::string(name) + " is NULL");
+    if (rows > 1 && (r.stride < width || r.stride > (int64_t)1 << 32))
+        return bad(std::string("the row stride of ") + name + " must be at least width");
+    if ((uintptr_t)r.data % (uintptr_t)dtype_bytes(dtype))
+        return report_error(RIKFAD_ERR_ALIGN, std::string(name) + " is not aligned to its element type");
+    return check_address(r.data, device, name);
+}
+
+int check(const rikfad_embedding *p, int &device)
+{
+    int rc = check_sizes(p);
+    if (rc)
+        return rc;
+    const cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess)
+        return report_cuda(e, "cudaGetDevice");
+    if (p->tokens > 0) {
+        if (p->ids == nullptr)
+            return bad("ids is NULL");
+        if ((uintptr_t)p->ids % (uintptr_t)p->id_bytes)
+            return report_error(RIKFAD_ERR_ALIGN, "ids is not aligned");
+        rc = check_address(p->ids, device, "ids");
+    }
+    if (!rc) rc = check_rows(p->table, "table", p->table_dtype, p->vocab, p->width, device);
+    if (!rc) rc = check_rows(p->rows, "rows", p->dtype, p->tokens, p->width, device);
+    return rc;
+}
+
+// The widest vectors, of at most 16 bytes in the wider type, that the width, the
+// strides and the addresses allow.
+int vector_of(const rikfad_embedding *p)
+{
+    const int tb = dtype_bytes(p->table_dtype), rb = dtype_bytes(p->dtype);
+    uint64_t parts = (uint64_t)p->width | (uint64_t)(uintptr_t)p->table.data / tb | (uint64_t)(uintptr_t)p->rows.data / rb;
+    if (p->vocab > 1)
+        parts |= (uint64_t)p->table.stride;
+    if (p->tokens > 1)
+        parts |= (uint64_t)p->rows.stride;
+    int v = 16 / std::max(tb, rb);
+    while (parts % v)
+        v /= 2;
+    return v;
+}
+
+EmbedParams params(const rikfad_embedding *p)
+{
+    EmbedParams e{};
+    e.ids = p->ids;
+    e.table = p->table.data;
+    e.rows = p->rows.data;
+    e.table_stride = p->vocab > 1 ? p->table.stride : 0;
+    e.row_stride = p->tokens > 1 ? p->rows.stride : 0;
+    e.tokens = p->tokens;
+    e.vocab = p->vocab;
+    e.width = (int32_t)p->width;
+    e.id_bytes = p->id_bytes;
+    e.accumulate = p->accumulate;
+    e.scale = (float)p->scale;
+    return e;
+}
+
+template <typename W, typename O, int V> cudaError_t launch_forward(EmbedParams p, cudaStream_t s)
+{
+    p.units = p.width / V;
+    int lanes = 32;
+    while (lanes < kForwardThreads && lanes < p.units)
+        lanes *= 2;
+    const int rows = kForwardThreads / lanes;
+    const int64_t blocks = (p.tokens + rows * kForwardRows - 1) / (rows * kForwardRows);
+    // few rows: several blocks for each
+    const int64_t most = (p.units + lanes - 1) / lanes;
+    const int64_t across = std::max<int64_t>(1, std::min<int64_t>(most, 4 * kSms / blocks));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks, (unsigned)across);
+    cfg.blockDim = dim3((unsigned)lanes, (unsigned)rows);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, rikfad_embed_forward_kernel<W, O, V>, p);
+}
+
+cudaError_t launch_sort(const SortParams &p, cudaStream_t s)
+{
+    const int bins = 1 << p.bits;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kSortCtas);
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.dynamicSmemBytes = sizeof(uint32_t) * (3 * bins + 32) + sizeof(uint16_t) * kSortWarps * bins;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kSortCtas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, rikfad_embed_sort_kernel, p);
+}
+
+struct Workspace {
+    int64_t chunk, chunks, pitch;
+    size_t entries, bytes;              // bytes of one list of entries, of all
+};
+
+Workspace workspace_of(const rikfad_embedding *p)
+{
+    Workspace w;
+    w.chunk = 32;
+    w.chunks = (p->tokens + w.chunk - 1) / w.chunk;
+    w.pitch = (p->width + 3) / 4 * 4;
+    w.entries = ((size_t)p->tokens * sizeof(uint2) + 15) / 16 * 16;
+    w.bytes = 2 * w.entries + 2 * (size_t)w.chunks * (size_t)w.pitch * sizeof(float);
+    return w;
+}
+
+template <typename W, typename O, int V> cudaError_t launch_backward(EmbedParams p, cudaStream_t s)
+{
+    p.units = p.width / V;
+    p.slabs = (p.units + 31) / 32;
+    p.sum_blocks = (p.chunks * p.slabs + kSumWarps - 1) / kSumWarps;
+    const int64_t zeros = p.accumulate ? 0 : (p.vocab + 32 * kSumWarps - 1) / (32 * kSumWarps);
+    if (p.sum_blocks + zeros == 0)
+        return cudaSuccess;
+    if (p.sum_blocks + zeros > INT32_MAX)
+        return cudaErrorInvalidConfiguration;
+    cudaError_t e = launch_chained(rikfad_embed_sum_kernel<W, O, V>, dim3((unsigned)(p.sum_blocks + zeros)), kSumThreads, 0, s, p);
+    if (e != cudaSuccess || p.chunks < 2)
+        return e;
+    return launch_chained(rikfad_embed_join_kernel<W>, dim3((unsigned)((p.chunks + 31) / 32), (unsigned)((p.pitch + 127) / 128)),
+                          kJoinThreads, 0, s, p);
+}
+
+template <typename W, typename O, bool BACKWARD, int V> cudaError_t launch(const EmbedParams &p, int v, cudaStream_t s)
+{
+    if constexpr (V > 1)
+        if (v < V)
+            return launch<W, O, BACKWARD, V / 2>(p, v, s);
+    if constexpr (BACKWARD)
+        return launch_backward<W, O, V>(p, s);
+    else
+        return launch_forward<W, O, V>(p, s);
+}
+
+template <typename W, bool BACKWARD> cudaError_t launch(const EmbedParams &p, int dtype, int v, cudaStream_t s)
+{
+    constexpr int kNarrow = sizeof(W) == 2 ? 8 : 4;
+    return dtype == RIKFAD_F32    ? launch<W, float, BACKWARD, 4>(p, v, s)
+           : dtype == RIKFAD_BF16 ? launch<W, __nv_bfloat16, BACKWARD, kNarrow>(p, v, s)
+                                  : launch<W, __half, BACKWARD, kNarrow>(p, v, s);
+}
+
+template <bool BACKWARD> cudaError_t launch(const rikfad_embedding *d, const EmbedParams &p, cudaStream_t s)
+{
+    const int v = vector_of(d);
+    return d->table_dtype == RIKFAD_F32    ? launch<float, BACKWARD>(p, d->dtype, v, s)
+           : d->table_dtype == RIKFAD_BF16 ? launch<__nv_bfloat16, BACKWARD>(p, d->dtype, v, s)
+                                           : launch<__half, BACKWARD>(p, d->dtype, v, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+RIKFAD_API size_t rikfad_embedding_workspace(const rikfad_embedding *p)
+{
+    RK_ENTRY_BEGIN
+    if (check_sizes(p))
+        return 0;
+    report_error(RIKFAD_OK, "");
+    return workspace_of(p).bytes;
+    }
+    catch (...)
+    {
+        return 0;
+    }
+}
+
+RIKFAD_API int rikfad_embedding_forward(const rikfad_embedding *p, void *stream)
+{
+    RK_ENTRY_BEGIN
+    int device = -1;
+    const int rc = check(p, device);
+    if (rc)
+        return rc;
+    cudaError_t e = cudaPeekAtLastError();
+    if (e != cudaSuccess)
+        return report_cuda(e, "earlier CUDA error");
+    if (p->tokens == 0)
+        return RIKFAD_OK;
+    e = launch<false>(p, params(p), (cudaStream_t)stream);
+    return e == cudaSuccess ? RIKFAD_OK : report_cuda(e, "launch rikfad_embed_forward_kernel");
+    RK_ENTRY_END
+}
+
+RIKFAD_API int rikfad_embedding_backward(const rikfad_embedding *p, void *stream)
+{
+    RK_ENTRY_BEGIN
+    int device = -1;
+    int rc = check(p, device);
+    if (rc)
+        return rc;
+    const Workspace w = workspace_of(p);
+    if (w.bytes > 0) {
+        if (p->workspace == nullptr || p->workspace_bytes < w.bytes)
+            return bad("the workspace is smaller than rikfad_embedding_workspace");
+        if ((uintptr_t)p->workspace % 16)
+            return report_error(RIKFAD_ERR_ALIGN, "workspace is not aligned");
+        rc = check_address(p->workspace, device, "workspace");
+        if (rc)
+            return rc;
+    }
+    cudaError_t e = cudaPeekAtLastError();
+    if (e != cudaSuccess)
+        return report_cuda(e, "earlier CUDA error");
+    if (p->vocab == 0)
+        return RIKFAD_OK;
+    EmbedParams q = params(p);
+    char *at = static_cast<char *>(p->workspace);
+    q.order = reinterpret_cast<uint2 *>(at);
+    q.head = reinterpret_cast<float *>(at + 2 * w.entries);
+    q.tail = q.head + w.chunks * w.pitch;
+    q.chunk = (int32_t)w.chunk;
+    q.chunks = w.chunks;
+    q.pitch = w.pitch;
+    const cudaStream_t s = (cudaStream_t)stream;
+    if (p->tokens > 0) {
+        SortParams r{};
+        r.ids = p->ids;
+        r.to = q.order;
+        r.from = reinterpret_cast<uint2 *>(at + w.entries);
+        r.vocab = p->vocab;
+        r.tokens = (int32_t)p->tokens;
+        r.id_bytes = p->id_bytes;
+        int bits = 1;                   // of ids up to vocab
+        while (p->vocab >> bits)
+            ++bits;
+        r.passes = (bits + kSortBits - 1) / kSortBits;
+        r.bits = (bits + r.passes - 1) / r.passes;
+        e = launch_sort(r, s);
+        if (e != cudaSuccess)
+            return report_cuda(e, "launch rikfad_embed_sort_kernel");
+    }
+    e = launch<true>(p, q, s);
+    return e == cudaSuccess ? RIKFAD_OK : report_cuda(e, "launch of the embedding's backward kernels");
+    RK_ENTRY_END
+}
+
+}  // extern "C"

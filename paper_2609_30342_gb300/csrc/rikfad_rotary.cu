@@ -41,46 +41,6 @@ struct RotaryParams {
     bool copy;                          // elements beyond rotary_dim are copied
 };
 
-// V elements as one load.
-template <int BYTES> struct Word;
-template <> struct Word<2> { using type = uint16_t; };
-template <> struct Word<4> { using type = uint32_t; };
-template <> struct Word<8> { using type = uint2; };
-template <> struct Word<16> { using type = uint4; };
-
-template <typename T, int V> union Vec {
-    typename Word<V * sizeof(T)>::type word;
-    uint32_t pairs[V * sizeof(T) >= 4 ? V * sizeof(T) / 4 : 1];
-    T v[V];
-    __device__ __forceinline__ Vec() {}
-};
-
-template <typename T, int V> __device__ __forceinline__ void widen(const Vec<T, V> &r, float (&f)[V])
-{
-    if constexpr (sizeof(T) == 2 && V > 1) {
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i)
-            unpack2(r.pairs[i], f[2 * i], f[2 * i + 1], T());
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            f[i] = to_f32(r.v[i]);
-    }
-}
-
-template <typename T, int V> __device__ __forceinline__ void narrow(const float (&f)[V], Vec<T, V> &r)
-{
-    if constexpr (sizeof(T) == 2 && V > 1) {
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i)
-            r.pairs[i] = pack2(f[2 * i], f[2 * i + 1], T());
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            r.v[i] = from_f32<T>(f[i]);
-    }
-}
-
 // Where a thread is in its tile, and how it goes on: divisions once, not per unit.
 struct Walk {
     int slot, head, unit;       // token within the tile, head of both lists, unit of the head

@@ -1,5 +1,5 @@
-// rikfad_types.cuh -- float32, bfloat16 and float16 elements as float32, alone
-// and eight at a time, for the operators beside the optimiser step.
+// rikfad_types.cuh -- float32, bfloat16 and float16 elements as float32, alone,
+// eight at a time and in vectors of a size given by the template, for the operators beside the optimiser step.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -98,6 +98,46 @@ template <> __device__ __forceinline__ void store_raw8_cs<float>(float *p, const
 {
     __stcs(reinterpret_cast<float4 *>(p), r.a);
     __stcs(reinterpret_cast<float4 *>(p) + 1, r.b);
+}
+
+// V elements as one load.
+template <int BYTES> struct Word;
+template <> struct Word<2> { using type = uint16_t; };
+template <> struct Word<4> { using type = uint32_t; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<16> { using type = uint4; };
+
+template <typename T, int V> union Vec {
+    typename Word<V * sizeof(T)>::type word;
+    uint32_t pairs[V * sizeof(T) >= 4 ? V * sizeof(T) / 4 : 1];
+    T v[V];
+    __device__ __forceinline__ Vec() {}
+};
+
+template <typename T, int V> __device__ __forceinline__ void widen(const Vec<T, V> &r, float (&f)[V])
+{
+    if constexpr (sizeof(T) == 2 && V > 1) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i)
+            unpack2(r.pairs[i], f[2 * i], f[2 * i + 1], T());
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            f[i] = to_f32(r.v[i]);
+    }
+}
+
+template <typename T, int V> __device__ __forceinline__ void narrow(const float (&f)[V], Vec<T, V> &r)
+{
+    if constexpr (sizeof(T) == 2 && V > 1) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i)
+            r.pairs[i] = pack2(f[2 * i], f[2 * i + 1], T());
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            r.v[i] = from_f32<T>(f[i]);
+    }
 }
 
 }  // namespace rikfad
