@@ -583,6 +583,57 @@ RIKFAD_API int rikfad_rotary_apply(const rikfad_rotary *p, void *stream);
 RIKFAD_API int rikfad_rotary_turns(const double *radians, int64_t n, uint64_t *turns);
 
 /*
+ * Norms of queries and keys per head with the rotation in the same pass: every
+ * head x of head_dim elements becomes
+ *   y = x r (.) weight,  r = 1 / sqrt(mean(x^2) + eps),  out = y turned
+ * by its token's position, as rikfad_rotary_apply turns it (layouts, turns,
+ * positions, magnitude; elements beyond rotary_dim are normed only).  The
+ * backward call gives, from dout,
+ *   dy = dout turned back,  g = dy (.) weight,
+ *   dx = r (g - x r^2 mean(g x)),  dweight = sum over heads and tokens of dy x r.
+ *   x          heads, element d of head j of token t of sequence b at
+ *              b x_batch + t x_token + j x_head + d; out and dout likewise
+ *   out        forward: the result; backward: dx.  May be x (equal strides), dx
+ *              may be dout too; otherwise it overlaps no input
+ *   weight     head_dim elements of param_dtype (RIKFAD_F32 or dtype); NULL: 1
+ *   dweight    backward: as weight, written; NULL: not wanted
+ *   workspace  backward: device memory of rikfad_rotary_norm_workspace bytes,
+ *              16-byte aligned; nothing kept
+ * 1 <= head_dim <= 512; batch, tokens and heads as for rikfad_rotary.  Sums are
+ * in float32 and in an order that goes by the sizes alone.  Nothing is
+ * synchronised or allocated.
+ */
+typedef struct {
+    const void *x, *dout, *weight;
+    void *out, *dweight;
+    int64_t heads;
+    int64_t x_batch, x_token, x_head;
+    int64_t out_batch, out_token, out_head;
+    int64_t dout_batch, dout_token, dout_head;
+} rikfad_rotary_norm_heads;
+
+typedef struct {
+    int64_t batch, tokens;
+    int32_t head_dim, rotary_dim, layout, dtype;
+    const uint64_t *turns;
+    const void *positions;
+    int64_t position_batch, start;
+    int32_t position_bytes, param_dtype;
+    int32_t nlists, reserved;
+    double magnitude, eps;
+    rikfad_rotary_norm_heads lists[2];
+    void *workspace;
+    size_t workspace_bytes;
+} rikfad_rotary_norm;
+
+RIKFAD_API int rikfad_rotary_norm_forward(const rikfad_rotary_norm *p, void *stream);
+RIKFAD_API int rikfad_rotary_norm_backward(const rikfad_rotary_norm *p, void *stream);
+
+/* Workspace bytes of the backward call for p's sizes (0 if it needs none); 0
+ * with a message in rikfad_last_error for sizes out of range. */
+RIKFAD_API size_t rikfad_rotary_norm_workspace(const rikfad_rotary_norm *p);
+
+/*
  * Token embedding: out_t = scale W[id_t] for `tokens` ids, a row of zeros for an
  * id outside [0, vocab) (padding), and the dense gradient of the table,
  *   dW_v = scale sum over the tokens t with id_t = v of dout_t,

@@ -21,6 +21,7 @@
 #include "rikfad.h"
 #include "rikfad_host.hpp"
 #include "rikfad_kernels.cuh"
+#include "rikfad_rotary.cuh"
 #include "rikfad_types.cuh"
 
 using namespace rikfad;
@@ -166,17 +167,9 @@ __global__ void __launch_bounds__(kRotaryThreads) rikfad_rotary_kernel(const __g
     for (int i = threadIdx.x; i < here * pairs; i += kRotaryThreads) {
         const int64_t at = token0 + i / pairs;
         const int64_t batch = p.d.batch == 1 ? 0 : at / p.d.tokens, token = at - batch * p.d.tokens;
-        int64_t position = p.d.start + token;
-        if (p.d.positions) {
-            const int64_t k = batch * p.d.position_batch + token;
-            position = p.d.position_bytes == 4 ? (int64_t)static_cast<const int32_t *>(p.d.positions)[k]
-                                               : static_cast<const int64_t *>(p.d.positions)[k];
-        }
-        // the turn's fraction in [-1/2, 1/2), in half turns for sincospi
-        const uint64_t turn = (uint64_t)position * p.d.turns[i % pairs];
-        float c, s;
-        sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &s, &c);
-        table[i] = make_float2(c * p.magnitude, s * p.sine_sign);
+        const int64_t position = token_position(p.d.positions, p.d.position_bytes, p.d.position_batch, p.d.start, batch, token);
+        const float2 cs = cosine_sine(position, p.d.turns[i % pairs]);
+        table[i] = make_float2(cs.x * p.magnitude, cs.y * p.sine_sign);
     }
     __syncthreads();
     allow_successor_launch();

@@ -2,11 +2,12 @@
 
 ``ResidualNorm``   u = residual_scale x + branch_scale gate * post(z),  h = pre(u), and all gradients
 ``Rotary``         heads turned by their token's position, and back
+``RotaryNorm``     heads normed, then turned, in one pass, and all gradients
 
 Each has explicit calls on CUDA tensors (``forward``/``backward``, ``rotate``) and is callable inside autograd.
-Argument checks and marshalling only: the work runs in the kernels behind ``rikfad_residual_norm_forward``,
-``rikfad_residual_norm_backward`` and ``rikfad_rotary_apply``, enqueued on the current stream of the tensors' device (or
-``stream``, to which what the call allocates then belongs; the inputs have to be ready on it).
+Argument checks and marshalling only: the work runs in the kernels behind ``rikfad_residual_norm_forward`` and
+``_backward``, ``rikfad_rotary_apply`` and ``rikfad_rotary_norm_forward`` and ``_backward``, enqueued on the current stream
+of the tensors' device (or ``stream``, to which what the call allocates then belongs; the inputs have to be ready on it).
 """
 import ctypes
 import math
@@ -26,10 +27,15 @@ _NORM = struct.Struct("=3q 4i 2i 4d 6q 4q 4q q 4q 6q 4q qQ")
 # struct rikfad_rotary: sizes, types, pointers, magnitude, two sets of heads
 _ROTARY = struct.Struct("=2q 4i qq2q 2i 2i d 18q")
 
+# struct rikfad_rotary_norm: sizes, types, pointers, positions, magnitude and eps, two sets of heads, workspace
+_ROTARY_NORM = struct.Struct("=2q 4i qq2q 2i 2i 2d 30q qQ")
+
 _NO_BACKWARD = (0,) * 16
 _NO_HEADS = (0,) * 9
+_NO_NORM_HEADS = (0,) * 15
 
 ResidualNormGrads = namedtuple("ResidualNormGrads", "x z gate post_weight post_bias pre_weight pre_bias")
+RotaryNormGrads = namedtuple("RotaryNormGrads", "q k q_weight k_weight")
 
 
 def _streaming(stream, t):
@@ -324,6 +330,37 @@ class Rotary:
             return t.data_ptr(), shape[1], 0, s[0], s[1]
         return t.data_ptr(), shape[2], s[0], s[1], s[2]
 
+    def _lead(self, q):
+        """(device, type, leading sizes, batch, tokens) of q."""
+        device, dtype = q.get_device(), q.dtype
+        if device < 0 or device != self._turns.get_device():
+            raise ValueError("q must be on %s, the device of the frequencies" % self._turns.device)
+        if dtype not in _TORCH:
+            raise ValueError("q must be float32, bfloat16 or float16")
+        lead = q.shape[:-2]
+        if len(lead) == 1:
+            return device, dtype, lead, 1, lead[0]
+        if len(lead) == 2:
+            return device, dtype, lead, *lead
+        raise ValueError("q must be [tokens, heads, head_dim] or [batch, tokens, heads, head_dim]")
+
+    @staticmethod
+    def _positions(positions, lead, tokens, device):
+        """(pointer, batch stride, bytes of a position)."""
+        if positions is None:
+            return 0, 0, 8
+        width = 4 if positions.dtype is torch.int32 else 8
+        if positions.get_device() != device or width == 8 and positions.dtype is not torch.int64:
+            raise ValueError("positions must be an int32 or int64 CUDA tensor on the device of q")
+        per_batch = 0
+        if len(lead) == 2 and positions.shape == lead:
+            per_batch = positions.stride(0)
+        elif positions.shape != (tokens,):
+            raise ValueError("positions must be [tokens] or [batch, tokens]")
+        if tokens > 1 and positions.stride(-1) != 1:
+            raise ValueError("positions must be contiguous along the tokens")
+        return positions.data_ptr(), per_batch, width
+
     def rotate(self, q, k=None, positions=None, start=0, inverse=False, out=None, stream=None):
         """(q', k') of queries and keys [tokens, heads, head_dim] or [batch, tokens, heads, head_dim] (k' None without
         k).  ``positions``: int32 or int64 CUDA tensor [tokens] or [batch, tokens]; default ``start`` + 0, 1, ...
@@ -335,30 +372,8 @@ class Rotary:
         for t in (q, k, positions):
             if t is not None and not isinstance(t, torch.Tensor):
                 raise ValueError("inputs must be tensors")
-        device, dtype, turns = q.get_device(), q.dtype, self._turns
-        if device < 0 or device != turns.get_device():
-            raise ValueError("q must be on %s, the device of the frequencies" % turns.device)
-        if dtype not in _TORCH:
-            raise ValueError("q must be float32, bfloat16 or float16")
-        lead = q.shape[:-2]
-        if len(lead) == 1:
-            batch, tokens = 1, lead[0]
-        elif len(lead) == 2:
-            batch, tokens = lead
-        else:
-            raise ValueError("q must be [tokens, heads, head_dim] or [batch, tokens, heads, head_dim]")
-        pp, pb, width = 0, 0, 8
-        if positions is not None:
-            width = 4 if positions.dtype is torch.int32 else 8
-            if positions.get_device() != device or width == 8 and positions.dtype is not torch.int64:
-                raise ValueError("positions must be an int32 or int64 CUDA tensor on the device of q")
-            if len(lead) == 2 and positions.shape == lead:
-                pb = positions.stride(0)
-            elif positions.shape != (tokens,):
-                raise ValueError("positions must be [tokens] or [batch, tokens]")
-            if tokens > 1 and positions.stride(-1) != 1:
-                raise ValueError("positions must be contiguous along the tokens")
-            pp = positions.data_ptr()
+        device, dtype, lead, batch, tokens = self._lead(q)
+        at, per_batch, width = self._positions(positions, lead, tokens, device)
         if out is None:
             dense = torch.contiguous_format
             out = (torch.empty_like(q, memory_format=dense),
@@ -374,7 +389,8 @@ class Rotary:
                 raise ValueError("the output of %s must have its shape" % name)
             lists += (ps, pd, heads, *from_, *to)
         block = _ROTARY.pack(batch, tokens, self.head_dim, self.rotary_dim, self._layout, _TORCH[dtype],
-                             turns.data_ptr(), pp, pb, start, width, 1 if inverse else 0, 1 if k is None else 2, 0,
+                             self._turns.data_ptr(), at, per_batch, start, width, 1 if inverse else 0,
+                             1 if k is None else 2, 0,
                              self.magnitude, *lists)
         rikfad._call_on(device, rikfad.lib().rikfad_rotary_apply, block, rikfad._raw_stream(device))
         return out[0], (None if k is None else out[1])
@@ -402,3 +418,130 @@ class _RotaryFunction(torch.autograd.Function):
             dq, dk = ctx.op.rotate(dq.contiguous(), None if dk is None else dk.contiguous(), positions=positions,
                                    start=ctx.start, inverse=True)
         return None, dq, dk, None, None
+
+
+class RotaryNorm(Rotary):
+    """Heads divided by their root mean square (of all ``head_dim`` elements, with ``eps``), times a weight per element,
+    then turned as ``Rotary`` turns them: out = R(position) (x / sqrt(mean(x^2) + eps) * weight).
+
+    Queries and keys have weights of their own, float32 or of the heads' type, arguments of the calls (absent: 1)."""
+
+    def __init__(self, head_dim, rotary_dim=None, base=10000.0, layout="half", scaling=None, frequencies=None,
+                 magnitude=None, eps=1e-6, device="cuda"):
+        if not 1 <= int(head_dim) <= 512:
+            raise ValueError("head_dim must be in [1, 512]")
+        if not (math.isfinite(eps) and eps >= 0):
+            raise ValueError("eps must be finite and >= 0")
+        super().__init__(head_dim, rotary_dim, base, layout, scaling, frequencies, magnitude, device)
+        self.eps = float(eps)
+
+    def _weights(self, weights, dtype, device):
+        """The weights' type, and their addresses."""
+        given = next((w for w in weights if w is not None), None)
+        if given is None:
+            return _F32, (0, 0)
+        pt = given.dtype
+        if pt is not _F32 and pt is not dtype:
+            raise ValueError("weights must be float32 or %s" % dtype)
+        for w in weights:
+            if w is not None and (w.dtype is not pt or w.get_device() != device or w.shape != (self.head_dim,)
+                                  or not w.is_contiguous()):
+                raise ValueError("weights must be %d contiguous elements of one type on the device of q" % self.head_dim)
+        return pt, tuple(0 if w is None else w.data_ptr() for w in weights)
+
+    def _block(self, first, positions, start, pt, lists, work=(0, 0)):
+        device, dtype, lead, batch, tokens = first
+        at, per_batch, width = self._positions(positions, lead, tokens, device)
+        return _ROTARY_NORM.pack(batch, tokens, self.head_dim, self.rotary_dim, self._layout, _TORCH[dtype],
+                                 self._turns.data_ptr(), at, per_batch, start, width, _TORCH[pt], len(lists) // 15, 0,
+                                 self.magnitude, self.eps, *lists, *(_NO_NORM_HEADS if len(lists) == 15 else ()), *work)
+
+    def forward(self, q, k=None, q_weight=None, k_weight=None, positions=None, start=0, out=None, stream=None):
+        """(q', k') of queries and keys [tokens, heads, head_dim] or [batch, tokens, heads, head_dim] (k' None without k),
+        with positions as for ``rotate``.  ``out``: (q', k') to write to; q and k themselves for in place."""
+        if stream is not None:
+            with _streaming(stream, q):
+                return self.forward(q, k, q_weight, k_weight, positions, start, out)
+        for t in (q, k, q_weight, k_weight, positions):
+            if t is not None and not isinstance(t, torch.Tensor):
+                raise ValueError("inputs must be tensors")
+        first = device, dtype, lead, batch, tokens = self._lead(q)
+        if k is None and k_weight is not None:
+            raise ValueError("k_weight needs k")
+        pt, weights = self._weights((q_weight, k_weight), dtype, device)
+        if out is None:
+            dense = torch.contiguous_format
+            out = (torch.empty_like(q, memory_format=dense),
+                   None if k is None else torch.empty_like(k, memory_format=dense))
+        lists = []
+        for name, src, dst, weight in (("q", q, out[0], weights[0]), ("k", k, out[1], weights[1])):
+            if src is None:
+                continue
+            px, heads, *from_ = self._heads(name, src, lead, dtype, device)
+            po, to_heads, *to = self._heads(name, dst, lead, dtype, device)
+            if to_heads != heads:
+                raise ValueError("the output of %s must have its shape" % name)
+            lists += (px, 0, weight, po, 0, heads, *from_, *to, 0, 0, 0)
+        rikfad._call_on(device, rikfad.lib().rikfad_rotary_norm_forward, self._block(first, positions, start, pt, lists),
+                        rikfad._raw_stream(device))
+        return out[0], (None if k is None else out[1])
+
+    def backward(self, dq, dk, q, k=None, q_weight=None, k_weight=None, positions=None, start=0, stream=None):
+        """``RotaryNormGrads`` of the forward call's inputs (None where the input is None), from the gradients of its
+        outputs.  Either of them may be None, with no gradients of that input and its weight then."""
+        if stream is not None:
+            with _streaming(stream, q):
+                return self.backward(dq, dk, q, k, q_weight, k_weight, positions, start)
+        for t in (dq, dk, q, k, q_weight, k_weight, positions):
+            if t is not None and not isinstance(t, torch.Tensor):
+                raise ValueError("inputs must be tensors")
+        first = device, dtype, lead, batch, tokens = self._lead(q)
+        if k is None and (dk is not None or k_weight is not None):
+            raise ValueError("dk and k_weight need k")
+        pt, weights = self._weights((q_weight, k_weight), dtype, device)
+        dense = torch.contiguous_format
+        lists, grads = [], []
+        for name, x, d, weight, pw in (("q", q, dq, q_weight, weights[0]), ("k", k, dk, k_weight, weights[1])):
+            if d is None:
+                grads += (None, None)
+                continue
+            px, heads, *from_ = self._heads(name, x, lead, dtype, device)
+            pd, d_heads, *d_from = self._heads("d" + name, d, lead, dtype, device)
+            if d_heads != heads:
+                raise ValueError("d%s must have the shape of %s" % (name, name))
+            dx, dw = torch.empty_like(x, memory_format=dense), None if weight is None else torch.empty_like(weight)
+            grads += (dx, dw)
+            st = dx.stride()
+            to = (0, st[0], st[1]) if len(st) == 3 else st[:3]
+            lists += (px, pd, pw, dx.data_ptr(), 0 if dw is None else dw.data_ptr(), heads, *from_, *to, *d_from)
+        if lists:
+            lib = rikfad.lib()
+            work = (0, 0)
+            if grads[1] is not None or grads[3] is not None:
+                nbytes = lib.rikfad_rotary_norm_workspace(self._block(first, positions, start, pt, lists))
+                buffer = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+                work = (buffer.data_ptr(), nbytes)
+            rikfad._call_on(device, lib.rikfad_rotary_norm_backward, self._block(first, positions, start, pt, lists, work),
+                            rikfad._raw_stream(device))
+        return RotaryNormGrads(grads[0], grads[2], grads[1], grads[3])
+
+    def __call__(self, q, k=None, q_weight=None, k_weight=None, positions=None, start=0):
+        """(q', k') inside autograd."""
+        return _RotaryNormFunction.apply(self, q, k, q_weight, k_weight, positions, start)
+
+
+class _RotaryNormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, op, q, k, q_weight, k_weight, positions, start):
+        ctx.op, ctx.start = op, start
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions)
+        return op.forward(q, k, q_weight, k_weight, positions, start)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq, dk):
+        dq, dk = (None if g is None else g.contiguous() for g in (dq, dk))
+        q, k, q_weight, k_weight, positions = ctx.saved_tensors
+        g = ctx.op.backward(dq, dk, q, k, q_weight, k_weight, positions, ctx.start)
+        return None, g.q, g.k, g.q_weight, g.k_weight, None, None

@@ -108,6 +108,9 @@ SIGNATURES = [
     ("rikfad_rotary_apply", ctypes.c_int, [_VP, _VP]),
     ("rikfad_rotary_turns", ctypes.c_int, [ctypes.POINTER(ctypes.c_double), ctypes.c_int64,
                                            ctypes.POINTER(ctypes.c_uint64)]),
+    ("rikfad_rotary_norm_forward", ctypes.c_int, [_VP, _VP]),
+    ("rikfad_rotary_norm_backward", ctypes.c_int, [_VP, _VP]),
+    ("rikfad_rotary_norm_workspace", ctypes.c_size_t, [_VP]),
     ("rikfad_embedding_forward", ctypes.c_int, [_VP, _VP]),
     ("rikfad_embedding_backward", ctypes.c_int, [_VP, _VP]),
     ("rikfad_embedding_workspace", ctypes.c_size_t, [_VP]),
