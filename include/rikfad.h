@@ -668,6 +668,51 @@ RIKFAD_API int rikfad_embedding_backward(const rikfad_embedding *p, void *stream
 RIKFAD_API size_t rikfad_embedding_workspace(const rikfad_embedding *p);
 
 /*
+ * Loss of rows of logits s against K logits t of a teacher at the indices i (its
+ * largest, say) and against a label, and its gradient:
+ *   p = softmax(t / T), q_T = softmax(s / T), q_1 = softmax(s)
+ *   loss = a T^2 sum_k p_k (log p_k - log q_T[i_k]) - b log q_1[label]
+ *   ds = grad_scale dloss (a T (q_T - p) + b (q_1 - e_label))
+ * with a = teacher_weight, b = label_weight, T = temperature.  A teacher's entry
+ * whose index is outside [0, vocab) or whose logit is -inf is absent, p is that of
+ * the others; a label outside [0, vocab) is absent.  A term with nothing left (or
+ * a weight of 0) adds nothing, and a row without a term has a loss of 0 and a
+ * gradient of 0, whatever its logits.  Entries that name one element add up.  Logits
+ * of -inf have a share of 0; a row of nothing else, or with NaN or +inf, has a loss
+ * and a gradient of NaN if it has a term.  Finite logits (the teacher's too)
+ * below -3.7e8 min(1, T), as masks are, count as that value; ones above 3.7e8
+ * min(1, T) count as +inf.
+ *   logits     `rows` rows of `vocab` elements of dtype
+ *   teacher    rows of k elements of teacher_dtype; index: of index_bytes (4 or 8)
+ *              bytes, signed.  Not read with k = 0
+ *   labels     device, label_bytes (4 or 8) bytes each, signed; NULL: none
+ *   loss       forward: device, `rows` floats
+ *   stats      device, 4 floats a row, 16-byte aligned: forward: written (NULL: not
+ *              kept); backward: what the forward call wrote for these inputs
+ *   dloss      device, `rows` floats, one for each row's loss; NULL: 1
+ *   dlogits    as logits: the gradient.  Forward: NULL if it is not wanted; with it,
+ *              one pass gives both.  May be logits (equal strides), otherwise it
+ *              overlaps nothing
+ * Rows are contiguous elements, `stride` apart (>= their columns where rows > 1).
+ * 0 <= rows <= 2^28, 1 <= vocab <= 2^24, 0 <= k <= 1024, 0.001 <= temperature <= 1000.
+ * Sums are in float32 and in an order that goes by the sizes and alignments alone.
+ * Nothing is synchronised or allocated.
+ */
+typedef struct {
+    int64_t rows, vocab;
+    int32_t k, dtype, teacher_dtype, index_bytes, label_bytes, reserved;
+    double temperature, teacher_weight, label_weight, grad_scale;
+    rikfad_rows logits, teacher, index;
+    const void *labels;
+    float *loss, *stats;
+    const float *dloss;
+    rikfad_rows dlogits;
+} rikfad_distillation;
+
+RIKFAD_API int rikfad_distillation_forward(const rikfad_distillation *p, void *stream);
+RIKFAD_API int rikfad_distillation_backward(const rikfad_distillation *p, void *stream);
+
+/*
  * Testing hooks.  These have no counterpart in the paper.
  *
  * rikfad_debug_check_failures: a library compiled with -DRIKFAD_CHECKED

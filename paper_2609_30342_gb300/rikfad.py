@@ -114,6 +114,8 @@ SIGNATURES = [
     ("rikfad_embedding_forward", ctypes.c_int, [_VP, _VP]),
     ("rikfad_embedding_backward", ctypes.c_int, [_VP, _VP]),
     ("rikfad_embedding_workspace", ctypes.c_size_t, [_VP]),
+    ("rikfad_distillation_forward", ctypes.c_int, [_VP, _VP]),
+    ("rikfad_distillation_backward", ctypes.c_int, [_VP, _VP]),
     ("rikfad_last_error", ctypes.c_char_p, []),
     ("rikfad_abi_version", ctypes.c_int, []),
 ]
