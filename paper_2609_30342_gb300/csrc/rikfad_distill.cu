@@ -17,6 +17,7 @@
 #include <cmath>
 #include <new>
 #include <string>
+#include <type_traits>
 
 #include "rikfad.h"
 #include "rikfad_host.hpp"
@@ -27,13 +28,16 @@ using namespace rikfad;
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxThreads = 1024;
 constexpr int kSms = 152;
 constexpr int kMaxEntries = 1024;           // of a teacher's row
 constexpr int kMaxCluster = 8;
+constexpr int64_t kResident = 540 << 10;   // bytes of rows under way on an SM
 // A reference's rounding is a factor of up to 2^(r 2^-24) in every power: r stays below
 // this, and lower logits count as the one there.
 constexpr float kFarthest = 0x1p29f;
+constexpr float kLargestSum = 0x1p40f;      // of a thread, beyond which its reference is too low
+constexpr int kEntriesAhead = 4;            // entries of a lane under way
 constexpr int kAhead = 4;                   // vectors of a thread under way
 
 struct Params {
@@ -45,19 +49,80 @@ struct Params {
     int64_t rows, logits_stride, teacher_stride, index_stride, dlogits_stride;
     int32_t vocab, k, teacher_dtype, index_bytes, label_bytes;
     int32_t cluster;                // blocks of a row
+    int32_t names;                  // places of the table of indices
     bool distils, labelled;         // the terms that the call has
     bool wide;                      // every row of dlogits starts as far from 16 bytes as the logits'
     float a, b;                     // a T and b, of the gradient
     float loss_a, loss_b;           // a T^2 ln 2 and b ln 2
     float c_t, c_1, grad_scale;     // log2(e) / T, log2(e)
     float lowest;                   // finite logits below it count as it
+    float lowest_t, lowest_1;       // references below which a row has nothing else
 };
+
+// Two float32 in one register pair: one instruction for both.
+struct Pair {
+    uint64_t w;
+};
+__device__ __forceinline__ Pair pair(float x, float y)
+{
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.w) : "f"(x), "f"(y));
+    return p;
+}
+__device__ __forceinline__ void apart(const Pair &p, float &x, float &y)
+{
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p.w));
+}
+__device__ __forceinline__ Pair fma2(const Pair &a, const Pair &b, const Pair &c)
+{
+    Pair p;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(p.w) : "l"(a.w), "l"(b.w), "l"(c.w));
+    return p;
+}
+__device__ __forceinline__ Pair add2(const Pair &a, const Pair &b)
+{
+    Pair p;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(p.w) : "l"(a.w), "l"(b.w));
+    return p;
+}
+__device__ __forceinline__ Pair mul2(const Pair &a, const Pair &b)
+{
+    Pair p;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(p.w) : "l"(a.w), "l"(b.w));
+    return p;
+}
 
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+__device__ __forceinline__ Pair exp2_fast(const Pair &p)
+{
+    float x, y;
+    apart(p, x, y);
+    return pair(exp2_fast(x), exp2_fast(y));
+}
+
+// The largest of a vector's elements; NaN is passed over.
+template <typename T, int V> __device__ __forceinline__ float largest(const Vec<T, V> &r)
+{
+    if constexpr (sizeof(T) == 2) {
+        using T2 = std::conditional_t<std::is_same_v<T, __half>, __half2, __nv_bfloat162>;
+        T2 m = *reinterpret_cast<const T2 *>(&r.pairs[0]);
+#pragma unroll
+        for (int i = 1; i < V / 2; ++i)
+            m = __hmax2(m, *reinterpret_cast<const T2 *>(&r.pairs[i]));
+        return fmaxf(to_f32(m.x), to_f32(m.y));
+    } else {
+        float m = r.v[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i)
+            m = fmaxf(m, r.v[i]);
+        return m;
+    }
 }
 
 __device__ __forceinline__ int64_t integer_at(const void *p, int bytes, int64_t i)
@@ -74,29 +139,64 @@ __device__ __forceinline__ float float_at(const void *p, int dtype, int64_t i)
 
 __device__ __forceinline__ float at_least(float x, float lowest) { return x < lowest && x > -INFINITY ? lowest : x; }
 
-// A maximum and the sums of 2^(x c - r), r = max c, at two temperatures.
-struct Sums {
-    float top, t, one;
+__device__ __forceinline__ float reference(float top, float c)
+{
+    const float r = top * c;
+    return top == -INFINITY ? 0.f : r > kFarthest ? INFINITY : r;
+}
 
-    __device__ __forceinline__ static float reference(float top, float c)
+// A row's element as it counts in sums: not below the lowest value.
+template <typename T> __device__ __forceinline__ float element(const T *row, int i, float lowest)
+{
+    return to_f32(from_f32<T>(at_least(to_f32(row[i]), lowest)));
+}
+
+// What a part's sum counts for a larger maximum.
+__device__ __forceinline__ float moved(float sum, float from, float to, float c)
+{
+    return sum == 0.f ? 0.f : sum * exp2_fast(reference(from, c) - reference(to, c));
+}
+
+// A maximum and the sums of 2^(x c - r), r = max c, at two temperatures (BOTH) or one.
+template <bool BOTH> struct Sums {
+    float top = -INFINITY, t = 0.f, one = 0.f;
+
+    __device__ __forceinline__ void add(float x, float sum_t, float sum_1, float c_t, float c_1)
     {
-        const float r = top * c;
-        return top == -INFINITY ? 0.f : r > kFarthest ? INFINITY : r;
-    }
-    // What a part's sum counts for a larger maximum.
-    __device__ __forceinline__ static float moved(float sum, float from, float to, float c)
-    {
-        return sum == 0.f ? 0.f : sum * exp2_fast(reference(from, c) - reference(to, c));
-    }
-    __device__ __forceinline__ void add(const Sums &o, float c_t, float c_1)
-    {
-        const float m = fmaxf(top, o.top);
-        t = moved(t, top, m, c_t) + moved(o.t, o.top, m, c_t);
-        one = moved(one, top, m, c_1) + moved(o.one, o.top, m, c_1);
+        const float m = fmaxf(top, x);
+        t = moved(t, top, m, c_t) + moved(sum_t, x, m, c_t);
+        if (BOTH)
+            one = moved(one, top, m, c_1) + moved(sum_1, x, m, c_1);
         top = m;
+    }
+    __device__ __forceinline__ void add_one(float x, float c_t, float c_1)
+    {
+        add(x, exp2_fast(fmaf(x, c_t, -reference(x, c_t))), exp2_fast(fmaf(x, c_1, -reference(x, c_1))), c_t, c_1);
+    }
+    // Those of the warp's lanes together, in all of them.
+    __device__ __forceinline__ void join(float c_t, float c_1)
+    {
+        float m = top;
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2)
+            m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+        t = moved(t, top, m, c_t);
+        if (BOTH)
+            one = moved(one, top, m, c_1);
+        top = m;
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) {
+            t += __shfl_xor_sync(~0u, t, d);
+            if (BOTH)
+                one += __shfl_xor_sync(~0u, one, d);
+        }
     }
 };
 
+__device__ __forceinline__ void cluster_arrive_relaxed()
+{
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void cluster_arrive()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -139,206 +239,234 @@ template <typename T> struct Slice {
 // from the statistics.
 enum Mode { kForward, kFused, kBackward };
 
-template <typename T, Mode MODE>
-__global__ void __launch_bounds__(kThreads) rikfad_distill_kernel(const __grid_constant__ Params p)
+// A row's entries in shared memory: log2 of the teacher's shares, the row's logits at
+// the indices and the indices; one that is absent, or whose logit is -inf, has index
+// -1.  The label is the last.
+struct Entries {
+    float *log_p, *at_index;
+    int *index, *names;
+    int terms;                  // which the row has: 1 the teacher's, 2 the label's
+    bool repeated;              // some of the teacher's in the block's slice name one element
+
+    __device__ __forceinline__ Entries(float *at, int count)
+        : log_p(at), at_index(at + count), index(reinterpret_cast<int *>(at + 2 * count)), names(index + count), terms(0), repeated(false)
+    {
+    }
+};
+
+// One warp loads row r's entries.
+template <typename T> __device__ __forceinline__ void load_entries(const Params &p, Entries &to, int64_t r, const Slice<T> &slice, int rank, bool gradient)
+{
+    const int lane = threadIdx.x & 31;
+    const T *row = static_cast<const T *>(p.logits) + r * p.logits_stride;
+    Sums<false> shares;
+    bool present = false;
+    const int64_t wanted = lane == 0 && p.labelled ? integer_at(p.labels, p.label_bytes, r) : -1;
+    const bool label = wanted >= 0 && wanted < p.vocab;
+    const int k = p.distils ? p.k : 0;
+    // all of a round's loads before the first one's use: a warp waits twice for kEntriesAhead x 32 entries
+    for (int e0 = lane; e0 < k; e0 += 32 * kEntriesAhead) {
+        int64_t i[kEntriesAhead];
+        float t[kEntriesAhead], x[kEntriesAhead];
+#pragma unroll
+        for (int j = 0; j < kEntriesAhead; ++j) {
+            const int e = e0 + 32 * j;
+            i[j] = e < k ? integer_at(p.index, p.index_bytes, r * p.index_stride + e) : -1;
+            t[j] = e < k ? float_at(p.teacher, p.teacher_dtype, r * p.teacher_stride + e) : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < kEntriesAhead; ++j) {
+            i[j] = i[j] < p.vocab && t[j] != -INFINITY ? i[j] : -1;
+            x[j] = i[j] >= 0 ? to_f32(row[i[j]]) : 0.f;
+        }
+        float top = shares.top;
+#pragma unroll
+        for (int j = 0; j < kEntriesAhead; ++j) {
+            const int e = e0 + 32 * j;
+            t[j] = at_least(t[j], p.lowest);
+            present = present || i[j] >= 0;
+            top = i[j] >= 0 ? fmaxf(top, t[j]) : top;
+            if (e < k) {
+                to.index[e] = i[j] >= 0 ? (int)i[j] : -1;
+                to.log_p[e] = t[j];
+                to.at_index[e] = x[j];
+            }
+        }
+        const float from = reference(top, p.c_t);
+        shares.t = moved(shares.t, shares.top, top, p.c_t);
+        shares.top = top;
+#pragma unroll
+        for (int j = 0; j < kEntriesAhead; ++j)
+            shares.t += i[j] >= 0 ? exp2_fast(fmaf(t[j], p.c_t, -from)) : 0.f;
+    }
+    if (lane == 0) {
+        to.index[p.k] = label ? (int)wanted : -1;
+        to.at_index[p.k] = label ? to_f32(row[wanted]) : 0.f;
+    }
+    to.terms = (__any_sync(~0u, present) ? 1 : 0) | (__any_sync(~0u, label) ? 2 : 0);
+    if (to.terms & 1) {
+        shares.join(p.c_t, p.c_1);
+        const float from = reference(shares.top, p.c_t), log_sum = log2f(shares.t);
+        for (int e = lane; e < k; e += 32)
+            to.log_p[e] = fmaf(to.log_p[e], p.c_t, -from) - log_sum;
+    }
+    __syncwarp();
+    if (gradient && (to.terms & 1)) {
+        // whether entries of the slice name one element: a hash table of their indices
+        const int size = 2 << (31 - __clz(k));          // more than k, at most 2 k
+        for (int n = lane; n < size; n += 32)
+            to.names[n] = -1;
+        __syncwarp();
+        bool met = false;
+        for (int e = lane; e < k; e += 32) {
+            const int i = to.index[e];
+            if (i < 0 || !slice.has(i, rank))
+                continue;
+            for (int n = i & (size - 1);; n = (n + 1) & (size - 1)) {       // ends: fewer names than places
+                const int there = atomicCAS(to.names + n, -1, i);
+                met = met || there == i;
+                if (there == -1 || there == i)
+                    break;
+            }
+        }
+        to.repeated = __any_sync(~0u, met);
+    }
+}
+
+// A row's block, or cluster of blocks, reads it for the sums and, from the L2 cache, again for the
+// gradient.  The last warp has the entries as well.  BOTH: the two temperatures differ.
+template <typename T, Mode MODE, bool BOTH>
+__global__ void __launch_bounds__(kMaxThreads) rikfad_distill_kernel(const __grid_constant__ Params p)
 {
     constexpr int V = 16 / sizeof(T);
-    extern __shared__ float entries[];
-    const int count = p.k + 1;                          // the label is the last entry
-    float *teacher = entries, *at_index = teacher + count;      // logits of the teacher, of the row at the indices
-    int *index = reinterpret_cast<int *>(at_index + count);
-    int *own = index + count;                           // entries of the block's slice, in order
-    __shared__ Sums warp_sums[kWarps];
-    __shared__ float2 warp_teacher[kWarps];
-    __shared__ float warp_loss[kWarps];
-    __shared__ float parts[kMaxCluster][3];
-    __shared__ int own_count;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    extern __shared__ float shared[];
+    __shared__ int terms;
+    const int threads = blockDim.x, warps = threads >> 5, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rank = p.cluster > 1 ? (int)(blockIdx.x % p.cluster) : 0;
     const int64_t r = p.cluster > 1 ? blockIdx.x / p.cluster : blockIdx.x;
+    const bool last_warp = warp == warps - 1;
+    Entries entries(shared, p.k + 1);
+    float *const parts = shared + 3 * (p.k + 1) + p.names;  // three of every warp of the row
     wait_for_predecessor();
     allow_successor_launch();
     if (MODE != kBackward && p.cluster > 1)
-        cluster_arrive();                               // the others have begun
+        cluster_arrive_relaxed();                           // this block has begun
     const T *row = static_cast<const T *>(p.logits) + r * p.logits_stride;
     const Slice<T> slice(row, p.vocab, p.cluster, rank);
-    const uint4 *vectors = reinterpret_cast<const uint4 *>(row + slice.lead);
-
-    // The entries: indices, the teacher's logits and the row's.  One that is absent, or
-    // whose logit is -inf, has index -1.
-    bool present = false;
-    float teacher_top = -INFINITY, teacher_sum = 0.f;
-    for (int e = threadIdx.x; e < count; e += kThreads) {
-        int64_t i = -1;
-        float t = 0.f;
-        if (e < p.k) {
-            if (p.distils) {
-                i = integer_at(p.index, p.index_bytes, r * p.index_stride + e);
-                t = float_at(p.teacher, p.teacher_dtype, r * p.teacher_stride + e);
-                i = t == -INFINITY ? -1 : i;
-                t = at_least(t, p.lowest);
-            }
-        } else if (p.labelled)
-            i = integer_at(p.labels, p.label_bytes, r);
-        const bool here = i >= 0 && i < p.vocab;
-        index[e] = here ? (int)i : -1;
-        teacher[e] = t;
-        at_index[e] = here ? to_f32(row[i]) : 0.f;
-        if (here && e < p.k) {
-            present = true;
-            const float m = fmaxf(teacher_top, t);
-            teacher_sum = Sums::moved(teacher_sum, teacher_top, m, p.c_t) + exp2_fast(fmaf(t, p.c_t, -Sums::reference(m, p.c_t)));
-            teacher_top = m;
-        }
-    }
-    const bool distils = __syncthreads_or(present);
-    const bool labelled = index[p.k] >= 0;
-
-    Sums sums = {-INFINITY, 0.f, 0.f};
-    if (MODE != kBackward) {
-        // this thread's maximum and sums, kAhead vectors at a time
-        auto take = [&](float (&x)[V], float top) {
-            if (top < p.lowest) {       // masked with the type's lowest value: such elements count if the row has no others
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    x[e] = at_least(x[e], p.lowest);
-                top = at_least(top, p.lowest);
-            }
-            if (top > sums.top) {
-                sums.t = Sums::moved(sums.t, sums.top, top, p.c_t);
-                sums.one = Sums::moved(sums.one, sums.top, top, p.c_1);
-                sums.top = top;
-            }
-            const float r_t = Sums::reference(sums.top, p.c_t), r_1 = Sums::reference(sums.top, p.c_1);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                sums.t += exp2_fast(fmaf(x[e], p.c_t, -r_t));
-                sums.one += exp2_fast(fmaf(x[e], p.c_1, -r_1));
-            }
-        };
-        for (int v = slice.begin + threadIdx.x; v < slice.end; v += kThreads * kAhead) {
-            Vec<T, V> in[kAhead];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j)
-                if (v + j * kThreads < slice.end)
-                    in[j].word = vectors[v + j * kThreads];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j)
-                if (v + j * kThreads < slice.end) {
-                    float x[V], top = -INFINITY;
-                    widen(in[j], x);
-#pragma unroll
-                    for (int e = 0; e < V; ++e)
-                        top = fmaxf(top, x[e]);
-                    take(x, top);
-                }
-        }
-        if (threadIdx.x < slice.edges) {
-            const float x = at_least(to_f32(row[slice.edge(threadIdx.x)]), p.lowest);
-            sums.add({x, exp2_fast(fmaf(x, p.c_t, -Sums::reference(x, p.c_t))),
-                      exp2_fast(fmaf(x, p.c_1, -Sums::reference(x, p.c_1)))}, p.c_t, p.c_1);
-        }
-        for (int d = 16; d > 0; d /= 2) {
-            const Sums o = {__shfl_xor_sync(~0u, sums.top, d), __shfl_xor_sync(~0u, sums.t, d), __shfl_xor_sync(~0u, sums.one, d)};
-            sums.add(o, p.c_t, p.c_1);
-        }
+    const uint4 *vectors = reinterpret_cast<const uint4 *>(row + slice.lead) + slice.begin;
+    const int mine = slice.end - slice.begin;
+    if (last_warp) {
+        load_entries<T>(p, entries, r, slice, rank, MODE != kForward);
         if (lane == 0)
-            warp_sums[warp] = sums;
-    }
-    if (distils) {
-        for (int d = 16; d > 0; d /= 2) {
-            const float top = __shfl_xor_sync(~0u, teacher_top, d), sum = __shfl_xor_sync(~0u, teacher_sum, d);
-            const float m = fmaxf(teacher_top, top);
-            teacher_sum = Sums::moved(teacher_sum, teacher_top, m, p.c_t) + Sums::moved(sum, top, m, p.c_t);
-            teacher_top = m;
-        }
-        if (lane == 0)
-            warp_teacher[warp] = make_float2(teacher_top, teacher_sum);
-    }
-    if (MODE != kForward && warp == kWarps - 1) {
-        // the entries of this block's slice, in order
-        int n = 0;
-        for (int e0 = 0; e0 < count; e0 += 32) {
-            const int e = e0 + lane;
-            const bool mine = e < count && index[e] >= 0 && slice.has(index[e], rank);
-            const uint32_t all = __ballot_sync(~0u, mine);
-            if (mine)
-                own[n + __popc(all & ((1u << lane) - 1))] = e;
-            n += __popc(all);
-        }
-        if (lane == 0)
-            own_count = n;
-    }
-    __syncthreads();
-    if (distils) {
-        teacher_top = -INFINITY;
-        teacher_sum = 0.f;
-        for (int w = 0; w < kWarps; ++w) {
-            const float2 o = warp_teacher[w];
-            const float m = fmaxf(teacher_top, o.x);
-            teacher_sum = Sums::moved(teacher_sum, teacher_top, m, p.c_t) + Sums::moved(o.y, o.x, m, p.c_t);
-            teacher_top = m;
-        }
+            terms = entries.terms;
     }
     float r_t, r_1, sum_t, sum_1;
     if (MODE != kBackward) {
-        sums = warp_sums[0];
-        for (int w = 1; w < kWarps; ++w)
-            sums.add(warp_sums[w], p.c_t, p.c_1);
+        // This thread's reference and sums.  Any element not far below the others does for a
+        // reference, and the largest of the first vector hardly ever is; if it was, or if
+        // that vector is masked, the thread goes over its part again and looks for the largest.
+        Sums<BOTH> sums;
+        if (threadIdx.x < mine) {
+            Pair of_t = pair(0.f, 0.f), of_1 = pair(0.f, 0.f);
+            float minus_t = 0.f, minus_1 = 0.f;
+            for (int v = threadIdx.x; v < mine; v += threads * kAhead) {
+                Vec<T, V> in[kAhead];
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j)
+                    if (v + j * threads < mine)
+                        in[j].word = vectors[v + j * threads];
+                if (v == threadIdx.x) {
+                    sums.top = largest(in[0]);
+                    minus_t = -reference(sums.top, p.c_t);
+                    minus_1 = -reference(sums.top, p.c_1);
+                }
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j)
+                    if (v + j * threads < mine) {
+                        float x[V];
+                        widen(in[j], x);
+#pragma unroll
+                        for (int e = 0; e < V; e += 2) {
+                            const Pair both = pair(x[e], x[e + 1]);
+                            of_t = add2(of_t, exp2_fast(fma2(both, pair(p.c_t, p.c_t), pair(minus_t, minus_t))));
+                            if (BOTH)
+                                of_1 = add2(of_1, exp2_fast(fma2(both, pair(p.c_1, p.c_1), pair(minus_1, minus_1))));
+                        }
+                    }
+            }
+            float even, odd;
+            apart(of_t, even, odd);
+            sums.t = even + odd;
+            apart(of_1, even, odd);
+            sums.one = even + odd;
+            if (!(sums.top > p.lowest && sums.t < kLargestSum && sums.one < kLargestSum)) {
+                sums = Sums<BOTH>();
+                for (int v = threadIdx.x; v < mine; v += threads)
+#pragma unroll 1
+                    for (int e = 0; e < V; ++e)
+                        sums.add_one(element<T>(row, slice.lead + (slice.begin + v) * V + e, p.lowest), p.c_t, p.c_1);
+            }
+        }
+        if (threadIdx.x < slice.edges)
+            sums.add_one(element<T>(row, slice.edge(threadIdx.x), p.lowest), p.c_t, p.c_1);
+        sums.join(p.c_t, p.c_1);
+        // every warp's to all blocks of the row, where every warp adds them up
         if (p.cluster > 1) {
             cluster_wait();
-            if (threadIdx.x < p.cluster) {
-                cluster_write(&parts[rank][0], threadIdx.x, sums.top);
-                cluster_write(&parts[rank][1], threadIdx.x, sums.t);
-                cluster_write(&parts[rank][2], threadIdx.x, sums.one);
+            if (lane < p.cluster) {
+                float *to = parts + 3 * (rank * warps + warp);
+                cluster_write(to, lane, sums.top);
+                cluster_write(to + 1, lane, sums.t);
+                cluster_write(to + 2, lane, sums.one);
             }
             cluster_arrive();
             cluster_wait();
-            sums = {parts[0][0], parts[0][1], parts[0][2]};
-            for (int c = 1; c < p.cluster; ++c)
-                sums.add({parts[c][0], parts[c][1], parts[c][2]}, p.c_t, p.c_1);
+        } else {
+            if (lane == 0) {
+                parts[3 * warp] = sums.top;
+                parts[3 * warp + 1] = sums.t;
+                parts[3 * warp + 2] = sums.one;
+            }
+            __syncthreads();
         }
-        r_t = Sums::reference(sums.top, p.c_t);
-        r_1 = Sums::reference(sums.top, p.c_1);
+        sums = Sums<BOTH>();
+        for (int i = lane; i < p.cluster * warps; i += 32)
+            sums.add(parts[3 * i], parts[3 * i + 1], parts[3 * i + 2], p.c_t, p.c_1);
+        sums.join(p.c_t, p.c_1);
+        r_t = reference(sums.top, p.c_t);
+        r_1 = reference(sums.top, p.c_1);
         sum_t = sums.t;
-        sum_1 = sums.one;
+        sum_1 = BOTH ? sums.one : sums.t;
     } else {
+        __syncthreads();
         const float4 s = p.stats[r];
         r_t = s.x;
         sum_t = s.y;
         r_1 = s.z;
         sum_1 = s.w;
     }
-    const float teacher_r = Sums::reference(teacher_top, p.c_t);
+    const bool distils = terms & 1, labelled = terms & 2;
     // The row has nothing above the lowest value that counts.
-    const bool low = p.c_t > p.c_1 ? r_t == p.lowest * p.c_t : r_1 == p.lowest * p.c_1;
-    auto logit = [&](float x) { return low ? at_least(x, p.lowest) : x; };
-    if (MODE != kBackward && rank == 0) {
+    const bool low = p.c_t > p.c_1 ? r_t <= p.lowest_t : r_1 <= p.lowest_1;
+    auto logit = [&](float x) { return low ? to_f32(from_f32<T>(at_least(x, p.lowest))) : x; };
+    if (MODE != kBackward && rank == 0 && last_warp) {
         float loss = 0.f;
         if (distils) {
-            const float log_q = log2f(sum_t), log_p = log2f(teacher_sum);
-            for (int e = threadIdx.x; e < p.k; e += kThreads)
-                if (index[e] >= 0) {
-                    const float lp = fmaf(teacher[e], p.c_t, -teacher_r) - log_p;
-                    const float share = exp2_fast(lp);
+            const float log_q = log2f(sum_t);
+            for (int e = lane; e < p.k; e += 32)
+                if (entries.index[e] >= 0) {
+                    const float lp = entries.log_p[e], share = exp2_fast(lp);
                     if (share != 0.f)
-                        loss += share * (lp - (fmaf(logit(at_index[e]), p.c_t, -r_t) - log_q));
+                        loss += share * (lp - (fmaf(logit(entries.at_index[e]), p.c_t, -r_t) - log_q));
                 }
+#pragma unroll
             for (int d = 16; d > 0; d /= 2)
                 loss += __shfl_xor_sync(~0u, loss, d);
-            if (lane == 0)
-                warp_loss[warp] = loss;
-            __syncthreads();
+            loss *= p.loss_a;
         }
-        if (threadIdx.x == 0) {
-            loss = 0.f;
-            if (distils) {
-                for (int w = 0; w < kWarps; ++w)
-                    loss += warp_loss[w];
-                loss *= p.loss_a;
-            }
-            if (labelled)
-                loss -= p.loss_b * (fmaf(logit(at_index[p.k]), p.c_1, -r_1) - log2f(sum_1));
+        if (labelled)
+            loss -= p.loss_b * (fmaf(logit(entries.at_index[p.k]), p.c_1, -r_1) - log2f(sum_1));
+        if (lane == 0) {
             p.loss[r] = loss;
             if (p.stats)
                 p.stats[r] = make_float4(r_t, sum_t, r_1, sum_1);
@@ -351,64 +479,90 @@ __global__ void __launch_bounds__(kThreads) rikfad_distill_kernel(const __grid_c
     const float scale = p.grad_scale * (p.dloss ? p.dloss[r] : 1.f);
     const float a = distils ? p.a * scale : 0.f, b = labelled ? p.b * scale : 0.f;
     const float f_t = a / sum_t, f_1 = b / sum_1;
-    auto dense = [&](float x) {         // a term that is absent adds nothing, whatever the row holds
-        float g = 0.f;
-        if (distils)
-            g = f_t * exp2_fast(fmaf(x, p.c_t, -r_t));
-        if (labelled)
-            g = fmaf(f_1, exp2_fast(fmaf(x, p.c_1, -r_1)), g);
-        return g;
+    // Without both terms at two temperatures one power does.
+    const bool none = !distils && !labelled, single = !BOTH || !distils || !labelled;
+    const float c = BOTH && !distils ? p.c_1 : p.c_t, minus_r = BOTH && !distils ? -r_1 : -r_t;
+    const float f = !BOTH ? f_t + f_1 : distils ? f_t : f_1;
+    auto dense = [&](float x, float y, auto one_power) {
+        const Pair both = pair(x, y);
+        if constexpr (decltype(one_power)::value)
+            return mul2(pair(f, f), exp2_fast(fma2(both, pair(c, c), pair(minus_r, minus_r))));
+        const Pair g = mul2(pair(f_t, f_t), exp2_fast(fma2(both, pair(p.c_t, p.c_t), pair(-r_t, -r_t))));
+        return fma2(pair(f_1, f_1), exp2_fast(fma2(both, pair(p.c_1, p.c_1), pair(-r_1, -r_1))), g);
+    };
+    auto dense_one = [&](float x) {
+        float g, other;
+        apart(single ? dense(logit(x), 0.f, std::true_type()) : dense(logit(x), 0.f, std::false_type()), g, other);
+        return none ? 0.f : g;
     };
     T *out = static_cast<T *>(p.dlogits) + r * p.dlogits_stride;
-    for (int v = slice.begin + threadIdx.x; v < slice.end; v += kThreads * kAhead) {
-        Vec<T, V> in[kAhead];
+    T *const to0 = out + slice.lead + (int64_t)slice.begin * V;
+    auto all = [&](auto one_power) {
+        for (int v = threadIdx.x; v < mine; v += threads * kAhead) {
+            Vec<T, V> in[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (v + j * kThreads < slice.end)
-                in[j].word = vectors[v + j * kThreads];
+            for (int j = 0; j < kAhead; ++j)
+                if (v + j * threads < mine)
+                    in[j].word = __ldcs(vectors + v + j * threads);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (v + j * kThreads < slice.end) {
-                float x[V];
-                widen(in[j], x);
-                if (low) {
+            for (int j = 0; j < kAhead; ++j)
+                if (v + j * threads < mine) {
+                    float x[V];
+                    widen(in[j], x);
 #pragma unroll
-                    for (int e = 0; e < V; ++e)
-                        x[e] = at_least(x[e], p.lowest);
+                    for (int e = 0; e < V; e += 2)
+                        apart(dense(x[e], x[e + 1], one_power), x[e], x[e + 1]);
+                    narrow(x, in[j]);
+                    T *to = to0 + (int64_t)(v + j * threads) * V;
+                    if (p.wide)
+                        __stcs(reinterpret_cast<uint4 *>(to), in[j].word);
+                    else
+#pragma unroll
+                        for (int e = 0; e < V; ++e)
+                            to[e] = in[j].v[e];
                 }
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    x[e] = dense(x[e]);
-                narrow(x, in[j]);
-                T *to = out + slice.lead + (int64_t)(v + j * kThreads) * V;
-                if (p.wide)
-                    *reinterpret_cast<uint4 *>(to) = in[j].word;
-                else
-#pragma unroll
-                    for (int e = 0; e < V; ++e)
-                        to[e] = in[j].v[e];
-            }
-    }
+        }
+    };
+    if (none || low) {                  // zeros whatever the row holds; a row masked all over
+#pragma unroll 1
+        for (int i = threadIdx.x; i < mine * V; i += threads)
+            to0[i] = from_f32<T>(dense_one(to_f32(row[slice.lead + slice.begin * V + i])));
+    } else if (single)
+        all(std::true_type());
+    else
+        all(std::false_type());
     if (threadIdx.x < slice.edges) {
         const int e = slice.edge(threadIdx.x);
-        out[e] = from_f32<T>(dense(logit(to_f32(row[e]))));
+        out[e] = from_f32<T>(dense_one(to_f32(row[e])));
     }
     __syncthreads();
-    // An element that several entries name: the first one's thread adds them up in order.
-    for (int n = threadIdx.x; n < own_count; n += kThreads) {
-        const int i = index[own[n]];
-        float part = 0.f;
-        bool first = true;
-        for (int m = 0; m < own_count; ++m) {
-            const int e = own[m];
-            if (index[e] != i)
+    if (!last_warp)
+        return;
+    const int label = entries.index[p.k];
+    bool named = false;                 // the label by one of the teacher's entries
+    if (distils)
+        for (int e = lane; e < p.k; e += 32) {
+            const int i = entries.index[e];
+            if (i < 0 || !slice.has(i, rank))
                 continue;
-            first = first && m >= n;
-            part -= e < p.k ? a * exp2_fast(fmaf(teacher[e], p.c_t, -teacher_r)) / teacher_sum : b;
+            float part = -a * exp2_fast(entries.log_p[e]);
+            bool first = true;
+            if (entries.repeated)       // the first one's lane adds up, in order, those that name the element
+                for (int m = 0; m < p.k; ++m)
+                    if (m != e && entries.index[m] == i) {
+                        first = first && m > e;
+                        part -= a * exp2_fast(entries.log_p[m]);
+                    }
+            if (i == label) {
+                part -= b;
+                named = true;
+            }
+            if (first)
+                out[i] = from_f32<T>(dense_one(entries.at_index[e]) + part);
         }
-        if (first)
-            out[i] = from_f32<T>(dense(logit(at_index[own[n]])) + part);
-    }
+    named = __any_sync(~0u, named);
+    if (lane == 0 && labelled && !named && slice.has(label, rank))
+        out[label] = from_f32<T>(dense_one(entries.at_index[p.k]) - b);
 }
 
 // ------------------------------------------------------------------------ host
@@ -478,19 +632,27 @@ int check(const rikfad_distillation *p, bool backward)
     return rc;
 }
 
-template <typename T, Mode MODE> cudaError_t launch(Params p, cudaStream_t s)
+template <typename T, Mode MODE, bool BOTH> cudaError_t launch(Params p, cudaStream_t s)
 {
-    // Few rows: several blocks for each, of 16 KB at least.
+    // 1024 threads an SM.  Blocks of fewer threads overlap one row's sums with another's
+    // gradient, as long as the rows under way stay in the L2 cache (kResident of an SM's).
     const int64_t bytes = (int64_t)p.vocab * sizeof(T);
+    int threads = 32;
+    while (threads < (MODE == kFused ? kMaxThreads : 256) && (threads < 256 ? bytes / 16 > 4 * threads : bytes * (1024 / threads) > kResident))
+        threads *= 2;
+    // Few rows: several blocks for each, of 16 KB at least; and where one row an SM is too much.
     p.cluster = 1;
-    while (p.cluster < kMaxCluster && p.rows * p.cluster < 2 * kSms && bytes / p.cluster > 16 << 10)
+    while (p.cluster < kMaxCluster && ((p.rows * p.cluster < 2 * kSms && bytes / p.cluster > 16 << 10) ||
+                                       (MODE == kFused && bytes / p.cluster * (1024 / threads) > kResident)))
         p.cluster *= 2;
     if (p.rows * p.cluster > INT32_MAX)
         return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(p.rows * p.cluster));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = 4 * sizeof(float) * ((size_t)p.k + 1);
+    cfg.blockDim = dim3((unsigned)threads);
+    while (MODE != kForward && p.names <= p.k && p.k > 0)
+        p.names = p.names ? 2 * p.names : 2;
+    cfg.dynamicSmemBytes = sizeof(float) * (3 * ((size_t)p.k + 1) + p.names + 3 * p.cluster * (threads / 32));
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -500,7 +662,12 @@ template <typename T, Mode MODE> cudaError_t launch(Params p, cudaStream_t s)
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = MODE != kBackward && p.cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, rikfad_distill_kernel<T, MODE>, p);
+    return cudaLaunchKernelEx(&cfg, rikfad_distill_kernel<T, MODE, BOTH>, p);
+}
+
+template <typename T, Mode MODE> cudaError_t launch(const Params &p, cudaStream_t s)
+{
+    return p.c_t != p.c_1 ? launch<T, MODE, true>(p, s) : launch<T, MODE, false>(p, s);
 }
 
 template <typename T> cudaError_t launch(const Params &p, bool backward, cudaStream_t s)
@@ -548,9 +715,12 @@ int run(const rikfad_distillation *p, bool backward, void *stream)
     q.b = (float)p->label_weight;
     q.loss_a = (float)(p->teacher_weight * T * T / kLog2E);
     q.loss_b = (float)(p->label_weight / kLog2E);
-    q.c_t = (float)(kLog2E / T);
-    q.c_1 = (float)kLog2E;
+    // a term that the call lacks has the other's temperature
+    q.c_t = (float)(q.distils ? kLog2E / T : kLog2E);
+    q.c_1 = (float)(q.labelled ? kLog2E : q.c_t);
     q.lowest = -kFarthest / std::max(q.c_t, q.c_1);
+    q.lowest_t = 0.99f * q.lowest * q.c_t;
+    q.lowest_1 = 0.99f * q.lowest * q.c_1;
     q.grad_scale = (float)p->grad_scale;
     const cudaStream_t s = (cudaStream_t)stream;
     e = p->dtype == RIKFAD_F32    ? launch<float>(q, backward, s)
