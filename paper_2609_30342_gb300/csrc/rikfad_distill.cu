@@ -28,17 +28,19 @@ using namespace rikfad;
 
 namespace {
 
-constexpr int kMaxThreads = 1024;
+constexpr int kMaxThreads = 256;
 constexpr int kSms = 152;
 constexpr int kMaxEntries = 1024;           // of a teacher's row
 constexpr int kMaxCluster = 8;
-constexpr int64_t kResident = 540 << 10;   // bytes of rows under way on an SM
+constexpr int64_t kUnderWay = 64 << 20;      // bytes of rows that blocks have at one time
+constexpr int kBlocksPerSm = 4;
+constexpr int kSmemPerSm = 228 << 10;
 // A reference's rounding is a factor of up to 2^(r 2^-24) in every power: r stays below
 // this, and lower logits count as the one there.
 constexpr float kFarthest = 0x1p29f;
 constexpr float kLargestSum = 0x1p40f;      // of a thread, beyond which its reference is too low
 constexpr int kEntriesAhead = 4;            // entries of a lane under way
-constexpr int kAhead = 4;                   // vectors of a thread under way
+constexpr int kAhead = 4;                    // vectors of a thread under way
 
 struct Params {
     const void *logits, *teacher, *index, *labels;
@@ -355,6 +357,8 @@ __global__ void __launch_bounds__(kMaxThreads) rikfad_distill_kernel(const __gri
     const Slice<T> slice(row, p.vocab, p.cluster, rank);
     const uint4 *vectors = reinterpret_cast<const uint4 *>(row + slice.lead) + slice.begin;
     const int mine = slice.end - slice.begin;
+    if (MODE != kBackward && threadIdx.x == 0 && mine > 0)      // all of the part under way, more than the loads below ask for at once
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(vectors), "r"(mine * 16));
     if (last_warp) {
         load_entries<T>(p, entries, r, slice, rank, MODE != kForward);
         if (lane == 0)
@@ -634,16 +638,17 @@ int check(const rikfad_distillation *p, bool backward)
 
 template <typename T, Mode MODE, bool BOTH> cudaError_t launch(Params p, cudaStream_t s)
 {
-    // 1024 threads an SM.  Blocks of fewer threads overlap one row's sums with another's
-    // gradient, as long as the rows under way stay in the L2 cache (kResident of an SM's).
     const int64_t bytes = (int64_t)p.vocab * sizeof(T);
     int threads = 32;
-    while (threads < (MODE == kFused ? kMaxThreads : 256) && (threads < 256 ? bytes / 16 > 4 * threads : bytes * (1024 / threads) > kResident))
+    while (threads < kMaxThreads && bytes / 16 > 4 * threads)
         threads *= 2;
-    // Few rows: several blocks for each, of 16 KB at least; and where one row an SM is too much.
+    // Blocks of a row: until the rows under way stay in the L2 cache between their sums and
+    // their gradient, and until there are a few rounds of blocks of 16 KB at least.
+    const int64_t rounds = (MODE == kFused ? 4 : 1) * kBlocksPerSm * kSms;
     p.cluster = 1;
-    while (p.cluster < kMaxCluster && ((p.rows * p.cluster < 2 * kSms && bytes / p.cluster > 16 << 10) ||
-                                       (MODE == kFused && bytes / p.cluster * (1024 / threads) > kResident)))
+    while (p.cluster < kMaxCluster && ((MODE == kFused && bytes / p.cluster * kBlocksPerSm * kSms > kUnderWay) ||
+                                       (p.rows * p.cluster < rounds && bytes / p.cluster > 32 << 10) ||
+                                       (p.rows * p.cluster < 2 * kSms && bytes / p.cluster > 16 << 10)))
         p.cluster *= 2;
     if (p.rows * p.cluster > INT32_MAX)
         return cudaErrorInvalidConfiguration;
@@ -653,6 +658,12 @@ template <typename T, Mode MODE, bool BOTH> cudaError_t launch(Params p, cudaStr
     while (MODE != kForward && p.names <= p.k && p.k > 0)
         p.names = p.names ? 2 * p.names : 2;
     cfg.dynamicSmemBytes = sizeof(float) * (3 * ((size_t)p.k + 1) + p.names + 3 * p.cluster * (threads / 32));
+    if (MODE == kFused && threads == kMaxThreads) {
+        // no more blocks on an SM than that: with more than a 1 / (n + 1) of the shared memory for each, n
+        const int64_t most = std::max<int64_t>(kBlocksPerSm, kUnderWay * p.cluster / (bytes * kSms));
+        if (most < 6)
+            cfg.dynamicSmemBytes = std::max<size_t>(cfg.dynamicSmemBytes, (size_t)(kSmemPerSm / (most + 1)));
+    }
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -667,7 +678,7 @@ template <typename T, Mode MODE, bool BOTH> cudaError_t launch(Params p, cudaStr
 
 template <typename T, Mode MODE> cudaError_t launch(const Params &p, cudaStream_t s)
 {
-    return p.c_t != p.c_1 ? launch<T, MODE, true>(p, s) : launch<T, MODE, false>(p, s);
+    return p.c_t == p.c_1 ? launch<T, MODE, false>(p, s) : launch<T, MODE, true>(p, s);
 }
 
 template <typename T> cudaError_t launch(const Params &p, bool backward, cudaStream_t s)
