@@ -31,7 +31,10 @@ constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortCtas = 8
 constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kSortBits = 9;            // of a pass: the warps' counts of 2^9 digits take 32 KB
 constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32, kSumAhead = 8;
-constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinAhead = 4, kJoinBlocks = 4 * kSms;
+constexpr double kZeroBytesPerUs = 5e6; // of all multiprocessors but the sorting ones
+constexpr int kShortRun = 32;           // chunks that a run joined by one warp goes on in, at most
+constexpr int kCountThreads = 256, kMostCounted = 6144;
 
 struct EmbedParams {
     const void *ids;
@@ -44,7 +47,9 @@ struct EmbedParams {
     // backward
     uint2 *order;                       // (id, token), sorted; ids outside the table last, as vocab
     float *head, *tail;                 // partial rows of chunks, `pitch` floats apart
+    int32_t *counts, *starts;           // chunks where a run over several starts: how many, which
     int64_t pitch, chunks;
+    int64_t zero_from;                  // rows from here on are zero already
     int32_t chunk, slabs;               // tokens of a chunk; warps side by side over a row
     int64_t sum_blocks;
 };
@@ -67,6 +72,17 @@ template <typename T, int V> __device__ __forceinline__ void load_once(Vec<T, V>
 template <typename T, int V> __device__ __forceinline__ void store(const Vec<T, V> &r, T *p)
 {
     *reinterpret_cast<decltype(r.word) *>(p) = r.word;
+}
+
+// Zeros to n elements, 16 bytes at a time wherever they start.
+template <typename W> __device__ __forceinline__ void zero(W *to, int64_t n, int64_t thread, int64_t threads)
+{
+    constexpr int E = 16 / sizeof(W);
+    const int64_t lead = min((int64_t)((16 - (uint32_t)(uintptr_t)to % 16) % 16 / sizeof(W)), n), vectors = (n - lead) / E;
+    for (int64_t i = thread; i < vectors; i += threads)
+        reinterpret_cast<uint4 *>(to + lead)[i] = make_uint4(0, 0, 0, 0);
+    if (thread < n - vectors * E)
+        to[thread < lead ? thread : thread + vectors * E] = from_f32<W>(0.f);
 }
 
 // A block's threads are `lanes` across a row (blockDim.x) and blockDim.y rows; a
@@ -117,7 +133,34 @@ struct SortParams {
     uint2 *from, *to;               // of the passes in turn; the last one writes to `to`
     int64_t vocab;
     int32_t tokens, id_bytes, passes, bits;
+    int32_t *counts;                // zeroed for the sums
+    // rows of the table from zero_from on get zeros from the blocks that do not sort
+    void *table;
+    int64_t table_stride, zero_from;
+    int32_t width, table_bytes;     // bytes of an element
 };
+
+// Rows from zero_from on, by `blocks` blocks of which this is the one numbered `block`.
+__device__ __forceinline__ void zero_rows(const SortParams &p, int64_t block, int64_t blocks)
+{
+    const int64_t rows = p.vocab - p.zero_from, size = (int64_t)p.width * p.table_bytes, stride = p.table_stride * p.table_bytes;
+    char *first = static_cast<char *>(p.table) + p.zero_from * stride;
+    if (rows <= 0)
+        return;
+    auto part = [&](char *at, int64_t n, int64_t thread, int64_t threads) {
+        if (p.table_bytes == 4)
+            zero(reinterpret_cast<float *>(at), n / 4, thread, threads);
+        else
+            zero(reinterpret_cast<__half *>(at), n / 2, thread, threads);
+    };
+    if (stride == size || rows == 1) {
+        part(first, rows * size, block * blockDim.x + threadIdx.x, blocks * blockDim.x);
+        return;
+    }
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    for (int64_t row = block * warps + (threadIdx.x >> 5); row < rows; row += blocks * warps)
+        part(first + row * stride, size, lane, 32);
+}
 
 __device__ __forceinline__ void cluster_barrier()
 {
@@ -172,6 +215,12 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
     const int begin = (int)min(share * rank, (int64_t)p.tokens), end = (int)min(share * (rank + 1), (int64_t)p.tokens);
     wait_for_predecessor();
     allow_successor_launch();
+    if (blockIdx.x >= kSortCtas) {
+        zero_rows(p, blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
+        return;
+    }
+    if (blockIdx.x == 0 && threadIdx.x < 2)
+        p.counts[threadIdx.x] = 0;
     for (int pass = 0; pass < p.passes; ++pass) {
         const uint2 *from = (p.passes - pass) % 2 ? p.from : p.to;
         uint2 *to = (p.passes - pass) % 2 ? p.to : p.from;
@@ -248,6 +297,36 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
     }
 }
 
+// Few tokens: each one's place is the number of ids below its own and of equal ids before
+// it, counted by a warp.  All blocks count, then all write zeros.
+__global__ void __launch_bounds__(kCountThreads) rikfad_embed_count_kernel(const __grid_constant__ SortParams p)
+{
+    __shared__ uint4 all[kMostCounted / 4];
+    uint32_t *const ids = reinterpret_cast<uint32_t *>(all);
+    const int lane = threadIdx.x & 31, warps = kCountThreads / 32, n4 = (p.tokens + 3) / 4;
+    wait_for_predecessor();
+    allow_successor_launch();
+    if (blockIdx.x == 0 && threadIdx.x < 2)
+        p.counts[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < 4 * n4; i += kCountThreads)
+        ids[i] = i < p.tokens ? id_at(p.ids, p.id_bytes, i, p.vocab) : ~0u;
+    __syncthreads();
+    for (int t = blockIdx.x * warps + (threadIdx.x >> 5); t < p.tokens; t += gridDim.x * warps) {
+        const uint32_t id = ids[t];
+        int before = 0;
+        for (int i = lane; i < n4; i += 32) {
+            const uint4 v = all[i];
+            before += (v.x < id) + (v.y < id) + (v.z < id) + (v.w < id);
+            before += (v.x == id && 4 * i < t) + (v.y == id && 4 * i + 1 < t) + (v.z == id && 4 * i + 2 < t) +
+                      (v.w == id && 4 * i + 3 < t);
+        }
+        before = __reduce_add_sync(~0u, before);
+        if (lane == 0)
+            p.to[before] = make_uint2(id, (uint32_t)t);
+    }
+    zero_rows(p, blockIdx.x, gridDim.x);
+}
+
 // -------------------------------------------------------------------- the sums
 
 // The first of the n sorted entries whose id is at least `id`.
@@ -294,23 +373,13 @@ __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __g
     if (blockIdx.x >= p.sum_blocks) {
         const int64_t row0 = ((blockIdx.x - p.sum_blocks) * kSumWarps + warp) * 32, row = row0 + lane;
         bool absent = false;
-        if (row < p.vocab) {
+        if (row < p.zero_from) {
             const int64_t at = lower_bound(p.order, p.tokens, (uint32_t)row);
             absent = at == p.tokens || p.order[at].x != row;
         }
         uint32_t todo = __ballot_sync(~0u, absent);
-        float zero[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            zero[e] = 0.f;
-        Vec<W, V> r;
-        narrow(zero, r);
-        while (todo) {
-            W *at = static_cast<W *>(p.table) + (row0 + __ffs(todo) - 1) * p.table_stride;
-            todo &= todo - 1;
-            for (int u = lane; u < p.units; u += 32)
-                store(r, at + (int64_t)u * V);
-        }
+        for (; todo; todo &= todo - 1)
+            zero(static_cast<W *>(p.table) + (row0 + __ffs(todo) - 1) * p.table_stride, p.width, lane, 32);
         return;
     }
     const int64_t item = blockIdx.x * kSumWarps + warp, chunk = item / p.slabs;
@@ -334,6 +403,12 @@ __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __g
 #pragma unroll
                 for (int e = 0; e < V; ++e)
                     part[e] = sum[e];
+                if (unit == 0 && !from_before) {        // a run over several chunks starts here
+                    const int64_t far = chunk + kShortRun + 1;
+                    const int longer = far < p.chunks && p.order[far * p.chunk].x == run;
+                    const int at = atomicAdd(p.counts + longer, 1);     // in any order: each writes its own row
+                    p.starts[longer ? p.chunks - 1 - at : at] = (int32_t)chunk;
+                }
             } else
                 write_row<W, V>(p, run, unit, sum);
         }
@@ -376,92 +451,76 @@ __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __g
 }
 
 // Runs over several chunks: the partial row of the chunk where one starts, then those
-// of the chunks that it goes on in.  A block has 128 columns of 32 chunks that may
-// start such a run; runs of up to 32 more chunks are a warp's, longer ones the block's.
+// of the chunks that it goes on in.  128 columns of a run that goes on in up to kShortRun
+// chunks are a warp's, of a longer one a block's.
 template <typename W> __global__ void __launch_bounds__(kJoinThreads) rikfad_embed_join_kernel(const __grid_constant__ EmbedParams p)
 {
     __shared__ float4 part[kJoinWarps][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slabs = (int)((p.pitch + 127) / 128);
     wait_for_predecessor();
     allow_successor_launch();
-    const int64_t mine = (int64_t)lane * gridDim.x + blockIdx.x;     // neighbours, often of one run, to different blocks
-    bool starts = false;
-    if (mine + 1 < p.chunks) {
-        const int64_t next = (mine + 1) * p.chunk;
-        const uint32_t id = p.order[next].x;
-        starts = id < p.vocab && p.order[next - 1].x == id && (mine == 0 || p.order[mine * p.chunk - 1].x != id);
-    }
-    const uint32_t owners = __ballot_sync(~0u, starts);
-    const int64_t column = (int64_t)blockIdx.y * 128 + lane * 4;
-    const bool active = column < p.pitch;
-    auto add = [&](float4 &s, const float *row) {
-        if (active) {
-            const float4 v = __ldcs(reinterpret_cast<const float4 *>(row + column));
-            s.x += v.x;
-            s.y += v.y;
-            s.z += v.z;
-            s.w += v.w;
+    const int64_t short_runs = (int64_t)p.counts[0] * slabs, long_runs = (int64_t)p.counts[1] * slabs;
+    auto add = [](float4 &s, const float4 &v) {
+        s.x += v.x;
+        s.y += v.y;
+        s.z += v.z;
+        s.w += v.w;
+    };
+    // columns from `column` on of the head rows [from, to), added to s
+    auto heads = [&](float4 &s, int64_t column, int64_t from, int64_t to) {
+        const float *row = p.head + from * p.pitch + column;
+        for (int64_t n = to - from; n > 0 && column < p.pitch; n -= kJoinAhead, row += kJoinAhead * p.pitch) {
+            float4 v[kJoinAhead];
+#pragma unroll
+            for (int j = 0; j < kJoinAhead; ++j)
+                if (j < n)
+                    v[j] = __ldcs(reinterpret_cast<const float4 *>(row + j * p.pitch));
+#pragma unroll
+            for (int j = 0; j < kJoinAhead; ++j)
+                if (j < n)
+                    add(s, v[j]);
         }
     };
-    auto write = [&](uint32_t id, const float4 &s) {
+    auto write = [&](uint32_t id, int64_t column, const float4 &s) {
         const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
         for (int e = 0; e < 4; ++e)
             if (column + e < p.width) {
                 float one[1] = {v[e]};
                 write_row<W, 1>(p, id, (int)(column + e), one);
             }
     };
-    uint32_t longer = 0;
-    int turn = 0;
-    for (uint32_t left = owners; left; left &= left - 1, ++turn) {
-        const int64_t chunk = (int64_t)(__ffs(left) - 1) * gridDim.x + blockIdx.x;
+    const float4 nothing = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int64_t i = blockIdx.x; i < long_runs; i += gridDim.x) {
+        const int64_t chunk = p.starts[p.chunks - 1 - i / slabs], column = i % slabs * 128 + lane * 4;
         const uint32_t id = p.order[(chunk + 1) * p.chunk].x;
-        const int64_t c = chunk + 1 + lane;
-        const uint32_t more = __ballot_sync(~0u, c < p.chunks && p.order[c * p.chunk].x == id);
-        if (more == ~0u) {
-            longer |= left & -left;
-            continue;
-        }
-        if (turn % kJoinWarps != warp)
-            continue;
-        const int n = __ffs(~more) - 1;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        add(s, p.tail + chunk * p.pitch);
-        for (int j = 0; j < n; ++j)
-            add(s, p.head + (chunk + 1 + j) * p.pitch);
-        write(id, s);
-    }
-    for (; longer; longer &= longer - 1) {
-        const int64_t chunk = (int64_t)(__ffs(longer) - 1) * gridDim.x + blockIdx.x;
-        const uint32_t id = p.order[(chunk + 1) * p.chunk].x;
-        int64_t lo = chunk + 33, n = p.chunks - lo;        // the first chunk that does not start with id
+        int64_t last = chunk + 1 + kShortRun, n = p.chunks - last;      // the first chunk that does not start with id
         while (n > 0) {
             const int64_t half = n / 2;
-            const bool same = p.order[(lo + half) * p.chunk].x == id;
-            lo = same ? lo + half + 1 : lo;
+            const bool same = p.order[(last + half) * p.chunk].x == id;
+            last = same ? last + half + 1 : last;
             n = same ? n - half - 1 : half;
         }
-        const int64_t count = lo - chunk - 1, share = (count + kJoinWarps - 1) / kJoinWarps;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (warp == 0)
-            add(s, p.tail + chunk * p.pitch);
-        const int64_t to = min(count, share * (warp + 1));
-#pragma unroll 8
-        for (int64_t j = share * warp; j < to; ++j)
-            add(s, p.head + (chunk + 1 + j) * p.pitch);
+        const int64_t share = (last - chunk - 1 + kJoinWarps - 1) / kJoinWarps, from = chunk + 1 + share * warp;
+        float4 s = warp == 0 && column < p.pitch ? *reinterpret_cast<const float4 *>(p.tail + chunk * p.pitch + column) : nothing;
+        heads(s, column, from, min(from + share, last));
         part[warp][lane] = s;
         __syncthreads();
         if (warp == 0) {
-            for (int w = 1; w < kJoinWarps; ++w) {
-                const float4 v = part[w][lane];
-                s.x += v.x;
-                s.y += v.y;
-                s.z += v.z;
-                s.w += v.w;
-            }
-            write(id, s);
+            for (int w = 1; w < kJoinWarps; ++w)
+                add(s, part[w][lane]);
+            write(id, column, s);
         }
         __syncthreads();
+    }
+    for (int64_t i = (int64_t)blockIdx.x * kJoinWarps + warp; i < short_runs; i += (int64_t)gridDim.x * kJoinWarps) {
+        const int64_t chunk = p.starts[i / slabs], column = i % slabs * 128 + lane * 4;
+        const uint32_t id = p.order[(chunk + 1) * p.chunk].x;
+        const int64_t c = chunk + 1 + lane;
+        const uint32_t more = __ballot_sync(~0u, c < p.chunks && p.order[c * p.chunk].x == id);
+        float4 s = column < p.pitch ? __ldcs(reinterpret_cast<const float4 *>(p.tail + chunk * p.pitch + column)) : nothing;
+        heads(s, column, chunk + 1, chunk + 1 + (more == ~0u ? 32 : __ffs(~more) - 1));
+        write(id, column, s);
     }
 }
 
@@ -579,7 +638,9 @@ cudaError_t launch_sort(const SortParams &p, cudaStream_t s)
 {
     const int bins = 1 << p.bits;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kSortCtas);
+    // the other multiprocessors write zeros
+    const int others = p.zero_from < p.vocab ? kSms / kSortCtas - 1 : 0;
+    cfg.gridDim = dim3(kSortCtas * (1 + others));
     cfg.blockDim = dim3(kSortThreads);
     cfg.dynamicSmemBytes = sizeof(uint32_t) * (3 * bins + 32) + sizeof(uint16_t) * kSortWarps * bins;
     cfg.stream = s;
@@ -596,17 +657,21 @@ cudaError_t launch_sort(const SortParams &p, cudaStream_t s)
 
 struct Workspace {
     int64_t chunk, chunks, pitch;
-    size_t entries, bytes;              // bytes of one list of entries, of all
+    size_t entries, lists, bytes;       // bytes of one list of entries, of the chunks where runs start, of all
 };
 
 Workspace workspace_of(const rikfad_embedding *p)
 {
     Workspace w;
+    // Chunks of more tokens leave fewer partial rows, as long as there are warps enough.
     w.chunk = 32;
+    while (w.chunk < 256 && p->tokens / w.chunk * ((p->width + 255) / 256) > kSms * 96)
+        w.chunk *= 2;
     w.chunks = (p->tokens + w.chunk - 1) / w.chunk;
     w.pitch = (p->width + 3) / 4 * 4;
     w.entries = ((size_t)p->tokens * sizeof(uint2) + 15) / 16 * 16;
-    w.bytes = 2 * w.entries + 2 * (size_t)w.chunks * (size_t)w.pitch * sizeof(float);
+    w.lists = p->tokens ? ((size_t)w.chunks + 2 + 3) / 4 * 4 * sizeof(int32_t) : 0;
+    w.bytes = 2 * w.entries + w.lists + 2 * (size_t)w.chunks * (size_t)w.pitch * sizeof(float);
     return w;
 }
 
@@ -615,7 +680,7 @@ template <typename W, typename O, int V> cudaError_t launch_backward(EmbedParams
     p.units = p.width / V;
     p.slabs = (p.units + 31) / 32;
     p.sum_blocks = (p.chunks * p.slabs + kSumWarps - 1) / kSumWarps;
-    const int64_t zeros = p.accumulate ? 0 : (p.vocab + 32 * kSumWarps - 1) / (32 * kSumWarps);
+    const int64_t zeros = (p.zero_from + 32 * kSumWarps - 1) / (32 * kSumWarps);
     if (p.sum_blocks + zeros == 0)
         return cudaSuccess;
     if (p.sum_blocks + zeros > INT32_MAX)
@@ -623,8 +688,8 @@ template <typename W, typename O, int V> cudaError_t launch_backward(EmbedParams
     cudaError_t e = launch_chained(rikfad_embed_sum_kernel<W, O, V>, dim3((unsigned)(p.sum_blocks + zeros)), kSumThreads, 0, s, p);
     if (e != cudaSuccess || p.chunks < 2)
         return e;
-    return launch_chained(rikfad_embed_join_kernel<W>, dim3((unsigned)((p.chunks + 31) / 32), (unsigned)((p.pitch + 127) / 128)),
-                          kJoinThreads, 0, s, p);
+    const int64_t slabs = (p.pitch + 127) / 128, blocks = (p.chunks * slabs + kJoinWarps - 1) / kJoinWarps;
+    return launch_chained(rikfad_embed_join_kernel<W>, dim3((unsigned)std::min<int64_t>(blocks, kJoinBlocks)), kJoinThreads, 0, s, p);
 }
 
 template <typename W, typename O, bool BACKWARD, int V> cudaError_t launch(const EmbedParams &p, int v, cudaStream_t s)
@@ -714,14 +779,30 @@ RIKFAD_API int rikfad_embedding_backward(const rikfad_embedding *p, void *stream
     EmbedParams q = params(p);
     char *at = static_cast<char *>(p->workspace);
     q.order = reinterpret_cast<uint2 *>(at);
-    q.head = reinterpret_cast<float *>(at + 2 * w.entries);
+    q.counts = reinterpret_cast<int32_t *>(at + 2 * w.entries);
+    q.starts = q.counts + 2;
+    q.head = reinterpret_cast<float *>(at + 2 * w.entries + w.lists);
     q.tail = q.head + w.chunks * w.pitch;
     q.chunk = (int32_t)w.chunk;
     q.chunks = w.chunks;
     q.pitch = w.pitch;
+    q.zero_from = p->accumulate ? 0 : p->vocab;
     const cudaStream_t s = (cudaStream_t)stream;
     if (p->tokens > 0) {
         SortParams r{};
+        // While a few multiprocessors sort, the others write zeros to the last rows of the
+        // table, about as many as that time allows; those with tokens are written again.
+        if (!p->accumulate) {
+            const double us = p->tokens <= kMostCounted ? 3 : 6 + (double)p->tokens / 2000;
+            const double rows = us * kZeroBytesPerUs / ((double)p->width * dtype_bytes(p->table_dtype));
+            q.zero_from = p->vocab - (int64_t)std::min((double)p->vocab, rows);
+        }
+        r.zero_from = p->accumulate ? p->vocab : q.zero_from;
+        r.counts = q.counts;
+        r.table = q.table;
+        r.table_stride = q.table_stride;
+        r.width = q.width;
+        r.table_bytes = dtype_bytes(p->table_dtype);
         r.ids = p->ids;
         r.to = q.order;
         r.from = reinterpret_cast<uint2 *>(at + w.entries);
@@ -733,9 +814,10 @@ RIKFAD_API int rikfad_embedding_backward(const rikfad_embedding *p, void *stream
             ++bits;
         r.passes = (bits + kSortBits - 1) / kSortBits;
         r.bits = (bits + r.passes - 1) / r.passes;
-        e = launch_sort(r, s);
+        e = p->tokens <= kMostCounted ? launch_chained(rikfad_embed_count_kernel, dim3(2 * kSms), kCountThreads, 0, s, r)
+                                      : launch_sort(r, s);
         if (e != cudaSuccess)
-            return report_cuda(e, "launch rikfad_embed_sort_kernel");
+            return report_cuda(e, "launch of the embedding's sort");
     }
     e = launch<true>(p, q, s);
     return e == cudaSuccess ? RIKFAD_OK : report_cuda(e, "launch of the embedding's backward kernels");
