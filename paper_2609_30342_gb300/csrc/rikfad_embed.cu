@@ -27,10 +27,10 @@ namespace {
 
 constexpr int kSms = 152;
 constexpr int kForwardThreads = 256, kForwardRows = 4;
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortCtas = 8, kSortItems = 4;
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortCtas = 8, kSortItems = 8;
 constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kSortBits = 9;            // of a pass: the warps' counts of 2^9 digits take 32 KB
-constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32, kSumAhead = 8;
+constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32, kSumAhead = 8, kNarrowAhead = 8;
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinAhead = 4, kJoinBlocks = 4 * kSms;
 constexpr double kZeroBytesPerUs = 5e6; // of all multiprocessors but the sorting ones
 constexpr int kShortRun = 32;           // chunks that a run joined by one warp goes on in, at most
@@ -228,15 +228,12 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
         auto entry = [&](int i) {
             return pass == 0 ? make_uint2(id_at(p.ids, p.id_bytes, i, p.vocab), (uint32_t)i) : __ldcg(from + i);
         };
-        for (int b = threadIdx.x; b < bins; b += kSortThreads)
-            total[b] = 0;
-        __syncthreads();
-        for (int i = begin + threadIdx.x; i < end; i += kSortThreads)
-            atomicAdd(total + (entry(i).x >> shift & (bins - 1)), 1u);      // integers: any order
-        cluster_barrier();
-        {
+        // a digit's first place for this block: after all lower digits and the blocks before it
+        auto first_places = [&] {
+            cluster_barrier();
             uint32_t before = 0, all = 0;
             if (threadIdx.x < bins)
+#pragma unroll
                 for (int r = 0; r < kSortCtas; ++r) {
                     const uint32_t n = cluster_read(total + threadIdx.x, r);
                     before += r < rank ? n : 0;
@@ -245,11 +242,17 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
             const uint32_t first = block_exclusive(all, sums);
             if (threadIdx.x < bins)
                 base[threadIdx.x] = first + before;
-        }
-        for (int tile = begin; tile < end; tile += kSortTile) {
-            for (int b = threadIdx.x; b < bins * kSortWarps / 2; b += kSortThreads)
-                reinterpret_cast<uint32_t *>(counts)[b] = 0;
+        };
+        const bool one_tile = end - begin <= kSortTile;
+        if (!one_tile) {
+            for (int b = threadIdx.x; b < bins; b += kSortThreads)
+                total[b] = 0;
             __syncthreads();
+            for (int i = begin + threadIdx.x; i < end; i += kSortThreads)
+                atomicAdd(total + (entry(i).x >> shift & (bins - 1)), 1u);      // integers: any order
+            first_places();
+        }
+        for (int tile = begin; tile < end || (one_tile && tile == begin); tile += kSortTile) {
             uint2 e[kSortItems];
             uint32_t place[kSortItems];
             uint16_t *mine = counts + warp * bins;
@@ -258,9 +261,14 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
                 const int i = tile + (warp * kSortItems + k) * 32 + lane;
                 e[k] = i < end ? entry(i) : make_uint2(0, 0);
             }
+            for (int b = threadIdx.x; b < bins * kSortWarps / 2; b += kSortThreads)
+                reinterpret_cast<uint32_t *>(counts)[b] = 0;
+            __syncthreads();
 #pragma unroll
             for (int k = 0; k < kSortItems; ++k) {
                 const int i = tile + (warp * kSortItems + k) * 32 + lane;
+                if (i - lane >= end)
+                    break;
                 const uint32_t digit = e[k].x >> shift & (bins - 1);
                 const uint32_t same = __match_any_sync(~0u, i < end ? digit : ~0u);
                 const int leader = __ffs(same) - 1;
@@ -273,13 +281,24 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
                 place[k] = __shfl_sync(~0u, old, leader) + __popc(same & ((1u << lane) - 1));
             }
             __syncthreads();
+            uint32_t n = 0;
             if (threadIdx.x < bins) {
-                uint32_t n = 0;
+                uint16_t here[kSortWarps];
+#pragma unroll
+                for (int w = 0; w < kSortWarps; ++w)
+                    here[w] = counts[w * bins + threadIdx.x];
+#pragma unroll
                 for (int w = 0; w < kSortWarps; ++w) {
-                    const uint32_t here = counts[w * bins + threadIdx.x];
                     counts[w * bins + threadIdx.x] = (uint16_t)n;
-                    n += here;
+                    n += here[w];
                 }
+            }
+            if (one_tile) {
+                if (threadIdx.x < bins)
+                    total[threadIdx.x] = n;
+                first_places();
+            }
+            if (threadIdx.x < bins) {
                 start[threadIdx.x] = base[threadIdx.x];
                 base[threadIdx.x] += n;
             }
@@ -362,16 +381,26 @@ __device__ __forceinline__ void write_row(const EmbedParams &p, uint32_t id, int
     store(r, at);
 }
 
-// The first sum_blocks blocks sum chunks of sorted tokens, a warp 32 vectors of the
-// row; the others write zeros to the rows without a token, 32 rows a warp.
+template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, const void *from)
+{
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+}
+
+// The first blocks write zeros to the rows without a token, 32 rows a warp; the last
+// sum_blocks sum chunks of sorted tokens, a warp 32 vectors of the row.
 template <typename W, typename O, int V>
 __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __grid_constant__ EmbedParams p)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     wait_for_predecessor();
     allow_successor_launch();
-    if (blockIdx.x >= p.sum_blocks) {
-        const int64_t row0 = ((blockIdx.x - p.sum_blocks) * kSumWarps + warp) * 32, row = row0 + lane;
+    // zeros first: their blocks begin with a search, during which the others' loads are under way
+    const int64_t zero_blocks = gridDim.x - p.sum_blocks;
+    if (blockIdx.x < zero_blocks) {
+        const int64_t row0 = ((int64_t)blockIdx.x * kSumWarps + warp) * 32, row = row0 + lane;
         bool absent = false;
         if (row < p.zero_from) {
             const int64_t at = lower_bound(p.order, p.tokens, (uint32_t)row);
@@ -382,7 +411,7 @@ __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __g
             zero(static_cast<W *>(p.table) + (row0 + __ffs(todo) - 1) * p.table_stride, p.width, lane, 32);
         return;
     }
-    const int64_t item = blockIdx.x * kSumWarps + warp, chunk = item / p.slabs;
+    const int64_t item = (blockIdx.x - zero_blocks) * kSumWarps + warp, chunk = item / p.slabs;
     if (chunk >= p.chunks)
         return;
     const int unit = (int)(item % p.slabs) * 32 + lane;
@@ -417,32 +446,66 @@ __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __g
             sum[e] = 0.f;
         from_before = false;
     };
-    for (int64_t base = first; base < last; base += 32) {
-        const uint2 mine = base + lane < last ? p.order[base + lane] : make_uint2(~0u, 0);
-        const int here = (int)min((int64_t)32, last - base);
-        for (int j = 0; j < here; j += kSumAhead) {
-            Vec<O, V> in[kSumAhead];
+    auto window = [&](int64_t base) { return base + lane < last ? p.order[base + lane] : make_uint2(~0u, 0); };
+    auto step = [&](uint32_t id, const Vec<O, V> &in) {
+        if (id != run) {
+            finish(false);
+            run = id;
+        }
+        if (active && id < p.vocab) {
+            float f[V];
+            widen(in, f);
 #pragma unroll
-            for (int k = 0; k < kSumAhead; ++k) {
-                const uint32_t id = __shfl_sync(~0u, mine.x, j + k), token = __shfl_sync(~0u, mine.y, j + k);
-                if (active && id < p.vocab)
-                    load_once(in[k], rows + token * p.row_stride);
+            for (int e = 0; e < V; ++e)
+                sum[e] += f[e];
+        }
+    };
+    constexpr int kBytes = V * sizeof(O);
+    if constexpr (kBytes >= 4) {
+        // a ring of kSumAhead rows, each lane's part copied and read by itself
+        extern __shared__ uint4 rings[];
+        const uint32_t ring = (uint32_t)__cvta_generic_to_shared(rings) + threadIdx.x * kBytes;
+        uint2 mine = window(first), then = window(first + 32);
+        auto ask = [&](int j, const uint2 &from) {          // row j % 32 of a window
+            const uint32_t id = __shfl_sync(~0u, from.x, j), token = __shfl_sync(~0u, from.y, j);
+            if (active && id < p.vocab)
+                copy_async<kBytes>(ring + (j % kSumAhead) * (kSumThreads * kBytes), rows + token * p.row_stride);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        for (int j = 0; j < kSumAhead - 1; ++j)
+            ask(j, mine);
+        for (int64_t base = first; base < last; base += 32) {
+            const int here = (int)min((int64_t)32, last - base);
+#pragma unroll 4
+            for (int j = 0; j < here; ++j) {
+                const int k = j + kSumAhead - 1;
+                ask(k % 32, k < 32 ? mine : then);
+                asm volatile("cp.async.wait_group %0;" ::"n"(kSumAhead - 1) : "memory");
+                Vec<O, V> in;
+                in.word = *reinterpret_cast<const decltype(in.word) *>(reinterpret_cast<const char *>(rings) +
+                                                                      ((j % kSumAhead) * kSumThreads + threadIdx.x) * kBytes);
+                step(__shfl_sync(~0u, mine.x, j), in);
             }
+            mine = then;
+            then = window(base + 64);
+        }
+    } else {
+        for (int64_t base = first; base < last; base += 32) {
+            const uint2 mine = window(base);
+            const int here = (int)min((int64_t)32, last - base);
+            for (int j = 0; j < here; j += kNarrowAhead) {
+                Vec<O, V> in[kNarrowAhead];
 #pragma unroll
-            for (int k = 0; k < kSumAhead; ++k) {
-                const uint32_t id = __shfl_sync(~0u, mine.x, j + k);
-                if (j + k >= here)
-                    break;
-                if (id != run) {
-                    finish(false);
-                    run = id;
+                for (int k = 0; k < kNarrowAhead; ++k) {
+                    const uint32_t id = __shfl_sync(~0u, mine.x, j + k), token = __shfl_sync(~0u, mine.y, j + k);
+                    if (active && id < p.vocab)
+                        load_once(in[k], rows + token * p.row_stride);
                 }
-                if (active && id < p.vocab) {
-                    float f[V];
-                    widen(in[k], f);
 #pragma unroll
-                    for (int e = 0; e < V; ++e)
-                        sum[e] += f[e];
+                for (int k = 0; k < kNarrowAhead; ++k) {
+                    const uint32_t id = __shfl_sync(~0u, mine.x, j + k);
+                    if (j + k < here)
+                        step(id, in[k]);
                 }
             }
         }
@@ -685,7 +748,8 @@ template <typename W, typename O, int V> cudaError_t launch_backward(EmbedParams
         return cudaSuccess;
     if (p.sum_blocks + zeros > INT32_MAX)
         return cudaErrorInvalidConfiguration;
-    cudaError_t e = launch_chained(rikfad_embed_sum_kernel<W, O, V>, dim3((unsigned)(p.sum_blocks + zeros)), kSumThreads, 0, s, p);
+    cudaError_t e = launch_chained(rikfad_embed_sum_kernel<W, O, V>, dim3((unsigned)(p.sum_blocks + zeros)), kSumThreads,
+                                   V * sizeof(O) >= 4 ? (size_t)kSumAhead * kSumThreads * V * sizeof(O) : 0, s, p);
     if (e != cudaSuccess || p.chunks < 2)
         return e;
     const int64_t slabs = (p.pitch + 127) / 128, blocks = (p.chunks * slabs + kJoinWarps - 1) / kJoinWarps;
