@@ -30,7 +30,7 @@ constexpr int kForwardThreads = 256, kForwardRows = 4;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortCtas = 8, kSortItems = 8;
 constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kSortBits = 9;            // of a pass: the warps' counts of 2^9 digits take 32 KB
-constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32, kSumAhead = 8, kNarrowAhead = 8;
+constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32, kSumAhead = 8;
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinAhead = 4, kJoinBlocks = 4 * kSms;
 constexpr double kZeroBytesPerUs = 5e6; // of all multiprocessors but the sorting ones
 constexpr int kShortRun = 32;           // chunks that a run joined by one warp goes on in, at most
@@ -105,24 +105,30 @@ __global__ void __launch_bounds__(kForwardThreads) rikfad_embed_forward_kernel(c
         from[r] = table + id * p.table_stride;
         to[r] = t < p.tokens ? static_cast<O *>(p.rows) + t * p.row_stride : nullptr;
     }
-    for (int u = blockIdx.y * blockDim.x + threadIdx.x; u < p.units; u += blockDim.x * gridDim.y) {
-        Vec<W, V> in[kForwardRows];
+    constexpr int kUnits = V == 1 ? 4 : 1;          // single elements: more of them at once
+    const int step = blockDim.x * gridDim.y;
+    for (int u0 = blockIdx.y * blockDim.x + threadIdx.x; u0 < p.units; u0 += step * kUnits) {
+        Vec<W, V> in[kUnits][kForwardRows];
 #pragma unroll
-        for (int r = 0; r < kForwardRows; ++r)
-            if (inside[r])
-                load(in[r], from[r] + (int64_t)u * V);
+        for (int k = 0; k < kUnits; ++k)
 #pragma unroll
-        for (int r = 0; r < kForwardRows; ++r) {
-            float f[V];
-            widen(in[r], f);
+            for (int r = 0; r < kForwardRows; ++r)
+                if (inside[r] && u0 + k * step < p.units)
+                    load(in[k][r], from[r] + (int64_t)(u0 + k * step) * V);
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                f[e] = inside[r] ? f[e] * p.scale : 0.f;
-            Vec<O, V> out;
-            narrow(f, out);
-            if (to[r])
-                store(out, to[r] + (int64_t)u * V);
-        }
+        for (int k = 0; k < kUnits; ++k)
+#pragma unroll
+            for (int r = 0; r < kForwardRows; ++r) {
+                float f[V];
+                widen(in[k][r], f);
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    f[e] = inside[r] ? f[e] * p.scale : 0.f;
+                Vec<O, V> out;
+                narrow(f, out);
+                if (to[r] && u0 + k * step < p.units)
+                    store(out, to[r] + (int64_t)(u0 + k * step) * V);
+            }
     }
 }
 
@@ -256,18 +262,19 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
             uint2 e[kSortItems];
             uint32_t place[kSortItems];
             uint16_t *mine = counts + warp * bins;
+            // every warp has `rounds` times 32 neighbours
+            const int rounds = (min(end - tile, kSortTile) + kSortThreads - 1) / kSortThreads, first = tile + warp * rounds * 32 + lane;
+            auto item = [&](int k) { return k < rounds ? first + k * 32 : end; };
 #pragma unroll
-            for (int k = 0; k < kSortItems; ++k) {
-                const int i = tile + (warp * kSortItems + k) * 32 + lane;
-                e[k] = i < end ? entry(i) : make_uint2(0, 0);
-            }
+            for (int k = 0; k < kSortItems; ++k)
+                e[k] = item(k) < end ? entry(item(k)) : make_uint2(0, 0);
             for (int b = threadIdx.x; b < bins * kSortWarps / 2; b += kSortThreads)
                 reinterpret_cast<uint32_t *>(counts)[b] = 0;
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < kSortItems; ++k) {
-                const int i = tile + (warp * kSortItems + k) * 32 + lane;
-                if (i - lane >= end)
+                const int i = item(k);
+                if (k >= rounds)
                     break;
                 const uint32_t digit = e[k].x >> shift & (bins - 1);
                 const uint32_t same = __match_any_sync(~0u, i < end ? digit : ~0u);
@@ -305,9 +312,8 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < kSortItems; ++k) {
-                const int i = tile + (warp * kSortItems + k) * 32 + lane;
                 const uint32_t digit = e[k].x >> shift & (bins - 1);
-                if (i < end)
+                if (item(k) < end)
                     to[start[digit] + mine[digit] + place[k]] = e[k];
             }
             __syncthreads();
@@ -317,7 +323,7 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
 }
 
 // Few tokens: each one's place is the number of ids below its own and of equal ids before
-// it, counted by a warp.  All blocks count, then all write zeros.
+// it, counted by a warp.  Every other block writes zeros.
 __global__ void __launch_bounds__(kCountThreads) rikfad_embed_count_kernel(const __grid_constant__ SortParams p)
 {
     __shared__ uint4 all[kMostCounted / 4];
@@ -325,25 +331,41 @@ __global__ void __launch_bounds__(kCountThreads) rikfad_embed_count_kernel(const
     const int lane = threadIdx.x & 31, warps = kCountThreads / 32, n4 = (p.tokens + 3) / 4;
     wait_for_predecessor();
     allow_successor_launch();
+    if (blockIdx.x % 2) {
+        zero_rows(p, blockIdx.x / 2, gridDim.x / 2);
+        return;
+    }
     if (blockIdx.x == 0 && threadIdx.x < 2)
         p.counts[threadIdx.x] = 0;
-    for (int i = threadIdx.x; i < 4 * n4; i += kCountThreads)
-        ids[i] = i < p.tokens ? id_at(p.ids, p.id_bytes, i, p.vocab) : ~0u;
+    for (int i0 = threadIdx.x; i0 < 4 * n4; i0 += 8 * kCountThreads) {
+        uint32_t id[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = i0 + j * kCountThreads;
+            id[j] = i < p.tokens ? id_at(p.ids, p.id_bytes, i, p.vocab) : ~0u;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i0 + j * kCountThreads < 4 * n4)
+                ids[i0 + j * kCountThreads] = id[j];
+    }
     __syncthreads();
-    for (int t = blockIdx.x * warps + (threadIdx.x >> 5); t < p.tokens; t += gridDim.x * warps) {
+    for (int t = blockIdx.x / 2 * warps + (threadIdx.x >> 5); t < p.tokens; t += gridDim.x / 2 * warps) {
         const uint32_t id = ids[t];
         int before = 0;
+        // ids up to its own before the four where it is, ids below its own from there on
+#pragma unroll 4
         for (int i = lane; i < n4; i += 32) {
             const uint4 v = all[i];
-            before += (v.x < id) + (v.y < id) + (v.z < id) + (v.w < id);
-            before += (v.x == id && 4 * i < t) + (v.y == id && 4 * i + 1 < t) + (v.z == id && 4 * i + 2 < t) +
-                      (v.w == id && 4 * i + 3 < t);
+            const uint32_t end = id + (i < t / 4);
+            before += (v.x < end) + (v.y < end) + (v.z < end) + (v.w < end);
         }
+        for (int i = t / 4 * 4; i < t; ++i)
+            before += lane == 0 && ids[i] == id;
         before = __reduce_add_sync(~0u, before);
         if (lane == 0)
             p.to[before] = make_uint2(id, (uint32_t)t);
     }
-    zero_rows(p, blockIdx.x, gridDim.x);
 }
 
 // -------------------------------------------------------------------- the sums
@@ -391,7 +413,7 @@ template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, con
 
 // The first blocks write zeros to the rows without a token, 32 rows a warp; the last
 // sum_blocks sum chunks of sorted tokens, a warp 32 vectors of the row.
-template <typename W, typename O, int V>
+template <typename W, typename O, int V, int M>
 __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __grid_constant__ EmbedParams p)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -414,101 +436,112 @@ __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __g
     const int64_t item = (blockIdx.x - zero_blocks) * kSumWarps + warp, chunk = item / p.slabs;
     if (chunk >= p.chunks)
         return;
-    const int unit = (int)(item % p.slabs) * 32 + lane;
-    const bool active = unit < p.units;
+    const int unit = (int)(item % p.slabs) * 32 * M + lane;         // and every 32nd after it, M in all
+    const int first_unit = unit - lane, here_units = min(32 * M, p.units - first_unit);
+    auto active = [&](int m) { return unit + 32 * m < p.units; };
     const int64_t first = chunk * p.chunk, last = min(first + p.chunk, p.tokens);
     const O *rows = static_cast<const O *>(p.rows) + (int64_t)unit * V;
     uint32_t run = p.order[first].x;
     bool from_before = first > 0 && p.order[first - 1].x == run;
     const uint32_t after = last < p.tokens ? p.order[last].x : ~0u;
-    float sum[V];
+    float sum[M][V];
+    auto clear = [&] {
 #pragma unroll
-    for (int e = 0; e < V; ++e)
-        sum[e] = 0.f;
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                sum[m][e] = 0.f;
+    };
+    clear();
     auto finish = [&](bool goes_on) {
-        if (active && run < p.vocab) {
-            if (from_before || goes_on) {
-                float *part = (from_before ? p.head : p.tail) + chunk * p.pitch + (int64_t)unit * V;
+        if (run < p.vocab) {
 #pragma unroll
-                for (int e = 0; e < V; ++e)
-                    part[e] = sum[e];
-                if (unit == 0 && !from_before) {        // a run over several chunks starts here
-                    const int64_t far = chunk + kShortRun + 1;
-                    const int longer = far < p.chunks && p.order[far * p.chunk].x == run;
-                    const int at = atomicAdd(p.counts + longer, 1);     // in any order: each writes its own row
-                    p.starts[longer ? p.chunks - 1 - at : at] = (int32_t)chunk;
-                }
-            } else
-                write_row<W, V>(p, run, unit, sum);
+            for (int m = 0; m < M; ++m) {
+                if (!active(m))
+                    continue;
+                if (from_before || goes_on) {
+                    float *part = (from_before ? p.head : p.tail) + chunk * p.pitch + (int64_t)(unit + 32 * m) * V;
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        part[e] = sum[m][e];
+                } else
+                    write_row<W, V>(p, run, unit + 32 * m, sum[m]);
+            }
+            if (unit == 0 && goes_on && !from_before) {     // a run over several chunks starts here
+                const int64_t far = chunk + kShortRun + 1;
+                const int longer = far < p.chunks && p.order[far * p.chunk].x == run;
+                const int at = atomicAdd(p.counts + longer, 1);     // in any order: each writes its own row
+                p.starts[longer ? p.chunks - 1 - at : at] = (int32_t)chunk;
+            }
         }
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            sum[e] = 0.f;
+        clear();
         from_before = false;
     };
     auto window = [&](int64_t base) { return base + lane < last ? p.order[base + lane] : make_uint2(~0u, 0); };
-    auto step = [&](uint32_t id, const Vec<O, V> &in) {
+    auto step = [&](uint32_t id, const Vec<O, V> (&in)[M]) {
         if (id != run) {
             finish(false);
             run = id;
         }
-        if (active && id < p.vocab) {
-            float f[V];
-            widen(in, f);
+        if (id < p.vocab) {             // elements beyond the row's end are added up, but not written
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                sum[e] += f[e];
+            for (int m = 0; m < M; ++m) {
+                float f[V];
+                widen(in[m], f);
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    sum[m][e] += f[e];
+            }
         }
     };
-    constexpr int kBytes = V * sizeof(O);
-    if constexpr (kBytes >= 4) {
-        // a ring of kSumAhead rows, each lane's part copied and read by itself
-        extern __shared__ uint4 rings[];
-        const uint32_t ring = (uint32_t)__cvta_generic_to_shared(rings) + threadIdx.x * kBytes;
-        uint2 mine = window(first), then = window(first + 32);
-        auto ask = [&](int j, const uint2 &from) {          // row j % 32 of a window
-            const uint32_t id = __shfl_sync(~0u, from.x, j), token = __shfl_sync(~0u, from.y, j);
-            if (active && id < p.vocab)
-                copy_async<kBytes>(ring + (j % kSumAhead) * (kSumThreads * kBytes), rows + token * p.row_stride);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-        for (int j = 0; j < kSumAhead - 1; ++j)
-            ask(j, mine);
-        for (int64_t base = first; base < last; base += 32) {
-            const int here = (int)min((int64_t)32, last - base);
-#pragma unroll 4
-            for (int j = 0; j < here; ++j) {
-                const int k = j + kSumAhead - 1;
-                ask(k % 32, k < 32 ? mine : then);
-                asm volatile("cp.async.wait_group %0;" ::"n"(kSumAhead - 1) : "memory");
-                Vec<O, V> in;
-                in.word = *reinterpret_cast<const decltype(in.word) *>(reinterpret_cast<const char *>(rings) +
-                                                                      ((j % kSumAhead) * kSumThreads + threadIdx.x) * kBytes);
-                step(__shfl_sync(~0u, mine.x, j), in);
-            }
-            mine = then;
-            then = window(base + 64);
-        }
-    } else {
-        for (int64_t base = first; base < last; base += 32) {
-            const uint2 mine = window(base);
-            const int here = (int)min((int64_t)32, last - base);
-            for (int j = 0; j < here; j += kNarrowAhead) {
-                Vec<O, V> in[kNarrowAhead];
-#pragma unroll
-                for (int k = 0; k < kNarrowAhead; ++k) {
-                    const uint32_t id = __shfl_sync(~0u, mine.x, j + k), token = __shfl_sync(~0u, mine.y, j + k);
-                    if (active && id < p.vocab)
-                        load_once(in[k], rows + token * p.row_stride);
-                }
-#pragma unroll
-                for (int k = 0; k < kNarrowAhead; ++k) {
-                    const uint32_t id = __shfl_sync(~0u, mine.x, j + k);
-                    if (j + k < here)
-                        step(id, in[k]);
-                }
+    // a ring of kSumAhead rows' parts in shared memory
+    extern __shared__ uint4 rings[];
+    constexpr int kSlot = V > 1 ? 32 * V * (int)sizeof(O) : 32 * M * (int)sizeof(O) + 16;
+    char *const ring = reinterpret_cast<char *>(rings) + warp * (kSumAhead * kSlot);
+    uint2 mine = window(first), then = window(first + 32);
+    auto ask = [&](int j, int slot, const uint2 &entries) {
+        const uint32_t id = __shfl_sync(~0u, entries.x, j), token = __shfl_sync(~0u, entries.y, j);
+        if (id < p.vocab) {
+            const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + slot * kSlot);
+            if constexpr (V > 1) {
+                if (active(0))          // each lane's vector, for itself
+                    copy_async<V * (int)sizeof(O)>(to + lane * (V * (int)sizeof(O)), rows + token * p.row_stride);
+            } else {                    // all of the 16 bytes that the part begins and ends in, wherever that is
+                const char *from = reinterpret_cast<const char *>(static_cast<const O *>(p.rows) + token * p.row_stride + first_unit);
+                const int skip = (int)((uintptr_t)from % 16), words = (skip + here_units * (int)sizeof(O) + 15) / 16;
+                for (int i = lane; i < words; i += 32)
+                    copy_async<16>(to + 16 * i, from - skip + 16 * i);
             }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int j = 0; j < kSumAhead - 1; ++j)
+        ask(j, j, mine);
+    for (int64_t base = first; base < last; base += 32) {
+        const int here = (int)min((int64_t)32, last - base);
+#pragma unroll(V > 1 ? 4 : 2)
+        for (int j = 0; j < here; ++j) {
+            const int k = j + kSumAhead - 1;
+            ask(k % 32, k % kSumAhead, k < 32 ? mine : then);
+            asm volatile("cp.async.wait_group %0;" ::"n"(kSumAhead - 1) : "memory");
+            const uint32_t id = __shfl_sync(~0u, mine.x, j);
+            const char *at = ring + j % kSumAhead * kSlot;
+            Vec<O, V> in[M];
+            if constexpr (V > 1)
+                in[0].word = *reinterpret_cast<const decltype(in[0].word) *>(at + lane * (V * (int)sizeof(O)));
+            else {
+                __syncwarp();           // other lanes' copies
+                const uint32_t token = __shfl_sync(~0u, mine.y, j);
+                at += (uintptr_t)(static_cast<const O *>(p.rows) + token * p.row_stride + first_unit) % 16;
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+                    in[m].v[0] = reinterpret_cast<const O *>(at)[lane + 32 * m];
+                __syncwarp();           // before the place is written again
+            }
+            step(id, in);
+        }
+        mine = then;
+        then = window(base + 64);
     }
     finish(run == after);
 }
@@ -641,8 +674,8 @@ int check(const rikfad_embedding *p, int &device)
     return rc;
 }
 
-// The widest vectors, of at most 16 bytes in the wider type, that the width, the
-// strides and the addresses allow.
+// Vectors of 16 bytes in the wider type where the width, the strides and the addresses
+// allow them, else single elements.
 int vector_of(const rikfad_embedding *p)
 {
     const int tb = dtype_bytes(p->table_dtype), rb = dtype_bytes(p->dtype);
@@ -651,10 +684,8 @@ int vector_of(const rikfad_embedding *p)
         parts |= (uint64_t)p->table.stride;
     if (p->tokens > 1)
         parts |= (uint64_t)p->rows.stride;
-    int v = 16 / std::max(tb, rb);
-    while (parts % v)
-        v /= 2;
-    return v;
+    const int v = 16 / std::max(tb, rb);
+    return parts % v ? 1 : v;
 }
 
 EmbedParams params(const rikfad_embedding *p)
@@ -726,9 +757,12 @@ struct Workspace {
 Workspace workspace_of(const rikfad_embedding *p)
 {
     Workspace w;
-    // Chunks of more tokens leave fewer partial rows, as long as there are warps enough.
-    w.chunk = 32;
-    while (w.chunk < 256 && p->tokens / w.chunk * ((p->width + 255) / 256) > kSms * 96)
+    // Chunks of more tokens leave fewer partial rows, as long as there are warps enough, of
+    // 512 bytes of a row each: some to have work at all (4099 tokens of 1001, forward and
+    // gradient: 47 us with 32 a chunk, 37 with 8), many before partial rows are few.
+    const int64_t slabs = (p->width * dtype_bytes(p->dtype) + 511) / 512;
+    w.chunk = 8;
+    while (w.chunk < 256 && p->tokens / w.chunk * slabs > kSms * (w.chunk < 32 ? 16 : 96))
         w.chunk *= 2;
     w.chunks = (p->tokens + w.chunk - 1) / w.chunk;
     w.pitch = (p->width + 3) / 4 * 4;
@@ -741,15 +775,16 @@ Workspace workspace_of(const rikfad_embedding *p)
 template <typename W, typename O, int V> cudaError_t launch_backward(EmbedParams p, cudaStream_t s)
 {
     p.units = p.width / V;
-    p.slabs = (p.units + 31) / 32;
+    constexpr int M = V > 1 ? 1 : 16 / (int)sizeof(O);      // vectors of a lane
+    p.slabs = (p.units + 32 * M - 1) / (32 * M);
     p.sum_blocks = (p.chunks * p.slabs + kSumWarps - 1) / kSumWarps;
     const int64_t zeros = (p.zero_from + 32 * kSumWarps - 1) / (32 * kSumWarps);
     if (p.sum_blocks + zeros == 0)
         return cudaSuccess;
     if (p.sum_blocks + zeros > INT32_MAX)
         return cudaErrorInvalidConfiguration;
-    cudaError_t e = launch_chained(rikfad_embed_sum_kernel<W, O, V>, dim3((unsigned)(p.sum_blocks + zeros)), kSumThreads,
-                                   V * sizeof(O) >= 4 ? (size_t)kSumAhead * kSumThreads * V * sizeof(O) : 0, s, p);
+    cudaError_t e = launch_chained(rikfad_embed_sum_kernel<W, O, V, M>, dim3((unsigned)(p.sum_blocks + zeros)), kSumThreads,
+                                   (size_t)kSumAhead * kSumWarps * (V > 1 ? 32 * V * sizeof(O) : 528), s, p);
     if (e != cudaSuccess || p.chunks < 2)
         return e;
     const int64_t slabs = (p.pitch + 127) / 128, blocks = (p.chunks * slabs + kJoinWarps - 1) / kJoinWarps;
@@ -760,7 +795,7 @@ template <typename W, typename O, bool BACKWARD, int V> cudaError_t launch(const
 {
     if constexpr (V > 1)
         if (v < V)
-            return launch<W, O, BACKWARD, V / 2>(p, v, s);
+            return launch<W, O, BACKWARD, 1>(p, v, s);
     if constexpr (BACKWARD)
         return launch_backward<W, O, V>(p, s);
     else
@@ -878,7 +913,7 @@ RIKFAD_API int rikfad_embedding_backward(const rikfad_embedding *p, void *stream
             ++bits;
         r.passes = (bits + kSortBits - 1) / kSortBits;
         r.bits = (bits + r.passes - 1) / r.passes;
-        e = p->tokens <= kMostCounted ? launch_chained(rikfad_embed_count_kernel, dim3(2 * kSms), kCountThreads, 0, s, r)
+        e = p->tokens <= kMostCounted ? launch_chained(rikfad_embed_count_kernel, dim3(4 * kSms), kCountThreads, 0, s, r)
                                       : launch_sort(r, s);
         if (e != cudaSuccess)
             return report_cuda(e, "launch of the embedding's sort");

@@ -30,6 +30,7 @@ class TokenEmbedding:
             raise ValueError("width must be in [1, 2^20]")
         if not math.isfinite(self.scale) or abs(self.scale) > 3e38:
             raise ValueError("scale must be finite in float32")
+        self._workspace = {}        # bytes by sizes and types
 
     def _ids(self, ids, device):
         """(address, bytes of an id, tokens)."""
@@ -100,7 +101,13 @@ class TokenEmbedding:
                 at, po, so, pd, sd)
         pw = nbytes = 0
         if tokens:
-            nbytes = lib.rikfad_embedding_workspace(_EMBEDDING.pack(*body, 0, 0))
+            shape = body[:5]            # the size of the workspace goes by sizes and types alone
+            nbytes = self._workspace.get(shape)
+            if nbytes is None:
+                nbytes = lib.rikfad_embedding_workspace(_EMBEDDING.pack(*body, 0, 0))
+                if len(self._workspace) >= 64:
+                    self._workspace.clear()
+                self._workspace[shape] = nbytes
             work = torch.empty(nbytes, dtype=torch.uint8, device=dout.device)
             pw = work.data_ptr()
         rikfad._call_on(device, lib.rikfad_embedding_backward, _EMBEDDING.pack(*body, pw, nbytes), rikfad._raw_stream(device))
