@@ -22,6 +22,7 @@
 #include "rikfad.h"
 #include "rikfad_host.hpp"
 #include "rikfad_kernels.cuh"
+#include "rikfad_pairs.cuh"
 #include "rikfad_types.cuh"
 
 using namespace rikfad;
@@ -61,39 +62,6 @@ struct Params {
     float lowest_t, lowest_1;       // references below which a row has nothing else
 };
 
-// Two float32 in one register pair: one instruction for both.
-struct Pair {
-    uint64_t w;
-};
-__device__ __forceinline__ Pair pair(float x, float y)
-{
-    Pair p;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(p.w) : "f"(x), "f"(y));
-    return p;
-}
-__device__ __forceinline__ void apart(const Pair &p, float &x, float &y)
-{
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p.w));
-}
-__device__ __forceinline__ Pair fma2(const Pair &a, const Pair &b, const Pair &c)
-{
-    Pair p;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(p.w) : "l"(a.w), "l"(b.w), "l"(c.w));
-    return p;
-}
-__device__ __forceinline__ Pair add2(const Pair &a, const Pair &b)
-{
-    Pair p;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(p.w) : "l"(a.w), "l"(b.w));
-    return p;
-}
-__device__ __forceinline__ Pair mul2(const Pair &a, const Pair &b)
-{
-    Pair p;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(p.w) : "l"(a.w), "l"(b.w));
-    return p;
-}
-
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;
@@ -101,7 +69,7 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
-__device__ __forceinline__ Pair exp2_fast(const Pair &p)
+__device__ __forceinline__ f2 exp2_fast(f2 p)
 {
     float x, y;
     apart(p, x, y);
@@ -371,7 +339,7 @@ __global__ void __launch_bounds__(kMaxThreads) rikfad_distill_kernel(const __gri
         // that vector is masked, the thread goes over its part again and looks for the largest.
         Sums<BOTH> sums;
         if (threadIdx.x < mine) {
-            Pair of_t = pair(0.f, 0.f), of_1 = pair(0.f, 0.f);
+            f2 of_t = pair(0.f, 0.f), of_1 = pair(0.f, 0.f);
             float minus_t = 0.f, minus_1 = 0.f;
             for (int v = threadIdx.x; v < mine; v += threads * kAhead) {
                 Vec<T, V> in[kAhead];
@@ -391,10 +359,10 @@ __global__ void __launch_bounds__(kMaxThreads) rikfad_distill_kernel(const __gri
                         widen(in[j], x);
 #pragma unroll
                         for (int e = 0; e < V; e += 2) {
-                            const Pair both = pair(x[e], x[e + 1]);
-                            of_t = add2(of_t, exp2_fast(fma2(both, pair(p.c_t, p.c_t), pair(minus_t, minus_t))));
+                            const f2 both = pair(x[e], x[e + 1]);
+                            of_t = add(of_t, exp2_fast(fma(both, pair(p.c_t, p.c_t), pair(minus_t, minus_t))));
                             if (BOTH)
-                                of_1 = add2(of_1, exp2_fast(fma2(both, pair(p.c_1, p.c_1), pair(minus_1, minus_1))));
+                                of_1 = add(of_1, exp2_fast(fma(both, pair(p.c_1, p.c_1), pair(minus_1, minus_1))));
                         }
                     }
             }
@@ -488,11 +456,11 @@ __global__ void __launch_bounds__(kMaxThreads) rikfad_distill_kernel(const __gri
     const float c = BOTH && !distils ? p.c_1 : p.c_t, minus_r = BOTH && !distils ? -r_1 : -r_t;
     const float f = !BOTH ? f_t + f_1 : distils ? f_t : f_1;
     auto dense = [&](float x, float y, auto one_power) {
-        const Pair both = pair(x, y);
+        const f2 both = pair(x, y);
         if constexpr (decltype(one_power)::value)
-            return mul2(pair(f, f), exp2_fast(fma2(both, pair(c, c), pair(minus_r, minus_r))));
-        const Pair g = mul2(pair(f_t, f_t), exp2_fast(fma2(both, pair(p.c_t, p.c_t), pair(-r_t, -r_t))));
-        return fma2(pair(f_1, f_1), exp2_fast(fma2(both, pair(p.c_1, p.c_1), pair(-r_1, -r_1))), g);
+            return mul(pair(f, f), exp2_fast(fma(both, pair(c, c), pair(minus_r, minus_r))));
+        const f2 g = mul(pair(f_t, f_t), exp2_fast(fma(both, pair(p.c_t, p.c_t), pair(-r_t, -r_t))));
+        return fma(pair(f_1, f_1), exp2_fast(fma(both, pair(p.c_1, p.c_1), pair(-r_1, -r_1))), g);
     };
     auto dense_one = [&](float x) {
         float g, other;

@@ -37,50 +37,10 @@
 #include "rikfad_host.hpp"
 #include "rikfad_kernels.cuh"
 #include "rikfad_norm.hpp"
+#include "rikfad_pairs.cuh"
 #include "rikfad_types.cuh"
 
 namespace rikfad {
-
-// ------------------------------------------------- pairs of float32
-
-typedef uint64_t f2;        // two float32, the first in the low half
-
-__device__ __forceinline__ f2 pair(float lo, float hi)
-{
-    f2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ f2 both(float v) { return pair(v, v); }
-__device__ __forceinline__ float2 halves(f2 v)
-{
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ f2 add(f2 a, f2 b)
-{
-    f2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f2 mul(f2 a, f2 b)
-{
-    f2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f2 fma(f2 a, f2 b, f2 c)
-{
-    f2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ float total(f2 v)
-{
-    const float2 t = halves(v);
-    return t.x + t.y;
-}
 
 // 8 elements as 4 pairs.
 struct Vec8 {

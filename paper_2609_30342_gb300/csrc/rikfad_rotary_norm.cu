@@ -20,6 +20,7 @@
 #include "rikfad.h"
 #include "rikfad_host.hpp"
 #include "rikfad_kernels.cuh"
+#include "rikfad_pairs.cuh"
 #include "rikfad_rotary.cuh"
 #include "rikfad_types.cuh"
 
@@ -27,11 +28,24 @@ using namespace rikfad;
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 128;
 constexpr int kSms = 152;
-constexpr int kForwardBlocksPerSm = 4, kBackwardBlocksPerSm = 2;
-constexpr int kTablePairs = 4096;           // cosines and sines of a tile of tokens: 32 KB at most
+#ifndef FB
+#define FB 6
+#endif
+#ifndef BB
+#define BB 3
+#endif
+#ifndef RD
+#define RD 64
+#endif
+constexpr int kForwardBlocksPerSm = FB, kBackwardBlocksPerSm = BB;
+constexpr int kTablePairs = 1024;           // cosines and sines of a tile of tokens: 8 KB at most
 constexpr int kMaxHeadDim = 512;
+#ifndef KL
+#define KL 8
+#endif
+constexpr int kLeast = KL;
 constexpr int kJoinThreads = 1024;
 
 struct Heads {
@@ -51,6 +65,8 @@ struct Params {
     int32_t tile;                       // tokens of a tile
     int32_t lanes, turn_units, units;   // of a head: lanes, units that turn (half layout), all units
     float magnitude, inv_dim, eps;
+    int32_t pitch;                      // of a token's cosines and sines
+    int32_t split;                      // groups of lanes that have heads of the first list; the others have the second's
     float *part;                        // [block][list][head_dim]
 };
 
@@ -82,16 +98,27 @@ template <int V> __device__ __forceinline__ Place place_of(const Params &p, int 
     return at;
 }
 
+template <int BYTES> __device__ __forceinline__ void copy_async(void *to, const void *from)
+{
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
+}
+
+// A lane's units as loaded; zeros where there are none.
 template <typename T, int V, int U> struct Raw {
     Vec<T, V> a[U], b[U];
 
-    __device__ __forceinline__ void load(const T *head, const Place (&at)[U])
+    __device__ __forceinline__ void load(const T *head, const Place (&at)[U], bool active)
     {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (at[u].first >= 0)
+            a[u].word = b[u].word = decltype(a[u].word){};
+            if (active && at[u].first >= 0)
                 a[u].word = __ldcs(reinterpret_cast<const decltype(a[u].word) *>(head + at[u].first));
-            if (at[u].second >= 0)
+            if (active && at[u].second >= 0)
                 b[u].word = __ldcs(reinterpret_cast<const decltype(b[u].word) *>(head + at[u].second));
         }
     }
@@ -105,233 +132,391 @@ template <typename T, int V, int U> struct Raw {
                 *reinterpret_cast<decltype(b[u].word) *>(head + at[u].second) = b[u].word;
         }
     }
-    // Values; zeros where there are none.
-    __device__ __forceinline__ void values(float (&v)[U][2 * V], const Place (&at)[U], bool active) const
+};
+
+// A unit's 2 V elements in float32, two to a register pair: the first vector's, then the
+// second's (with V = 1, both vectors' elements are one pair).
+template <int V> struct Values {
+    f2 p[V];
+
+    template <typename T> __device__ __forceinline__ void from(const Vec<T, V> &a, const Vec<T, V> &b)
     {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float x[V], y[V];
-            widen(a[u], x);
-            widen(b[u], y);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                v[u][e] = active && at[u].first >= 0 ? x[e] : 0.f;
-                v[u][V + e] = active && at[u].second >= 0 ? y[e] : 0.f;
-            }
-        }
+        float x[V], y[V];
+        widen(a, x);
+        widen(b, y);
+        put(x, y);
     }
-    __device__ __forceinline__ void take(const float (&v)[U][2 * V])
+    template <typename T> __device__ __forceinline__ void to(Vec<T, V> &a, Vec<T, V> &b) const
     {
+        float x[V], y[V];
+        get(x, y);
+        narrow(x, a);
+        narrow(y, b);
+    }
+    __device__ __forceinline__ void put(const float (&x)[V], const float (&y)[V])
+    {
+        if constexpr (V == 1)
+            p[0] = pair(x[0], y[0]);
+        else
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float x[V], y[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                x[e] = v[u][e];
-                y[e] = v[u][V + e];
+            for (int e = 0; e < V; e += 2) {
+                p[e / 2] = pair(x[e], x[e + 1]);
+                p[V / 2 + e / 2] = pair(y[e], y[e + 1]);
             }
-            narrow(x, a[u]);
-            narrow(y, b[u]);
-        }
+    }
+    __device__ __forceinline__ void get(float (&x)[V], float (&y)[V]) const
+    {
+        if constexpr (V == 1)
+            apart(p[0], x[0], y[0]);
+        else
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+                apart(p[e / 2], x[e], x[e + 1]);
+                apart(p[V / 2 + e / 2], y[e], y[e + 1]);
+            }
     }
 };
 
-__device__ __forceinline__ void turn_pair(float &x, float &y, const float2 &cs)
+__device__ __forceinline__ void turn_pair(float &x, float &y, float c, float s)
 {
     const float u = x, v = y;
-    x = fmaf(u, cs.x, -v * cs.y);
-    y = fmaf(v, cs.x, u * cs.y);
+    x = fmaf(u, c, -v * s);
+    y = fmaf(v, c, u * s);
 }
 
-// The pairs of the lane's units turned by the token's cosines and sines.
-template <int V, int U>
-__device__ __forceinline__ void turn(const Params &p, float (&v)[U][2 * V], const Place (&at)[U], const float2 *table)
+// A unit's pairs turned by the token's cosines and sines.
+template <int V> __device__ __forceinline__ void turn(const Params &p, Values<V> &v, const Place &at, const float *cosines, const float *sines)
 {
+    if (at.pair < 0)
+        return;
+    constexpr int L = V < 4 ? V : 4;            // elements of one load
+    Vec<float, L> c[V / L], s[V / L];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        if (at[u].pair < 0)
-            continue;
-        if (p.interleaved) {            // pair e is elements 2 e and 2 e + 1; the last unit may reach beyond rotary_dim
+    for (int i = 0; i < V / L; ++i) {
+        c[i].word = reinterpret_cast<const decltype(c[i].word) *>(cosines + at.pair)[i];
+        s[i].word = reinterpret_cast<const decltype(s[i].word) *>(sines + at.pair)[i];
+    }
+    if constexpr (V > 1)
+        if (!p.interleaved) {
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                if (at[u].pair + e < p.pairs)
-                    turn_pair(v[u][2 * e], v[u][2 * e + 1], table[at[u].pair + e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                turn_pair(v[u][e], v[u][V + e], table[at[u].pair + e]);
+            for (int e = 0; e < V; e += 2) {
+                const f2 ce = pair(c[e / L].v[e % L], c[e / L].v[e % L + 1]), se = pair(s[e / L].v[e % L], s[e / L].v[e % L + 1]);
+                f2 &a = v.p[e / 2], &b = v.p[V / 2 + e / 2];
+                const f2 x = a;
+                a = sub(mul(a, ce), mul(b, se));
+                b = fma(x, se, mul(b, ce));
+            }
+            return;
         }
+    // pair e is elements 2 e and 2 e + 1; the last unit may reach beyond rotary_dim
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        float x, y;
+        apart(v.p[e], x, y);
+        if (at.pair + e < p.pairs)
+            turn_pair(x, y, c[e / L].v[e % L], s[e / L].v[e % L]);
+        v.p[e] = pair(x, y);
     }
 }
 
-// Where a group of lanes is in its tile's heads, and how it goes on.
-struct Walk {
-    int slot, head, slots, heads;
+// A tile of tokens of one sequence.
+struct Tile {
+    int64_t batch, token0;
+    int here;                   // tokens; none beyond the last tile
 
-    __device__ __forceinline__ Walk(int item, int step, int count)
-        : slot(item / count), head(item % count), slots(step / count), heads(step % count)
+    __device__ __forceinline__ Tile(const Params &p, int64_t tile)
     {
-    }
-    __device__ __forceinline__ void next(int count)
-    {
-        head += heads;
-        const int over = head >= count;
-        head -= over ? count : 0;
-        slot += slots + over;
+        batch = p.tiles_per_sequence == p.tiles ? 0 : tile / p.tiles_per_sequence;
+        token0 = (tile - batch * p.tiles_per_sequence) * p.tile;
+        here = tile < p.tiles ? (int)min((int64_t)p.tile, p.tokens - token0) : 0;
     }
 };
 
+// How the groups that share a list go on from head to head: by `step` elements, and by
+// `wrap` more into the next token.
+struct Steps {
+    int64_t batch, token, first, step, wrap;
+
+    __device__ __forceinline__ Steps(int64_t per_batch, int64_t per_token, int64_t per_head, int g, int n, int heads)
+        : batch(per_batch), token(per_token)
+    {
+        const int slot = g / heads, slots = n / heads;
+        first = slot * per_token + (g - slot * heads) * per_head;
+        step = slots * per_token + (n - slots * heads) * per_head;
+        wrap = per_token - heads * per_head;
+    }
+    template <typename T> __device__ __forceinline__ T *at(T *base, const Tile &t) const
+    {
+        return base + (t.batch * batch + t.token0 * token + first);
+    }
+};
+
+// Bytes that a lane loads of a head, and how many of its heads are on their way.
+template <typename T, int V, int U, bool BACKWARD> struct Ring {
+    static constexpr int kWord = V * (int)sizeof(T), kWords = (BACKWARD ? 4 : 2) * U;
+    static constexpr int kDepth = kWord < 4 ? 1 : kWord * kWords > RD ? 2 : BACKWARD ? 4 : 4;
+    static constexpr int kBytes = kWord < 4 ? 0 : kDepth * kWords * kWord * kThreads;
+};
+
+// A block has tile after tile of tokens: their cosines and sines, formed once a tile, and
+// all heads, shared by its groups of lanes.  A group has heads of one list, and their
+// weights' gradients in registers.  Its next kDepth heads are on their way meanwhile, each
+// lane's vectors to a place of shared memory of its own (types of 2 bytes in single
+// elements: the next head, to registers).
 template <typename T, int V, int U, bool BACKWARD>
 __global__ void __launch_bounds__(kThreads, BACKWARD ? kBackwardBlocksPerSm : kForwardBlocksPerSm)
 rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
 {
-    extern __shared__ float2 table[];
-    __shared__ float weights[2][kMaxHeadDim];
-    const int groups = kThreads / p.lanes, group = threadIdx.x / p.lanes, lane = threadIdx.x % p.lanes;
-    const int warp_group = (threadIdx.x & ~31) / p.lanes;       // the first of the warp
+    using R = Ring<T, V, U, BACKWARD>;
+    extern __shared__ float4 shared[];
+    float *const cosines = reinterpret_cast<float *>(reinterpret_cast<char *>(shared) + R::kBytes), *const sines = cosines + p.tile * p.pitch;
+    const int group = threadIdx.x / p.lanes, lane = threadIdx.x % p.lanes;
     Place at[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
         at[u] = place_of<V>(p, lane + u * p.lanes);
-    float sums[2][U][2 * V];
+    const bool list = group >= p.split;
+    const int g = list ? group - p.split : group, n = list ? kThreads / p.lanes - p.split : p.split;
+    const Heads &h0 = p.lists[0], &h1 = p.lists[1];
+    const int heads = list ? h1.heads : h0.heads, more_heads = n - n / heads * heads;
+    auto steps = [&](int64_t b0, int64_t b1, int64_t t0, int64_t t1, int64_t s0, int64_t s1) {
+        return Steps(list ? b1 : b0, list ? t1 : t0, list ? s1 : s0, g, n, heads);
+    };
+    const Steps of_x = steps(h0.x_batch, h1.x_batch, h0.x_token, h1.x_token, h0.x_head, h1.x_head);
+    const Steps of_dout = steps(h0.dout_batch, h1.dout_batch, h0.dout_token, h1.dout_token, h0.dout_head, h1.dout_head);
+    const Steps of_out = steps(h0.out_batch, h1.out_batch, h0.out_token, h1.out_token, h0.out_head, h1.out_head);
+    const T *const x = static_cast<const T *>(list ? h1.x : h0.x), *const dout = static_cast<const T *>(list ? h1.dout : h0.dout);
+    T *const out = static_cast<T *>(list ? h1.out : h0.out);
+    // heads of a group in a tile of that many tokens: the same for all groups
+    auto rounds_of = [&](int here) {
+        const int q = (here * h0.heads + p.split - 1) / max(p.split, 1), others = kThreads / p.lanes - p.split;
+        return max(q, (here * h1.heads + others - 1) / max(others, 1));
+    };
+    Values<V> sums[U];
     if constexpr (BACKWARD)
 #pragma unroll
-        for (int l = 0; l < 2; ++l)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int e = 0; e < 2 * V; ++e)
-                    sums[l][u][e] = 0.f;
+            for (int e = 0; e < V; ++e)
+                sums[u].p[e] = pair(0.f, 0.f);
     wait_for_predecessor();
     allow_successor_launch();
-    for (int i = threadIdx.x; i < 2 * p.head_dim; i += kThreads) {
-        const int l = i / p.head_dim, e = i % p.head_dim;
-        const void *w = p.lists[l].weight;
-        weights[l][e] = w == nullptr ? 1.f : p.param_f32 ? static_cast<const float *>(w)[e] : to_f32(static_cast<const T *>(w)[e]);
+    // the head to load next
+    int64_t ask_tile = blockIdx.x;
+    int ask_round = 0, ask_rounds, ask_item, ask_items, ask_head;
+    const T *from, *dfrom;
+    auto ask_enter = [&] {
+        const Tile t(p, ask_tile);
+        from = of_x.at(x, t);
+        dfrom = of_dout.at(dout, t);
+        ask_round = 0;
+        ask_rounds = rounds_of(t.here);
+        ask_item = g;
+        ask_items = t.here * heads;
+        ask_head = g % heads;
+    };
+    auto ask_next = [&] {
+        if (++ask_round >= ask_rounds) {
+            ask_tile += gridDim.x;
+            ask_enter();
+            return;
+        }
+        ask_item += n;
+        ask_head += more_heads;
+        const bool over = ask_head >= heads;
+        ask_head -= over ? heads : 0;
+        from += of_x.step + (over ? of_x.wrap : 0);
+        dfrom += of_dout.step + (over ? of_dout.wrap : 0);
+    };
+    // Vector i of a lane's in place j of the ring: the thread's own, neighbours side by side.
+    auto place = [&](int j, int i) {
+        return reinterpret_cast<char *>(shared) + ((j * R::kWords + i) * kThreads + threadIdx.x) * R::kWord;
+    };
+    auto request = [&](int j) {
+        if constexpr (R::kBytes > 0) {
+            if (ask_item < ask_items) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (at[u].first >= 0) {
+                        copy_async<R::kWord>(place(j, 2 * u), from + at[u].first);
+                        if (BACKWARD)
+                            copy_async<R::kWord>(place(j, 2 * U + 2 * u), dfrom + at[u].first);
+                    }
+                    if (at[u].second >= 0) {
+                        copy_async<R::kWord>(place(j, 2 * u + 1), from + at[u].second);
+                        if (BACKWARD)
+                            copy_async<R::kWord>(place(j, 2 * U + 2 * u + 1), dfrom + at[u].second);
+                    }
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            ask_next();
+        }
+    };
+    Raw<T, V, U> in, din;
+    ask_enter();
+    if constexpr (R::kBytes > 0) {
+#pragma unroll
+        for (int j = 0; j < R::kDepth; ++j)
+            request(j);
+    } else {
+        in.load(from, at, ask_item < ask_items);
+        if constexpr (BACKWARD)
+            din.load(dfrom, at, ask_item < ask_items);
     }
+    Values<V> w[U];
+    const void *const weights = list ? h1.weight : h0.weight;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        auto weight = [&](int e) {
+            return weights == nullptr ? 1.f
+                   : p.param_f32      ? static_cast<const float *>(weights)[e]
+                                      : to_f32(static_cast<const T *>(weights)[e]);
+        };
+        float a[V], b[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            a[e] = at[u].first >= 0 ? weight(at[u].first + e) : 0.f;
+            b[e] = at[u].second >= 0 ? weight(at[u].second + e) : 0.f;
+        }
+        w[u].put(a, b);
+    }
+    int turn_of_ring = 0;
     for (int64_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
-        const int64_t batch = p.tiles_per_sequence == p.tiles ? 0 : tile / p.tiles_per_sequence;
-        const int64_t token0 = (tile - batch * p.tiles_per_sequence) * p.tile;
-        const int here = (int)min((int64_t)p.tile, p.tokens - token0);
+        const Tile t(p, tile);
         __syncthreads();
-        for (int i = threadIdx.x; i < here * p.pairs; i += kThreads) {
-            const int64_t position =
-                token_position(p.positions, p.position_bytes, p.position_batch, p.start, batch, token0 + i / p.pairs);
-            const float2 cs = cosine_sine(position, p.turns[i % p.pairs]);
-            table[i] = make_float2(cs.x * p.magnitude, cs.y * (BACKWARD ? -p.magnitude : p.magnitude));
+        for (int i = threadIdx.x; i < t.here * p.pairs; i += kThreads) {
+            const int slot = i / p.pairs, e = i - slot * p.pairs;
+            const int64_t position = token_position(p.positions, p.position_bytes, p.position_batch, p.start, t.batch, t.token0 + slot);
+            const float2 cs = cosine_sine(position, p.turns[e]);
+            cosines[slot * p.pitch + e] = cs.x * p.magnitude;
+            sines[slot * p.pitch + e] = cs.y * (BACKWARD ? -p.magnitude : p.magnitude);
         }
         __syncthreads();
+        const int rounds = rounds_of(t.here), items = t.here * heads, table_step = n / heads * p.pitch;
+        T *to = of_out.at(out, t);
+        int head = g % heads, table = g / heads * p.pitch, item = g;
+        for (int round = 0; round < rounds; ++round) {
+            const bool active = item < items;
+            Raw<T, V, U> next, dnext;
+            if constexpr (R::kBytes > 0) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(R::kDepth - 1) : "memory");
 #pragma unroll
-        for (int l = 0; l < 2; ++l) {
-            const Heads &h = p.lists[l];
-            const int items = here * h.heads;
-            if (items == 0)
-                continue;
-            float w[U][2 * V];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    w[u][e] = at[u].first >= 0 ? weights[l][at[u].first + e] : 0.f;
-                    w[u][V + e] = at[u].second >= 0 ? weights[l][at[u].second + e] : 0.f;
+                for (int u = 0; u < U; ++u) {
+                    auto take = [&](Vec<T, V> &v, int i, bool there) {
+                        v.word = decltype(v.word){};
+                        if (there && active)
+                            v.word = *reinterpret_cast<const decltype(v.word) *>(place(turn_of_ring, i));
+                    };
+                    take(in.a[u], 2 * u, at[u].first >= 0);
+                    take(in.b[u], 2 * u + 1, at[u].second >= 0);
+                    if constexpr (BACKWARD) {
+                        take(din.a[u], 2 * U + 2 * u, at[u].first >= 0);
+                        take(din.b[u], 2 * U + 2 * u + 1, at[u].second >= 0);
+                    }
                 }
-            const T *x = static_cast<const T *>(h.x) + batch * h.x_batch + token0 * h.x_token;
-            const T *dout = static_cast<const T *>(h.dout) + batch * h.dout_batch + token0 * h.dout_token;
-            T *out = static_cast<T *>(h.out) + batch * h.out_batch + token0 * h.out_token;
-            Walk walk(group, groups, h.heads);
-            Raw<T, V, U> in, din;
-            if (group < items) {
-                in.load(x + walk.slot * h.x_token + walk.head * h.x_head, at);
+            } else {
+                ask_next();
+                next.load(from, at, ask_item < ask_items);
                 if constexpr (BACKWARD)
-                    din.load(dout + walk.slot * h.dout_token + walk.head * h.dout_head, at);
+                    dnext.load(dfrom, at, ask_item < ask_items);
             }
-            for (int first = warp_group, item = group; first < items; first += groups, item += groups) {
-                const bool active = item < items;
-                const int slot = walk.slot;
-                T *to = out + walk.slot * h.out_token + walk.head * h.out_head;
-                Raw<T, V, U> next, dnext;
-                walk.next(h.heads);
-                if (item + groups < items) {
-                    next.load(x + walk.slot * h.x_token + walk.head * h.x_head, at);
-                    if constexpr (BACKWARD)
-                        dnext.load(dout + walk.slot * h.dout_token + walk.head * h.dout_head, at);
+            const float *const c = cosines + (active ? table : 0), *const s = sines + (active ? table : 0);
+            Values<V> v[U];
+            f2 squares2 = pair(0.f, 0.f);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                v[u].from(in.a[u], in.b[u]);
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    squares2 = fma(v[u].p[e], v[u].p[e], squares2);
+            }
+            float squares = total(squares2);
+            if constexpr (BACKWARD) {
+                Values<V> d[U];
+                f2 product2 = pair(0.f, 0.f);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    d[u].from(din.a[u], din.b[u]);
+                    turn<V>(p, d[u], at[u], c, s);
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        product2 = fma(mul(d[u].p[e], w[u].p[e]), v[u].p[e], product2);
                 }
-                float v[U][2 * V], squares = 0.f;
-                in.values(v, at, active);
+                float product = total(product2);
+                // the next head on its way, now that this one has been taken
+                request(turn_of_ring);
+                for (int d = p.lanes / 2; d > 0; d /= 2) {
+                    squares += __shfl_xor_sync(~0u, squares, d);
+                    product += __shfl_xor_sync(~0u, product, d);
+                }
+                const float r = active ? rsqrtf(fmaf(squares, p.inv_dim, p.eps)) : 0.f;
+                const f2 rr = both(r), minus = both(-product * p.inv_dim * r * r);
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int e = 0; e < 2 * V; ++e)
-                        squares = fmaf(v[u][e], v[u][e], squares);
-                if constexpr (BACKWARD) {
-                    float d[U][2 * V], product = 0.f;
-                    din.values(d, at, active);
-                    if (active)
-                        turn<V, U>(p, d, at, table + slot * p.pairs);
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-#pragma unroll
-                        for (int e = 0; e < 2 * V; ++e)
-                            product = fmaf(d[u][e] * w[u][e], v[u][e], product);
-                    for (int s = p.lanes / 2; s > 0; s /= 2) {
-                        squares += __shfl_xor_sync(~0u, squares, s);
-                        product += __shfl_xor_sync(~0u, product, s);
+                    for (int e = 0; e < V; ++e) {
+                        sums[u].p[e] = fma(d[u].p[e], mul(v[u].p[e], rr), sums[u].p[e]);
+                        v[u].p[e] = mul(rr, fma(minus, v[u].p[e], mul(d[u].p[e], w[u].p[e])));
                     }
-                    const float r = active ? rsqrtf(fmaf(squares, p.inv_dim, p.eps)) : 0.f;
-                    const float back = product * p.inv_dim * r * r;
+            } else {
+                request(turn_of_ring);
+                for (int d = p.lanes / 2; d > 0; d /= 2)
+                    squares += __shfl_xor_sync(~0u, squares, d);
+                const f2 rr = both(rsqrtf(fmaf(squares, p.inv_dim, p.eps)));
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
+                for (int u = 0; u < U; ++u) {
 #pragma unroll
-                        for (int e = 0; e < 2 * V; ++e) {
-                            sums[l][u][e] = fmaf(d[u][e], v[u][e] * r, sums[l][u][e]);
-                            v[u][e] = r * fmaf(-back, v[u][e], d[u][e] * w[u][e]);
-                        }
-                } else {
-                    for (int s = p.lanes / 2; s > 0; s /= 2)
-                        squares += __shfl_xor_sync(~0u, squares, s);
-                    const float r = rsqrtf(fmaf(squares, p.inv_dim, p.eps));
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-#pragma unroll
-                        for (int e = 0; e < 2 * V; ++e)
-                            v[u][e] *= r * w[u][e];
-                    if (active)
-                        turn<V, U>(p, v, at, table + slot * p.pairs);
+                    for (int e = 0; e < V; ++e)
+                        v[u].p[e] = mul(v[u].p[e], mul(rr, w[u].p[e]));
+                    turn<V>(p, v[u], at[u], c, s);
                 }
-                if (active) {
-                    in.take(v);
-                    in.store(to, at);
-                }
+            }
+            if (active) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    v[u].to(in.a[u], in.b[u]);
+                in.store(to, at);
+            }
+            if constexpr (R::kBytes > 0)
+                turn_of_ring = turn_of_ring + 1 == R::kDepth ? 0 : turn_of_ring + 1;
+            else {
                 in = next;
                 din = dnext;
             }
+            item += n;
+            head += more_heads;
+            const bool over = head >= heads;
+            head -= over ? heads : 0;
+            table += table_step + (over ? p.pitch : 0);
+            to += of_out.step + (over ? of_out.wrap : 0);
         }
     }
     if constexpr (BACKWARD) {
         if (p.part == nullptr)
             return;
-        float *sum = reinterpret_cast<float *>(table);      // [warp][element]
-        const int in_warp = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        for (int l = 0; l < p.nlists; ++l) {
-            __syncthreads();
+        // every group's sums, then those of a list's groups in order
+        float *sum = reinterpret_cast<float *>(shared);         // [group][element]
+        __syncthreads();
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            float a[V], b[V];
+            sums[u].get(a, b);
 #pragma unroll
-                for (int e = 0; e < 2 * V; ++e) {
-                    float s = l == 0 ? sums[0][u][e] : sums[1][u][e];
-                    for (int d = 16; d >= p.lanes; d /= 2)
-                        s += __shfl_xor_sync(~0u, s, d);
-                    const int first = e < V ? at[u].first : at[u].second;
-                    if (in_warp < p.lanes && first >= 0)
-                        sum[warp * p.head_dim + first + e % V] = s;
-                }
-            __syncthreads();
-            for (int e = threadIdx.x; e < p.head_dim; e += kThreads) {
-                float s = 0.f;
-                for (int w = 0; w < kWarps; ++w)
-                    s += sum[w * p.head_dim + e];
-                p.part[((int64_t)blockIdx.x * 2 + l) * p.head_dim + e] = s;
+            for (int e = 0; e < V; ++e) {
+                if (at[u].first >= 0)
+                    sum[group * p.head_dim + at[u].first + e] = a[e];
+                if (at[u].second >= 0)
+                    sum[group * p.head_dim + at[u].second + e] = b[e];
             }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * p.head_dim; i += kThreads) {
+            const int l = i >= p.head_dim, e = i - l * p.head_dim;
+            float s = 0.f;
+            for (int group = l ? p.split : 0; group < (l ? kThreads / p.lanes : p.split); ++group)
+                s += sum[group * p.head_dim + e];
+            p.part[((int64_t)blockIdx.x * 2 + l) * p.head_dim + e] = s;
         }
     }
 }
@@ -462,22 +647,25 @@ template <typename T, int V, int U, bool BACKWARD> cudaError_t launch(Params p, 
 {
     const int groups = kThreads / p.lanes;
     const int64_t heads = p.lists[0].heads + p.lists[1].heads, tokens = p.tiles * p.tokens;   // p.tiles: sequences, here
-    // Heads of a group in a tile: 2 to 16, so that a launch has a dozen rounds of blocks
-    // where it can, within the table's size.
-    const int64_t share = tokens * heads / ((int64_t)12 * kForwardBlocksPerSm * kSms * groups);
-    const int64_t each = std::max<int64_t>(2, std::min<int64_t>(16, share));
-    const int64_t most = std::min<int64_t>(p.tokens, p.pairs ? std::max(1, kTablePairs / p.pairs) : 1 << 10);
-    p.tile = (int32_t)std::max<int64_t>(1, std::min(most, each * groups / heads));
-    while (p.tile > 1 && (tokens + p.tile - 1) / p.tile < 2 * kSms)
-        p.tile /= 2;
+    // the groups of a block shared among the lists as their heads are
+    p.split = p.lists[1].heads == 0   ? groups
+              : p.lists[0].heads == 0 ? 0
+                                      : std::max(1, std::min(groups - 1, (int)((groups * (int64_t)p.lists[0].heads + heads / 2) / heads)));
+    // the last unit of the interleaved layout reads a vector's worth of the table
+    p.pitch = (std::max(p.pairs, p.interleaved && p.pairs ? (p.pairs + V - 1) / V * V : 0) + 3) / 4 * 4;
+    // As many tiles a block as leave a group kLeast heads of each, all of the same size; within
+    // the table's, and a token's at least.
+    const int64_t all = kSms * (BACKWARD ? kBackwardBlocksPerSm : kForwardBlocksPerSm);
+    const int64_t wish = std::max<int64_t>(1, kLeast * groups / heads);
+    const int64_t most = std::min<int64_t>(wish, p.pairs ? std::max(1, kTablePairs / p.pitch) : 1 << 10);
+    const int64_t each = (tokens + all * most - 1) / (all * most);
+    p.tile = (int32_t)std::min<int64_t>(p.tokens, std::max<int64_t>(1, (tokens + all * each - 1) / (all * each)));
     p.tiles_per_sequence = (p.tokens + p.tile - 1) / p.tile;
     p.tiles *= p.tiles_per_sequence;
-    if (!BACKWARD && p.tiles > INT32_MAX)
-        return cudaErrorInvalidConfiguration;
-    const int64_t blocks = BACKWARD ? std::min<int64_t>(p.tiles, kSms * kBackwardBlocksPerSm) : p.tiles;
-    size_t smem = sizeof(float2) * (size_t)p.tile * p.pairs;
+    const int64_t blocks = std::min(p.tiles, all);
+    size_t smem = Ring<T, V, U, BACKWARD>::kBytes + 2 * sizeof(float) * (size_t)p.tile * p.pitch;
     if (BACKWARD && p.part)
-        smem = std::max(smem, sizeof(float) * kWarps * (size_t)p.head_dim);
+        smem = std::max(smem, sizeof(float) * groups * (size_t)p.head_dim);
     const cudaError_t e =
         launch_chained(rikfad_rotary_norm_kernel<T, V, U, BACKWARD>, dim3((unsigned)blocks), kThreads, smem, s, p);
     if (e != cudaSuccess || !BACKWARD || p.part == nullptr)
