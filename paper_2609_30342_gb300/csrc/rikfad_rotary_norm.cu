@@ -30,22 +30,10 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kSms = 152;
-#ifndef FB
-#define FB 6
-#endif
-#ifndef BB
-#define BB 3
-#endif
-#ifndef RD
-#define RD 64
-#endif
-constexpr int kForwardBlocksPerSm = FB, kBackwardBlocksPerSm = BB;
+constexpr int kForwardBlocksPerSm = 4, kBackwardBlocksPerSm = 3;
 constexpr int kTablePairs = 1024;           // cosines and sines of a tile of tokens: 8 KB at most
 constexpr int kMaxHeadDim = 512;
-#ifndef KL
-#define KL 8
-#endif
-constexpr int kLeast = KL;
+constexpr int kWish = 32;                   // heads of a group in a tile
 constexpr int kJoinThreads = 1024;
 
 struct Heads {
@@ -254,7 +242,7 @@ struct Steps {
 // Bytes that a lane loads of a head, and how many of its heads are on their way.
 template <typename T, int V, int U, bool BACKWARD> struct Ring {
     static constexpr int kWord = V * (int)sizeof(T), kWords = (BACKWARD ? 4 : 2) * U;
-    static constexpr int kDepth = kWord < 4 ? 1 : kWord * kWords > RD ? 2 : BACKWARD ? 4 : 4;
+    static constexpr int kDepth = kWord < 4 ? 1 : kWord * kWords > 64 ? 2 : 4;
     static constexpr int kBytes = kWord < 4 ? 0 : kDepth * kWords * kWord * kThreads;
 };
 
@@ -356,6 +344,13 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
     Raw<T, V, U> in, din;
     ask_enter();
     if constexpr (R::kBytes > 0) {
+        // vectors that a lane has not stay zeros
+#pragma unroll
+        for (int i = 0; i < R::kDepth * R::kWords; ++i) {
+            Vec<T, V> none;
+            none.word = decltype(none.word){};
+            *reinterpret_cast<decltype(none.word) *>(place(0, i)) = none.word;
+        }
 #pragma unroll
         for (int j = 0; j < R::kDepth; ++j)
             request(j);
@@ -403,16 +398,12 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
                 asm volatile("cp.async.wait_group %0;" ::"n"(R::kDepth - 1) : "memory");
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    auto take = [&](Vec<T, V> &v, int i, bool there) {
-                        v.word = decltype(v.word){};
-                        if (there && active)
-                            v.word = *reinterpret_cast<const decltype(v.word) *>(place(turn_of_ring, i));
-                    };
-                    take(in.a[u], 2 * u, at[u].first >= 0);
-                    take(in.b[u], 2 * u + 1, at[u].second >= 0);
+                    auto take = [&](Vec<T, V> &v, int i) { v.word = *reinterpret_cast<const decltype(v.word) *>(place(turn_of_ring, i)); };
+                    take(in.a[u], 2 * u);
+                    take(in.b[u], 2 * u + 1);
                     if constexpr (BACKWARD) {
-                        take(din.a[u], 2 * U + 2 * u, at[u].first >= 0);
-                        take(din.b[u], 2 * U + 2 * u + 1, at[u].second >= 0);
+                        take(din.a[u], 2 * U + 2 * u);
+                        take(din.b[u], 2 * U + 2 * u + 1);
                     }
                 }
             } else {
@@ -450,15 +441,19 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
                     squares += __shfl_xor_sync(~0u, squares, d);
                     product += __shfl_xor_sync(~0u, product, d);
                 }
-                const float r = active ? rsqrtf(fmaf(squares, p.inv_dim, p.eps)) : 0.f;
+                const float r = rsqrtf(fmaf(squares, p.inv_dim, p.eps));
                 const f2 rr = both(r), minus = both(-product * p.inv_dim * r * r);
+                if (active)                     // else what was there before
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int e = 0; e < V; ++e)
+                            sums[u].p[e] = fma(d[u].p[e], mul(v[u].p[e], rr), sums[u].p[e]);
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        sums[u].p[e] = fma(d[u].p[e], mul(v[u].p[e], rr), sums[u].p[e]);
+                    for (int e = 0; e < V; ++e)
                         v[u].p[e] = mul(rr, fma(minus, v[u].p[e], mul(d[u].p[e], w[u].p[e])));
-                    }
             } else {
                 request(turn_of_ring);
                 for (int d = p.lanes / 2; d > 0; d /= 2)
@@ -653,12 +648,13 @@ template <typename T, int V, int U, bool BACKWARD> cudaError_t launch(Params p, 
                                       : std::max(1, std::min(groups - 1, (int)((groups * (int64_t)p.lists[0].heads + heads / 2) / heads)));
     // the last unit of the interleaved layout reads a vector's worth of the table
     p.pitch = (std::max(p.pairs, p.interleaved && p.pairs ? (p.pairs + V - 1) / V * V : 0) + 3) / 4 * 4;
-    // As many tiles a block as leave a group kLeast heads of each, all of the same size; within
-    // the table's, and a token's at least.
+    // As many tiles a block as leave a group kWish heads of each, all of the same size, within
+    // the table's; two at least where they are large, so that one's table and another's heads
+    // are formed at one time.
     const int64_t all = kSms * (BACKWARD ? kBackwardBlocksPerSm : kForwardBlocksPerSm);
-    const int64_t wish = std::max<int64_t>(1, kLeast * groups / heads);
+    const int64_t wish = std::max<int64_t>(1, kWish * groups / heads);
     const int64_t most = std::min<int64_t>(wish, p.pairs ? std::max(1, kTablePairs / p.pitch) : 1 << 10);
-    const int64_t each = (tokens + all * most - 1) / (all * most);
+    const int64_t each = std::max<int64_t>((tokens + all * most - 1) / (all * most), tokens > 16 * all ? 2 : 1);
     p.tile = (int32_t)std::min<int64_t>(p.tokens, std::max<int64_t>(1, (tokens + all * each - 1) / (all * each)));
     p.tiles_per_sequence = (p.tokens + p.tile - 1) / p.tile;
     p.tiles *= p.tiles_per_sequence;
