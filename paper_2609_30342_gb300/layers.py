@@ -30,6 +30,7 @@ _ROTARY = struct.Struct("=2q 4i qq2q 2i 2i d 18q")
 # struct rikfad_rotary_norm: sizes, types, pointers, positions, magnitude and eps, two sets of heads, workspace
 _ROTARY_NORM = struct.Struct("=2q 4i qq2q 2i 2i 2d 30q qQ")
 
+_DENSE = torch.contiguous_format
 _NO_BACKWARD = (0,) * 16
 _NO_HEADS = (0,) * 9
 _NO_NORM_HEADS = (0,) * 15
@@ -434,6 +435,11 @@ class RotaryNorm(Rotary):
             raise ValueError("eps must be finite and >= 0")
         super().__init__(head_dim, rotary_dim, base, layout, scaling, frequencies, magnitude, device)
         self.eps = float(eps)
+        self._workspace = None
+
+    def _dense(self, tokens, heads):
+        """Batch, token and head strides of a contiguous tensor."""
+        return tokens * heads * self.head_dim, heads * self.head_dim, self.head_dim
 
     def _weights(self, weights, dtype, device):
         """The weights' type, and their addresses."""
@@ -469,18 +475,19 @@ class RotaryNorm(Rotary):
         if k is None and k_weight is not None:
             raise ValueError("k_weight needs k")
         pt, weights = self._weights((q_weight, k_weight), dtype, device)
-        if out is None:
-            dense = torch.contiguous_format
-            out = (torch.empty_like(q, memory_format=dense),
-                   None if k is None else torch.empty_like(k, memory_format=dense))
-        lists = []
+        lists, fresh = [], out is None
+        if fresh:
+            out = (torch.empty_like(q, memory_format=_DENSE), None if k is None else torch.empty_like(k, memory_format=_DENSE))
         for name, src, dst, weight in (("q", q, out[0], weights[0]), ("k", k, out[1], weights[1])):
             if src is None:
                 continue
             px, heads, *from_ = self._heads(name, src, lead, dtype, device)
-            po, to_heads, *to = self._heads(name, dst, lead, dtype, device)
-            if to_heads != heads:
-                raise ValueError("the output of %s must have its shape" % name)
+            if fresh:
+                po, to = dst.data_ptr(), self._dense(tokens, heads)
+            else:
+                po, to_heads, *to = self._heads(name, dst, lead, dtype, device)
+                if to_heads != heads:
+                    raise ValueError("the output of %s must have its shape" % name)
             lists += (px, 0, weight, po, 0, heads, *from_, *to, 0, 0, 0)
         rikfad._call_on(device, rikfad.lib().rikfad_rotary_norm_forward, self._block(first, positions, start, pt, lists),
                         rikfad._raw_stream(device))
@@ -499,7 +506,6 @@ class RotaryNorm(Rotary):
         if k is None and (dk is not None or k_weight is not None):
             raise ValueError("dk and k_weight need k")
         pt, weights = self._weights((q_weight, k_weight), dtype, device)
-        dense = torch.contiguous_format
         lists, grads = [], []
         for name, x, d, weight, pw in (("q", q, dq, q_weight, weights[0]), ("k", k, dk, k_weight, weights[1])):
             if d is None:
@@ -509,16 +515,18 @@ class RotaryNorm(Rotary):
             pd, d_heads, *d_from = self._heads("d" + name, d, lead, dtype, device)
             if d_heads != heads:
                 raise ValueError("d%s must have the shape of %s" % (name, name))
-            dx, dw = torch.empty_like(x, memory_format=dense), None if weight is None else torch.empty_like(weight)
+            dx, dw = torch.empty_like(x, memory_format=_DENSE), None if weight is None else torch.empty_like(weight)
             grads += (dx, dw)
-            st = dx.stride()
-            to = (0, st[0], st[1]) if len(st) == 3 else st[:3]
-            lists += (px, pd, pw, dx.data_ptr(), 0 if dw is None else dw.data_ptr(), heads, *from_, *to, *d_from)
+            lists += (px, pd, pw, dx.data_ptr(), 0 if dw is None else dw.data_ptr(), heads, *from_,
+                      *self._dense(tokens, heads), *d_from)
         if lists:
             lib = rikfad.lib()
             work = (0, 0)
-            if grads[1] is not None or grads[3] is not None:
-                nbytes = lib.rikfad_rotary_norm_workspace(self._block(first, positions, start, pt, lists))
+            if grads[1] is not None or grads[-1] is not None:
+                nbytes = self._workspace
+                if nbytes is None:          # it goes by head_dim alone
+                    nbytes = self._workspace = lib.rikfad_rotary_norm_workspace(
+                        self._block(first, positions, start, pt, lists))
                 buffer = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
                 work = (buffer.data_ptr(), nbytes)
             rikfad._call_on(device, lib.rikfad_rotary_norm_backward, self._block(first, positions, start, pt, lists, work),
