@@ -373,10 +373,11 @@ __global__ void __launch_bounds__(kMaxThreads) rikfad_distill_kernel(const __gri
             sums.one = even + odd;
             if (!(sums.top > p.lowest && sums.t < kLargestSum && sums.one < kLargestSum)) {
                 sums = Sums<BOTH>();
-                for (int v = threadIdx.x; v < mine; v += threads)
+                for (int v = threadIdx.x; v < mine; v += threads) {
 #pragma unroll 1
                     for (int e = 0; e < V; ++e)
                         sums.add_one(element<T>(row, slice.lead + (slice.begin + v) * V + e, p.lowest), p.c_t, p.c_1);
+                }
             }
         }
         if (threadIdx.x < slice.edges)
@@ -488,10 +489,11 @@ __global__ void __launch_bounds__(kMaxThreads) rikfad_distill_kernel(const __gri
                     T *to = to0 + (int64_t)(v + j * threads) * V;
                     if (p.wide)
                         __stcs(reinterpret_cast<uint4 *>(to), in[j].word);
-                    else
+                    else {
 #pragma unroll
                         for (int e = 0; e < V; ++e)
                             to[e] = in[j].v[e];
+                    }
                 }
         }
     };

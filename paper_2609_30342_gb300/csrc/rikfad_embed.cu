@@ -52,6 +52,7 @@ struct EmbedParams {
     int64_t zero_from;                  // rows from here on are zero already
     int32_t chunk, slabs;               // tokens of a chunk; warps side by side over a row
     int64_t sum_blocks;
+    int32_t zero_rows;                  // of a warp that writes zeros
 };
 
 // An id outside the table as vocab.
@@ -110,13 +111,14 @@ __global__ void __launch_bounds__(kForwardThreads) rikfad_embed_forward_kernel(c
     for (int u0 = blockIdx.y * blockDim.x + threadIdx.x; u0 < p.units; u0 += step * kUnits) {
         Vec<W, V> in[kUnits][kForwardRows];
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k)
+        for (int k = 0; k < kUnits; ++k) {
 #pragma unroll
             for (int r = 0; r < kForwardRows; ++r)
                 if (inside[r] && u0 + k * step < p.units)
                     load(in[k][r], from[r] + (int64_t)(u0 + k * step) * V);
+        }
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k)
+        for (int k = 0; k < kUnits; ++k) {
 #pragma unroll
             for (int r = 0; r < kForwardRows; ++r) {
                 float f[V];
@@ -129,6 +131,7 @@ __global__ void __launch_bounds__(kForwardThreads) rikfad_embed_forward_kernel(c
                 if (to[r] && u0 + k * step < p.units)
                     store(out, to[r] + (int64_t)(u0 + k * step) * V);
             }
+        }
     }
 }
 
@@ -139,6 +142,7 @@ struct SortParams {
     uint2 *from, *to;               // of the passes in turn; the last one writes to `to`
     int64_t vocab;
     int32_t tokens, id_bytes, passes, bits;
+    int32_t count_blocks;
     int32_t *counts;                // zeroed for the sums
     // rows of the table from zero_from on get zeros from the blocks that do not sort
     void *table;
@@ -238,13 +242,14 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
         auto first_places = [&] {
             cluster_barrier();
             uint32_t before = 0, all = 0;
-            if (threadIdx.x < bins)
+            if (threadIdx.x < bins) {
 #pragma unroll
                 for (int r = 0; r < kSortCtas; ++r) {
                     const uint32_t n = cluster_read(total + threadIdx.x, r);
                     before += r < rank ? n : 0;
                     all += n;
                 }
+            }
             const uint32_t first = block_exclusive(all, sums);
             if (threadIdx.x < bins)
                 base[threadIdx.x] = first + before;
@@ -254,8 +259,12 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
             for (int b = threadIdx.x; b < bins; b += kSortThreads)
                 total[b] = 0;
             __syncthreads();
-            for (int i = begin + threadIdx.x; i < end; i += kSortThreads)
-                atomicAdd(total + (entry(i).x >> shift & (bins - 1)), 1u);      // integers: any order
+            for (int i = begin + warp * 32; i < end; i += kSortThreads) {
+                const uint32_t digit = i + lane < end ? entry(i + lane).x >> shift & (bins - 1) : ~0u;
+                const uint32_t same = __match_any_sync(~0u, digit);
+                if (lane == __ffs(same) - 1 && digit != ~0u)
+                    atomicAdd(total + digit, __popc(same));     // integers: any order
+            }
             first_places();
         }
         for (int tile = begin; tile < end || (one_tile && tile == begin); tile += kSortTile) {
@@ -323,7 +332,7 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
 }
 
 // Few tokens: each one's place is the number of ids below its own and of equal ids before
-// it, counted by a warp.  Every other block writes zeros.
+// it, counted by a warp.  The blocks from count_blocks on write zeros.
 __global__ void __launch_bounds__(kCountThreads) rikfad_embed_count_kernel(const __grid_constant__ SortParams p)
 {
     __shared__ uint4 all[kMostCounted / 4];
@@ -331,8 +340,8 @@ __global__ void __launch_bounds__(kCountThreads) rikfad_embed_count_kernel(const
     const int lane = threadIdx.x & 31, warps = kCountThreads / 32, n4 = (p.tokens + 3) / 4;
     wait_for_predecessor();
     allow_successor_launch();
-    if (blockIdx.x % 2) {
-        zero_rows(p, blockIdx.x / 2, gridDim.x / 2);
+    if (blockIdx.x >= p.count_blocks) {
+        zero_rows(p, blockIdx.x - p.count_blocks, gridDim.x - p.count_blocks);
         return;
     }
     if (blockIdx.x == 0 && threadIdx.x < 2)
@@ -350,7 +359,7 @@ __global__ void __launch_bounds__(kCountThreads) rikfad_embed_count_kernel(const
                 ids[i0 + j * kCountThreads] = id[j];
     }
     __syncthreads();
-    for (int t = blockIdx.x / 2 * warps + (threadIdx.x >> 5); t < p.tokens; t += gridDim.x / 2 * warps) {
+    for (int t = blockIdx.x * warps + (threadIdx.x >> 5); t < p.tokens; t += p.count_blocks * warps) {
         const uint32_t id = ids[t];
         int before = 0;
         // ids up to its own before the four where it is, ids below its own from there on
@@ -411,7 +420,7 @@ template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, con
         asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
 }
 
-// The first blocks write zeros to the rows without a token, 32 rows a warp; the last
+// The first blocks write zeros to the rows without a token, zero_rows of them a warp; the last
 // sum_blocks sum chunks of sorted tokens, a warp 32 vectors of the row.
 template <typename W, typename O, int V, int M>
 __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __grid_constant__ EmbedParams p)
@@ -422,9 +431,9 @@ __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __g
     // zeros first: their blocks begin with a search, during which the others' loads are under way
     const int64_t zero_blocks = gridDim.x - p.sum_blocks;
     if (blockIdx.x < zero_blocks) {
-        const int64_t row0 = ((int64_t)blockIdx.x * kSumWarps + warp) * 32, row = row0 + lane;
+        const int64_t row0 = ((int64_t)blockIdx.x * kSumWarps + warp) * p.zero_rows, row = row0 + lane;
         bool absent = false;
-        if (row < p.zero_from) {
+        if (lane < p.zero_rows && row < p.zero_from) {
             const int64_t at = lower_bound(p.order, p.tokens, (uint32_t)row);
             absent = at == p.tokens || p.order[at].x != row;
         }
@@ -447,10 +456,11 @@ __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __g
     float sum[M][V];
     auto clear = [&] {
 #pragma unroll
-        for (int m = 0; m < M; ++m)
+        for (int m = 0; m < M; ++m) {
 #pragma unroll
             for (int e = 0; e < V; ++e)
                 sum[m][e] = 0.f;
+        }
     };
     clear();
     auto finish = [&](bool goes_on) {
@@ -778,7 +788,10 @@ template <typename W, typename O, int V> cudaError_t launch_backward(EmbedParams
     constexpr int M = V > 1 ? 1 : 16 / (int)sizeof(O);      // vectors of a lane
     p.slabs = (p.units + 32 * M - 1) / (32 * M);
     p.sum_blocks = (p.chunks * p.slabs + kSumWarps - 1) / kSumWarps;
-    const int64_t zeros = (p.zero_from + 32 * kSumWarps - 1) / (32 * kSumWarps);
+    p.zero_rows = 32;                   // some 32 KB
+    while (p.zero_rows > 1 && p.zero_rows * (int64_t)p.width * (int64_t)sizeof(W) > 32 << 10)
+        p.zero_rows /= 2;
+    const int64_t zeros = (p.zero_from + p.zero_rows * kSumWarps - 1) / (p.zero_rows * kSumWarps);
     if (p.sum_blocks + zeros == 0)
         return cudaSuccess;
     if (p.sum_blocks + zeros > INT32_MAX)
@@ -891,7 +904,10 @@ RIKFAD_API int rikfad_embedding_backward(const rikfad_embedding *p, void *stream
         SortParams r{};
         // While a few multiprocessors sort, the others write zeros to the last rows of the
         // table, about as many as that time allows; those with tokens are written again.
-        if (!p->accumulate) {
+        // To all rows where tokens are few to them: what is written twice is an eighth at most.
+        if (!p->accumulate && p->tokens <= p->vocab / 8)
+            q.zero_from = 0;
+        else if (!p->accumulate) {
             const double us = p->tokens <= kMostCounted ? 3 : 6 + (double)p->tokens / 2000;
             const double rows = us * kZeroBytesPerUs / ((double)p->width * dtype_bytes(p->table_dtype));
             q.zero_from = p->vocab - (int64_t)std::min((double)p->vocab, rows);
@@ -913,8 +929,11 @@ RIKFAD_API int rikfad_embedding_backward(const rikfad_embedding *p, void *stream
             ++bits;
         r.passes = (bits + kSortBits - 1) / kSortBits;
         r.bits = (bits + r.passes - 1) / r.passes;
-        e = p->tokens <= kMostCounted ? launch_chained(rikfad_embed_count_kernel, dim3(4 * kSms), kCountThreads, 0, s, r)
-                                      : launch_sort(r, s);
+        r.count_blocks = (int32_t)std::min<int64_t>(2 * kSms, (p->tokens + 7) / 8);
+        const int zero_blocks = r.zero_from < p->vocab ? 6 * kSms : 0;
+        e = p->tokens <= kMostCounted
+                ? launch_chained(rikfad_embed_count_kernel, dim3((unsigned)(r.count_blocks + zero_blocks)), kCountThreads, 0, s, r)
+                : launch_sort(r, s);
         if (e != cudaSuccess)
             return report_cuda(e, "launch of the embedding's sort");
     }

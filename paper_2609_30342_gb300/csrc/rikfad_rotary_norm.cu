@@ -99,17 +99,6 @@ template <int BYTES> __device__ __forceinline__ void copy_async(void *to, const 
 template <typename T, int V, int U> struct Raw {
     Vec<T, V> a[U], b[U];
 
-    __device__ __forceinline__ void load(const T *head, const Place (&at)[U], bool active)
-    {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            a[u].word = b[u].word = decltype(a[u].word){};
-            if (active && at[u].first >= 0)
-                a[u].word = __ldcs(reinterpret_cast<const decltype(a[u].word) *>(head + at[u].first));
-            if (active && at[u].second >= 0)
-                b[u].word = __ldcs(reinterpret_cast<const decltype(b[u].word) *>(head + at[u].second));
-        }
-    }
     __device__ __forceinline__ void store(T *head, const Place (&at)[U]) const
     {
 #pragma unroll
@@ -145,23 +134,25 @@ template <int V> struct Values {
     {
         if constexpr (V == 1)
             p[0] = pair(x[0], y[0]);
-        else
+        else {
 #pragma unroll
             for (int e = 0; e < V; e += 2) {
                 p[e / 2] = pair(x[e], x[e + 1]);
                 p[V / 2 + e / 2] = pair(y[e], y[e + 1]);
             }
+        }
     }
     __device__ __forceinline__ void get(float (&x)[V], float (&y)[V]) const
     {
         if constexpr (V == 1)
             apart(p[0], x[0], y[0]);
-        else
+        else {
 #pragma unroll
             for (int e = 0; e < V; e += 2) {
                 apart(p[e / 2], x[e], x[e + 1]);
                 apart(p[V / 2 + e / 2], y[e], y[e + 1]);
             }
+        }
     }
 };
 
@@ -239,25 +230,30 @@ struct Steps {
     }
 };
 
-// Bytes that a lane loads of a head, and how many of its heads are on their way.
+// Heads on their way.  Vectors of 4 bytes or more: each lane's at a place of shared memory
+// of its own.  Single elements of 2 bytes: all of the 16 bytes that a head begins and ends in,
+// wherever that is, copied by the group's lanes, each of which reads its elements there.
 template <typename T, int V, int U, bool BACKWARD> struct Ring {
     static constexpr int kWord = V * (int)sizeof(T), kWords = (BACKWARD ? 4 : 2) * U;
-    static constexpr int kDepth = kWord < 4 ? 1 : kWord * kWords > 64 ? 2 : 4;
-    static constexpr int kBytes = kWord < 4 ? 0 : kDepth * kWords * kWord * kThreads;
+    static constexpr bool kWhole = kWord < 4;
+    static constexpr int kDepth = !kWhole && kWord * kWords > 64 ? 2 : 4;
+    __host__ __device__ static constexpr int whole_bytes(int head_dim) { return (head_dim * 2 + 14 + 15) / 16 * 16; }
+    __host__ __device__ static constexpr int bytes(int head_dim, int groups)
+    {
+        return kWhole ? kDepth * groups * (BACKWARD ? 2 : 1) * whole_bytes(head_dim) : kDepth * kWords * kWord * kThreads;
+    }
 };
 
 // A block has tile after tile of tokens: their cosines and sines, formed once a tile, and
 // all heads, shared by its groups of lanes.  A group has heads of one list, and their
-// weights' gradients in registers.  Its next kDepth heads are on their way meanwhile, each
-// lane's vectors to a place of shared memory of its own (types of 2 bytes in single
-// elements: the next head, to registers).
+// weights' gradients in registers.  Its next kDepth heads are on their way meanwhile.
 template <typename T, int V, int U, bool BACKWARD>
 __global__ void __launch_bounds__(kThreads, BACKWARD ? kBackwardBlocksPerSm : kForwardBlocksPerSm)
 rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
 {
     using R = Ring<T, V, U, BACKWARD>;
     extern __shared__ float4 shared[];
-    float *const cosines = reinterpret_cast<float *>(reinterpret_cast<char *>(shared) + R::kBytes), *const sines = cosines + p.tile * p.pitch;
+    float *const cosines = reinterpret_cast<float *>(reinterpret_cast<char *>(shared) + R::bytes(p.head_dim, kThreads / p.lanes)), *const sines = cosines + p.tile * p.pitch;
     const int group = threadIdx.x / p.lanes, lane = threadIdx.x % p.lanes;
     Place at[U];
 #pragma unroll
@@ -281,12 +277,12 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
         return max(q, (here * h1.heads + others - 1) / max(others, 1));
     };
     Values<V> sums[U];
-    if constexpr (BACKWARD)
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                sums[u].p[e] = pair(0.f, 0.f);
+        for (int e = 0; e < V; ++e)
+            sums[u].p[e] = pair(0.f, 0.f);
+    }
     wait_for_predecessor();
     allow_successor_launch();
     // the head to load next
@@ -320,9 +316,26 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
     auto place = [&](int j, int i) {
         return reinterpret_cast<char *>(shared) + ((j * R::kWords + i) * kThreads + threadIdx.x) * R::kWord;
     };
+    // Whole heads: at which element of each place x and dout begin, 4 bits for each.
+    const int whole = R::whole_bytes(p.head_dim);
+    uint32_t skips = 0;
+    auto whole_place = [&](int j, int tensor) {
+        return reinterpret_cast<char *>(shared) + ((j * (kThreads / p.lanes) + group) * (BACKWARD ? 2 : 1) + tensor) * whole;
+    };
+    auto request_whole = [&](int j, int tensor, const T *head) {
+        const int skip = (int)((uintptr_t)head % 16), words = (skip + 2 * p.head_dim + 15) / 16;
+        for (int i = lane; i < words; i += p.lanes)
+            copy_async<16>(whole_place(j, tensor) + 16 * i, reinterpret_cast<const char *>(head) - skip + 16 * i);
+        const int bits = 8 * j + 4 * tensor;
+        skips = (skips & ~(15u << bits)) | (uint32_t)(skip / 2) << bits;
+    };
     auto request = [&](int j) {
-        if constexpr (R::kBytes > 0) {
-            if (ask_item < ask_items) {
+        if (ask_item < ask_items) {
+            if constexpr (R::kWhole) {
+                request_whole(j, 0, from);
+                if (BACKWARD)
+                    request_whole(j, 1, dfrom);
+            } else {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (at[u].first >= 0) {
@@ -337,28 +350,23 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
                     }
                 }
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            ask_next();
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        ask_next();
     };
     Raw<T, V, U> in, din;
     ask_enter();
-    if constexpr (R::kBytes > 0) {
-        // vectors that a lane has not stay zeros
+    if constexpr (!R::kWhole) {     // vectors that a lane has not stay zeros
 #pragma unroll
         for (int i = 0; i < R::kDepth * R::kWords; ++i) {
             Vec<T, V> none;
             none.word = decltype(none.word){};
             *reinterpret_cast<decltype(none.word) *>(place(0, i)) = none.word;
         }
-#pragma unroll
-        for (int j = 0; j < R::kDepth; ++j)
-            request(j);
-    } else {
-        in.load(from, at, ask_item < ask_items);
-        if constexpr (BACKWARD)
-            din.load(dfrom, at, ask_item < ask_items);
     }
+#pragma unroll
+    for (int j = 0; j < R::kDepth; ++j)
+        request(j);
     Values<V> w[U];
     const void *const weights = list ? h1.weight : h0.weight;
 #pragma unroll
@@ -393,12 +401,29 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
         int head = g % heads, table = g / heads * p.pitch, item = g;
         for (int round = 0; round < rounds; ++round) {
             const bool active = item < items;
-            Raw<T, V, U> next, dnext;
-            if constexpr (R::kBytes > 0) {
-                asm volatile("cp.async.wait_group %0;" ::"n"(R::kDepth - 1) : "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(R::kDepth - 1) : "memory");
+            if constexpr (R::kWhole) {
+                __syncwarp();           // the other lanes' copies
+                auto take = [&](Vec<T, V> &v, int tensor, int element) {
+                    const uint32_t skip = skips >> (8 * turn_of_ring + 4 * tensor) & 15;
+                    v.word = decltype(v.word){};
+                    if (element >= 0)
+                        v.v[0] = reinterpret_cast<const T *>(whole_place(turn_of_ring, tensor))[skip + element];
+                };
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    auto take = [&](Vec<T, V> &v, int i) { v.word = *reinterpret_cast<const decltype(v.word) *>(place(turn_of_ring, i)); };
+                    take(in.a[u], 0, at[u].first);
+                    take(in.b[u], 0, at[u].second);
+                    if constexpr (BACKWARD) {
+                        take(din.a[u], 1, at[u].first);
+                        take(din.b[u], 1, at[u].second);
+                    }
+                }
+                __syncwarp();           // before the place is filled again
+            } else {
+                auto take = [&](Vec<T, V> &v, int i) { v.word = *reinterpret_cast<const decltype(v.word) *>(place(turn_of_ring, i)); };
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
                     take(in.a[u], 2 * u);
                     take(in.b[u], 2 * u + 1);
                     if constexpr (BACKWARD) {
@@ -406,11 +431,6 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
                         take(din.b[u], 2 * U + 2 * u + 1);
                     }
                 }
-            } else {
-                ask_next();
-                next.load(from, at, ask_item < ask_items);
-                if constexpr (BACKWARD)
-                    dnext.load(dfrom, at, ask_item < ask_items);
             }
             const float *const c = cosines + (active ? table : 0), *const s = sines + (active ? table : 0);
             Values<V> v[U];
@@ -443,17 +463,20 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
                 }
                 const float r = rsqrtf(fmaf(squares, p.inv_dim, p.eps));
                 const f2 rr = both(r), minus = both(-product * p.inv_dim * r * r);
-                if (active)                     // else what was there before
+                if (active) {                   // else what was there before
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
+                    for (int u = 0; u < U; ++u) {
 #pragma unroll
                         for (int e = 0; e < V; ++e)
                             sums[u].p[e] = fma(d[u].p[e], mul(v[u].p[e], rr), sums[u].p[e]);
+                    }
+                }
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+                for (int u = 0; u < U; ++u) {
 #pragma unroll
                     for (int e = 0; e < V; ++e)
                         v[u].p[e] = mul(rr, fma(minus, v[u].p[e], mul(d[u].p[e], w[u].p[e])));
+                }
             } else {
                 request(turn_of_ring);
                 for (int d = p.lanes / 2; d > 0; d /= 2)
@@ -473,12 +496,7 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
                     v[u].to(in.a[u], in.b[u]);
                 in.store(to, at);
             }
-            if constexpr (R::kBytes > 0)
-                turn_of_ring = turn_of_ring + 1 == R::kDepth ? 0 : turn_of_ring + 1;
-            else {
-                in = next;
-                din = dnext;
-            }
+            turn_of_ring = turn_of_ring + 1 == R::kDepth ? 0 : turn_of_ring + 1;
             item += n;
             head += more_heads;
             const bool over = head >= heads;
@@ -527,10 +545,11 @@ rikfad_rotary_norm_join_kernel(const float *part, int blocks, int head_dim, T *d
     wait_for_predecessor();
     allow_successor_launch();
     float s = 0.f;
-    if (e < head_dim)
+    if (e < head_dim) {
 #pragma unroll 4
         for (int b = warp; b < blocks; b += kJoinThreads / 32)
             s += part[((int64_t)b * 2 + blockIdx.y) * head_dim + e];
+    }
     sum[warp][lane] = s;
     __syncthreads();
     if (warp == 0 && e < head_dim) {
@@ -659,7 +678,7 @@ template <typename T, int V, int U, bool BACKWARD> cudaError_t launch(Params p, 
     p.tiles_per_sequence = (p.tokens + p.tile - 1) / p.tile;
     p.tiles *= p.tiles_per_sequence;
     const int64_t blocks = std::min(p.tiles, all);
-    size_t smem = Ring<T, V, U, BACKWARD>::kBytes + 2 * sizeof(float) * (size_t)p.tile * p.pitch;
+    size_t smem = Ring<T, V, U, BACKWARD>::bytes(p.head_dim, groups) + 2 * sizeof(float) * (size_t)p.tile * p.pitch;
     if (BACKWARD && p.part)
         smem = std::max(smem, sizeof(float) * groups * (size_t)p.head_dim);
     const cudaError_t e =
