@@ -51,7 +51,8 @@ struct Params {
     int32_t position_bytes, nlists, head_dim, rotary_dim, pairs;
     int32_t interleaved, param_f32;
     int32_t tile;                       // tokens of a tile
-    int32_t lanes, turn_units, units;   // of a head: lanes, units that turn (half layout), all units
+    int32_t lanes, turn_units, units;   // of a head: lanes, units that turn (half layout), all units (whole heads: pairs)
+    int32_t rest_half;                  // how far the elements of a pair beyond rotary_dim are apart
     float magnitude, inv_dim, eps;
     int32_t pitch;                      // of a token's cosines and sines
     int32_t split;                      // groups of lanes that have heads of the first list; the others have the second's
@@ -112,7 +113,7 @@ template <typename T, int V, int U> struct Raw {
 };
 
 // A unit's 2 V elements in float32, two to a register pair: the first vector's, then the
-// second's (with V = 1, both vectors' elements are one pair).
+// second's.
 template <int V> struct Values {
     f2 p[V];
 
@@ -132,26 +133,18 @@ template <int V> struct Values {
     }
     __device__ __forceinline__ void put(const float (&x)[V], const float (&y)[V])
     {
-        if constexpr (V == 1)
-            p[0] = pair(x[0], y[0]);
-        else {
 #pragma unroll
-            for (int e = 0; e < V; e += 2) {
-                p[e / 2] = pair(x[e], x[e + 1]);
-                p[V / 2 + e / 2] = pair(y[e], y[e + 1]);
-            }
+        for (int e = 0; e < V; e += 2) {
+            p[e / 2] = pair(x[e], x[e + 1]);
+            p[V / 2 + e / 2] = pair(y[e], y[e + 1]);
         }
     }
     __device__ __forceinline__ void get(float (&x)[V], float (&y)[V]) const
     {
-        if constexpr (V == 1)
-            apart(p[0], x[0], y[0]);
-        else {
 #pragma unroll
-            for (int e = 0; e < V; e += 2) {
-                apart(p[e / 2], x[e], x[e + 1]);
-                apart(p[V / 2 + e / 2], y[e], y[e + 1]);
-            }
+        for (int e = 0; e < V; e += 2) {
+            apart(p[e / 2], x[e], x[e + 1]);
+            apart(p[V / 2 + e / 2], y[e], y[e + 1]);
         }
     }
 };
@@ -168,15 +161,14 @@ template <int V> __device__ __forceinline__ void turn(const Params &p, Values<V>
 {
     if (at.pair < 0)
         return;
-    constexpr int L = V < 4 ? V : 4;            // elements of one load
+    constexpr int L = 4;                        // elements of one load
     Vec<float, L> c[V / L], s[V / L];
 #pragma unroll
     for (int i = 0; i < V / L; ++i) {
         c[i].word = reinterpret_cast<const decltype(c[i].word) *>(cosines + at.pair)[i];
         s[i].word = reinterpret_cast<const decltype(s[i].word) *>(sines + at.pair)[i];
     }
-    if constexpr (V > 1)
-        if (!p.interleaved) {
+    if (!p.interleaved) {
 #pragma unroll
             for (int e = 0; e < V; e += 2) {
                 const f2 ce = pair(c[e / L].v[e % L], c[e / L].v[e % L + 1]), se = pair(s[e / L].v[e % L], s[e / L].v[e % L + 1]);
@@ -185,8 +177,8 @@ template <int V> __device__ __forceinline__ void turn(const Params &p, Values<V>
                 a = sub(mul(a, ce), mul(b, se));
                 b = fma(x, se, mul(b, ce));
             }
-            return;
-        }
+        return;
+    }
     // pair e is elements 2 e and 2 e + 1; the last unit may reach beyond rotary_dim
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -230,28 +222,85 @@ struct Steps {
     }
 };
 
-// Heads on their way.  Vectors of 4 bytes or more: each lane's at a place of shared memory
-// of its own.  Single elements of 2 bytes: all of the 16 bytes that a head begins and ends in,
-// wherever that is, copied by the group's lanes, each of which reads its elements there.
-template <typename T, int V, int U, bool BACKWARD> struct Ring {
+// The V pairs of a lane where heads are copied whole: pairs lane, lane + lanes, ..., so that
+// neighbours read neighbouring elements.  Beyond rotary_dim any two elements are a pair.
+template <int V> struct Spread {
+    uint32_t at[V];             // first and second element, 0xffff where there is none
+    int turning;                // pairs that turn: the first so many
+
+    __device__ __forceinline__ Spread(const Params &p, int lane)
+    {
+        turning = 0;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int k = lane + e * p.lanes;
+            int first, second;
+            if (p.interleaved) {
+                first = 2 * k;
+                second = first + 1;
+            } else {
+                first = k < p.pairs ? k : k + p.pairs;
+                second = first + (k < p.pairs ? p.pairs : p.rest_half);
+            }
+            first = k < p.units ? first : 0xffff;
+            second = k < p.units && second < p.head_dim ? second : 0xffff;
+            at[e] = (uint32_t)first | (uint32_t)second << 16;
+            turning += k < p.pairs;
+        }
+    }
+    __device__ __forceinline__ int first(int e) const { return at[e] & 0xffff; }
+    __device__ __forceinline__ int second(int e) const { return at[e] >> 16; }
+    template <typename F> __device__ __forceinline__ void each(float (&x)[V], float (&y)[V], F element) const
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            x[e] = first(e) != 0xffff ? element(first(e)) : 0.f;
+            y[e] = second(e) != 0xffff ? element(second(e)) : 0.f;
+        }
+    }
+    __device__ __forceinline__ void turn(const Params &p, Values<V> &v, int lane, const float *cosines, const float *sines) const
+    {
+        float c[V], s[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            c[e] = e < turning ? cosines[lane + e * p.lanes] : 1.f;
+            s[e] = e < turning ? sines[lane + e * p.lanes] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+            const f2 ce = pair(c[e], c[e + 1]), se = pair(s[e], s[e + 1]);
+            f2 &a = v.p[e / 2], &b = v.p[V / 2 + e / 2];
+            const f2 x = a;
+            a = sub(mul(a, ce), mul(b, se));
+            b = fma(x, se, mul(b, ce));
+        }
+    }
+};
+
+// Heads on their way.  Vectors of 8 or 16 bytes: each lane's at a place of shared memory of its
+// own.  Other heads whole: all of the 16 bytes that one begins and ends in, wherever that is,
+// copied by the group's lanes, each of which reads its elements there.
+template <typename T, int V, int U, bool WHOLE, bool BACKWARD> struct Ring {
     static constexpr int kWord = V * (int)sizeof(T), kWords = (BACKWARD ? 4 : 2) * U;
-    static constexpr bool kWhole = kWord < 4;
-    static constexpr int kDepth = !kWhole && kWord * kWords > 64 ? 2 : 4;
-    __host__ __device__ static constexpr int whole_bytes(int head_dim) { return (head_dim * 2 + 14 + 15) / 16 * 16; }
+    static constexpr int kDepth = WHOLE ? 8 / (int)sizeof(T) : kWord * kWords > 64 ? 2 : 4;
+    __host__ __device__ static constexpr int whole_bytes(int head_dim)
+    {
+        return (head_dim * (int)sizeof(T) + 31 - (int)sizeof(T)) / 16 * 16;
+    }
     __host__ __device__ static constexpr int bytes(int head_dim, int groups)
     {
-        return kWhole ? kDepth * groups * (BACKWARD ? 2 : 1) * whole_bytes(head_dim) : kDepth * kWords * kWord * kThreads;
+        return WHOLE ? kDepth * groups * (BACKWARD ? 2 : 1) * whole_bytes(head_dim) : kDepth * kWords * kWord * kThreads;
     }
 };
 
 // A block has tile after tile of tokens: their cosines and sines, formed once a tile, and
 // all heads, shared by its groups of lanes.  A group has heads of one list, and their
 // weights' gradients in registers.  Its next kDepth heads are on their way meanwhile.
-template <typename T, int V, int U, bool BACKWARD>
+template <typename T, int V, int U, bool WHOLE, bool BACKWARD>
 __global__ void __launch_bounds__(kThreads, BACKWARD ? kBackwardBlocksPerSm : kForwardBlocksPerSm)
 rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
 {
-    using R = Ring<T, V, U, BACKWARD>;
+    using R = Ring<T, V, U, WHOLE, BACKWARD>;
     extern __shared__ float4 shared[];
     float *const cosines = reinterpret_cast<float *>(reinterpret_cast<char *>(shared) + R::bytes(p.head_dim, kThreads / p.lanes)), *const sines = cosines + p.tile * p.pitch;
     const int group = threadIdx.x / p.lanes, lane = threadIdx.x % p.lanes;
@@ -259,6 +308,7 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
 #pragma unroll
     for (int u = 0; u < U; ++u)
         at[u] = place_of<V>(p, lane + u * p.lanes);
+    const Spread<V> spread(p, lane);
     const bool list = group >= p.split;
     const int g = list ? group - p.split : group, n = list ? kThreads / p.lanes - p.split : p.split;
     const Heads &h0 = p.lists[0], &h1 = p.lists[1];
@@ -316,22 +366,47 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
     auto place = [&](int j, int i) {
         return reinterpret_cast<char *>(shared) + ((j * R::kWords + i) * kThreads + threadIdx.x) * R::kWord;
     };
-    // Whole heads: at which element of each place x and dout begin, 4 bits for each.
-    const int whole = R::whole_bytes(p.head_dim);
+    // Whole heads: at which byte of its place each begins, 4 bits for every place of x and dout.
+    const int whole = R::whole_bytes(p.head_dim), head_bytes = p.head_dim * (int)sizeof(T);
     uint32_t skips = 0;
     auto whole_place = [&](int j, int tensor) {
         return reinterpret_cast<char *>(shared) + ((j * (kThreads / p.lanes) + group) * (BACKWARD ? 2 : 1) + tensor) * whole;
     };
     auto request_whole = [&](int j, int tensor, const T *head) {
-        const int skip = (int)((uintptr_t)head % 16), words = (skip + 2 * p.head_dim + 15) / 16;
+        const int skip = (int)((uintptr_t)head % 16), words = (skip + head_bytes + 15) / 16;
         for (int i = lane; i < words; i += p.lanes)
             copy_async<16>(whole_place(j, tensor) + 16 * i, reinterpret_cast<const char *>(head) - skip + 16 * i);
         const int bits = 8 * j + 4 * tensor;
-        skips = (skips & ~(15u << bits)) | (uint32_t)(skip / 2) << bits;
+        skips = (skips & ~(15u << bits)) | (uint32_t)skip << bits;
+    };
+    // The group's results, by way of x's place: 16 bytes at a time, elements at the ends.
+    auto store_whole = [&](int j, T *head, const float (&a)[V], const float (&b)[V], bool active) {
+        constexpr int E = 16 / sizeof(T);
+        const int skip = (int)((uintptr_t)head % 16);
+        const int lead = min((16 - skip) % 16 / (int)sizeof(T), p.head_dim), words = (p.head_dim - lead) / E, edges = p.head_dim - words * E;
+        T *const place = reinterpret_cast<T *>(whole_place(j, 0) + skip);
+        __syncwarp();                   // all lanes have taken theirs
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            if (spread.first(e) != 0xffff)
+                place[spread.first(e)] = from_f32<T>(a[e]);
+            if (spread.second(e) != 0xffff)
+                place[spread.second(e)] = from_f32<T>(b[e]);
+        }
+        __syncwarp();
+        if (active) {
+            for (int i = lane; i < words; i += p.lanes)
+                reinterpret_cast<uint4 *>(head + lead)[i] = reinterpret_cast<const uint4 *>(place + lead)[i];
+            for (int i = lane; i < edges; i += p.lanes) {
+                const int e = i < lead ? i : i + words * E;
+                head[e] = place[e];
+            }
+        }
+        __syncwarp();                   // before the place is filled again
     };
     auto request = [&](int j) {
         if (ask_item < ask_items) {
-            if constexpr (R::kWhole) {
+            if constexpr (WHOLE) {
                 request_whole(j, 0, from);
                 if (BACKWARD)
                     request_whole(j, 1, dfrom);
@@ -354,9 +429,8 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
         asm volatile("cp.async.commit_group;" ::: "memory");
         ask_next();
     };
-    Raw<T, V, U> in, din;
     ask_enter();
-    if constexpr (!R::kWhole) {     // vectors that a lane has not stay zeros
+    if constexpr (!WHOLE) {     // vectors that a lane has not stay zeros
 #pragma unroll
         for (int i = 0; i < R::kDepth * R::kWords; ++i) {
             Vec<T, V> none;
@@ -369,18 +443,22 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
         request(j);
     Values<V> w[U];
     const void *const weights = list ? h1.weight : h0.weight;
+    auto weight = [&](int e) {
+        return weights == nullptr ? 1.f
+               : p.param_f32      ? static_cast<const float *>(weights)[e]
+                                  : to_f32(static_cast<const T *>(weights)[e]);
+    };
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        auto weight = [&](int e) {
-            return weights == nullptr ? 1.f
-                   : p.param_f32      ? static_cast<const float *>(weights)[e]
-                                      : to_f32(static_cast<const T *>(weights)[e]);
-        };
         float a[V], b[V];
+        if constexpr (WHOLE) {
+            spread.each(a, b, weight);
+        } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            a[e] = at[u].first >= 0 ? weight(at[u].first + e) : 0.f;
-            b[e] = at[u].second >= 0 ? weight(at[u].second + e) : 0.f;
+            for (int e = 0; e < V; ++e) {
+                a[e] = at[u].first >= 0 ? weight(at[u].first + e) : 0.f;
+                b[e] = at[u].second >= 0 ? weight(at[u].second + e) : 0.f;
+            }
         }
         w[u].put(a, b);
     }
@@ -402,64 +480,67 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
         for (int round = 0; round < rounds; ++round) {
             const bool active = item < items;
             asm volatile("cp.async.wait_group %0;" ::"n"(R::kDepth - 1) : "memory");
-            if constexpr (R::kWhole) {
+            Values<V> v[U], d[U];
+            if constexpr (WHOLE) {
                 __syncwarp();           // the other lanes' copies
-                auto take = [&](Vec<T, V> &v, int tensor, int element) {
-                    const uint32_t skip = skips >> (8 * turn_of_ring + 4 * tensor) & 15;
-                    v.word = decltype(v.word){};
-                    if (element >= 0)
-                        v.v[0] = reinterpret_cast<const T *>(whole_place(turn_of_ring, tensor))[skip + element];
+                auto take = [&](Values<V> &v, int tensor) {
+                    const T *head = reinterpret_cast<const T *>(whole_place(turn_of_ring, tensor) + (skips >> (8 * turn_of_ring + 4 * tensor) & 15));
+                    float a[V], b[V];
+                    spread.each(a, b, [&](int e) { return to_f32(head[e]); });
+                    v.put(a, b);
+                };
+                take(v[0], 0);
+                if constexpr (BACKWARD) {
+                    take(d[0], 1);
+                }
+            } else {
+                auto take = [&](Values<V> &v, int i) {
+                    Vec<T, V> a, b;
+                    a.word = *reinterpret_cast<const decltype(a.word) *>(place(turn_of_ring, i));
+                    b.word = *reinterpret_cast<const decltype(b.word) *>(place(turn_of_ring, i + 1));
+                    v.from(a, b);
                 };
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    take(in.a[u], 0, at[u].first);
-                    take(in.b[u], 0, at[u].second);
+                    take(v[u], 2 * u);
                     if constexpr (BACKWARD) {
-                        take(din.a[u], 1, at[u].first);
-                        take(din.b[u], 1, at[u].second);
-                    }
-                }
-                __syncwarp();           // before the place is filled again
-            } else {
-                auto take = [&](Vec<T, V> &v, int i) { v.word = *reinterpret_cast<const decltype(v.word) *>(place(turn_of_ring, i)); };
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    take(in.a[u], 2 * u);
-                    take(in.b[u], 2 * u + 1);
-                    if constexpr (BACKWARD) {
-                        take(din.a[u], 2 * U + 2 * u);
-                        take(din.b[u], 2 * U + 2 * u + 1);
+                        take(d[u], 2 * U + 2 * u);
                     }
                 }
             }
+            auto turn_all = [&](Values<V> (&v)[U], const float *c, const float *s) {
+                if constexpr (WHOLE) {
+                    spread.turn(p, v[0], lane, c, s);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        turn<V>(p, v[u], at[u], c, s);
+                }
+            };
             const float *const c = cosines + (active ? table : 0), *const s = sines + (active ? table : 0);
-            Values<V> v[U];
             f2 squares2 = pair(0.f, 0.f);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                v[u].from(in.a[u], in.b[u]);
 #pragma unroll
                 for (int e = 0; e < V; ++e)
                     squares2 = fma(v[u].p[e], v[u].p[e], squares2);
             }
             float squares = total(squares2);
             if constexpr (BACKWARD) {
-                Values<V> d[U];
+                turn_all(d, c, s);
                 f2 product2 = pair(0.f, 0.f);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    d[u].from(din.a[u], din.b[u]);
-                    turn<V>(p, d[u], at[u], c, s);
 #pragma unroll
                     for (int e = 0; e < V; ++e)
                         product2 = fma(mul(d[u].p[e], w[u].p[e]), v[u].p[e], product2);
                 }
                 float product = total(product2);
-                // the next head on its way, now that this one has been taken
-                request(turn_of_ring);
-                for (int d = p.lanes / 2; d > 0; d /= 2) {
-                    squares += __shfl_xor_sync(~0u, squares, d);
-                    product += __shfl_xor_sync(~0u, product, d);
+                if constexpr (!WHOLE)           // the next head on its way, now that this one has been taken
+                    request(turn_of_ring);
+                for (int far = p.lanes / 2; far > 0; far /= 2) {
+                    squares += __shfl_xor_sync(~0u, squares, far);
+                    product += __shfl_xor_sync(~0u, product, far);
                 }
                 const float r = rsqrtf(fmaf(squares, p.inv_dim, p.eps));
                 const f2 rr = both(r), minus = both(-product * p.inv_dim * r * r);
@@ -478,23 +559,30 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
                         v[u].p[e] = mul(rr, fma(minus, v[u].p[e], mul(d[u].p[e], w[u].p[e])));
                 }
             } else {
-                request(turn_of_ring);
-                for (int d = p.lanes / 2; d > 0; d /= 2)
-                    squares += __shfl_xor_sync(~0u, squares, d);
+                if constexpr (!WHOLE)
+                    request(turn_of_ring);
+                for (int far = p.lanes / 2; far > 0; far /= 2)
+                    squares += __shfl_xor_sync(~0u, squares, far);
                 const f2 rr = both(rsqrtf(fmaf(squares, p.inv_dim, p.eps)));
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
 #pragma unroll
                     for (int e = 0; e < V; ++e)
                         v[u].p[e] = mul(v[u].p[e], mul(rr, w[u].p[e]));
-                    turn<V>(p, v[u], at[u], c, s);
                 }
+                turn_all(v, c, s);
             }
-            if (active) {
+            if constexpr (WHOLE) {
+                float a[V], b[V];
+                v[0].get(a, b);
+                store_whole(turn_of_ring, to, a, b, active);
+                request(turn_of_ring);
+            } else if (active) {
+                Raw<T, V, U> result;
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-                    v[u].to(in.a[u], in.b[u]);
-                in.store(to, at);
+                    v[u].to(result.a[u], result.b[u]);
+                result.store(to, at);
             }
             turn_of_ring = turn_of_ring + 1 == R::kDepth ? 0 : turn_of_ring + 1;
             item += n;
@@ -517,10 +605,11 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
             sums[u].get(a, b);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                if (at[u].first >= 0)
-                    sum[group * p.head_dim + at[u].first + e] = a[e];
-                if (at[u].second >= 0)
-                    sum[group * p.head_dim + at[u].second + e] = b[e];
+                const int first = WHOLE ? spread.first(e) : at[u].first + e, second = WHOLE ? spread.second(e) : at[u].second + e;
+                if (WHOLE ? first != 0xffff : at[u].first >= 0)
+                    sum[group * p.head_dim + first] = a[e];
+                if (WHOLE ? second != 0xffff : at[u].second >= 0)
+                    sum[group * p.head_dim + second] = b[e];
             }
         }
         __syncthreads();
@@ -657,7 +746,7 @@ size_t workspace_of(const rikfad_rotary_norm *p)
     return (size_t)kSms * kBackwardBlocksPerSm * 2 * (size_t)p->head_dim * sizeof(float);
 }
 
-template <typename T, int V, int U, bool BACKWARD> cudaError_t launch(Params p, const rikfad_rotary_norm *d, cudaStream_t s)
+template <typename T, int V, int U, bool WHOLE, bool BACKWARD> cudaError_t launch(Params p, const rikfad_rotary_norm *d, cudaStream_t s)
 {
     const int groups = kThreads / p.lanes;
     const int64_t heads = p.lists[0].heads + p.lists[1].heads, tokens = p.tiles * p.tokens;   // p.tiles: sequences, here
@@ -678,11 +767,11 @@ template <typename T, int V, int U, bool BACKWARD> cudaError_t launch(Params p, 
     p.tiles_per_sequence = (p.tokens + p.tile - 1) / p.tile;
     p.tiles *= p.tiles_per_sequence;
     const int64_t blocks = std::min(p.tiles, all);
-    size_t smem = Ring<T, V, U, BACKWARD>::bytes(p.head_dim, groups) + 2 * sizeof(float) * (size_t)p.tile * p.pitch;
+    size_t smem = Ring<T, V, U, WHOLE, BACKWARD>::bytes(p.head_dim, groups) + 2 * sizeof(float) * (size_t)p.tile * p.pitch;
     if (BACKWARD && p.part)
         smem = std::max(smem, sizeof(float) * groups * (size_t)p.head_dim);
     const cudaError_t e =
-        launch_chained(rikfad_rotary_norm_kernel<T, V, U, BACKWARD>, dim3((unsigned)blocks), kThreads, smem, s, p);
+        launch_chained(rikfad_rotary_norm_kernel<T, V, U, WHOLE, BACKWARD>, dim3((unsigned)blocks), kThreads, smem, s, p);
     if (e != cudaSuccess || !BACKWARD || p.part == nullptr)
         return e;
     void *const dq = d->lists[0].dweight, *const dk = d->nlists > 1 ? d->lists[1].dweight : nullptr;
@@ -693,7 +782,7 @@ template <typename T, int V, int U, bool BACKWARD> cudaError_t launch(Params p, 
 }
 
 // Lanes of a head: enough for one unit each, up to a warp.
-template <typename T, int V, bool BACKWARD> cudaError_t launch(Params p, const rikfad_rotary_norm *d, cudaStream_t s)
+template <typename T, int V, bool BACKWARD> cudaError_t launch_vectors(Params p, const rikfad_rotary_norm *d, cudaStream_t s)
 {
     if (p.interleaved) {
         p.units = (p.head_dim + 2 * V - 1) / (2 * V);
@@ -704,16 +793,22 @@ template <typename T, int V, bool BACKWARD> cudaError_t launch(Params p, const r
     p.lanes = 1;
     while (p.lanes < 32 && p.lanes < p.units)
         p.lanes *= 2;
-    if constexpr (V <= 1)
-        if (p.units > 128)
-            return launch<T, V, 8, BACKWARD>(p, d, s);
-    if constexpr (V <= 2)
-        if (p.units > 64)
-            return launch<T, V, 4, BACKWARD>(p, d, s);
     if constexpr (V <= 4)
         if (p.units > 32)
-            return launch<T, V, 2, BACKWARD>(p, d, s);
-    return launch<T, V, 1, BACKWARD>(p, d, s);
+            return launch<T, V, 2, false, BACKWARD>(p, d, s);
+    return launch<T, V, 1, false, BACKWARD>(p, d, s);
+}
+
+// As many as have eight pairs each (or six), and four at least: the groups' rings fit 40 KB.
+template <typename T, bool BACKWARD> cudaError_t launch_whole(Params p, const rikfad_rotary_norm *d, cudaStream_t s)
+{
+    const int rest = p.head_dim - p.rotary_dim;
+    p.rest_half = (rest + 1) / 2;
+    p.units = p.interleaved ? (p.head_dim + 1) / 2 : p.pairs + p.rest_half;
+    p.lanes = 4;
+    while (p.lanes < 32 && p.lanes * 8 < p.units)
+        p.lanes *= 2;
+    return p.units <= p.lanes * 6 ? launch<T, 6, 1, true, BACKWARD>(p, d, s) : launch<T, 8, 1, true, BACKWARD>(p, d, s);
 }
 
 template <typename T, bool BACKWARD> cudaError_t launch(const rikfad_rotary_norm *d, cudaStream_t s)
@@ -736,7 +831,7 @@ template <typename T, bool BACKWARD> cudaError_t launch(const rikfad_rotary_norm
     p.tokens = d->tokens;
     p.tiles = d->batch;
     bool wanted = false;
-    // The widest vectors that the heads' layout and addresses allow: every part of a
+    // Vectors of 8 or 4 elements if the heads' layout and addresses allow them: every part of a
     // head and every stride is a whole number of vectors, and so are the addresses.
     uint64_t parts = (uint64_t)d->head_dim;
     if (!p.interleaved)
@@ -777,10 +872,8 @@ template <typename T, bool BACKWARD> cudaError_t launch(const rikfad_rotary_norm
         p.part = static_cast<float *>(d->workspace);
     if constexpr (sizeof(T) == 2)
         if (parts % 8 == 0)
-            return launch<T, 8, BACKWARD>(p, d, s);
-    return parts % 4 == 0   ? launch<T, 4, BACKWARD>(p, d, s)
-           : parts % 2 == 0 ? launch<T, 2, BACKWARD>(p, d, s)
-                            : launch<T, 1, BACKWARD>(p, d, s);
+            return launch_vectors<T, 8, BACKWARD>(p, d, s);
+    return parts % 4 == 0 ? launch_vectors<T, 4, BACKWARD>(p, d, s) : launch_whole<T, BACKWARD>(p, d, s);
 }
 
 template <bool BACKWARD> int run(const rikfad_rotary_norm *p, void *stream)
