@@ -27,6 +27,7 @@ namespace {
 
 constexpr int kSms = 152;
 constexpr int kForwardThreads = 256, kForwardRows = 4;
+constexpr int kNarrowThreads = 128, kNarrowColumns = 256;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortCtas = 8, kSortItems = 8;
 constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kSortBits = 9;            // of a pass: the warps' counts of 2^9 digits take 32 KB
@@ -106,31 +107,108 @@ __global__ void __launch_bounds__(kForwardThreads) rikfad_embed_forward_kernel(c
         from[r] = table + id * p.table_stride;
         to[r] = t < p.tokens ? static_cast<O *>(p.rows) + t * p.row_stride : nullptr;
     }
-    constexpr int kUnits = V == 1 ? 4 : 1;          // single elements: more of them at once
-    const int step = blockDim.x * gridDim.y;
-    for (int u0 = blockIdx.y * blockDim.x + threadIdx.x; u0 < p.units; u0 += step * kUnits) {
-        Vec<W, V> in[kUnits][kForwardRows];
+    for (int u = blockIdx.y * blockDim.x + threadIdx.x; u < p.units; u += blockDim.x * gridDim.y) {
+        Vec<W, V> in[kForwardRows];
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
+        for (int r = 0; r < kForwardRows; ++r)
+            if (inside[r])
+                load(in[r], from[r] + (int64_t)u * V);
 #pragma unroll
-            for (int r = 0; r < kForwardRows; ++r)
-                if (inside[r] && u0 + k * step < p.units)
-                    load(in[k][r], from[r] + (int64_t)(u0 + k * step) * V);
+        for (int r = 0; r < kForwardRows; ++r) {
+            float f[V];
+            widen(in[r], f);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                f[e] = inside[r] ? f[e] * p.scale : 0.f;
+            Vec<O, V> out;
+            narrow(f, out);
+            if (to[r])
+                store(out, to[r] + (int64_t)u * V);
         }
+    }
+}
+
+// Rows that start anywhere: a warp has 256 columns of kForwardRows rows, read and written 16
+// bytes at a time where elements have 2 bytes, by way of shared memory, and neighbours side by
+// side where they have 4.
+template <typename W, typename O>
+__global__ void __launch_bounds__(kNarrowThreads) rikfad_embed_forward_narrow_kernel(const __grid_constant__ EmbedParams p)
+{
+    constexpr int kSlot = kNarrowColumns * 2 + 16, kEach = kNarrowColumns / 32;
+    __shared__ uint4 buffers[kNarrowThreads / 32][kForwardRows][kSlot / 16];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slabs = p.slabs;
+    const int64_t item = (int64_t)blockIdx.x * (kNarrowThreads / 32) + warp;
+    const int64_t first = item / slabs * kForwardRows;
+    const int column = (int)(item % slabs) * kNarrowColumns, here = min(kNarrowColumns, p.width - column);
+    wait_for_predecessor();
+    allow_successor_launch();
+    if (first >= p.tokens)
+        return;
+    const W *from[kForwardRows];
+    bool inside[kForwardRows];
+    uint4 in[kForwardRows][2];
+    float f[kForwardRows][kEach];
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
+    for (int r = 0; r < kForwardRows; ++r) {
+        const uint32_t id = first + r < p.tokens ? id_at(p.ids, p.id_bytes, first + r, p.vocab) : (uint32_t)p.vocab;
+        inside[r] = id < p.vocab;
+        from[r] = static_cast<const W *>(p.table) + id * p.table_stride + column;
+    }
 #pragma unroll
-            for (int r = 0; r < kForwardRows; ++r) {
-                float f[V];
-                widen(in[k][r], f);
+    for (int r = 0; r < kForwardRows; ++r) {
+        if constexpr (sizeof(W) == 2) {
+            const int skip = (int)((uintptr_t)from[r] % 16), words = (skip + here * 2 + 15) / 16;
+            const uint4 *words_from = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(from[r]) - skip);
+            if (inside[r] && lane < words)
+                in[r][0] = words_from[lane];
+            if (inside[r] && lane + 32 < words)
+                in[r][1] = words_from[lane + 32];
+        } else {
 #pragma unroll
-                for (int e = 0; e < V; ++e)
-                    f[e] = inside[r] ? f[e] * p.scale : 0.f;
-                Vec<O, V> out;
-                narrow(f, out);
-                if (to[r] && u0 + k * step < p.units)
-                    store(out, to[r] + (int64_t)(u0 + k * step) * V);
-            }
+            for (int j = 0; j < kEach; ++j)
+                f[r][j] = inside[r] && lane + 32 * j < here ? to_f32(from[r][lane + 32 * j]) : 0.f;
+        }
+    }
+    if constexpr (sizeof(W) == 2) {
+#pragma unroll
+        for (int r = 0; r < kForwardRows; ++r) {
+            buffers[warp][r][lane] = in[r][0];
+            if (lane + 32 < kSlot / 16)
+                buffers[warp][r][lane + 32] = in[r][1];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int r = 0; r < kForwardRows; ++r) {
+            const W *at = reinterpret_cast<const W *>(reinterpret_cast<const char *>(buffers[warp][r]) + (uintptr_t)from[r] % 16);
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                f[r][j] = inside[r] && lane + 32 * j < here ? to_f32(at[lane + 32 * j]) : 0.f;
+        }
+        __syncwarp();
+    }
+#pragma unroll
+    for (int r = 0; r < kForwardRows; ++r) {
+        if (first + r >= p.tokens)
+            break;
+        O *to = static_cast<O *>(p.rows) + (first + r) * p.row_stride + column;
+        if constexpr (sizeof(O) == 2) {
+            constexpr int E = 8;
+            const int skip = (int)((uintptr_t)to % 16), lead = min((16 - skip) % 16 / 2, here), words = (here - lead) / E, edges = here - words * E;
+            O *const place = reinterpret_cast<O *>(reinterpret_cast<char *>(buffers[warp][r]) + skip);
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (lane + 32 * j < here)
+                    place[lane + 32 * j] = from_f32<O>(f[r][j] * p.scale);
+            __syncwarp();
+            if (lane < words)
+                reinterpret_cast<uint4 *>(to + lead)[lane] = reinterpret_cast<const uint4 *>(place + lead)[lane];
+            if (lane < edges)
+                to[lane < lead ? lane : lane + words * E] = place[lane < lead ? lane : lane + words * E];
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (lane + 32 * j < here)
+                    to[lane + 32 * j] = from_f32<O>(f[r][j] * p.scale);
         }
     }
 }
@@ -183,6 +261,19 @@ __device__ __forceinline__ uint32_t cluster_read(const uint32_t *mine, int rank)
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
     return v;
+}
+
+// The lanes that have this lane's digit; `there`: whether it has one.
+__device__ __forceinline__ uint32_t lanes_alike(uint32_t digit, bool there, int bits)
+{
+    uint32_t same = __ballot_sync(~0u, there);
+#pragma unroll
+    for (int b = 0; b < kSortBits; ++b)
+        if (b < bits) {
+            const uint32_t set = __ballot_sync(~0u, digit >> b & 1);
+            same &= digit >> b & 1 ? set : ~set;
+        }
+    return same;
 }
 
 // Exclusive sum over the block's threads.
@@ -260,9 +351,10 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
                 total[b] = 0;
             __syncthreads();
             for (int i = begin + warp * 32; i < end; i += kSortThreads) {
-                const uint32_t digit = i + lane < end ? entry(i + lane).x >> shift & (bins - 1) : ~0u;
-                const uint32_t same = __match_any_sync(~0u, digit);
-                if (lane == __ffs(same) - 1 && digit != ~0u)
+                const bool there = i + lane < end;
+                const uint32_t digit = there ? entry(i + lane).x >> shift & (bins - 1) : 0;
+                const uint32_t same = lanes_alike(digit, there, p.bits);
+                if (there && lane == __ffs(same) - 1)
                     atomicAdd(total + digit, __popc(same));     // integers: any order
             }
             first_places();
@@ -286,7 +378,7 @@ __global__ void __launch_bounds__(kSortThreads) rikfad_embed_sort_kernel(const _
                 if (k >= rounds)
                     break;
                 const uint32_t digit = e[k].x >> shift & (bins - 1);
-                const uint32_t same = __match_any_sync(~0u, i < end ? digit : ~0u);
+                const uint32_t same = lanes_alike(digit, i < end, p.bits);
                 const int leader = __ffs(same) - 1;
                 uint32_t old = 0;
                 if (lane == leader && i < end) {
@@ -717,25 +809,33 @@ EmbedParams params(const rikfad_embedding *p)
 
 template <typename W, typename O, int V> cudaError_t launch_forward(EmbedParams p, cudaStream_t s)
 {
-    p.units = p.width / V;
-    int lanes = 32;
-    while (lanes < kForwardThreads && lanes < p.units)
-        lanes *= 2;
-    const int rows = kForwardThreads / lanes;
-    const int64_t blocks = (p.tokens + rows * kForwardRows - 1) / (rows * kForwardRows);
-    // few rows: several blocks for each
-    const int64_t most = (p.units + lanes - 1) / lanes;
-    const int64_t across = std::max<int64_t>(1, std::min<int64_t>(most, 4 * kSms / blocks));
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)blocks, (unsigned)across);
-    cfg.blockDim = dim3((unsigned)lanes, (unsigned)rows);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, rikfad_embed_forward_kernel<W, O, V>, p);
+    if constexpr (V == 1) {
+        p.slabs = (p.width + kNarrowColumns - 1) / kNarrowColumns;
+        const int64_t items = (p.tokens + kForwardRows - 1) / kForwardRows * p.slabs, warps = kNarrowThreads / 32;
+        if ((items + warps - 1) / warps > INT32_MAX)
+            return cudaErrorInvalidConfiguration;
+        return launch_chained(rikfad_embed_forward_narrow_kernel<W, O>, dim3((unsigned)((items + warps - 1) / warps)), kNarrowThreads, 0, s, p);
+    } else {
+        p.units = p.width / V;
+        int lanes = 32;
+        while (lanes < kForwardThreads && lanes < p.units)
+            lanes *= 2;
+        const int rows = kForwardThreads / lanes;
+        const int64_t blocks = (p.tokens + rows * kForwardRows - 1) / (rows * kForwardRows);
+        // few rows: several blocks for each
+        const int64_t most = (p.units + lanes - 1) / lanes;
+        const int64_t across = std::max<int64_t>(1, std::min<int64_t>(most, 4 * kSms / blocks));
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)blocks, (unsigned)across);
+        cfg.blockDim = dim3((unsigned)lanes, (unsigned)rows);
+        cfg.stream = s;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, rikfad_embed_forward_kernel<W, O, V>, p);
+    }
 }
 
 cudaError_t launch_sort(const SortParams &p, cudaStream_t s)
