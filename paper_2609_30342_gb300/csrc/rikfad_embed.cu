@@ -32,8 +32,8 @@ constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortCtas = 8
 constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kSortBits = 9;            // of a pass: the warps' counts of 2^9 digits take 32 KB
 constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32, kSumAhead = 8;
-constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinAhead = 4, kJoinBlocks = 4 * kSms;
-constexpr double kZeroBytesPerUs = 5e6; // of all multiprocessors but the sorting ones
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinAhead = 8, kJoinBlocks = 4 * kSms;
+constexpr double kZeroBytesPerUs = 4.2e6; // of all multiprocessors but the sorting ones
 constexpr int kShortRun = 32;           // chunks that a run joined by one warp goes on in, at most
 constexpr int kCountThreads = 256, kMostCounted = 6144;
 
@@ -692,12 +692,12 @@ template <typename W> __global__ void __launch_bounds__(kJoinThreads) rikfad_emb
     for (int64_t i = blockIdx.x; i < long_runs; i += gridDim.x) {
         const int64_t chunk = p.starts[p.chunks - 1 - i / slabs], column = i % slabs * 128 + lane * 4;
         const uint32_t id = p.order[(chunk + 1) * p.chunk].x;
-        int64_t last = chunk + 1 + kShortRun, n = p.chunks - last;      // the first chunk that does not start with id
-        while (n > 0) {
-            const int64_t half = n / 2;
-            const bool same = p.order[(last + half) * p.chunk].x == id;
-            last = same ? last + half + 1 : last;
-            n = same ? n - half - 1 : half;
+        int64_t last = chunk + 1 + kShortRun, end = p.chunks;           // the first chunk that does not start with id
+        while (last < end) {            // 32 places at a time
+            const int64_t step = (end - last + 31) / 32, c = last + lane * step;
+            const int same = __popc(__ballot_sync(~0u, c < end && p.order[c * p.chunk].x == id));
+            end = min(end, last + same * step);
+            last = same ? last + (same - 1) * step + 1 : end;
         }
         const int64_t share = (last - chunk - 1 + kJoinWarps - 1) / kJoinWarps, from = chunk + 1 + share * warp;
         float4 s = warp == 0 && column < p.pitch ? *reinterpret_cast<const float4 *>(p.tail + chunk * p.pitch + column) : nothing;
@@ -1008,7 +1008,7 @@ RIKFAD_API int rikfad_embedding_backward(const rikfad_embedding *p, void *stream
         if (!p->accumulate && p->tokens <= p->vocab / 8)
             q.zero_from = 0;
         else if (!p->accumulate) {
-            const double us = p->tokens <= kMostCounted ? 3 : 6 + (double)p->tokens / 2000;
+            const double us = p->tokens <= kMostCounted ? 3 : 9 + (double)p->tokens / 2800;      // 12.3 at 8192, 32.7 at 65536
             const double rows = us * kZeroBytesPerUs / ((double)p->width * dtype_bytes(p->table_dtype));
             q.zero_from = p->vocab - (int64_t)std::min((double)p->vocab, rows);
         }
