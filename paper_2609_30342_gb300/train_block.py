@@ -1,18 +1,24 @@
 """A small language model trained with the library's operators around its matrix products.
 
-    python -m paper_2609_30342_gb300.train_block [--steps 60] [--layers 2] [--width 256]
+    python -m paper_2609_30342_gb300.train_block [--steps 60] [--layers 2] [--width 256] [--student-layers 1]
 
 Transformer blocks with norms before and after each branch and a learned gate per channel (``layers.ResidualNorm``),
 rotary positions over packed sequences (``layers.Rotary``), the gradients clipped to a largest global norm
 (``RIKFADOptimizer.clip_grad_norm``) and the R-iKFAD step.  Activations are bfloat16, the residual stream and the
 parameters float32.  The data are synthetic: every token is a fixed function of the two before it, with some noise.
+
+With ``--student-layers`` a smaller model then learns from the first one's largest logits and the labels together
+(``losses.DistillationLoss``); its tokens are embedded by ``embedding.TokenEmbedding``, and its queries and keys normed per
+head as they are turned (``layers.RotaryNorm``).
 """
 import argparse
 
 import torch
 from torch import nn
 
-from .layers import ResidualNorm, Rotary
+from .embedding import TokenEmbedding
+from .layers import ResidualNorm, Rotary, RotaryNorm
+from .losses import DistillationLoss
 from .optim import RIKFADOptimizer
 
 
@@ -29,11 +35,17 @@ class Block(nn.Module):
             self.register_parameter(name + "_gate", nn.Parameter(torch.ones(1, width)))
             self.register_parameter(name + "_post", nn.Parameter(torch.ones(width)))
             self.register_parameter(name + "_pre", nn.Parameter(torch.ones(width)))
+        self.normed = getattr(rotary, "eps", None) is not None      # queries and keys, per head
+        if self.normed:
+            self.q_scale, self.k_scale = (nn.Parameter(torch.ones(width // heads)) for _ in range(2))
 
     def attend(self, h, positions, mask):
         tokens, width = h.shape
         q, k, v = torch.nn.functional.linear(h, self.qkv.weight.to(h.dtype)).view(tokens, 3, self.heads, -1).unbind(1)
-        q, k = self.rotary(q, k, positions=positions)
+        if self.normed:
+            q, k = self.rotary(q, k, self.q_scale, self.k_scale, positions=positions)
+        else:
+            q, k = self.rotary(q, k, positions=positions)
         scores = torch.einsum("ihd,jhd->hij", q, k).float() * q.shape[-1] ** -0.5
         weights = torch.softmax(scores.masked_fill(~mask, float("-inf")), -1).to(h.dtype)
         mixed = torch.einsum("hij,jhd->ihd", weights, v).reshape(tokens, width)
@@ -50,9 +62,10 @@ class Block(nn.Module):
 
 
 class Model(nn.Module):
-    def __init__(self, vocab=512, width=256, layers=2, heads=4, dtype=torch.bfloat16, norm=None, first=None, rotary=None):
+    def __init__(self, vocab=512, width=256, layers=2, heads=4, dtype=torch.bfloat16, norm=None, first=None, rotary=None,
+                 table=None):
         super().__init__()
-        self.dtype = dtype
+        self.dtype, self.table = dtype, table
         self.embed = nn.Embedding(vocab, width)
         nn.init.normal_(self.embed.weight, std=0.02)
         self.first = ResidualNorm(width, pre="rms") if first is None else first
@@ -66,7 +79,8 @@ class Model(nn.Module):
         sequence = torch.cumsum(positions == 0, 0)
         at = torch.arange(tokens.numel(), device=tokens.device)
         mask = (sequence[:, None] == sequence[None]) & (at[:, None] >= at[None])
-        x, h = self.first(self.embed(tokens), pre_weight=self.scale, dtype=self.dtype)
+        x = self.embed(tokens) if self.table is None else self.table(self.embed.weight, tokens)
+        x, h = self.first(x, pre_weight=self.scale, dtype=self.dtype)
         for block in self.blocks:
             x, h = block(x, h, positions, mask)
         return torch.nn.functional.linear(h, self.embed.weight.to(h.dtype)).float()
@@ -98,6 +112,12 @@ def loss_of(model, tokens, positions):
 def train(steps=60, vocab=512, width=256, layers=2, lengths=(200, 57, 1, 254), max_norm=1.0, lr=0.05, alpha=0.1, mu=1e-2,
           seed=0, report=None):
     """Train on synthetic sequences; returns the losses and gradient norms of the steps."""
+    return train_model(steps, vocab, width, layers, lengths, max_norm, lr, alpha, mu, seed, report)[1:]
+
+
+def train_model(steps=60, vocab=512, width=256, layers=2, lengths=(200, 57, 1, 254), max_norm=1.0, lr=0.05, alpha=0.1,
+                mu=1e-2, seed=0, report=None):
+    """``train``, with the model before the losses and gradient norms."""
     torch.manual_seed(seed)
     model = Model(vocab, width, layers).cuda()
     opt = RIKFADOptimizer(model.parameters(), lr=lr, alpha=alpha, mu=mu)
@@ -114,7 +134,45 @@ def train(steps=60, vocab=512, width=256, layers=2, lengths=(200, 57, 1, 254), m
             report("step %4d  loss %.4f  gradient norm %.4f" % (step, float(loss.detach()), float(norm)))
     opt.check_finite()
     opt.close()
-    return [float(v) for v, _ in history], [float(n) for _, n in history]
+    return model, [float(v) for v, _ in history], [float(n) for _, n in history]
+
+
+def distillation_loss(model, tokens, positions, loss, teacher=None, index=None):
+    """Mean of ``loss`` over every token but the sequences' first, against a teacher's largest logits at ``index``."""
+    logits = model(tokens, positions)
+    follows = positions[1:] > 0
+    labels = torch.where(follows, tokens[1:], torch.full_like(tokens[1:], -100))
+    if teacher is not None:
+        index = torch.where(follows[:, None], index[:-1], torch.full_like(index[:-1], -1))
+        teacher = teacher[:-1].contiguous()
+    return loss(logits[:-1], teacher, index, labels).sum() / follows.sum()
+
+
+def distil(teacher, steps=60, layers=1, width=None, top=16, temperature=2.0, lengths=(200, 57, 1, 254), max_norm=1.0,
+           lr=0.05, alpha=0.1, mu=1e-2, seed=1, report=None):
+    """Train a smaller model on a larger one's ``top`` logits and the labels; returns it, the losses and gradient norms."""
+    torch.manual_seed(seed)
+    vocab, full = teacher.embed.weight.shape
+    width = full if width is None else width
+    model = Model(vocab, width, layers, rotary=RotaryNorm(width // 4), table=TokenEmbedding(vocab, width)).cuda()
+    loss = DistillationLoss(temperature, teacher_weight=0.5, label_weight=0.5)
+    opt = RIKFADOptimizer(model.parameters(), lr=lr, alpha=alpha, mu=mu)
+    history = []
+    for step in range(steps):
+        tokens, positions = batch(step, vocab, lengths)
+        with torch.no_grad():
+            logits, index = teacher(tokens, positions).topk(min(top, vocab), -1)
+        opt.zero_grad()
+        value = distillation_loss(model, tokens, positions, loss, logits, index)
+        value.backward()
+        norm = opt.clip_grad_norm(max_norm)
+        opt.step()
+        history.append((value.detach(), norm))
+        if report and (step % 10 == 0 or step == steps - 1):
+            report("student  step %4d  loss %.4f  gradient norm %.4f" % (step, float(value.detach()), float(norm)))
+    opt.check_finite()
+    opt.close()
+    return model, [float(v) for v, _ in history], [float(n) for _, n in history]
 
 
 def main():
@@ -123,8 +181,11 @@ def main():
     p.add_argument("--layers", type=int, default=2)
     p.add_argument("--width", type=int, default=256)
     p.add_argument("--max-norm", type=float, default=1.0)
+    p.add_argument("--student-layers", type=int, default=0)
     a = p.parse_args()
-    train(a.steps, layers=a.layers, width=a.width, max_norm=a.max_norm, report=print)
+    model = train_model(a.steps, layers=a.layers, width=a.width, max_norm=a.max_norm, report=print)[0]
+    if a.student_layers:
+        distil(model, a.steps, layers=a.student_layers, max_norm=a.max_norm, report=print)
 
 
 if __name__ == "__main__":
