@@ -298,7 +298,8 @@ __device__ __forceinline__ void load_entries(const Params &p, Entries &to, int64
             const int i = to.index[e];
             if (i < 0 || !slice.has(i, rank))
                 continue;
-            for (int n = i & (size - 1);; n = (n + 1) & (size - 1)) {       // ends: fewer names than places
+            // indices are often evenly spaced: a multiplicative hash.  Ends: fewer names than places
+            for (int n = (uint32_t)i * 2654435769u >> __clz(k);; n = (n + 1) & (size - 1)) {
                 const int there = atomicCAS(to.names + n, -1, i);
                 met = met || there == i;
                 if (there == -1 || there == i)

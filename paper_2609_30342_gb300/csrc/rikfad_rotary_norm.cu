@@ -904,8 +904,13 @@ template <bool BACKWARD> int run(const rikfad_rotary_norm *p, void *stream)
     if (any && wanted) {
         if (p->workspace == nullptr || p->workspace_bytes < workspace_of(p))
             return bad("the workspace is smaller than rikfad_rotary_norm_workspace");
-        if ((uintptr_t)p->workspace % 16)
-            return report_error(RIKFAD_ERR_ALIGN, "workspace is not aligned");
+        int device = -1;
+        const cudaError_t e = cudaGetDevice(&device);
+        if (e != cudaSuccess)
+            return report_cuda(e, "cudaGetDevice");
+        const int bad_place = check_place(p->workspace, "workspace", 16, device);
+        if (bad_place)
+            return bad_place;
     }
     cudaError_t e = cudaPeekAtLastError();
     if (e != cudaSuccess)

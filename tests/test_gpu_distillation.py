@@ -246,6 +246,13 @@ def test_entries_that_name_one_element():
         assert torch.equal(_all_ways(op, logits, t, index, labels)[3], g)
 
 
+@pytest.mark.parametrize("k,gap", [(1024, 128), (64, 2048), (3, 40000), (2, 1)])
+def test_evenly_spaced_entries(k, gap):
+    logits, t, _, labels = _inputs(3, 131072, k)
+    index = (torch.arange(k, device="cuda") * gap + torch.tensor([[0], [5], [131071]], device="cuda")) % 131072
+    _all_ways(DistillationLoss(2.0, 1.0, 0.5), logits, t, index, index[:, -1].contiguous())
+
+
 @pytest.mark.parametrize("vocab,pad", [(1000, 8), (1000, 3), (1001, 7), (1001, 0), (50257, 15)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strided_rows_at_any_offset(dtype, vocab, pad):

@@ -9,6 +9,7 @@ import pytest
 import torch
 
 from paper_2609_30342_gb300 import build as pkg_build
+from paper_2609_30342_gb300 import rikfad
 from paper_2609_30342_gb300.layers import Rotary, RotaryNorm
 
 pytestmark = pytest.mark.gpu
@@ -155,6 +156,25 @@ def test_in_place():
     want = op.forward(q, k, w, w)
     got = op.forward(q, k, w, w, out=(q, k))
     assert got[0] is q and torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
+@pytest.mark.parametrize("over", ["x", "dout"])
+@pytest.mark.parametrize("head_dim,rotary_dim", [(64, 64), (80, 40), (70, 70), (131, 102)])
+def test_gradients_over_their_inputs(head_dim, rotary_dim, over):
+    """dx may be x or dout: the same results to the bit."""
+    op = RotaryNorm(head_dim, rotary_dim)
+    q, dq = _rand(300, 5, head_dim, seed=1, dtype=torch.bfloat16), _rand(300, 5, head_dim, seed=2, dtype=torch.bfloat16)
+    w = _rand(head_dim, seed=3)
+    want = op.backward(dq, None, q, q_weight=w)
+    first = device, dtype, lead, batch, tokens = op._lead(q)
+    strides, dw, to = op._dense(tokens, 5), torch.empty_like(w), q if over == "x" else dq
+    lists = (q.data_ptr(), dq.data_ptr(), w.data_ptr(), to.data_ptr(), dw.data_ptr(), 5, *strides, *strides, *strides)
+    lib = rikfad.lib()
+    nbytes = lib.rikfad_rotary_norm_workspace(op._block(first, None, 0, torch.float32, lists))
+    work = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    rikfad._check(lib.rikfad_rotary_norm_backward(
+        op._block(first, None, 0, torch.float32, lists, (work.data_ptr(), nbytes)), rikfad._raw_stream(0)))
+    assert torch.equal(to, want.q) and torch.equal(dw, want.q_weight)
 
 
 @pytest.mark.parametrize("shape", [(0, 2, 64), (2, 0, 2, 64), (0, 3, 2, 64), (3, 0, 64)])
