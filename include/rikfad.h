@@ -600,8 +600,11 @@ RIKFAD_API int rikfad_rotary_turns(const double *radians, int64_t n, uint64_t *t
  *   workspace  backward: device memory of rikfad_rotary_norm_workspace bytes,
  *              16-byte aligned; nothing kept
  * 1 <= head_dim <= 512; batch, tokens and heads as for rikfad_rotary.  Sums are
- * in float32 and in an order that goes by the sizes alone.  Nothing is
- * synchronised or allocated.
+ * in float32 and in an order that goes by the sizes and alignments alone.  Squares
+ * beyond float32's range are infinite, as for the residual norm; a head of zeros
+ * with eps = 0 is NaN.  Heads that do not begin and end on vectors of 8 or 16 bytes
+ * are read 16 bytes at a time, with what else lies in their first and last 16.
+ * Nothing is synchronised or allocated.
  */
 typedef struct {
     const void *x, *dout, *weight;
@@ -647,8 +650,10 @@ RIKFAD_API size_t rikfad_rotary_norm_workspace(const rikfad_rotary_norm *p);
  *   workspace  backward: device memory of rikfad_embedding_workspace bytes, 16-byte
  *              aligned; nothing kept
  * Any two of the element types.  Rows are `width` contiguous elements, `stride`
- * apart; 0 <= tokens <= 2^30, 0 <= vocab <= 2^30, 1 <= width <= 2^20.  Nothing is
- * synchronised or allocated.
+ * apart; 0 <= tokens <= 2^30, 0 <= vocab <= 2^30, 1 <= width <= 2^20.  The rows that
+ * a call writes overlap nothing else.  Rows that do not begin and end on vectors are
+ * read 16 bytes at a time, with what else lies in their first and last 16.  Nothing
+ * is synchronised or allocated.
  */
 typedef struct {
     int64_t tokens, vocab, width;
