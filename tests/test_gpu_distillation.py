@@ -151,6 +151,17 @@ def test_temperatures(temperature, rows):
     _all_ways(op, *_inputs(rows, 3001, 12, "bf16", absent=0.2))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_largest_vocabulary(dtype):
+    op = DistillationLoss(2.0, 1.0, 0.5)
+    logits, t, index, labels = _inputs(2, 1 << 24, 64, dtype)
+    index[:, 0], labels[1] = (1 << 24) - 1, (1 << 24) - 1
+    loss, g = op.loss_and_gradient(logits, t, index, labels)
+    _check(op, logits, t, index, labels, loss, g)
+    apart, stats = op.forward(logits, t, index, labels)
+    _check(op, logits, t, index, labels, apart, op.backward(None, logits, t, index, labels, stats))
+
+
 def test_terms_apart():
     logits, t, index, labels = _inputs(50, 777, 10, absent=0.3)
     for op, args in ((DistillationLoss(2.0), (logits, t, index, None)), (DistillationLoss(2.0, 0.0, 1.0), (logits, None, None, labels)),

@@ -196,6 +196,15 @@ def test_autograd_and_differences():
         g.sum().backward()
 
 
+@pytest.mark.parametrize("tokens,vocab,width", [(3, 5, 1 << 20), (2, 3, (1 << 20) - 1), (200003, 1 << 24, 1), (7000, 1 << 22, 3)])
+def test_widest_rows_and_largest_tables(tokens, vocab, width):
+    op = TokenEmbedding(vocab, width)
+    w, d = _rand(vocab, width, seed=1, dtype=torch.bfloat16), _rand(tokens, width, seed=2, dtype=torch.bfloat16)
+    ids = _ids(tokens, vocab, "skewed")
+    _check_forward(op.forward(w, ids), w, ids, 1.0)
+    _check_backward(op.backward(d, ids), d, ids, 1.0)
+
+
 def test_far_rows():
     """A table and rows beyond 2^31 elements."""
     vocab, width = 70000, 32768
