@@ -103,7 +103,7 @@ class TokenEmbedding:
         if tokens:
             shape = body[:5]            # the size of the workspace goes by sizes and types alone
             nbytes = self._workspace.get(shape)
-            if nbytes is None:
+            if not nbytes:              # 0: this call is refused below, and later ones may not be
                 nbytes = lib.rikfad_embedding_workspace(_EMBEDDING.pack(*body, 0, 0))
                 if len(self._workspace) >= 64:
                     self._workspace.clear()

@@ -435,7 +435,7 @@ class RotaryNorm(Rotary):
             raise ValueError("eps must be finite and >= 0")
         super().__init__(head_dim, rotary_dim, base, layout, scaling, frequencies, magnitude, device)
         self.eps = float(eps)
-        self._workspace = None
+        self._workspace = 0         # bytes, when a call has asked for them
 
     def _dense(self, tokens, heads):
         """Batch, token and head strides of a contiguous tensor."""
@@ -524,7 +524,7 @@ class RotaryNorm(Rotary):
             work = (0, 0)
             if grads[1] is not None or grads[-1] is not None:
                 nbytes = self._workspace
-                if nbytes is None:          # it goes by head_dim alone
+                if not nbytes:              # it goes by head_dim alone; 0: this call's sizes are refused below
                     nbytes = self._workspace = lib.rikfad_rotary_norm_workspace(
                         self._block(first, positions, start, pt, lists))
                 buffer = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
