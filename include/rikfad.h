@@ -685,8 +685,9 @@ RIKFAD_API size_t rikfad_embedding_workspace(const rikfad_embedding *p);
  * gradient of 0, whatever its logits.  Entries that name one element add up.  Logits
  * of -inf have a share of 0; a row of nothing else, or with NaN or +inf, has a loss
  * and a gradient of NaN if it has a term.  Finite logits (the teacher's too)
- * below -3.7e8 min(1, T), as masks are, count as that value; ones above 3.7e8
- * min(1, T) count as +inf.
+ * below -3.7e8 min(1, T), as masks are, count as that value in the softmax: a
+ * row of nothing else has equal shares.  In any other row a loss that names one
+ * has its own value.  Logits above 3.7e8 min(1, T) count as +inf.
  *   logits     `rows` rows of `vocab` elements of dtype
  *   teacher    rows of k elements of teacher_dtype; index: of index_bytes (4 or 8)
  *              bytes, signed.  Not read with k = 0

@@ -41,6 +41,9 @@ constexpr int kSmemPerSm = 228 << 10;
 // A reference's rounding is a factor of up to 2^(r 2^-24) in every power: r stays below
 // this, and lower logits count as the one there.
 constexpr float kFarthest = 0x1p29f;
+// A named element below it (a type's lowest value; its product with c may leave float32's range) adds x c to a log share
+// that is less than 2^-60 of that beside it.
+constexpr float kRemote = -0x1p100f;
 constexpr float kLargestSum = 0x1p40f;      // of a thread, beyond which its reference is too low
 constexpr int kEntriesAhead = 4;            // entries of a lane under way
 constexpr int kAhead = 4;                      // vectors of a thread under way
@@ -438,21 +441,35 @@ __global__ void __launch_bounds__(kMaxThreads) rikfad_distill_kernel(const __gri
     auto logit = [&](float x) { return low ? to_f32(from_f32<T>(at_least(x, p.lowest))) : x; };
     if (MODE != kBackward && rank == 0 && last_warp) {
         float loss = 0.f;
+        // log2 of the share without a remote element's x c, and that element: it is in the loss by a T (or b) times x
+        auto log_share = [&](float at, float c, float ref, float log_sum, float &remote) {
+            const float x = logit(at);
+            remote = x < kRemote && x > -INFINITY ? x : 0.f;
+            return fmaf(remote != 0.f ? 0.f : x, c, -ref) - log_sum;
+        };
+        float remote;
         if (distils) {
             const float log_q = log2f(sum_t);
+            float remotes = 0.f;
             for (int e = lane; e < p.k; e += 32)
                 if (entries.index[e] >= 0) {
                     const float lp = entries.log_p[e], share = exp2_fast(lp);
-                    if (share != 0.f)
-                        loss += share * (lp - (fmaf(logit(entries.at_index[e]), p.c_t, -r_t) - log_q));
+                    if (share != 0.f) {
+                        loss += share * (lp - log_share(entries.at_index[e], p.c_t, r_t, log_q, remote));
+                        remotes += share * remote;
+                    }
                 }
 #pragma unroll
-            for (int d = 16; d > 0; d /= 2)
+            for (int d = 16; d > 0; d /= 2) {
                 loss += __shfl_xor_sync(~0u, loss, d);
-            loss *= p.loss_a;
+                remotes += __shfl_xor_sync(~0u, remotes, d);
+            }
+            loss = loss * p.loss_a - p.a * remotes;
         }
-        if (labelled)
-            loss -= p.loss_b * (fmaf(logit(entries.at_index[p.k]), p.c_1, -r_1) - log2f(sum_1));
+        if (labelled) {
+            loss -= p.loss_b * log_share(entries.at_index[p.k], p.c_1, r_1, log2f(sum_1), remote);
+            loss -= p.b * remote;
+        }
         if (lane == 0) {
             p.loss[r] = loss;
             if (p.stats)
