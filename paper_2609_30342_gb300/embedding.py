@@ -3,7 +3,7 @@
 ``TokenEmbedding`` has explicit calls on CUDA tensors (``forward``, ``backward``) and is callable inside autograd.
 Argument checks and marshalling only: the work runs in the kernels behind ``rikfad_embedding_forward`` and
 ``rikfad_embedding_backward``, enqueued on the current stream of the tensors' device (or ``stream``, to which what the
-call allocates then belongs; the inputs have to be ready on it).
+call allocates then belongs; the inputs have to be ready on it).  A tensor given as ``out`` counts as changed in autograd.
 """
 import math
 import struct
@@ -64,7 +64,8 @@ class TokenEmbedding:
         device, width = self._device(weight), self.width
         at, id_bytes, tokens = self._ids(ids, device)
         pw, sw = _rows("weight", weight, width, weight.dtype, device, self.vocab)
-        if out is None:
+        fresh = out is None
+        if fresh:
             out = torch.empty(*ids.shape, width, dtype=self._dtype(dtype, weight.dtype), device=weight.device)
             po, so = out.data_ptr(), width
         else:
@@ -74,6 +75,8 @@ class TokenEmbedding:
         block = _EMBEDDING.pack(tokens, self.vocab, width, _TORCH[weight.dtype], _TORCH[out.dtype], id_bytes, 0, self.scale,
                                 at, pw, sw, po, so, 0, 0)
         rikfad._call_on(device, rikfad.lib().rikfad_embedding_forward, block, rikfad._raw_stream(device))
+        if not fresh:
+            rikfad._written(out)
         return out
 
     def backward(self, dout, ids, dtype=None, out=None, accumulate=False, stream=None):
@@ -87,7 +90,8 @@ class TokenEmbedding:
         if dout.shape != (*ids.shape, width):
             raise ValueError("dout must have the shape of ids and %d columns" % width)
         pd, sd = _rows("dout", dout, width, dout.dtype, device, tokens)
-        if out is None:
+        fresh = out is None
+        if fresh:
             if accumulate:
                 raise ValueError("accumulate needs out")
             out = torch.empty(vocab, width, dtype=self._dtype(dtype, dout.dtype), device=dout.device)
@@ -111,6 +115,8 @@ class TokenEmbedding:
             work = torch.empty(nbytes, dtype=torch.uint8, device=dout.device)
             pw = work.data_ptr()
         rikfad._call_on(device, lib.rikfad_embedding_backward, _EMBEDDING.pack(*body, pw, nbytes), rikfad._raw_stream(device))
+        if not fresh:
+            rikfad._written(out)
         return out
 
     def __call__(self, weight, ids, dtype=None):

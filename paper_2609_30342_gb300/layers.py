@@ -464,7 +464,8 @@ class RotaryNorm(Rotary):
 
     def forward(self, q, k=None, q_weight=None, k_weight=None, positions=None, start=0, out=None, stream=None):
         """(q', k') of queries and keys [tokens, heads, head_dim] or [batch, tokens, heads, head_dim] (k' None without k),
-        with positions as for ``rotate``.  ``out``: (q', k') to write to; q and k themselves for in place."""
+        with positions as for ``rotate``.  ``out``: (q', k') to write to; q and k themselves for in place.  Tensors given as
+        ``out`` count as changed in autograd: a graph that holds them refuses its backward pass."""
         if stream is not None:
             with _streaming(stream, q):
                 return self.forward(q, k, q_weight, k_weight, positions, start, out)
@@ -491,6 +492,8 @@ class RotaryNorm(Rotary):
             lists += (px, 0, weight, po, 0, heads, *from_, *to, 0, 0, 0)
         rikfad._call_on(device, rikfad.lib().rikfad_rotary_norm_forward, self._block(first, positions, start, pt, lists),
                         rikfad._raw_stream(device))
+        if not fresh:
+            rikfad._written(out[0], None if k is None else out[1])
         return out[0], (None if k is None else out[1])
 
     def backward(self, dq, dk, q, k=None, q_weight=None, k_weight=None, positions=None, start=0, stream=None):

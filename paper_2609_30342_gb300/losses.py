@@ -5,7 +5,7 @@
 It has explicit calls on CUDA tensors (``forward``, ``loss_and_gradient``, ``backward``) and is callable inside autograd.
 Argument checks and marshalling only: the work runs in the kernels behind ``rikfad_distillation_forward`` and
 ``rikfad_distillation_backward``, enqueued on the current stream of the tensors' device (or ``stream``, to which what the
-call allocates then belongs; the inputs have to be ready on it).
+call allocates then belongs; the inputs have to be ready on it).  A tensor given as ``out`` counts as changed in autograd.
 """
 import math
 import struct
@@ -134,9 +134,12 @@ class DistillationLoss:
         head, inputs, lead, rows, vocab, device = self._inputs(logits, teacher, index, labels)
         per_row = 0 if dloss is None else self._per_row(dloss, lead, device)
         loss = torch.empty(lead, dtype=_F32, device=logits.device)
+        given = out
         out, to = self._gradient(logits, out, rows, vocab, device)
         block = _DISTILLATION.pack(*head, float(grad_scale), *inputs, loss.data_ptr(), 0, per_row, *to)
         rikfad._call_on(device, rikfad.lib().rikfad_distillation_forward, block, rikfad._raw_stream(device))
+        if given is not None:
+            rikfad._written(given)
         return loss, out
 
     def backward(self, dloss, logits, teacher=None, index=None, labels=None, stats=None, grad_scale=1.0, out=None,
@@ -150,9 +153,12 @@ class DistillationLoss:
         if not isinstance(stats, torch.Tensor) or stats.dtype is not _F32 or stats.shape != (rows, 4) \
                 or not stats.is_contiguous() or stats.get_device() != device:
             raise ValueError("stats must be what forward returned for these inputs")
+        given = out
         out, to = self._gradient(logits, out, rows, vocab, device)
         block = _DISTILLATION.pack(*head, float(grad_scale), *inputs, 0, stats.data_ptr(), per_row, *to)
         rikfad._call_on(device, rikfad.lib().rikfad_distillation_backward, block, rikfad._raw_stream(device))
+        if given is not None:
+            rikfad._written(given)
         return out
 
     def __call__(self, logits, teacher=None, index=None, labels=None):

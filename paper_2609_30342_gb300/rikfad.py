@@ -178,6 +178,13 @@ def _streaming(stream, index):
     return torch.cuda.stream(stream)
 
 
+def _written(*tensors):
+    """Tell autograd that a call is to write to these tensors of the caller's: a graph that holds one of them refuses its
+    backward pass."""
+    import torch
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 def _call_on(index, function, *args):
     """``function(*args)``, checked, with device ``index`` current."""
     import torch
