@@ -660,10 +660,12 @@ template <typename T, Mode MODE, bool BOTH> cudaError_t launch(Params p, cudaStr
     while (MODE != kForward && p.names <= p.k && p.k > 0)
         p.names = p.names ? 2 * p.names : 2;
     cfg.dynamicSmemBytes = sizeof(float) * (3 * ((size_t)p.k + 1) + p.names + 3 * p.cluster * (threads / 32));
-    if (MODE == kFused && threads == kMaxThreads) {
+    if (MODE == kFused && !BOTH && threads == kMaxThreads) {
         // No more blocks on an SM than that: with more than a 1 / (n + 1) of the shared memory for
-        // each, n.  8192 rows of 50257 took 303 us with four blocks of a kernel whose registers
-        // allow five, 339 with five.
+        // each, n.  At one temperature registers allow five (elements of 16 bits) or six: cross
+        // entropy of 8192 rows of 50257 takes 275 us in bfloat16 with four, 317 with five, 562 in
+        // float32 with four, 682 with six.  At two they allow four; to ask for the memory all the
+        // same left less of it to the L1 cache (325 us instead of 316 in bfloat16).
         const int64_t most = std::max<int64_t>(kBlocksPerSm, kUnderWay * p.cluster / (bytes * kSms));
         if (most < 6)
             cfg.dynamicSmemBytes = std::max<size_t>(cfg.dynamicSmemBytes, (size_t)(kSmemPerSm / (most + 1)));
