@@ -70,10 +70,6 @@ template <typename T, int V> __device__ __forceinline__ void load(Vec<T, V> &r, 
 {
     r.word = *reinterpret_cast<const decltype(r.word) *>(p);
 }
-template <typename T, int V> __device__ __forceinline__ void load_once(Vec<T, V> &r, const T *p)
-{
-    r.word = __ldcs(reinterpret_cast<const decltype(r.word) *>(p));
-}
 template <typename T, int V> __device__ __forceinline__ void store(const Vec<T, V> &r, T *p)
 {
     *reinterpret_cast<decltype(r.word) *>(p) = r.word;

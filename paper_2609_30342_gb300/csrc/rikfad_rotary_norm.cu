@@ -317,10 +317,12 @@ rikfad_rotary_norm_kernel(const __grid_constant__ Params p)
     float *const cosines = reinterpret_cast<float *>(reinterpret_cast<char *>(shared) + R::bytes(p.head_dim, kThreads / p.lanes));
     float *const sines = cosines + p.tile * p.pitch;
     const int group = threadIdx.x / p.lanes, lane = threadIdx.x % p.lanes;
-    Place at[U];
+    Place at[U];                        // of vectors; whole heads have a spread instead
+    if constexpr (!WHOLE) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        at[u] = place_of<V>(p, lane + u * p.lanes);
+        for (int u = 0; u < U; ++u)
+            at[u] = place_of<V>(p, lane + u * p.lanes);
+    }
     const Spread<V> spread(p, lane);
     const bool list = group >= p.split;
     const int g = list ? group - p.split : group, n = list ? kThreads / p.lanes - p.split : p.split;
