@@ -5,13 +5,17 @@
 //   ds = g (a T (q_T - p) + b (q_1 - e_label))
 //
 // Everything is in powers of two of x c - r, with c = log2(e) / T (or log2(e)) and a
-// reference r = max(x) c that is rounded once and used alike for sums, losses and
-// gradients: its rounding cancels.
+// reference r = m c that is rounded once and used alike for sums, losses and gradients:
+// its rounding cancels.  m is the largest of some of the row's elements, of every thread's
+// first vector; where a thread's sum shows that this is too low for its others (by 40 powers
+// of two), the largest of all of its elements.
 //
 // Memory bounds it: the logits are read once for the sums, once more, from the L2 cache,
 // for the gradient, and the gradient is written once.  8192 rows of 50257 in bfloat16 at
-// two temperatures take 305 to 316 us (1.65 GB, 5.3 TB/s; four powers an element, which
-// alone take 180), of 131072 at one 727 (4.3 GB, 5.9 TB/s); cross entropy of 50257 280.
+// two temperatures take 305 us (1.65 GB, 5.4 TB/s; four powers an element, which alone
+// take 180), of 131072 at one 726 (4.3 GB, 5.9 TB/s); cross entropy of 50257 276.  Rows go
+// element by element, at several times that, where they have no term, where a thread's first
+// vector is masked, and where rows of the gradient start elsewhere than the logits'.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -321,7 +325,7 @@ __device__ __forceinline__ void load_entries(const Params &p, Entries &to, int64
 // with 256 (before the entries' table), 8192 x 131072 939 with two blocks a row and 727 with
 // four, whose rows stay in L2.  Rows held in shared memory between the two readings were slower
 // (452 and 1085 us): clusters' barriers and too few warps cost more than the second reading.
-// The prefetch of a block's whole part took 8192 x 50257 from 336 to 315 us.
+// The prefetch of a block's whole part took 8192 x 50257 from 336 to 315 us (305 since).
 template <typename T, Mode MODE, bool BOTH>
 __global__ void __launch_bounds__(kMaxThreads) rikfad_distill_kernel(const __grid_constant__ Params p)
 {

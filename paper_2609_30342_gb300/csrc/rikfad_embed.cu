@@ -9,9 +9,9 @@
 //
 // Memory bounds both: dout is read once, every row of dW written once (rows without
 // a token as zeros, while the tokens are sorted and beside the sums).  65536 tokens of
-// 4096 in bfloat16, table of 131072: forward 118 us (0.74 GB, 6.2 TB/s), gradient 280
-// (1.6 GB, 5.8 TB/s); 16384 of 768 in float32, table of 50257: 15 and 50 us, the latter
-// 20 for the sort, beside which the others write zeros to 76 MB.
+// 4096 in bfloat16, table of 131072: forward 121 us (0.74 GB, 6.1 TB/s), gradient 276
+// (1.6 GB, 5.8 TB/s); 16384 of 768 in float32, table of 50257: 12 and 49 us, the latter
+// 18 for the sort, beside which the others write zeros to 62 MB.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -36,7 +36,9 @@ constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kSortBits = 9;            // of a pass: the warps' counts of 2^9 digits take 32 KB
 constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32, kSumAhead = 8;
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinAhead = 8, kJoinBlocks = 4 * kSms;
-constexpr double kZeroBytesPerUs = 4.2e6; // of all multiprocessors but the sorting ones
+// Of all multiprocessors but the sorting ones: 62 MB beside the sort of 16384 tokens, which takes 18 us with them and 15
+// alone, 136 MB beside that of 65536, 37 and 35.
+constexpr double kZeroBytesPerUs = 4.2e6;
 constexpr int kShortRun = 32;           // chunks that a run joined by one warp goes on in, at most
 constexpr int kCountThreads = 256, kMostCounted = 6144;
 
@@ -521,7 +523,8 @@ template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t to, con
 //
 // The ring holds kSumAhead rows' parts on their way for every warp without registers: 16384
 // tokens of 768 and 65536 of 4096, forward and gradient, took 68 and 443 us with eight rows
-// in registers, 67 and 414 with eight in the ring, 69 and 426 with sixteen.
+// in registers, 67 and 414 with eight in the ring, 69 and 426 with sixteen (with all that follows
+// 65 and 397).
 template <typename W, typename O, int V, int M>
 __global__ void __launch_bounds__(kSumThreads) rikfad_embed_sum_kernel(const __grid_constant__ EmbedParams p)
 {

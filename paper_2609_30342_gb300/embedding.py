@@ -20,7 +20,7 @@ _EMBEDDING = struct.Struct("=3q 4i d q 4q qQ")
 class TokenEmbedding:
     """out = scale * weight[ids], a row of zeros where an id is outside [0, vocab) (padding).
 
-    weight and rows are float32, bfloat16 or float16, in any combination; ids int32 or int64 of any shape."""
+    weight and rows are float32, bfloat16 or float16, in any combination; ids int32 or int64 of any shape, contiguous."""
 
     def __init__(self, vocab, width, scale=1.0):
         self.vocab, self.width, self.scale = int(vocab), int(width), float(scale)

@@ -46,7 +46,8 @@ class DistillationLoss:
     that name one element add up.  K is 1024 at most.
 
     Logits are [..., vocab] in float32, bfloat16 or float16, the teacher's [..., K] in any of them, ``index`` [..., K] and
-    ``labels`` [...] int32 or int64.  Losses are float32, one a row.  Only the logits have a gradient."""
+    ``labels`` [...] int32 or int64.  Rows are contiguous and evenly spaced, labels contiguous.  Losses are float32, one a
+    row.  Only the logits have a gradient."""
 
     def __init__(self, temperature=1.0, teacher_weight=1.0, label_weight=0.0):
         self.temperature, self.teacher_weight, self.label_weight = float(temperature), float(teacher_weight), float(label_weight)
